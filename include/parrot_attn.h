@@ -399,6 +399,210 @@ parrot_status parrot_validate_prefill_inputs(
     const int32_t* group_ids, int32_t* scratch, void* stream);
 
 /*
+ * Rotary position embedding of a model, as the fill below takes it.  A pair of
+ * elements (a, b) of a head at position n turns by the angle n * f_i:
+ *   a' = amplitude * (a cos - b sin),  b' = amplitude * (b cos + a sin).
+ * parrot_rotary_init (or parrot_rotary_from_frequencies) fills the struct; it is
+ * plain host data, may be copied, and holds no pointer.  Angles are kept as 64-bit
+ * binary fractions of a turn, so n * f_i is exact modulo a turn to 2^-32 at any
+ * int32 position (negative ones turn backwards).
+ */
+#define PARROT_ROTARY_MAX_PAIRS 64
+typedef struct {
+  int32_t rotary_dim;     /* RD: the first RD elements of a head turn, the rest pass */
+  int32_t interleaved;    /* 0: pairs (i, i + RD/2); 1: pairs (2i, 2i + 1) */
+  float amplitude;
+  int32_t reserved;
+  uint64_t turns[PARROT_ROTARY_MAX_PAIRS];   /* f_i / (2 pi) * 2^64, i < RD/2 */
+} parrot_rotary;
+
+/* f_i = base^(-2i / RD), then scaled for contexts longer than the trained one: */
+typedef enum {
+  PARROT_ROTARY_SCALE_NONE = 0,
+  PARROT_ROTARY_SCALE_LINEAR = 1,      /* f_i / factor */
+  PARROT_ROTARY_SCALE_NTK = 2,         /* base * factor^(RD / (RD - 2)) for base */
+  PARROT_ROTARY_SCALE_YARN = 3,        /* f_i where pair i turns more than `high` times in
+                                          original_length positions, f_i / factor below `low`
+                                          turns, a linear blend over i between; amplitude
+                                          0.1 ln(factor) + 1 */
+  PARROT_ROTARY_SCALE_WAVELENGTH = 4   /* the same with a blend linear in the turns
+                                          themselves; amplitude 1 */
+} parrot_rotary_scaling;
+typedef struct {
+  int32_t rotary_dim;       /* even, in [2, 128] */
+  int32_t interleaved;      /* 0 or 1 */
+  double base;              /* > 1 */
+  int32_t scaling;          /* parrot_rotary_scaling */
+  double factor;            /* >= 1 (unused for SCALE_NONE) */
+  double original_length;   /* trained positions, >= 1 (YARN and WAVELENGTH) */
+  double low, high;         /* turns, 0 < low < high; both 0: 1 and 32 (YARN), 1 and 4
+                               (WAVELENGTH) */
+  double amplitude;         /* > 0, or 0 for the scaling's own */
+} parrot_rotary_config;
+parrot_status parrot_rotary_init(parrot_rotary* rotary, const parrot_rotary_config* config);
+
+/* A rotary embedding from its frequencies: radians[i] (host, RD/2 values in [0, 2 pi)) is
+ * the angle of pair i per position. */
+parrot_status parrot_rotary_from_frequencies(parrot_rotary* rotary, int32_t rotary_dim,
+                                             int32_t interleaved, const double* radians,
+                                             double amplitude);
+
+/*
+ * Fill of new rows (Section 7: Fill and Generate write a context's new tokens
+ * into its KV cache): normalises each head of the new queries and keys (optional),
+ * rotates them to their positions (optional), writes the queries to q_out and the
+ * keys and values into the paged cache, where the decode, prefill and tree calls
+ * below and above read them.  Rows belong to requests as in prefill: rows
+ * [query_offsets[r], query_offsets[r+1]) are request r's last Q_r own tokens
+ * (suffix_lens[r] counts them), and row query_offsets[r] + j goes to own position
+ * S_r - Q_r + j.  Per head x of a query or key row:
+ *   y = x / sqrt(mean(x^2) + norm_eps) * weight   (weight given),
+ *   then the rotation by positions[row],
+ * computed in fp32 and rounded once; values are copied.
+ *
+ *   p                    num_requests, num_heads (H, of the cache), head_dim,
+ *                        block_size, max_suffix_len, suffix_table_stride,
+ *                        num_suffix_blocks and dtype are used; the group fields only
+ *                        have to be valid (num_groups = 0 will do)
+ *   q                    row t, head h at q + t * q_stride + h * D, likewise k and v
+ *                        (H heads): slices of one projection's output need no copy.
+ *                        16-byte aligned, strides a multiple of 16 bytes and at least
+ *                        the row's length
+ *   q, q_out             both NULL: only keys and values
+ *   q_out                [T][HQ][D] dtype, 16-byte aligned; may be q itself when
+ *                        q_stride = HQ * D, and must not overlap q otherwise
+ *   q_norm, k_norm       [D] dtype, 16-byte aligned, or NULL: no normalisation
+ *   rotary               (host) or NULL: no rotation; RD <= D
+ *   positions            int32 [T] (unused when rotary is NULL; may be NULL then)
+ *   query_offsets        int32 [R + 1], non-decreasing, query_offsets[R] <= T
+ * Rows from query_offsets[R] on are padding: nothing of them is read into a result
+ * and their q_out rows are left as they were.  No two rows may share a cache slot.
+ * To fill a group's prefix, pass its table and length as a request's and the prefix
+ * pools as the suffix pools.  Needs no workspace.
+ */
+typedef struct {
+  int32_t num_query_rows;    /* T >= query_offsets[R]; T = 0 is a no-op */
+  int32_t max_query_rows;    /* >= every Q_r; in [1, max_suffix_len] when T > 0 */
+  int32_t num_query_heads;   /* HQ >= 1 (unused when q is NULL) */
+  float norm_eps;            /* finite, >= 0 */
+  int64_t q_stride, k_stride, v_stride;   /* elements between rows */
+} parrot_fill_rows;
+
+parrot_status parrot_rotary_fill(
+    const parrot_problem* p, const parrot_fill_rows* rows, const parrot_rotary* rotary,
+    const void* q, const void* k, const void* v,
+    const void* q_norm, const void* k_norm,
+    const int32_t* positions, const int32_t* query_offsets,
+    const int32_t* suffix_block_tables, const int32_t* suffix_lens,
+    void* q_out, void* suffix_k, void* suffix_v,
+    void* stream, const parrot_trace* trace);
+
+/*
+ * Attention for trees of drafted tokens over the cache (speculative decoding on top
+ * of shared prefixes; Section 5.3 for the sharing).  Request r's last Q_r own
+ * tokens are drafted ones, whose keys and values are already in the suffix pools
+ * (parrot_rotary_fill writes them).  They form a forest:
+ *   tree_parents         int32 [T]: the parent of row query_offsets[r] + j, as a
+ *                        row index within the request, lower than j, or -1 for a
+ *                        row that follows the last cached token.  NULL: chains
+ *                        (each row follows the one before)
+ * Row j attends to the prefixes of r's group chain, r's own tokens before the
+ * drafted ones, the ancestors of j and j itself:
+ *   out, lse             the decode formula over those keys.
+ * Keys and values of tokens a row does not see never reach its result, whatever
+ * they hold (NaN and infinities too).
+ *
+ * Query heads may outnumber the cache's heads (grouped-query attention): query head
+ * i reads cache head i / (HQ / H), p->num_heads = H.  With one row per request this
+ * is a decode step of such a model.
+ *
+ *   q, out               [T][HQ][D] dtype, 16-byte aligned;  lse float32 [T][HQ]
+ *   query_offsets        int32 [R + 1], non-decreasing, query_offsets[0] = 0,
+ *                        query_offsets[R] <= T, Q_r <= min(S_r, max_query_rows)
+ *   prefix_parents       as parrot_nested_prefix_decode, or NULL for flat groups
+ *   workspace            >= parrot_tree_workspace_bytes(p, rows) bytes, 256-byte
+ *                        aligned
+ * Rows from query_offsets[R] on are padding: their out and lse are left as they
+ * were (so one captured graph serves batches of fewer rows).  Other arguments as
+ * parrot_shared_prefix_prefill.
+ */
+#define PARROT_MAX_TREE_ROWS 128
+typedef struct {
+  int32_t num_query_rows;    /* T >= query_offsets[R]; T = 0 is a no-op */
+  int32_t max_query_rows;    /* >= every Q_r; in [1, min(max_suffix_len,
+                                PARROT_MAX_TREE_ROWS)] when T > 0 */
+  int32_t max_group_rows;    /* >= the rows that read any one group's prefix */
+  int32_t num_query_heads;   /* HQ: a multiple of p->num_heads */
+} parrot_tree_rows;
+
+/* Bytes of workspace parrot_shared_prefix_tree_decode needs (0 when T = 0); depends
+ * on the current device's compute-unit count like parrot_workspace_bytes.
+ * (size_t)-1 if the arguments are invalid. */
+size_t parrot_tree_workspace_bytes(const parrot_problem* p, const parrot_tree_rows* rows);
+
+parrot_status parrot_shared_prefix_tree_decode(
+    const parrot_problem* p, const parrot_tree_rows* rows,
+    const void* q, const int32_t* query_offsets, const int32_t* tree_parents,
+    const void* prefix_k, const void* prefix_v,
+    const void* suffix_k, const void* suffix_v,
+    const int32_t* prefix_block_tables, const int32_t* prefix_lens,
+    const int32_t* prefix_parents,
+    const int32_t* suffix_block_tables, const int32_t* suffix_lens,
+    const int32_t* group_ids,
+    void* out, float* lse,
+    void* workspace, size_t workspace_bytes,
+    void* stream, const parrot_trace* trace);
+
+/* parrot_validate_prefill_inputs for a tree call: query_offsets[R] may be below T,
+ * and every tree parent of a row (tree_parents not NULL) must be in [-1, its row). */
+parrot_status parrot_validate_tree_inputs(
+    const parrot_problem* p, const parrot_tree_rows* rows,
+    const int32_t* query_offsets, const int32_t* tree_parents,
+    const int32_t* prefix_block_tables, const int32_t* prefix_lens,
+    const int32_t* prefix_parents,
+    const int32_t* suffix_block_tables, const int32_t* suffix_lens,
+    const int32_t* group_ids, int32_t* scratch, void* stream);
+
+/*
+ * The drafted tokens that a greedy model agrees with.  target_tokens[row] is the
+ * token the model chose after the row's path, root_tokens[r] the one it chose after
+ * r's last cached token, draft_tokens[row] the drafted token itself.  From the
+ * cached context the walk takes, again and again, the lowest row whose parent is
+ * the row reached last (-1 at first) and whose token the model chose there.
+ *   accept_rows          int32 [T]: the taken rows of r, as row indexes within the
+ *                        request, in order from query_offsets[r]; -1 behind them
+ *   accept_lens          int32 [R]: how many
+ *   next_tokens          int32 [R]: what the model chose after the last taken row
+ *                        (root_tokens[r] when none was taken)
+ * All arrays are int32 device arrays; outputs must not overlap inputs.  Entries
+ * of accept_rows from query_offsets[R] on are left as they were.  tree_parents NULL:
+ * chains.  Needs no workspace.
+ */
+parrot_status parrot_tree_accept(
+    int32_t num_requests, const parrot_tree_rows* rows,
+    const int32_t* query_offsets, const int32_t* tree_parents,
+    const int32_t* draft_tokens, const int32_t* target_tokens, const int32_t* root_tokens,
+    int32_t* accept_rows, int32_t* accept_lens, int32_t* next_tokens,
+    void* stream, const parrot_trace* trace);
+
+/*
+ * Keeps the accepted drafted tokens in the cache: the keys and values of row
+ * accept_rows[query_offsets[r] + i] move to own position S_r - Q_r + i, for
+ * i < accept_lens[r] (rows strictly increasing within a request, as
+ * parrot_tree_accept gives them), in one layer's pools; slots of other tokens keep
+ * their contents.  committed_lens[r] = S_r - Q_r + accept_lens[r] is r's own length
+ * then.  committed_lens must be another array than suffix_lens and accept_lens.
+ * On the host, parrot_store_truncate gives the blocks behind it back.  Needs no
+ * workspace.
+ */
+parrot_status parrot_tree_commit(
+    const parrot_problem* p, const parrot_tree_rows* rows,
+    const int32_t* query_offsets, const int32_t* accept_rows, const int32_t* accept_lens,
+    const int32_t* suffix_block_tables, const int32_t* suffix_lens,
+    void* suffix_k, void* suffix_v, int32_t* committed_lens,
+    void* stream, const parrot_trace* trace);
+
+/*
  * Measurement aid: the device's attainable HBM read bandwidth, the ceiling of
  * the bandwidth-bound decode kernels (Section 8.3: token generation is bound
  * by memory bandwidth).  Reads every byte of

@@ -55,6 +55,11 @@ int32_t parrot_store_fill(parrot_context_store* st, const int32_t* tokens, int32
  * tokens).  PARROT_ERR_WORKSPACE_TOO_SMALL when no block is free. */
 parrot_status parrot_store_append(parrot_context_store* st, int32_t ctx, int32_t token);
 
+/* Drop a context's last own tokens so that `own_tokens` remain (drafted tokens that
+ * were not accepted); blocks that hold none of them any more become free.
+ * PARROT_ERR_INVALID_ARGUMENT when own_tokens is negative or above the context's. */
+parrot_status parrot_store_truncate(parrot_context_store* st, int32_t ctx, int32_t own_tokens);
+
 /* FreeContext: release the context's own blocks and its references. */
 parrot_status parrot_store_free(parrot_context_store* st, int32_t ctx);
 

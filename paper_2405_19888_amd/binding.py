@@ -68,6 +68,51 @@ class ParrotPrefillRows(ctypes.Structure):
     ]
 
 
+class ParrotRotary(ctypes.Structure):
+    _fields_ = [
+        ("rotary_dim", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+        ("amplitude", ctypes.c_float),
+        ("reserved", ctypes.c_int32),
+        ("turns", ctypes.c_uint64 * 64),
+    ]
+
+
+class ParrotRotaryConfig(ctypes.Structure):
+    _fields_ = [
+        ("rotary_dim", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+        ("base", ctypes.c_double),
+        ("scaling", ctypes.c_int32),
+        ("factor", ctypes.c_double),
+        ("original_length", ctypes.c_double),
+        ("low", ctypes.c_double),
+        ("high", ctypes.c_double),
+        ("amplitude", ctypes.c_double),
+    ]
+
+
+class ParrotFillRows(ctypes.Structure):
+    _fields_ = [
+        ("num_query_rows", ctypes.c_int32),
+        ("max_query_rows", ctypes.c_int32),
+        ("num_query_heads", ctypes.c_int32),
+        ("norm_eps", ctypes.c_float),
+        ("q_stride", ctypes.c_int64),
+        ("k_stride", ctypes.c_int64),
+        ("v_stride", ctypes.c_int64),
+    ]
+
+
+class ParrotTreeRows(ctypes.Structure):
+    _fields_ = [
+        ("num_query_rows", ctypes.c_int32),
+        ("max_query_rows", ctypes.c_int32),
+        ("max_group_rows", ctypes.c_int32),
+        ("num_query_heads", ctypes.c_int32),
+    ]
+
+
 EXPORTED = (
     "parrot_workspace_bytes", "parrot_shared_prefix_decode", "parrot_per_request_decode",
     "parrot_nested_prefix_decode", "parrot_shared_prefix_decode_append",
@@ -75,6 +120,9 @@ EXPORTED = (
     "parrot_prefill_workspace_bytes", "parrot_prefill_single_pass", "parrot_shared_prefix_prefill",
     "parrot_validate_prefill_inputs", "parrot_last_error", "parrot_abi_version",
     "parrot_shared_prefix_decode_noalloc", "parrot_hbm_read_ceiling", "parrot_mfma_issue_ceiling",
+    "parrot_rotary_init", "parrot_rotary_from_frequencies", "parrot_rotary_fill",
+    "parrot_tree_workspace_bytes", "parrot_shared_prefix_tree_decode", "parrot_validate_tree_inputs",
+    "parrot_tree_accept", "parrot_tree_commit",
 )
 
 STATIC_SCRATCH_BYTES = 64 << 20   # PARROT_STATIC_SCRATCH_BYTES
@@ -130,6 +178,23 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.parrot_mfma_issue_ceiling.argtypes = [vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, vp,
                                               ctypes.POINTER(ParrotTrace)]
     lib.parrot_mfma_issue_ceiling.restype = ctypes.c_int
+    trace_p, tree_p = ctypes.POINTER(ParrotTrace), ctypes.POINTER(ParrotTreeRows)
+    rotary_p = ctypes.POINTER(ParrotRotary)
+    drafting = {
+        "parrot_rotary_init": [rotary_p, ctypes.POINTER(ParrotRotaryConfig)],
+        "parrot_rotary_from_frequencies": [rotary_p, ctypes.c_int32, ctypes.c_int32,
+                                           ctypes.POINTER(ctypes.c_double), ctypes.c_double],
+        "parrot_rotary_fill": [prob_p, ctypes.POINTER(ParrotFillRows), rotary_p] + [vp] * 13 + [trace_p],
+        "parrot_shared_prefix_tree_decode": [prob_p, tree_p] + [vp] * 16 + [sz, vp, trace_p],
+        "parrot_validate_tree_inputs": [prob_p, tree_p] + [vp] * 10,
+        "parrot_tree_accept": [ctypes.c_int32, tree_p] + [vp] * 9 + [trace_p],
+        "parrot_tree_commit": [prob_p, tree_p] + [vp] * 9 + [trace_p],
+    }
+    for name, args in drafting.items():
+        getattr(lib, name).argtypes = args
+        getattr(lib, name).restype = ctypes.c_int
+    lib.parrot_tree_workspace_bytes.argtypes = [prob_p, tree_p]
+    lib.parrot_tree_workspace_bytes.restype = sz
     lib.parrot_last_error.argtypes = []
     lib.parrot_last_error.restype = ctypes.c_char_p
     lib.parrot_abi_version.argtypes = []

@@ -16,7 +16,7 @@ from .binding import ParrotError, _check, load_library
 
 STORE_EXPORTED = (
     "parrot_store_create", "parrot_store_destroy", "parrot_store_fill", "parrot_store_append",
-    "parrot_store_free", "parrot_store_free_blocks", "parrot_store_num_prefixes",
+    "parrot_store_truncate", "parrot_store_free", "parrot_store_free_blocks", "parrot_store_num_prefixes",
     "parrot_store_prefix_tokens", "parrot_store_own_tokens", "parrot_store_batch_shape",
     "parrot_store_build_batch",
 )
@@ -42,6 +42,8 @@ def _lib():
     lib.parrot_store_fill.restype = i32
     lib.parrot_store_append.argtypes = [vp, i32, i32]
     lib.parrot_store_append.restype = ctypes.c_int
+    lib.parrot_store_truncate.argtypes = [vp, i32, i32]
+    lib.parrot_store_truncate.restype = ctypes.c_int
     lib.parrot_store_free.argtypes = [vp, i32]
     lib.parrot_store_free.restype = ctypes.c_int
     for name in ("parrot_store_free_blocks", "parrot_store_num_prefixes"):
@@ -110,6 +112,11 @@ class ContextStore:
 
     def append(self, ctx: int, token: int = 0):
         _check(self._lib.parrot_store_append(self._h, int(ctx), int(token)))
+
+    def truncate(self, ctx: int, own_tokens: int):
+        """Keep the first `own_tokens` own tokens (drafted ones that were not
+        accepted go, with the blocks only they held)."""
+        _check(self._lib.parrot_store_truncate(self._h, int(ctx), int(own_tokens)))
 
     def free(self, ctx: int):
         _check(self._lib.parrot_store_free(self._h, int(ctx)))

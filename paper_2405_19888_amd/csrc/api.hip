@@ -14,6 +14,7 @@
 #include "ceiling.h"
 #include "common.h"
 #include "errors.h"
+#include "host.h"
 #include "prefill_args.h"
 #include "prefill_shape.h"
 
@@ -250,6 +251,24 @@ parrot_status check_problem(const parrot_problem* p, parrot::Plan* pl) {
   pl->total_bytes = p->num_requests > 0 ? pl->o_bytes + pl->lse_bytes + pl->info_bytes : 0;
   return PARROT_OK;
 }
+
+}  // namespace
+
+namespace parrot {
+
+parrot_status check_problem_fields(const parrot_problem* p) {
+  if (!p) return fail(PARROT_ERR_INVALID_ARGUMENT, "problem is NULL");
+  parrot_problem d = *p;
+  if (d.num_groups > 0) d.max_group_size = d.num_requests > 0 ? 1 : d.max_group_size;
+  Plan pl;
+  return check_problem(&d, &pl);
+}
+
+int device_cus() { return num_cus(); }
+
+}  // namespace parrot
+
+namespace {
 
 // The workspace layout of one shared-path call sized for that call alone: the
 // prefix chunks of this call's chunk size and its split-KV pieces, with no
@@ -1035,11 +1054,12 @@ parrot_status validate(const parrot_problem* p, const int32_t* prefix_block_tabl
                        const int32_t* suffix_block_tables, const int32_t* suffix_lens,
                        const int32_t* group_ids, int32_t* scratch, void* stream,
                        const parrot_prefill_rows* rows = nullptr,
-                       const int32_t* query_offsets = nullptr) {
+                       const int32_t* query_offsets = nullptr,
+                       const parrot::ValidateTree* tree = nullptr) {
   parrot::Plan pl;
   if (rows) {
     PrefillPlan fp;
-    PARROT_TRY(check_prefill(p, rows, prefix_parents != nullptr, &fp));
+    if (!tree) PARROT_TRY(check_prefill(p, rows, prefix_parents != nullptr, &fp));
     if (!query_offsets || !aligned(query_offsets, 4))
       return fail(PARROT_ERR_INVALID_ARGUMENT, "query_offsets is NULL or misaligned");
   } else {
@@ -1066,6 +1086,7 @@ parrot_status validate(const parrot_problem* p, const int32_t* prefix_block_tabl
   if (rows) {
     a.qoff = query_offsets; a.T = rows->num_query_rows;
     a.max_q = rows->max_query_rows; a.max_grp = rows->max_group_rows;
+    if (tree) { a.padded = 1; a.tree = tree->parents; }
   } else {
     a.max_grp = p->max_group_size;
   }
@@ -1083,7 +1104,9 @@ parrot_status validate(const parrot_problem* p, const int32_t* prefix_block_tabl
                                "query_offsets not 0 = offsets[0] <= ... <= offsets[R] = num_query_rows",
                                "query rows of a request > min(suffix length, max_query_rows)",
                                "rows reading a group's prefix > max_group_rows",
-                               "requests reading a group's prefix > max_group_size"};
+                               "requests reading a group's prefix > max_group_size",
+                               "query_offsets[R] not in [0, num_query_rows]",
+                               "tree parent not in [-1, row)"};
   constexpr int kCodes = (int)(sizeof what / sizeof what[0]) - 1;
   if (res[0] != 0)
     return fail(PARROT_ERR_INVALID_ARGUMENT, "%s at entry %d (value %d)",
@@ -1093,6 +1116,20 @@ parrot_status validate(const parrot_problem* p, const int32_t* prefix_block_tabl
 }
 
 }  // namespace
+
+namespace parrot {
+
+parrot_status validate_inputs(const parrot_problem* p, const int32_t* prefix_block_tables,
+                              const int32_t* prefix_lens, const int32_t* prefix_parents,
+                              const int32_t* suffix_block_tables, const int32_t* suffix_lens,
+                              const int32_t* group_ids, int32_t* scratch, void* stream,
+                              const parrot_prefill_rows* rows, const int32_t* query_offsets,
+                              const ValidateTree* tree) {
+  return validate(p, prefix_block_tables, prefix_lens, prefix_parents, suffix_block_tables, suffix_lens,
+                  group_ids, scratch, stream, rows, query_offsets, tree);
+}
+
+}  // namespace parrot
 
 extern "C" {
 

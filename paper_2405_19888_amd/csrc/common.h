@@ -103,6 +103,8 @@ struct ValidateArgs {
   int pstride, sstride, max_p, max_s, npblk, nsblk;
   const int* qoff;       // prefill row offsets [R + 1] (NULL: decode)
   int T, max_q, max_grp; // prefill rows, rows per request, rows per group
+  int padded;            // tree rows: qoff[R] may be below T
+  const int* tree;       // tree rows: parents [T] (NULL: not checked)
 };
 
 // dtype codes follow parrot_dtype

@@ -189,6 +189,21 @@ parrot_status parrot_store_append(parrot_context_store* st, int32_t ctx, int32_t
   return parrot::set_error(PARROT_OK, "");
 }
 
+parrot_status parrot_store_truncate(parrot_context_store* st, int32_t ctx, int32_t own_tokens) {
+  if (!st || !st->context(ctx)) return parrot::set_error(PARROT_ERR_INVALID_ARGUMENT, "unknown context %d", ctx);
+  Context& c = st->ctxs[ctx];
+  if (own_tokens < 0 || own_tokens > c.own)
+    return parrot::set_error(PARROT_ERR_INVALID_ARGUMENT, "own_tokens %d not in [0, %d]", own_tokens, c.own);
+  const size_t keep = st->blocks_for(own_tokens);
+  // (the free list was made with room for every block: nothing here allocates)
+  while (c.blocks.size() > keep) {
+    st->free_list.push_back(c.blocks.back());
+    c.blocks.pop_back();
+  }
+  c.own = own_tokens;
+  return parrot::set_error(PARROT_OK, "");
+}
+
 parrot_status parrot_store_free(parrot_context_store* st, int32_t ctx) {
   if (!st || !st->context(ctx)) return parrot::set_error(PARROT_ERR_INVALID_ARGUMENT, "unknown context %d", ctx);
   Context& c = st->ctxs[ctx];

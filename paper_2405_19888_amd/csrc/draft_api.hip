@@ -1,0 +1,384 @@
+// C ABI of a drafting step: rotary embeddings (host), fill of new rows, tree decode,
+// accept and commit.  Argument checks, sizing and launches; host scalars only.
+#include <algorithm>
+#include <cmath>
+
+#include "draft_args.h"
+#include "host.h"
+#include "tree_args.h"
+
+using parrot::set_error;
+
+namespace {
+
+#define PARROT_TRY(x) do { parrot_status _s = (x); if (_s != PARROT_OK) return _s; } while (0)
+
+long ceil_div(long a, long b) { return (a + b - 1) / b; }
+hipEvent_t ev(void* p) { return reinterpret_cast<hipEvent_t>(p); }
+
+parrot_status bad(const char* fmt, long a = 0, long b = 0) {
+  return set_error(PARROT_ERR_INVALID_ARGUMENT, fmt, a, b);
+}
+
+parrot_status launched(hipError_t e, const char* what) {
+  if (e != hipSuccess) return set_error(PARROT_ERR_HIP, "%s launch failed: %s", what, hipGetErrorString(e));
+  return set_error(PARROT_OK, "");
+}
+
+static_assert(PARROT_ROTARY_MAX_PAIRS == parrot::kRotaryPairs && PARROT_MAX_TREE_ROWS == parrot::kTreeRows,
+              "header and kernels agree");
+
+constexpr double kTwoPi = 6.283185307179586476925286766559;
+
+parrot_status check_rotary(int32_t rotary_dim, int32_t interleaved) {
+  if (rotary_dim < 2 || rotary_dim > 2 * PARROT_ROTARY_MAX_PAIRS || rotary_dim % 2 != 0)
+    return bad("rotary_dim %ld is not even and in [2, %ld]", rotary_dim, 2 * PARROT_ROTARY_MAX_PAIRS);
+  if (interleaved != 0 && interleaved != 1) return bad("interleaved %ld is not 0 or 1", interleaved);
+  return PARROT_OK;
+}
+
+}  // namespace
+
+// -------------------------------------------------------------------- rotary
+extern "C" {
+
+parrot_status parrot_rotary_from_frequencies(parrot_rotary* rotary, int32_t rotary_dim,
+                                             int32_t interleaved, const double* radians,
+                                             double amplitude) {
+  if (!rotary || !radians) return bad(rotary ? "radians is NULL" : "rotary is NULL");
+  PARROT_TRY(check_rotary(rotary_dim, interleaved));
+  if (!(amplitude > 0) || !std::isfinite((float)amplitude)) return bad("amplitude is not positive and finite");
+  parrot_rotary out{};
+  out.rotary_dim = rotary_dim;
+  out.interleaved = interleaved;
+  out.amplitude = (float)amplitude;
+  for (int i = 0; i < rotary_dim / 2; ++i) {
+    const double turns = radians[i] / kTwoPi;
+    if (!(turns >= 0.0 && turns < 1.0)) return bad("frequency %ld is not in [0, 2 pi)", i);
+    // the nearest multiple of 2^-64; turns < 1 is at most 1 - 2^-53, so this fits
+    out.turns[i] = (uint64_t)std::ldexp(turns, 64);
+  }
+  *rotary = out;
+  return set_error(PARROT_OK, "");
+}
+
+parrot_status parrot_rotary_init(parrot_rotary* rotary, const parrot_rotary_config* c) {
+  if (!rotary || !c) return bad(rotary ? "config is NULL" : "rotary is NULL");
+  PARROT_TRY(check_rotary(c->rotary_dim, c->interleaved));
+  if (!(c->base > 1.0) || !std::isfinite(c->base)) return bad("base is not finite and above 1");
+  if (c->scaling < PARROT_ROTARY_SCALE_NONE || c->scaling > PARROT_ROTARY_SCALE_WAVELENGTH)
+    return set_error(PARROT_ERR_UNSUPPORTED, "rotary scaling %d", (int)c->scaling);
+  const bool yarn = c->scaling == PARROT_ROTARY_SCALE_YARN, blended = yarn || c->scaling == PARROT_ROTARY_SCALE_WAVELENGTH;
+  const double s = c->scaling == PARROT_ROTARY_SCALE_NONE ? 1.0 : c->factor;
+  if (!(s >= 1.0) || !std::isfinite(s)) return bad("factor is not finite and at least 1");
+  double low = c->low, high = c->high;
+  if (blended) {
+    if (!(c->original_length >= 1.0) || !std::isfinite(c->original_length))
+      return bad("original_length is not finite and at least 1");
+    if (low == 0.0 && high == 0.0) { low = 1.0; high = yarn ? 32.0 : 4.0; }
+    if (!(low > 0.0) || !(high > low) || !std::isfinite(high)) return bad("low and high are not 0 < low < high");
+  }
+  if (c->scaling == PARROT_ROTARY_SCALE_NTK && c->rotary_dim < 4) return bad("NTK scaling needs rotary_dim >= 4");
+  if (!(c->amplitude >= 0.0)) return bad("amplitude is negative");
+  const double rd = c->rotary_dim;
+  const double base = c->scaling == PARROT_ROTARY_SCALE_NTK ? c->base * std::pow(s, rd / (rd - 2.0)) : c->base;
+  // YaRN: the pairs that turn `high` and `low` times in the trained length, rounded
+  // outwards, bound the blend
+  double first = 0.0, last = 0.0;
+  if (yarn) {
+    auto pair_of = [&](double turns) { return rd * std::log(c->original_length / (turns * kTwoPi)) / (2.0 * std::log(c->base)); };
+    first = std::max(std::floor(pair_of(high)), 0.0);
+    last = std::min(std::ceil(pair_of(low)), rd - 1.0);
+  }
+  double radians[PARROT_ROTARY_MAX_PAIRS];
+  for (int i = 0; i < c->rotary_dim / 2; ++i) {
+    const double f = std::pow(base, -2.0 * i / rd);
+    double keep = 1.0;                                      // share of the unscaled frequency
+    if (c->scaling == PARROT_ROTARY_SCALE_LINEAR) keep = 0.0;
+    if (yarn) keep = 1.0 - std::min(1.0, std::max(0.0, (i - first) / std::max(last - first, 1e-3)));
+    if (c->scaling == PARROT_ROTARY_SCALE_WAVELENGTH)
+      keep = std::min(1.0, std::max(0.0, (c->original_length * f / kTwoPi - low) / (high - low)));
+    radians[i] = c->scaling == PARROT_ROTARY_SCALE_NTK ? f : f * keep + f / s * (1.0 - keep);
+  }
+  const double amplitude = c->amplitude > 0.0 ? c->amplitude : yarn ? 0.1 * std::log(s) + 1.0 : 1.0;
+  return parrot_rotary_from_frequencies(rotary, c->rotary_dim, c->interleaved, radians, amplitude);
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------- fill
+namespace {
+
+parrot_status check_fill_rows(const parrot_problem* p, const parrot_fill_rows* rows) {
+  PARROT_TRY(parrot::check_problem_fields(p));
+  if (!rows) return bad("rows is NULL");
+  if (rows->num_query_rows < 0) return bad("num_query_rows %ld < 0", rows->num_query_rows);
+  if (rows->num_query_rows == 0) return PARROT_OK;
+  if (p->num_requests == 0) return bad("num_query_rows %ld > 0 with no requests", rows->num_query_rows);
+  if (rows->max_query_rows < 1 || rows->max_query_rows > p->max_suffix_len)
+    return bad("max_query_rows %ld not in [1, max_suffix_len = %ld]", rows->max_query_rows, p->max_suffix_len);
+  if (!(rows->norm_eps >= 0.f) || !std::isfinite(rows->norm_eps)) return bad("norm_eps is not finite and >= 0");
+  return PARROT_OK;
+}
+
+}  // namespace
+
+extern "C" parrot_status parrot_rotary_fill(
+    const parrot_problem* p, const parrot_fill_rows* rows, const parrot_rotary* rotary, const void* q,
+    const void* k, const void* v, const void* q_norm, const void* k_norm, const int32_t* positions,
+    const int32_t* query_offsets, const int32_t* suffix_block_tables, const int32_t* suffix_lens,
+    void* q_out, void* suffix_k, void* suffix_v, void* stream, const parrot_trace* trace) {
+  PARROT_TRY(check_fill_rows(p, rows));
+  if (rows->num_query_rows == 0) return set_error(PARROT_OK, "");
+  if ((q == nullptr) != (q_out == nullptr)) return bad(q ? "q_out is NULL and q is not" : "q is NULL and q_out is not");
+  const parrot::PtrCheck need[] = {
+      {k, "k", 16}, {v, "v", 16}, {query_offsets, "query_offsets", 4},
+      {suffix_block_tables, "suffix_block_tables", 4}, {suffix_lens, "suffix_lens", 4},
+      {suffix_k, "suffix_k", 16}, {suffix_v, "suffix_v", 16}};
+  PARROT_TRY(parrot::check_pointers(need));
+  const long T = rows->num_query_rows, D = p->head_dim, H = p->num_heads;
+  const long elt = p->dtype == PARROT_DTYPE_F32 ? 4 : 2;
+  const long HQ = q ? rows->num_query_heads : 0;
+  if (q) {
+    if (HQ < 1) return bad("num_query_heads %ld < 1", HQ);
+    const parrot::PtrCheck qs[] = {{q, "q", 16}, {q_out, "q_out", 16}};
+    PARROT_TRY(parrot::check_pointers(qs));
+  }
+  for (const parrot::PtrCheck& c : {parrot::PtrCheck{q_norm, "q_norm", 16}, parrot::PtrCheck{k_norm, "k_norm", 16}})
+    if (c.ptr) {
+      const parrot::PtrCheck one[] = {c};
+      PARROT_TRY(parrot::check_pointers(one));
+    }
+  struct { const char* name; int64_t stride; long width; } strides[] = {
+      {"q_stride", rows->q_stride, HQ * D}, {"k_stride", rows->k_stride, H * D}, {"v_stride", rows->v_stride, H * D}};
+  for (auto& s : strides) {
+    if (s.width == 0) continue;
+    if (s.stride < s.width || s.stride > (1LL << 40))
+      return set_error(PARROT_ERR_INVALID_ARGUMENT, "%s %lld not in [%ld, 2^40]", s.name, (long long)s.stride, s.width);
+    if (s.stride * elt % 16 != 0)
+      return set_error(PARROT_ERR_INVALID_ARGUMENT, "%s %lld is not a multiple of 16 bytes", s.name, (long long)s.stride);
+  }
+  if (q && q == q_out && rows->q_stride != HQ * D)
+    return bad("q_out = q needs q_stride %ld = num_query_heads * head_dim", (long)rows->q_stride);
+  if (q && HQ > 0x7fffffffL / 128) return set_error(PARROT_ERR_UNSUPPORTED, "num_query_heads %ld", HQ);
+  if (rotary) {
+    PARROT_TRY(check_rotary(rotary->rotary_dim, rotary->interleaved));
+    if (rotary->rotary_dim > D) return bad("rotary_dim %ld > head_dim %ld", rotary->rotary_dim, D);
+    const parrot::PtrCheck pos[] = {{positions, "positions", 4}};
+    PARROT_TRY(parrot::check_pointers(pos));
+  }
+
+  parrot::FillArgs a{};
+  a.q = q; a.k = k; a.v = v;
+  a.q_stride = rows->q_stride * elt; a.k_stride = rows->k_stride * elt; a.v_stride = rows->v_stride * elt;
+  a.q_norm = q ? q_norm : nullptr; a.k_norm = k_norm;
+  a.positions = positions; a.qoff = query_offsets; a.stab = suffix_block_tables; a.slen = suffix_lens;
+  a.q_out = q_out; a.sk = suffix_k; a.sv = suffix_v;
+  a.T = (int)T; a.R = p->num_requests; a.HQ = (int)HQ; a.H = (int)H;
+  a.sstride = p->suffix_table_stride; a.max_s = p->max_suffix_len; a.max_q = rows->max_query_rows;
+  a.nsblk = p->num_suffix_blocks;
+  a.eps = rows->norm_eps; a.amplitude = 1.f;
+  int partner = parrot::kRotaryNone;
+  if (rotary) {
+    a.rd = rotary->rotary_dim;
+    a.amplitude = rotary->amplitude;
+    std::copy(rotary->turns, rotary->turns + PARROT_ROTARY_MAX_PAIRS, a.turns);
+    const int per_lane = 16 / (int)elt;
+    partner = rotary->interleaved ? parrot::kRotaryInterleaved
+              : a.rd / 2 % per_lane == 0 ? parrot::kRotaryHalfVector : parrot::kRotaryHalfScalar;
+  }
+  // a row's heads over several workgroups where rows alone do not fill the device
+  const long heads = HQ + 2 * H, step = 4096 / (D * elt);
+  const long slabs = std::max(1L, std::min(ceil_div(heads, step), ceil_div(4L * parrot::device_cus(), T)));
+  a.slab_heads = (int)(ceil_div(ceil_div(heads, slabs), step) * step);
+  a.slabs = (int)ceil_div(heads, a.slab_heads);
+  if (T * a.slabs > 0x7fffffffL) return set_error(PARROT_ERR_UNSUPPORTED, "fill needs %ld workgroups", T * a.slabs);
+  return launched(parrot::launch_fill(a, partner, (int)p->dtype, (int)D, reinterpret_cast<hipStream_t>(stream),
+                                      trace ? ev(trace->partials_start) : nullptr,
+                                      trace ? ev(trace->partials_stop) : nullptr),
+                  "fill kernel");
+}
+
+// --------------------------------------------------------------- tree decode
+namespace {
+
+struct TreePlan {
+  int depth, tiles;
+  size_t total_bytes;
+};
+
+// The row counts of a tree call (or of accept and commit, which have no heads).
+parrot_status check_tree_counts(int32_t requests, const parrot_tree_rows* rows) {
+  if (!rows) return bad("rows is NULL");
+  const long T = rows->num_query_rows;
+  if (T < 0) return bad("num_query_rows %ld < 0", T);
+  if (T == 0) return PARROT_OK;
+  if (requests == 0) return bad("num_query_rows %ld > 0 with no requests", T);
+  if (rows->max_query_rows < 1 || rows->max_query_rows > PARROT_MAX_TREE_ROWS)
+    return bad("max_query_rows %ld not in [1, %ld]", rows->max_query_rows, PARROT_MAX_TREE_ROWS);
+  return PARROT_OK;
+}
+
+parrot_status check_tree(const parrot_problem* p, const parrot_tree_rows* rows, bool nested, TreePlan* pl) {
+  PARROT_TRY(parrot::check_problem_fields(p));
+  PARROT_TRY(check_tree_counts(p->num_requests, rows));
+  *pl = TreePlan{};
+  const long T = rows->num_query_rows;
+  if (T == 0) return PARROT_OK;
+  if (rows->max_query_rows > p->max_suffix_len)
+    return bad("max_query_rows %ld > max_suffix_len %ld", rows->max_query_rows, p->max_suffix_len);
+  if (rows->num_query_heads < 1 || rows->num_query_heads % p->num_heads != 0)
+    return bad("num_query_heads %ld is not a multiple of num_heads %ld", rows->num_query_heads, p->num_heads);
+  if (p->num_groups > 0 && (rows->max_group_rows < 0 || rows->max_group_rows > T))
+    return bad("max_group_rows %ld not in [0, num_query_rows]", rows->max_group_rows);
+  if (T * rows->num_query_heads > 0x7fffffffL)
+    return set_error(PARROT_ERR_UNSUPPORTED, "num_query_rows * num_query_heads > 2^31 - 1");
+  const long G = rows->num_query_heads / p->num_heads;
+  pl->depth = p->num_groups > 0 ? (nested ? std::max(1, (int)p->max_prefix_depth) : 1) : 0;
+  pl->tiles = (int)ceil_div(rows->max_query_rows * G, parrot::tree_cols(p->dtype));
+  if (ceil_div((long)p->num_requests * p->num_heads, 8) * 8 * pl->tiles > 0x7fffffffL)
+    return set_error(PARROT_ERR_UNSUPPORTED, "tree decode needs too many workgroups");
+  return PARROT_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t parrot_tree_workspace_bytes(const parrot_problem* p, const parrot_tree_rows* rows) {
+  TreePlan pl;
+  if (check_tree(p, rows, true, &pl) != PARROT_OK) return (size_t)-1;
+  set_error(PARROT_OK, "");
+  return pl.total_bytes;
+}
+
+parrot_status parrot_shared_prefix_tree_decode(
+    const parrot_problem* p, const parrot_tree_rows* rows, const void* q, const int32_t* query_offsets,
+    const int32_t* tree_parents, const void* prefix_k, const void* prefix_v, const void* suffix_k,
+    const void* suffix_v, const int32_t* prefix_block_tables, const int32_t* prefix_lens,
+    const int32_t* prefix_parents, const int32_t* suffix_block_tables, const int32_t* suffix_lens,
+    const int32_t* group_ids, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream,
+    const parrot_trace* trace) {
+  TreePlan pl;
+  PARROT_TRY(check_tree(p, rows, prefix_parents != nullptr, &pl));
+  if (rows->num_query_rows == 0) return set_error(PARROT_OK, "");
+  const parrot::PtrCheck need[] = {
+      {q, "q", 16}, {query_offsets, "query_offsets", 4}, {suffix_k, "suffix_k", 16}, {suffix_v, "suffix_v", 16},
+      {suffix_block_tables, "suffix_block_tables", 4}, {suffix_lens, "suffix_lens", 4}, {group_ids, "group_ids", 4},
+      {out, "out", 16}, {lse, "lse", 4}, {workspace, "workspace", 256}};
+  PARROT_TRY(parrot::check_pointers(need));
+  if (tree_parents && reinterpret_cast<uintptr_t>(tree_parents) % 4) return bad("tree_parents is not 4-byte aligned");
+  if (p->num_groups > 0) {
+    const parrot::PtrCheck pre[] = {{prefix_k, "prefix_k", 16}, {prefix_v, "prefix_v", 16},
+                                    {prefix_block_tables, "prefix_block_tables", 4}, {prefix_lens, "prefix_lens", 4}};
+    PARROT_TRY(parrot::check_pointers(pre));
+    if (prefix_parents && reinterpret_cast<uintptr_t>(prefix_parents) % 4)
+      return bad("prefix_parents is not 4-byte aligned");
+  }
+  if (workspace_bytes < pl.total_bytes)
+    return set_error(PARROT_ERR_WORKSPACE_TOO_SMALL, "workspace is %zu bytes, need %zu", workspace_bytes, pl.total_bytes);
+
+  parrot::TreeArgs a{};
+  a.q = q; a.pk = prefix_k; a.pv = prefix_v; a.sk = suffix_k; a.sv = suffix_v;
+  a.ptab = prefix_block_tables; a.plen = prefix_lens; a.stab = suffix_block_tables; a.slen = suffix_lens;
+  a.gid = group_ids; a.parents = p->num_groups > 0 ? prefix_parents : nullptr;
+  a.qoff = query_offsets; a.tree = tree_parents;
+  a.out = out; a.lse = lse;
+  a.T = rows->num_query_rows; a.R = p->num_requests; a.H = p->num_heads;
+  a.G = rows->num_query_heads / p->num_heads; a.NG = p->num_groups; a.depth = pl.depth;
+  a.pstride = p->prefix_table_stride; a.sstride = p->suffix_table_stride;
+  a.max_p = p->max_prefix_len; a.max_s = p->max_suffix_len; a.max_q = rows->max_query_rows;
+  a.npblk = p->num_groups > 0 ? p->num_prefix_blocks : 1; a.nsblk = p->num_suffix_blocks;
+  a.tiles = pl.tiles;
+  a.scale_log2 = p->sm_scale * parrot::kLog2e;
+  return launched(parrot::launch_tree(a, (int)p->dtype, p->head_dim, reinterpret_cast<hipStream_t>(stream),
+                                      trace ? ev(trace->partials_start) : nullptr,
+                                      trace ? ev(trace->partials_stop) : nullptr),
+                  "tree kernel");
+}
+
+parrot_status parrot_validate_tree_inputs(
+    const parrot_problem* p, const parrot_tree_rows* rows, const int32_t* query_offsets,
+    const int32_t* tree_parents, const int32_t* prefix_block_tables, const int32_t* prefix_lens,
+    const int32_t* prefix_parents, const int32_t* suffix_block_tables, const int32_t* suffix_lens,
+    const int32_t* group_ids, int32_t* scratch, void* stream) {
+  TreePlan pl;
+  PARROT_TRY(check_tree(p, rows, prefix_parents != nullptr, &pl));
+  if (rows->num_query_rows == 0) return set_error(PARROT_OK, "");
+  const parrot_prefill_rows as_prefill = {rows->num_query_rows, rows->max_query_rows, rows->max_group_rows};
+  const parrot::ValidateTree tree = {tree_parents};
+  return parrot::validate_inputs(p, prefix_block_tables, prefix_lens, prefix_parents, suffix_block_tables,
+                                 suffix_lens, group_ids, scratch, stream, &as_prefill, query_offsets, &tree);
+}
+
+// --------------------------------------------------------- accept and commit
+parrot_status parrot_tree_accept(
+    int32_t num_requests, const parrot_tree_rows* rows, const int32_t* query_offsets, const int32_t* tree_parents,
+    const int32_t* draft_tokens, const int32_t* target_tokens, const int32_t* root_tokens, int32_t* accept_rows,
+    int32_t* accept_lens, int32_t* next_tokens, void* stream, const parrot_trace* trace) {
+  if (num_requests < 0) return bad("num_requests %ld < 0", num_requests);
+  PARROT_TRY(check_tree_counts(num_requests, rows));
+  if (num_requests == 0) return set_error(PARROT_OK, "");
+  const parrot::PtrCheck need[] = {{query_offsets, "query_offsets", 4}, {root_tokens, "root_tokens", 4},
+                                   {accept_lens, "accept_lens", 4}, {next_tokens, "next_tokens", 4}};
+  PARROT_TRY(parrot::check_pointers(need));
+  if (rows->num_query_rows > 0) {
+    const parrot::PtrCheck more[] = {{draft_tokens, "draft_tokens", 4}, {target_tokens, "target_tokens", 4},
+                                     {accept_rows, "accept_rows", 4}};
+    PARROT_TRY(parrot::check_pointers(more));
+    if (tree_parents && reinterpret_cast<uintptr_t>(tree_parents) % 4) return bad("tree_parents is not 4-byte aligned");
+  }
+  const void* outs[] = {accept_rows, accept_lens, next_tokens};
+  const void* ins[] = {query_offsets, tree_parents, draft_tokens, target_tokens, root_tokens};
+  for (const void* o : outs)
+    for (const void* i : ins)
+      if (o && o == i) return bad("an output array is also an input");
+  parrot::AcceptArgs a{};
+  a.qoff = query_offsets; a.parents = tree_parents; a.draft = draft_tokens; a.target = target_tokens;
+  a.root = root_tokens; a.rows = accept_rows; a.lens = accept_lens; a.next = next_tokens;
+  a.R = num_requests; a.T = rows->num_query_rows; a.max_q = rows->num_query_rows > 0 ? rows->max_query_rows : 0;
+  return launched(parrot::launch_accept(a, reinterpret_cast<hipStream_t>(stream),
+                                        trace ? ev(trace->partials_start) : nullptr,
+                                        trace ? ev(trace->partials_stop) : nullptr),
+                  "accept kernel");
+}
+
+parrot_status parrot_tree_commit(
+    const parrot_problem* p, const parrot_tree_rows* rows, const int32_t* query_offsets, const int32_t* accept_rows,
+    const int32_t* accept_lens, const int32_t* suffix_block_tables, const int32_t* suffix_lens, void* suffix_k,
+    void* suffix_v, int32_t* committed_lens, void* stream, const parrot_trace* trace) {
+  PARROT_TRY(parrot::check_problem_fields(p));
+  PARROT_TRY(check_tree_counts(p->num_requests, rows));
+  if (p->num_requests == 0) return set_error(PARROT_OK, "");
+  if (rows->num_query_rows > 0 && rows->max_query_rows > p->max_suffix_len)
+    return bad("max_query_rows %ld > max_suffix_len %ld", rows->max_query_rows, p->max_suffix_len);
+  const parrot::PtrCheck need[] = {{query_offsets, "query_offsets", 4}, {accept_lens, "accept_lens", 4},
+                                   {suffix_block_tables, "suffix_block_tables", 4}, {suffix_lens, "suffix_lens", 4},
+                                   {suffix_k, "suffix_k", 16}, {suffix_v, "suffix_v", 16},
+                                   {committed_lens, "committed_lens", 4}};
+  PARROT_TRY(parrot::check_pointers(need));
+  if (rows->num_query_rows > 0) {
+    const parrot::PtrCheck more[] = {{accept_rows, "accept_rows", 4}};
+    PARROT_TRY(parrot::check_pointers(more));
+  }
+  if (committed_lens == suffix_lens || committed_lens == accept_lens || committed_lens == accept_rows ||
+      committed_lens == query_offsets)
+    return bad("committed_lens is also an input");
+  if (suffix_k == suffix_v) return bad("suffix_k and suffix_v are the same pool");
+  if ((long)p->num_suffix_blocks * p->block_size > 0x7fffffffL || (long)p->num_requests * ceil_div(p->num_heads, 8) > 0x7fffffffL)
+    return set_error(PARROT_ERR_UNSUPPORTED, "commit: num_suffix_blocks %d or num_requests %d too large",
+                     p->num_suffix_blocks, p->num_requests);
+  parrot::CommitArgs a{};
+  a.qoff = query_offsets; a.rows = accept_rows; a.lens = accept_lens;
+  a.stab = suffix_block_tables; a.slen = suffix_lens;
+  a.sk = suffix_k; a.sv = suffix_v; a.committed = committed_lens;
+  a.R = p->num_requests; a.T = rows->num_query_rows; a.H = p->num_heads;
+  a.sstride = p->suffix_table_stride; a.max_s = p->max_suffix_len;
+  a.max_q = rows->num_query_rows > 0 ? rows->max_query_rows : 0; a.nsblk = p->num_suffix_blocks;
+  return launched(parrot::launch_commit(a, (int)p->dtype, p->head_dim, reinterpret_cast<hipStream_t>(stream),
+                                        trace ? ev(trace->partials_start) : nullptr,
+                                        trace ? ev(trace->partials_stop) : nullptr),
+                  "commit kernel");
+}
+
+}  // extern "C"

@@ -167,7 +167,8 @@ hipError_t launch_merge(const MergeArgs& a, int dtype, int D, hipStream_t s, hip
 // too deep; prefill rows: 9 bad row offsets, 10 too many rows for a request,
 // 11 too many rows reading a group; decode: 12 more requests read a group's
 // prefix than max_group_size (the prefix role sizes its query tiles from that
-// bound, so readers past it would get no prefix partial).  result[1] is the
+// bound, so readers past it would get no prefix partial); tree rows: 13 offsets that
+// end outside [0, T], 14 a bad parent.  result[1] is the
 // entry index, result[2] the offending value.
 PARROT_DEV void report(int* res, int code, int idx, int val) {
   if (atomicCAS(res, 0, code) == 0) { res[1] = idx; res[2] = val; }
@@ -206,12 +207,18 @@ __global__ __launch_bounds__(256) void k_validate(ValidateArgs a) {
   if (a.qoff) {
     if (threadIdx.x == 0) {
       if (a.qoff[0] != 0) report(a.result, 9, 0, a.qoff[0]);
-      if (a.qoff[a.R] != a.T) report(a.result, 9, a.R, a.qoff[a.R]);
+      const int end = a.qoff[a.R];
+      if (a.padded ? end < 0 || end > a.T : end != a.T) report(a.result, a.padded ? 13 : 9, a.R, end);
     }
     for (int r = threadIdx.x; r < a.R; r += blockDim.x) {
       const long n = (long)a.qoff[r + 1] - a.qoff[r];
       if (n < 0) { report(a.result, 9, r + 1, a.qoff[r + 1]); continue; }
-      if (n > a.slen[r] || n > a.max_q) report(a.result, 10, r, (int)n);
+      if (n > a.slen[r] || n > a.max_q) { report(a.result, 10, r, (int)n); continue; }
+      if (a.tree && a.qoff[r] >= 0 && a.qoff[r + 1] <= a.T)
+        for (int j = 0; j < (int)n; ++j) {
+          const int par = a.tree[a.qoff[r] + j];
+          if (par < -1 || par >= j) { report(a.result, 14, a.qoff[r] + j, par); break; }
+        }
     }
   }
   // readers of each group's prefix: its members and its descendants' members

@@ -1,0 +1,32 @@
+// Arguments of the tree-decode kernels, shared by the kernels and the host code.
+#pragma once
+
+#include "draft_args.h"
+
+namespace parrot {
+
+// Columns of a tree tile: (row, query head) pairs that read one cache head.  Four
+// waves with sets of 16 columns each.
+constexpr int kTreeSets16 = 2;           // 16-bit caches: 128 columns
+constexpr int kTreeSets32 = 1;           // fp32 caches: 64 columns
+constexpr int tree_cols(int dtype) { return 64 * (dtype == kF32 ? kTreeSets32 : kTreeSets16); }
+constexpr int kTreeSpan = 128;           // key blocks whose ids are held at a time
+
+struct TreeArgs {
+  const void* q;                         // [T][HQ][D]
+  const void* pk; const void* pv;
+  const void* sk; const void* sv;
+  const int* ptab; const int* plen; const int* stab; const int* slen; const int* gid;
+  const int* parents;                    // nested groups (NULL: flat)
+  const int* qoff;                       // [R + 1]
+  const int* tree;                       // drafted rows' parents (NULL: chains)
+  void* out; float* lse;                 // [T][HQ][D] dtype, [T][HQ]
+  int T, R, H, G, NG, depth;             // G query heads per cache head
+  int pstride, sstride, max_p, max_s, max_q, npblk, nsblk;
+  int tiles;                             // column tiles per request
+  float scale_log2;
+};
+
+hipError_t launch_tree(const TreeArgs& a, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
+
+}  // namespace parrot

@@ -1,0 +1,479 @@
+// The tree-decode query tile on MFMA (gfx950): up to 128 (fp32 caches: 64) columns
+// against ranges of paged key sequences.
+//
+// A column is one (drafted row, query head) pair; the columns of a tile read the same
+// cache head, so with grouped queries a key fetched once serves G heads of every row.
+// Per 16-token block
+//   S^T  = K Q^T    (tokens x columns)      v_mfma_f32_16x16x32_{f16,bf16} / 16x16x4f32
+//   O^T += V^T P^T  (D x columns)
+// with an online softmax in fp32 whose reference moves only when a column's logits
+// exceed it by more than 2^8 (as the prefill tile's), so most blocks need no
+// cross-lane maximum.  Probabilities are rounded to the cache's type for the product
+// (16-bit caches), and the output is divided by the sum of the rounded ones, so a
+// dominant weight's rounding cancels; the lse keeps the sum of the unrounded ones.
+//
+// Keys and values pass through LDS in 16 KiB stages (8 of each: 32 tokens of 128
+// 16-bit elements) by direct-to-LDS loads into a ring of three, two stages ahead.
+// Column sets of 16 go round the waves (set w + 4 c to wave w), so a tile of up to 64
+// columns gives each wave one set.
+//
+// Mask: drafted tokens follow the cached ones, from own position `base` on.  The
+// bits of the tokens a column sees are kept per 32-token word counted from base
+// rounded down to 32 (bits below base set, bits past the last token clear), so a
+// pair of blocks takes one word per column and needs no other test.
+//
+// A drafted token's value that is no finite number must not reach the columns that
+// do not see it, though its probability there is 0 (0 * NaN).  Stages that hold
+// drafted tokens are scanned: such elements are cleared in LDS, and added afterwards,
+// element by element, to the columns that see them.
+#pragma once
+
+#include <cfloat>
+
+#include "prefill_tile.h"
+#include "tree_args.h"
+
+namespace parrot {
+
+namespace tree_detail {
+
+using namespace prefix_detail;
+
+template <int DT> constexpr int kSets = DT == kF32 ? kTreeSets32 : kTreeSets16;
+template <int DT> constexpr int kCols = 64 * kSets<DT>;
+constexpr int kRing3 = 3;
+constexpr int kMaskWords = (kTreeRows + 31 + 31) / 32;      // a request's rows from any alignment
+
+template <int DT>
+struct Lds {
+  char ring[kRing3][kStageBytes];
+  unsigned mask[kMaskWords][kCols<DT>];   // visible drafted tokens of each column
+  int tbl[kTreeSpan];                     // block ids of the current span, clamped
+  unsigned bad[kRing3][4];                // tokens of a stage with cleared values, a bit each
+};
+// three workgroups of a CU share its 160 KiB, handed out in pieces of 1280 bytes
+static_assert(sizeof(Lds<kF16>) <= 42 * 1280, "three workgroups per CU");
+
+// Swizzle of a stage's rows (see the two tiles this follows).
+template <int DT, int D>
+PARROT_DEV int swizzle(int t) {
+  if constexpr (DT == kF32) return swz(t);
+  else return swz_wide<D * 2 / 16>(t);
+}
+
+PARROT_DEV bool any_nonfinite16(const u32x4& v, unsigned expo) {   // expo: the type's exponent mask
+  bool bad = false;
+  const unsigned w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    bad = bad || (w[i] & expo) == expo || ((w[i] >> 16) & expo) == expo;
+  return bad;
+}
+// the 16 bytes with every element that is no finite number cleared; true if any was
+template <int DT>
+PARROT_DEV bool clear_nonfinite(u32x4& v) {
+  unsigned w[4] = {v.x, v.y, v.z, v.w};
+  bool bad = false;
+  if constexpr (DT == kF32) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if ((w[i] & 0x7F800000u) == 0x7F800000u) { w[i] = 0u; bad = true; }
+  } else {
+    constexpr unsigned expo = DT == kF16 ? 0x7C00u : 0x7F80u;
+    if (!any_nonfinite16(v, expo)) return false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if ((w[i] & expo) == expo) w[i] &= 0xFFFF0000u;
+      if (((w[i] >> 16) & expo) == expo) w[i] &= 0x0000FFFFu;
+    }
+    bad = true;
+  }
+  v = u32x4{w[0], w[1], w[2], w[3]};
+  return bad;
+}
+
+template <int DT>
+PARROT_DEV float elem_at(const char* p) {
+  if constexpr (DT == kF32) return *reinterpret_cast<const float*>(p);
+  else if constexpr (DT == kF16) return (float)*reinterpret_cast<const _Float16*>(p);
+  else return __uint_as_float((unsigned)*reinterpret_cast<const unsigned short*>(p) << 16);
+}
+
+}  // namespace tree_detail
+
+// One key range of a tile.
+struct TreeRange {
+  const void* pk; const void* pv;   // pools
+  const int* tbl;                   // block table row of the sequence
+  int npool;                        // blocks in the pools
+  int t0, t1;                       // tokens [t0, t1), t0 a multiple of 32
+  int mask0;                        // first token of mask word 0 (a multiple of 32); tokens
+                                    // from there on go by the mask.  t1 or more: no mask
+  int base, end;                    // masked ranges: the drafted tokens are [base, end)
+};
+
+// The tile's state: columns, softmax statistics and output, in registers.
+template <int DT, int D>
+struct TreeTile {
+  static constexpr int NS = tree_detail::kSets<DT>;
+  static constexpr int EB = Elem<DT>::kBytes;
+  static constexpr int ROW_B = D * EB;
+  static constexpr int GRAN = ROW_B / 16;                    // 16-byte granules per row
+  static constexpr int BLK_B = kBlock * ROW_B;               // one block of one head
+  static constexpr int STAGE_BLK = prefix_detail::kTensorStage / BLK_B;
+  static constexpr int DT16 = D / 16;
+  static constexpr int KS = DT == kF32 ? D / 4 : D / 32;     // MFMA k-steps over D
+  static constexpr int PER_WAVE = prefix_detail::kStageChunks / 4;
+  static constexpr float kLazy = 8.f;
+  using L = tree_detail::Lds<DT>;
+
+  L& lds;
+  int lane, wave, H, h;
+  float scale, inv_scale;
+  unsigned qsign;
+  bool act[NS];                       // wave-uniform: the set has columns
+  u32x4 qf[NS][DT == kF32 ? 1 : KS];
+  float qs[NS][DT == kF32 ? KS : 1];
+  float mref[NS], thr[NS], lsum[NS], lsr[NS];
+  f32x4 o[NS][DT16];
+
+  PARROT_DEV TreeTile(L& l, int heads, int head, float scale_log2) : lds(l), H(heads), h(head) {
+    lane = threadIdx.x & 63;
+    wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // a negative scale flips the sign of q (exact); a zero scale is taken as 1e-30
+    scale = fmaxf(fabsf(scale_log2), 1e-30f);
+    inv_scale = 1.f / scale;
+    qsign = scale_log2 < 0.f ? (DT == kF32 ? 0x80000000u : 0x80008000u) : 0u;
+  }
+  // column of the tile that this lane holds in set c
+  PARROT_DEV int column(int c) const { return (wave + 4 * c) * 16 + (lane & 15); }
+
+  // Loads the queries of `ncols` columns; qrow(col) is the column's row of q in units
+  // of heads (row * HQ + query head).
+  template <class F>
+  PARROT_DEV void load_queries(const void* q, int ncols, F qrow) {
+#pragma unroll
+    for (int c = 0; c < NS; ++c) {
+      act[c] = (wave + 4 * c) * 16 < ncols;
+      const int col = column(c);
+      const bool ok = col < ncols;
+      const char* src = (const char*)q + (size_t)(ok ? qrow(col) : 0) * ROW_B;
+      if constexpr (DT == kF32) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const float x = ok ? reinterpret_cast<const float*>(src)[4 * ks + (lane >> 4)] : 0.f;
+          qs[c][ks] = __uint_as_float(__float_as_uint(x) ^ qsign);
+        }
+      } else {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const u32x4 x = ok ? ld16(src + (32 * ks + 8 * (lane >> 4)) * 2) : u32x4{0u, 0u, 0u, 0u};
+          qf[c][ks] = x ^ u32x4{qsign, qsign, qsign, qsign};
+        }
+      }
+      mref[c] = -FLT_MAX; thr[c] = -INFINITY; lsum[c] = 0.f; lsr[c] = 0.f;
+#pragma unroll
+      for (int i = 0; i < DT16; ++i) o[c][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+
+  // S^T of one block for set c; kb: the block's K in LDS
+  PARROT_DEV f32x4 scores32(const char* kb, int c) const {
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    const int row = lane & 15;
+    const char* krow = kb + row * ROW_B + 4 * (lane >> 4);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const float kv = *reinterpret_cast<const float*>(krow + ((ks ^ tree_detail::swizzle<DT, D>(row)) << 4));
+      s = __builtin_amdgcn_mfma_f32_16x16x4f32(kv, qs[c][ks], s, 0, 0, 0);
+    }
+    return s;
+  }
+
+  // Softmax step of set c over NX logits a lane: token tok0 + 16 (i / 4) + 4 (lane / 16) + i % 4
+  // is visible where its bit of `vis` (from tok0 on) is set.  x becomes the
+  // probabilities.
+  template <int NX>
+  PARROT_DEV void softmax(float* x, int c, unsigned vis) {
+    const unsigned mine = vis >> (4 * (lane >> 4));
+    if (__builtin_amdgcn_ballot_w64(vis != (NX == 8 ? 0xFFFFFFFFu : 0xFFFFu)) != 0) {
+#pragma unroll
+      for (int i = 0; i < NX; ++i) x[i] = (mine >> ((i >> 2) * 16 + (i & 3))) & 1u ? x[i] : -INFINITY;
+    }
+    float lm = x[0];
+#pragma unroll
+    for (int i = 1; i < NX; ++i) lm = fmaxf(lm, x[i]);
+    if (__builtin_amdgcn_ballot_w64(lm > thr[c]) != 0) {
+      const float mn = fmaxf(mref[c], max_xor32(max_xor16(lm)) * scale);
+      const float alpha = fast_exp2(mref[c] - mn);
+      lsum[c] *= alpha;
+      lsr[c] *= alpha;
+#pragma unroll
+      for (int i = 0; i < DT16; ++i) o[c][i] *= alpha;
+      mref[c] = mn;
+      thr[c] = (mn + kLazy) * inv_scale;
+    }
+    float ps = 0.f;
+#pragma unroll
+    for (int i = 0; i < NX; ++i) {
+      x[i] = fast_exp2(__builtin_fmaf(x[i], scale, -mref[c]));
+      ps += x[i];
+    }
+    lsum[c] += ps;
+  }
+
+  // Adds the cleared elements of the values (see the head of this file) of the tokens in
+  // `bad` (from tok0 on) to set c: p are the lane's probabilities, vis its column's bits.
+  template <int NX>
+  PARROT_DEV void add_cleared(const TreeRange& rg, int span0, const float* p, int c, unsigned vis, unsigned bad, int tok0) {
+    while (bad) {                                            // wave-uniform
+      const int t = __ffs((int)bad) - 1;
+      bad &= bad - 1;
+      float mine = 0.f;                                      // held by lane group (t % 16) / 4
+#pragma unroll
+      for (int i = 0; i < NX; ++i)
+        if (i == (t >> 4) * 4 + (t & 3)) mine = p[i];
+      const float pt = __shfl(mine, (lane & 15) + 16 * ((t & 15) >> 2));
+      const int tok = tok0 + t;
+      const int blk = lds.tbl[tok / kBlock - span0];
+      const char* row = (const char*)rg.pv + (((size_t)blk * H + h) * kBlock + tok % kBlock) * ROW_B;
+#pragma unroll
+      for (int dt = 0; dt < DT16; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float v = tree_detail::elem_at<DT>(row + (dt * 16 + 4 * (lane >> 4) + i) * EB);
+          if (!(fabsf(v) <= FLT_MAX) && ((vis >> t) & 1u)) o[c][dt][i] = __builtin_fmaf(pt, v, o[c][dt][i]);
+        }
+    }
+  }
+
+  // One pair of blocks (32 tokens from tok0) of a stage; 16-bit caches.
+  template <bool MASKED>
+  PARROT_DEV void pair(const TreeRange& rg, int span0, int buf, int bl, int tok0) {
+    using namespace prefix_detail;
+    const char* kb = lds.ring[buf] + bl * BLK_B;
+    const char* vb = kb + kTensorStage;
+    const int krow = lane & 15;
+    unsigned pw[NS][4];
+    f32x4 s[NS][2];
+#pragma unroll
+    for (int c = 0; c < NS; ++c) s[c][0] = s[c][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const int off = krow * ROW_B + (((4 * ks + (lane >> 4)) ^ tree_detail::swizzle<DT, D>(krow)) << 4);
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const u32x4 kf = *reinterpret_cast<const u32x4*>(kb + b * BLK_B + off);
+#pragma unroll
+        for (int c = 0; c < NS; ++c)
+          if (act[c]) s[c][b] = Mfma<DT>::qk(kf, qf[c][ks], s[c][b]);
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < NS; ++c) {
+      if (!act[c]) continue;
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { x[i] = s[c][0][i]; x[4 + i] = s[c][1][i]; }
+      unsigned vis = 0xFFFFFFFFu;
+      if constexpr (MASKED) {
+        if (tok0 >= rg.mask0) vis = lds.mask[(tok0 - rg.mask0) >> 5][column(c)];
+        else if (rg.t1 - tok0 < 32) vis = (1u << (rg.t1 - tok0)) - 1u;
+      }
+      softmax<8>(x, c, vis);
+      if constexpr (MASKED) {
+        const unsigned bad = __builtin_amdgcn_readfirstlane(lds.bad[buf][bl >> 1]);
+        if (bad) add_cleared<8>(rg, span0, x, c, vis, bad, tok0);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        pw[c][i] = pack2<DT>(x[2 * i], x[2 * i + 1]);
+        lsr[c] = add_pair<DT>(pw[c][i], lsr[c]);
+      }
+    }
+    const int vrow = 4 * (lane >> 4) + ((lane & 15) >> 2);
+    const char* va = vb + vrow * ROW_B + 8 * (lane & 1);
+#pragma unroll
+    for (int dt = 0; dt < DT16; ++dt) {
+      const int off = ((2 * dt + ((lane & 3) >> 1)) ^ tree_detail::swizzle<DT, D>(vrow)) << 4;
+      const unsigned long long v0 = Mfma<DT>::tr_read(va + off), v1 = Mfma<DT>::tr_read(va + BLK_B + off);
+#pragma unroll
+      for (int c = 0; c < NS; ++c) {
+        if (!act[c]) continue;
+        const unsigned long long b0 = pw[c][0] | ((unsigned long long)pw[c][1] << 32);
+        const unsigned long long b1 = pw[c][2] | ((unsigned long long)pw[c][3] << 32);
+        o[c][dt] = Mfma<DT>::pv2(v0, v1, b0, b1, o[c][dt]);
+      }
+    }
+  }
+
+  // One block (16 tokens from tok0) of a stage; fp32 caches.
+  template <bool MASKED>
+  PARROT_DEV void block32(const TreeRange& rg, int span0, int buf, int bl, int tok0) {
+    const char* kb = lds.ring[buf] + bl * BLK_B;
+    const char* vb = kb + prefix_detail::kTensorStage;
+#pragma unroll
+    for (int c = 0; c < NS; ++c) {
+      if (!act[c]) continue;
+      const f32x4 s = scores32(kb, c);
+      float x[4] = {s[0], s[1], s[2], s[3]};
+      unsigned vis = 0xFFFFu;
+      if constexpr (MASKED) {
+        if (tok0 >= rg.mask0) vis = (lds.mask[(tok0 - rg.mask0) >> 5][column(c)] >> (tok0 & 16)) & 0xFFFFu;
+        else if (rg.t1 - tok0 < 16) vis = (1u << (rg.t1 - tok0)) - 1u;
+      }
+      softmax<4>(x, c, vis);
+      if constexpr (MASKED) {
+        const unsigned bad = __builtin_amdgcn_readfirstlane(lds.bad[buf][bl >> 1]) >> (16 * (bl & 1)) & 0xFFFFu;
+        if (bad) add_cleared<4>(rg, span0, x, c, vis, bad, tok0);
+      }
+      // O^T[d][col] += V^T[d][t] P^T[t][col] with k index kk <-> token 4 kk + kt
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt) {
+        const int row = 4 * (lane >> 4) + kt;
+        const char* vrow = vb + row * ROW_B + 4 * (lane & 3);
+#pragma unroll
+        for (int dt = 0; dt < DT16; ++dt) {
+          const float v = *reinterpret_cast<const float*>(
+              vrow + (((4 * dt + ((lane & 15) >> 2)) ^ tree_detail::swizzle<DT, D>(row)) << 4));
+          o[c][dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, x[kt], o[c][dt], 0, 0, 0);
+        }
+      }
+    }
+  }
+
+  // The range's tokens: every wave of the workgroup calls it, whether it has columns
+  // or not (all of them load and synchronise).
+  PARROT_DEV void run(const TreeRange& rg) {
+    using namespace prefix_detail;
+    for (int t = rg.t0; t < rg.t1; t += kTreeSpan * kBlock) {
+      const int b0 = t / kBlock;
+      const int nb = (min(rg.t1, t + kTreeSpan * kBlock) - t + kBlock - 1) / kBlock;
+      __syncthreads();                                       // the LDS of what ran before is free
+      if ((int)threadIdx.x < nb) lds.tbl[threadIdx.x] = clampi(rg.tbl[b0 + threadIdx.x], 0, rg.npool - 1);
+      __syncthreads();
+      span(rg, b0, nb);
+    }
+  }
+
+  PARROT_DEV void span(const TreeRange& rg, int b0, int nb) {
+    using namespace prefix_detail;
+    const int tid = threadIdx.x;
+    const size_t blk_stride = (size_t)H * BLK_B;
+    const int nstages = (nb + STAGE_BLK - 1) / STAGE_BLK, last = nstages - 1;
+    // Direct-to-LDS loads: wave w issues the 1 KiB chunks w, w + 4, ... of a stage;
+    // lane l fills bytes [16 l, 16 l + 16) of its chunk from the granule that the
+    // swizzle puts there.
+    int c_bl[PER_WAVE];
+    unsigned c_src[PER_WAVE];
+    bool c_v[PER_WAVE];
+#pragma unroll
+    for (int j = 0; j < PER_WAVE; ++j) {
+      const int q = wave + j * 4;
+      const int off = (q % (kStageChunks / 2)) * 1024 + lane * 16;
+      c_v[j] = q >= kStageChunks / 2;
+      c_bl[j] = off / BLK_B;
+      const int t = (off % BLK_B) / ROW_B, pos = (off % ROW_B) / 16;
+      c_src[j] = (unsigned)(h * BLK_B + t * ROW_B + ((pos ^ tree_detail::swizzle<DT, D>(t)) << 4));
+    }
+    int tb[PER_WAVE];
+    auto table = [&](int st) {
+#pragma unroll
+      for (int j = 0; j < PER_WAVE; ++j) tb[j] = lds.tbl[min(st * STAGE_BLK + c_bl[j], nb - 1)];   // past the end: re-read
+    };
+    auto issue = [&](int buf) {
+#pragma unroll
+      for (int j = 0; j < PER_WAVE; ++j) {
+        const unsigned blk = min((unsigned)__builtin_amdgcn_readfirstlane(tb[j]), (unsigned)(rg.npool - 1));
+        const char* base = (const char*)(c_v[j] ? rg.pv : rg.pk) + (size_t)blk * blk_stride;
+        lds_dma16_sbase(base, c_src[j], lds_addr(&lds.ring[buf][(wave + j * 4) * 1024]));
+      }
+    };
+    table(0);
+    issue(0);
+    table(min(1, last));
+    issue(1);
+    table(min(2, last));
+    // the compiler tracks the query loads but not the direct-to-LDS ones: it waits for
+    // the queries here, once, and not inside the loop
+#pragma unroll
+    for (int c = 0; c < NS; ++c) {
+      if constexpr (DT == kF32) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) asm volatile("" : : "v"(qs[c][ks]));
+      } else {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) asm volatile("" : : "v"(qf[c][ks]));
+      }
+    }
+    wait_vmcnt<0>();
+    int buf = 0;
+    for (int st = 0; st < nstages; ++st) {
+      wait_vmcnt<PER_WAVE>();            // this stage's loads are the oldest two rounds'
+      lds_sync();
+      const int tok_st = (b0 + st * STAGE_BLK) * kBlock;
+      const bool masked = tok_st + STAGE_BLK * kBlock > min(rg.t1, rg.mask0);   // workgroup-uniform
+      if (masked) {
+        // rows past the range end are cleared (0 * NaN), and the values of drafted
+        // tokens that are no finite numbers, with a bit for their token
+        if (tid < 4) lds.bad[buf][tid] = 0u;
+        lds_sync();
+        const int stop = min(rg.t1, rg.end);
+        for (int i = tid; i < kTensorStage / 16; i += 256) {
+          const int row = i / GRAN, tok = tok_st + row;
+          if (tok >= rg.base) {
+            u32x4* at = reinterpret_cast<u32x4*>(lds.ring[buf] + kTensorStage + i * 16);
+            u32x4 v = u32x4{0u, 0u, 0u, 0u};
+            bool write = tok >= stop;
+            if (!write) {
+              v = *at;
+              write = tree_detail::clear_nonfinite<DT>(v);
+              if (write) atomicOr(&lds.bad[buf][row >> 5], 1u << (row & 31));
+            }
+            if (write) *at = v;
+          }
+        }
+        lds_sync();
+      }
+      const int next = buf == 0 ? 2 : buf - 1;               // (st + 2) % 3
+      issue(next);
+      table(min(st + 3, last));
+      if (act[0]) {
+        if constexpr (DT == kF32) {
+#pragma unroll 1
+          for (int bl = 0; bl < STAGE_BLK; ++bl) {
+            const int tok0 = tok_st + bl * kBlock;
+            if (tok0 >= rg.t1) break;
+            if (masked) block32<true>(rg, b0, buf, bl, tok0);
+            else block32<false>(rg, b0, buf, bl, tok0);
+          }
+        } else {
+#pragma unroll 1
+          for (int bl = 0; bl < STAGE_BLK; bl += 2) {
+            const int tok0 = tok_st + bl * kBlock;
+            if (tok0 >= rg.t1) break;
+            if (masked) pair<true>(rg, b0, buf, bl, tok0);
+            else pair<false>(rg, b0, buf, bl, tok0);
+          }
+        }
+      }
+      buf = buf == 2 ? 0 : buf + 1;
+    }
+    wait_vmcnt<0>();                     // the re-read stages issued by the last iterations
+  }
+
+  // The tile's result: f(c, col, value(dt) scaled, lse2) per set with columns; the lane
+  // holds elements dt * 16 + 4 (lane / 16) .. + 3 of its column.
+  template <class F>
+  PARROT_DEV void finish(F f) {
+#pragma unroll
+    for (int c = 0; c < NS; ++c) {
+      if (!act[c]) continue;
+      const float lt = sum_xor32(sum_xor16(lsum[c]));
+      const float lw = DT == kF32 ? lt : sum_xor32(sum_xor16(lsr[c]));
+      f(c, column(c), lw, mref[c] + fast_log2(lt), lt);
+    }
+  }
+};
+
+}  // namespace parrot

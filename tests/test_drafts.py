@@ -1,0 +1,291 @@
+"""A drafting step on the host: refusals before any device work, rotary embeddings,
+the store's truncation, and pins of the oracle the GPU tests compare with."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import drafts_util as du
+import paper_2405_19888_amd as parrot
+from drafts_util import oracle
+from oracle import shared_prefix_prefill
+from paper_2405_19888_amd import binding as B
+from paper_2405_19888_amd.context import ContextStore
+
+FAKE = 1 << 20          # aligned fake device addresses: never dereferenced here
+
+
+def problem(**over):
+    kw = dict(num_requests=8, num_heads=4, head_dim=128, block_size=16, num_groups=2, max_group_size=8,
+              max_prefix_len=500, max_suffix_len=300, prefix_table_stride=32, suffix_table_stride=19,
+              num_prefix_blocks=100, num_suffix_blocks=100, dtype=1, sm_scale=0.1)
+    kw.update(over)
+    return B.make_problem(**kw)
+
+
+def fill_rows(**over):
+    kw = dict(num_query_rows=20, max_query_rows=10, num_query_heads=8, norm_eps=1e-6, q_stride=1024, k_stride=512,
+              v_stride=512)
+    kw.update(over)
+    return B.ParrotFillRows(*kw.values())
+
+
+def addresses(names, over):
+    vals = {n: FAKE + 4096 * i for i, n in enumerate(names)}
+    vals.update(over)
+    return [vals[n] for n in names]
+
+
+FILL = ["q", "k", "v", "q_norm", "k_norm", "positions", "query_offsets", "suffix_block_tables", "suffix_lens", "q_out",
+        "suffix_k", "suffix_v"]
+TREE = ["q", "query_offsets", "tree_parents", "prefix_k", "prefix_v", "suffix_k", "suffix_v", "prefix_block_tables",
+        "prefix_lens", "prefix_parents", "suffix_block_tables", "suffix_lens", "group_ids", "out", "lse", "workspace"]
+ACCEPT = ["query_offsets", "tree_parents", "draft_tokens", "target_tokens", "root_tokens", "accept_rows",
+          "accept_lens", "next_tokens"]
+COMMIT = ["query_offsets", "accept_rows", "accept_lens", "suffix_block_tables", "suffix_lens", "suffix_k", "suffix_v",
+          "committed_lens"]
+
+
+def call(lib, fn, prob=None, rows=None, rotary=None, requests=8, ws=1 << 45, **over):
+    prob = problem() if prob is None else prob
+    if fn == "parrot_rotary_fill":
+        rows = fill_rows() if rows is None else rows
+        return lib.parrot_rotary_fill(ctypes.byref(prob), ctypes.byref(rows), rotary, *addresses(FILL, over), None, None)
+    rows = parrot.make_tree_rows(20, 10, 20, 8) if rows is None else rows
+    if fn == "parrot_shared_prefix_tree_decode":
+        return lib.parrot_shared_prefix_tree_decode(ctypes.byref(prob), ctypes.byref(rows), *addresses(TREE, over), ws,
+                                                    None, None)
+    if fn == "parrot_tree_accept":
+        return lib.parrot_tree_accept(requests, ctypes.byref(rows), *addresses(ACCEPT, over), None, None)
+    return lib.parrot_tree_commit(ctypes.byref(prob), ctypes.byref(rows), *addresses(COMMIT, over), None, None)
+
+
+def test_struct_layouts():
+    assert ctypes.sizeof(B.ParrotRotary) == 16 + 64 * 8
+    assert ctypes.sizeof(B.ParrotRotaryConfig) == 8 + 8 + 8 + 5 * 8
+    assert ctypes.sizeof(B.ParrotFillRows) == 4 * 4 + 3 * 8
+    assert ctypes.sizeof(B.ParrotTreeRows) == 4 * 4
+
+
+@pytest.mark.parametrize("fn,names,optional", [
+    ("parrot_rotary_fill", FILL, {"q_norm", "k_norm", "positions"}),
+    ("parrot_shared_prefix_tree_decode", TREE, {"tree_parents", "prefix_parents"}),
+    ("parrot_tree_accept", ACCEPT, {"tree_parents"}),
+    ("parrot_tree_commit", COMMIT, set())])
+def test_pointers(parrot_lib, fn, names, optional):
+    """Every pointer is refused when NULL (but for the optional ones) or misaligned."""
+    for n in names:
+        if n not in optional:
+            assert call(parrot_lib, fn, **{n: None}) == B.PARROT_ERR_INVALID_ARGUMENT, n
+            assert "NULL" in B.parrot_last_error(), n
+        if n != "positions":             # (unused without a rotation)
+            assert call(parrot_lib, fn, **{n: FAKE + 1}) == B.PARROT_ERR_INVALID_ARGUMENT, n
+            assert "aligned" in B.parrot_last_error(), n
+    rot = ctypes.byref(parrot.make_rotary(64))
+    if fn == "parrot_rotary_fill":
+        for bad in (None, FAKE + 2):
+            assert call(parrot_lib, fn, rotary=rot, positions=bad) == B.PARROT_ERR_INVALID_ARGUMENT
+
+
+@pytest.mark.parametrize("over,msg", [
+    (dict(num_query_rows=-1), "num_query_rows"), (dict(max_query_rows=0), "max_query_rows"),
+    (dict(max_query_rows=301), "max_query_rows"), (dict(num_query_heads=0), "num_query_heads"),
+    (dict(norm_eps=-1.0), "norm_eps"), (dict(norm_eps=float("nan")), "norm_eps"),
+    (dict(q_stride=1016), "q_stride"), (dict(k_stride=516), "16 bytes"), (dict(v_stride=-512), "v_stride"),
+    (dict(q_stride=1 << 41), "q_stride")])
+def test_fill_refusals(parrot_lib, over, msg):
+    assert call(parrot_lib, "parrot_rotary_fill", rows=fill_rows(**over)) == B.PARROT_ERR_INVALID_ARGUMENT
+    assert msg in B.parrot_last_error()
+
+
+def test_fill_more_refusals(parrot_lib):
+    wide = ctypes.byref(parrot.make_rotary(128))
+    assert call(parrot_lib, "parrot_rotary_fill", prob=problem(head_dim=64), rotary=wide) == B.PARROT_ERR_INVALID_ARGUMENT
+    assert "head_dim" in B.parrot_last_error()
+    broken = parrot.make_rotary(64)
+    broken.rotary_dim = 63
+    assert call(parrot_lib, "parrot_rotary_fill", rotary=ctypes.byref(broken)) == B.PARROT_ERR_INVALID_ARGUMENT
+    assert call(parrot_lib, "parrot_rotary_fill", rows=fill_rows(q_stride=2048), q=FAKE, q_out=FAKE) == \
+        B.PARROT_ERR_INVALID_ARGUMENT
+    assert "q_out" in B.parrot_last_error()
+    assert call(parrot_lib, "parrot_rotary_fill", prob=problem(head_dim=80)) == B.PARROT_ERR_UNSUPPORTED
+    assert call(parrot_lib, "parrot_rotary_fill", prob=problem(num_requests=0)) == B.PARROT_ERR_INVALID_ARGUMENT
+    assert call(parrot_lib, "parrot_rotary_fill", rows=fill_rows(num_query_rows=0), k=None) == B.PARROT_OK
+
+
+@pytest.mark.parametrize("rows,msg,status", [
+    ((-1, 10, 20, 8), "num_query_rows", 1), ((20, 0, 20, 8), "max_query_rows", 1), ((20, 129, 20, 8), "128", 1),
+    ((20, 10, 21, 8), "max_group_rows", 1), ((20, 10, -1, 8), "max_group_rows", 1), ((20, 10, 20, 6), "multiple", 1),
+    ((20, 10, 20, 0), "multiple", 1), ((1 << 30, 128, 20, 8), "2^31", 2)])
+def test_tree_refusals(parrot_lib, rows, msg, status):
+    r = parrot.make_tree_rows(*rows)
+    assert call(parrot_lib, "parrot_shared_prefix_tree_decode", rows=r) == status
+    assert msg in B.parrot_last_error()
+    with pytest.raises(B.ParrotError, match=msg.replace("^", r"\^")):
+        parrot.parrot_tree_workspace_bytes(problem(), r)
+
+
+def test_tree_more_refusals(parrot_lib):
+    fn = "parrot_shared_prefix_tree_decode"
+    assert call(parrot_lib, fn, prob=problem(max_suffix_len=9, suffix_table_stride=1)) == B.PARROT_ERR_INVALID_ARGUMENT
+    assert call(parrot_lib, fn, prob=problem(sm_scale=float("inf"))) == B.PARROT_ERR_INVALID_ARGUMENT
+    assert call(parrot_lib, fn, rows=parrot.make_tree_rows(0, 0, 0, 0), q=None) == B.PARROT_OK
+    need = parrot.parrot_tree_workspace_bytes(problem(), parrot.make_tree_rows(20, 10, 20, 8))
+    if need:
+        assert call(parrot_lib, fn, ws=need - 1) == B.PARROT_ERR_WORKSPACE_TOO_SMALL
+
+
+def test_accept_and_commit_refusals(parrot_lib):
+    assert call(parrot_lib, "parrot_tree_accept", requests=-1) == B.PARROT_ERR_INVALID_ARGUMENT
+    assert call(parrot_lib, "parrot_tree_accept", requests=0, query_offsets=None,
+                rows=parrot.make_tree_rows(0, 0, 0, 0)) == B.PARROT_OK
+    assert call(parrot_lib, "parrot_tree_accept", requests=0) == B.PARROT_ERR_INVALID_ARGUMENT   # rows without requests
+    assert call(parrot_lib, "parrot_tree_accept", accept_rows=FAKE, tree_parents=FAKE) == B.PARROT_ERR_INVALID_ARGUMENT
+    for other in ("suffix_lens", "accept_lens"):
+        assert call(parrot_lib, "parrot_tree_commit", committed_lens=FAKE, **{other: FAKE}) == \
+            B.PARROT_ERR_INVALID_ARGUMENT
+        assert "committed_lens" in B.parrot_last_error()
+    assert call(parrot_lib, "parrot_tree_commit", suffix_k=FAKE, suffix_v=FAKE) == B.PARROT_ERR_INVALID_ARGUMENT
+    assert call(parrot_lib, "parrot_tree_commit", prob=problem(num_suffix_blocks=1 << 28)) == B.PARROT_ERR_UNSUPPORTED
+    with pytest.raises(ValueError):
+        parrot.tree_accept(torch.zeros(2, dtype=torch.int32), None, *[torch.zeros(1, dtype=torch.int32)] * 3)
+
+
+# ------------------------------------------------------------ rotary embeddings
+@pytest.mark.parametrize("scaling,kw", [("none", {}), ("linear", dict(factor=4.0)), ("ntk", dict(factor=8.0)),
+                                        ("yarn", dict(factor=16.0, original_length=4096)),
+                                        ("wavelength", dict(factor=8.0, original_length=8192)),
+                                        ("wavelength", dict(factor=2.0, original_length=512, low=0.5, high=3.0))])
+@pytest.mark.parametrize("rd,base", [(128, 10000.0), (64, 500000.0), (20, 10000.0)])
+def test_rotary_frequencies(parrot_lib, scaling, kw, rd, base):
+    rot = parrot.make_rotary(rd, base=base, scaling=scaling, **kw)
+    radians, amplitude = oracle.rotary_frequencies(rd, base, scaling, **kw)
+    assert rot.rotary_dim == rd and rot.amplitude == np.float32(amplitude)
+    for i, f in enumerate(radians):
+        # pow and the division by 2 pi: a few steps of 2^-53
+        assert abs(rot.turns[i] / 2.0 ** 64 - f / (2 * math.pi)) <= 16 * 2.0 ** -53 * f / (2 * math.pi) + 2.0 ** -64
+    same = parrot.rotary_from_frequencies(radians, amplitude=amplitude)
+    assert all(abs(same.turns[i] - rot.turns[i]) <= 16 * 2.0 ** -53 * rot.turns[i] + 1 for i in range(rd // 2))
+
+
+@pytest.mark.parametrize("kw", [
+    dict(rotary_dim=0), dict(rotary_dim=7), dict(rotary_dim=130), dict(base=1.0), dict(base=float("nan")),
+    dict(scaling="linear", factor=0.5), dict(scaling="yarn", factor=4.0), dict(scaling="ntk", rotary_dim=2, factor=2.0),
+    dict(scaling="yarn", factor=float("inf"), original_length=4096), dict(amplitude=-1.0),
+    dict(scaling="wavelength", factor=2.0, original_length=100, low=4.0, high=1.0), dict(amplitude=1e39)])
+def test_rotary_refusals(parrot_lib, kw):
+    with pytest.raises(B.ParrotError):
+        parrot.make_rotary(**{"rotary_dim": 64, **kw})
+
+
+def test_rotary_from_frequencies_refusals(parrot_lib):
+    for bad in ([-0.1], [7.0], [float("nan")], [0.1] * 65, []):
+        with pytest.raises(B.ParrotError):
+            parrot.rotary_from_frequencies(bad)
+    with pytest.raises(ValueError):
+        parrot.make_rotary(64, scaling="unknown")
+
+
+# -------------------------------------------------------------------- the store
+def test_truncate(parrot_lib):
+    st = ContextStore(16, 10)
+    c = st.fill(list(range(20)), [16])
+    for _ in range(30):
+        st.append(c)
+    assert st.own_tokens(c) == 34 and st.free_blocks == 10 - 1 - 3
+    st.truncate(c, 33)
+    assert st.free_blocks == 6 and st.own_tokens(c) == 33
+    st.truncate(c, 32)
+    assert st.free_blocks == 7
+    st.append(c)                                         # a new block again
+    assert st.free_blocks == 6 and st.own_tokens(c) == 33
+    table = st.build_batch([c]).suffix_tables[0].copy()
+    st.truncate(c, 20)
+    st.append(c)
+    assert np.array_equal(st.build_batch([c]).suffix_tables[0][:2], table[:2]) and st.own_tokens(c) == 21
+    for bad in (-1, 22):
+        with pytest.raises(B.ParrotError):
+            st.truncate(c, bad)
+    with pytest.raises(B.ParrotError):
+        st.truncate(c + 1, 0)
+    st.truncate(c, 0)
+    assert st.free_blocks == 9
+    st.free(c)
+    assert st.free_blocks == 10
+
+
+# ------------------------------------------------------------------ oracle pins
+def small_tree(parents, heads=2, ratio=2, dim=64, cached=5):
+    rows = [len(parents)]
+    plan = du.tree_plan("float32", heads, dim, [0], [7], [cached], rows, seed=1)
+    batch = du.make_batch(plan, seed=2)
+    return plan, batch, du.queries(rows[0], heads * ratio, dim, "float32")
+
+
+def tree_oracle(plan, batch, q, parents, **over):
+    kw = dict(sm_scale=plan.sm_scale)
+    kw.update(over)
+    return oracle.shared_prefix_tree(q, [0, q.shape[0]], parents, batch.k_pool, batch.v_pool, batch.k_pool,
+                                     batch.v_pool, plan.prefix_tables, plan.prefix_lens, plan.suffix_tables,
+                                     plan.suffix_lens, plan.group_ids, **kw)
+
+
+def test_tree_oracle_against_masked_attention():
+    parents = np.array([-1, 0, 0, 1, -1, 3])
+    plan, batch, q = small_tree(parents)
+    out, lse, _, _ = tree_oracle(plan, batch, q, parents)
+    seen = {0: [0], 1: [0, 1], 2: [0, 2], 3: [0, 1, 3], 4: [4], 5: [0, 1, 3, 5]}        # by hand
+    mask = torch.zeros(6, 18, dtype=torch.bool)
+    mask[:, :12] = True
+    for j, s in seen.items():
+        mask[j, [12 + a for a in s]] = True
+    from oracle import request_kv
+    K, V = request_kv(0, prefix_k=batch.k_pool, prefix_v=batch.v_pool, suffix_k=batch.k_pool, suffix_v=batch.v_pool,
+                      prefix_tables=plan.prefix_tables, prefix_lens=plan.prefix_lens, suffix_tables=plan.suffix_tables,
+                      suffix_lens=plan.suffix_lens, group_ids=plan.group_ids)
+    k, v = (torch.from_numpy(x).transpose(0, 1).repeat_interleave(2, 0) for x in (K, V))
+    want = torch.nn.functional.scaled_dot_product_attention(q.double().transpose(0, 1), k, v, attn_mask=mask,
+                                                            scale=plan.sm_scale).transpose(0, 1)
+    assert np.abs(out - want.numpy()).max() <= 1e-12
+
+
+def test_tree_oracle_chain_is_prefill():
+    plan, batch, q = small_tree([-1, 0, 1, 2], ratio=1)
+    for parents in (None, [-1, 0, 1, 2]):
+        out, lse, _, _ = tree_oracle(plan, batch, q, parents)
+        pout, plse = shared_prefix_prefill(q, [0, 4], batch.k_pool, batch.v_pool, batch.k_pool, batch.v_pool,
+                                           plan.prefix_tables, plan.prefix_lens, plan.suffix_tables, plan.suffix_lens,
+                                           plan.group_ids, plan.sm_scale)
+        assert np.abs(out - pout).max() <= 1e-12 and np.abs(lse - plse).max() <= 1e-12
+
+
+def test_rotate_keeps_lengths_and_relative_angles():
+    """A rotation keeps each pair's length, and the product of a query and a key depends
+    on the difference of their positions alone."""
+    rng = np.random.default_rng(0)
+    q, k = rng.normal(size=(1, 1, 64)), rng.normal(size=(1, 1, 64))
+    f, a = oracle.rotary_frequencies(64)
+    for inter in (False, True):
+        turn = lambda x, p: oracle.rotate(x, [p], f, inter, a)[0]
+        assert abs((turn(q, 77) ** 2).sum() - (q ** 2).sum()) <= 1e-10
+        assert abs((turn(q, 5) * turn(k, 2)).sum() - (turn(q, 1003) * turn(k, 1000)).sum()) <= 1e-9
+        assert np.abs(turn(q, 0) - q).max() == 0
+    # pair (1, 0) at a quarter turn becomes (0, 1)
+    x = np.zeros((1, 1, 4))
+    x[0, 0, 0] = 1
+    y = oracle.rotate(x, [1], [math.pi / 2, 0.0], False, 1.0)[0][0, 0]
+    assert np.allclose(y, [0, 0, 1, 0], atol=1e-15)
+
+
+def test_accept_oracle_by_hand():
+    # rows 0 and 1 start; 2 and 3 follow 0; 4 follows 3; tokens 9 from the root, 5 after row 0, 6 after row 3
+    up, draft, target = [-1, -1, 0, 0, 3], [9, 9, 4, 5, 6], [5, 0, 0, 6, 8]
+    rows, lens, follow = oracle.tree_accept([0, 5], up, draft, target, [9])
+    assert list(rows) == [0, 3, 4, -1, -1] and lens[0] == 3 and follow[0] == 8
+
+
+def test_commit_oracle_by_hand():
+    moves, after = oracle.tree_commit([0, 4], [0, 2, 3, -1], [3], [[7, 3]], [18])
+    assert moves == [((7, 14), (7, 14)), ((3, 0), (7, 15)), ((3, 1), (3, 0))] and after[0] == 17
