@@ -15,7 +15,7 @@ __global__ __launch_bounds__(64) void k_tree_accept(AcceptArgs a) {
   constexpr int NR = kTreeRows / kWave;
   const int lane = threadIdx.x;
   const int r = blockIdx.x;
-  int want = a.root[r];
+  int want = ld_uniform(a.root + r);
   const RowSpan rw = row_span(a.qoff, r, a.T, a.max_q);
   int parent[NR], draft[NR], target[NR], taken[NR];
 #pragma unroll
@@ -78,9 +78,9 @@ __global__ __launch_bounds__(256) void k_tree_commit(CommitArgs a) {
   __shared__ int s_n;
   const int slabs = (a.H + 7) / 8;
   const int r = blockIdx.x / slabs, slab = blockIdx.x % slabs;
-  const int S = clampi(a.slen[r], 0, a.max_s);
+  const int S = clampi(ld_uniform(a.slen + r), 0, a.max_s);
   const RowSpan rw = row_span(a.qoff, r, a.T, min(S, a.max_q));
-  const int m = clampi(a.lens[r], 0, rw.count);
+  const int m = clampi(ld_uniform(a.lens + r), 0, rw.count);
   const int cached = S - rw.count;
   if (slab == 0 && threadIdx.x == 0) a.committed[r] = cached + m;
   // the moves, in slot order without those in place: two rows per lane of wave 0

@@ -204,8 +204,18 @@ namespace {
 
 struct TreePlan {
   int depth, tiles;
-  size_t total_bytes;
+  bool split;                    // partial results and join, else one launch
+  int cp, tiles_p, seg_p, seg_pre, seg, runs, min_run;
+  long n_pre;
+  size_t o_bytes, lse_bytes, total_bytes;
 };
+
+// Overrides the estimate below for tests and tuning (per thread, set through
+// parrot_test_tree_path): 0 one launch, 1 partial results and join.
+thread_local int g_tree_path = -1;
+
+constexpr int kTreeMinRun = 10;      // cost of a run at least: 8 units and a tile's setup
+constexpr int kTreeChunkMax = 8192, kTreeChunkMin = 256;
 
 // The row counts of a tree call (or of accept and commit, which have no heads).
 parrot_status check_tree_counts(int32_t requests, const parrot_tree_rows* rows) {
@@ -236,9 +246,42 @@ parrot_status check_tree(const parrot_problem* p, const parrot_tree_rows* rows, 
   const long G = rows->num_query_heads / p->num_heads;
   pl->depth = p->num_groups > 0 ? (nested ? std::max(1, (int)p->max_prefix_depth) : 1) : 0;
   pl->tiles = (int)ceil_div(rows->max_query_rows * G, parrot::tree_cols(p->dtype));
-  if (ceil_div((long)p->num_requests * p->num_heads, 8) * 8 * pl->tiles > 0x7fffffffL)
+  const long H = p->num_heads, R = p->num_requests, cus = parrot::device_cus(), cols = parrot::tree_cols(p->dtype);
+  if (ceil_div(R * H, 8) * 8 * pl->tiles > 0x7fffffffL)
     return set_error(PARROT_ERR_UNSUPPORTED, "tree decode needs too many workgroups");
+  // the split plan: prefix chunks as long as their workgroups still fill the device
+  const long mg = p->num_groups > 0 ? rows->max_group_rows : 0;
+  pl->tiles_p = (int)ceil_div(mg * G, cols);
+  pl->cp = kTreeChunkMax;
+  if (pl->tiles_p > 0) {
+    while (pl->cp > kTreeChunkMin && p->num_groups * pl->tiles_p * H * ceil_div(p->max_prefix_len, pl->cp) < 2 * cus)
+      pl->cp /= 2;
+    pl->seg_p = (int)ceil_div(p->max_prefix_len, pl->cp);
+    pl->n_pre = ceil_div((long)p->num_groups * pl->seg_p * H, 8) * 8 * pl->tiles_p;
+  }
+  pl->seg_pre = pl->depth * pl->seg_p;
+  // own tokens: two workgroups per CU beside prefix work, else three
+  pl->runs = (int)std::max(1L, (pl->n_pre > 0 ? 2 : 3) * cus / H);
+  pl->min_run = kTreeMinRun;
+  const long units = ceil_div(p->max_suffix_len, parrot::tree_unit(p->dtype, p->head_dim));
+  const long seg = pl->seg_pre + std::min(ceil_div(units, pl->min_run) + 1, (long)pl->runs);
+  const double cost = (double)R * pl->tiles * (units + parrot::kTreeSetup);
+  if (pl->runs * H + pl->n_pre > 0x7fffffffL || cost > 2e9 || (double)T * rows->num_query_heads * seg * p->head_dim > 4e18)
+    return set_error(PARROT_ERR_UNSUPPORTED, "tree decode: %.3g units of own tokens", cost);
+  pl->seg = (int)seg;
+  pl->split = g_tree_path >= 0 ? g_tree_path == 1 : true;
+  auto align256 = [](size_t x) { return (x + 255) & ~(size_t)255; };
+  const size_t slots = (size_t)T * rows->num_query_heads * seg;
+  pl->o_bytes = align256(slots * p->head_dim * sizeof(float));
+  pl->lse_bytes = align256(slots * sizeof(float));
+  pl->total_bytes = pl->o_bytes + pl->lse_bytes + align256((R + 2) * sizeof(int32_t));
   return PARROT_OK;
+}
+
+parrot_status record_none(const parrot_trace& tr, hipStream_t s) {
+  for (void* e : {tr.merge_start, tr.merge_stop})
+    if (e && hipEventRecord(ev(e), s) != hipSuccess) return set_error(PARROT_ERR_HIP, "hipEventRecord failed");
+  return set_error(PARROT_OK, "");
 }
 
 }  // namespace
@@ -291,10 +334,22 @@ parrot_status parrot_shared_prefix_tree_decode(
   a.npblk = p->num_groups > 0 ? p->num_prefix_blocks : 1; a.nsblk = p->num_suffix_blocks;
   a.tiles = pl.tiles;
   a.scale_log2 = p->sm_scale * parrot::kLog2e;
-  return launched(parrot::launch_tree(a, (int)p->dtype, p->head_dim, reinterpret_cast<hipStream_t>(stream),
-                                      trace ? ev(trace->partials_start) : nullptr,
-                                      trace ? ev(trace->partials_stop) : nullptr),
-                  "tree kernel");
+  a.cp = pl.cp; a.tiles_p = pl.tiles_p; a.seg = pl.seg; a.seg_p = pl.seg_p; a.seg_pre = pl.seg_pre;
+  a.runs = pl.runs; a.min_run = pl.min_run; a.n_pre = (int)pl.n_pre;
+  a.o_part = reinterpret_cast<float*>(workspace);
+  a.lse_part = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + pl.o_bytes);
+  a.starts = reinterpret_cast<int*>(reinterpret_cast<char*>(workspace) + pl.o_bytes + pl.lse_bytes);
+  const parrot_trace none = {nullptr, nullptr, nullptr, nullptr};
+  const parrot_trace& tr = trace ? *trace : none;
+  const int dt = (int)p->dtype, D = p->head_dim;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  if (!pl.split) {
+    PARROT_TRY(launched(parrot::launch_tree(a, dt, D, s, ev(tr.partials_start), ev(tr.partials_stop)), "tree kernel"));
+    return record_none(tr, s);
+  }
+  PARROT_TRY(launched(parrot::launch_tree_partials(a, dt, D, s, ev(tr.partials_start), ev(tr.partials_stop)),
+                      "tree partials kernel"));
+  return launched(parrot::launch_tree_join(a, dt, D, s, ev(tr.merge_start), ev(tr.merge_stop)), "tree join kernel");
 }
 
 parrot_status parrot_validate_tree_inputs(
@@ -309,6 +364,14 @@ parrot_status parrot_validate_tree_inputs(
   const parrot::ValidateTree tree = {tree_parents};
   return parrot::validate_inputs(p, prefix_block_tables, prefix_lens, prefix_parents, suffix_block_tables,
                                  suffix_lens, group_ids, scratch, stream, &as_prefill, query_offsets, &tree);
+}
+
+// Test hooks (not in parrot_attn.h): the path of this thread's tree calls (see
+// g_tree_path; -1 gives the choice back), and the path these arguments take (-1: invalid).
+void parrot_test_tree_path(int path) { g_tree_path = path == 0 || path == 1 ? path : -1; }
+int parrot_test_tree_split(const parrot_problem* p, const parrot_tree_rows* rows, int nested) {
+  TreePlan pl;
+  return check_tree(p, rows, nested != 0, &pl) == PARROT_OK ? pl.split : -1;
 }
 
 // --------------------------------------------------------- accept and commit

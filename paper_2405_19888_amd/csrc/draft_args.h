@@ -68,12 +68,13 @@ PARROT_DEV int request_of_row(const int* qoff, int R, int t, int lane) {
   return r;
 }
 
-// Rows of request r, clamped so that every row index stays in [0, T) and the
-// request has at most `most` of them.
+// Rows of request r (wave-uniform), clamped so that every row index stays in [0, T) and
+// the request has at most `most` of them.
 struct RowSpan { int first, count; };
 PARROT_DEV RowSpan row_span(const int* qoff, int r, int T, int most) {
-  const int first = clampi(qoff[r], 0, T);
-  const long n = (long)qoff[r + 1] - qoff[r];
+  const int begin = ld_uniform(qoff + r), end = ld_uniform(qoff + r + 1);
+  const int first = clampi(begin, 0, T);
+  const long n = (long)end - begin;
   const int cap = min(most, T - first);
   return {first, (int)(n < 0 ? 0 : n > cap ? cap : n)};
 }

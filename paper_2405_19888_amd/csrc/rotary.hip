@@ -82,13 +82,13 @@ __global__ __launch_bounds__(256) void k_rotary_fill(FillArgs a) {
   const int half = a.rd >> 1;
 
   // the row's cache slot
-  const int r = request_of_row(a.qoff, a.R, t, lane);
+  const int r = __builtin_amdgcn_readfirstlane(request_of_row(a.qoff, a.R, t, lane));
   if (r < 0) return;
-  const int S = clampi(a.slen[r], 0, a.max_s);
+  const int S = clampi(ld_uniform(a.slen + r), 0, a.max_s);
   const RowSpan rw = row_span(a.qoff, r, a.T, min(S, a.max_q));
   if (t < rw.first || t >= rw.first + rw.count) return;      // padding
   const int own = S - rw.count + (t - rw.first);
-  const int blk = clampi(a.stab[(long)r * a.sstride + own / kBlock], 0, a.nsblk - 1);
+  const int blk = clampi(ld_uniform(a.stab + (long)r * a.sstride + own / kBlock), 0, a.nsblk - 1);
   const size_t slot = ((size_t)blk * a.H * kBlock + own % kBlock) * (D * EB);   // head 0
 
   // c[i], s[i]: factors of the lane's element i and of its partner, for queries

@@ -25,8 +25,30 @@ struct TreeArgs {
   int pstride, sstride, max_p, max_s, max_q, npblk, nsblk;
   int tiles;                             // column tiles per request
   float scale_log2;
+
+  // Split plan only.  Partial results o_part [T][HQ][seg][D] (normalised) and lse_part
+  // [T][HQ][seg] (base 2): slots [l * seg_p, (l + 1) * seg_p) hold the chunks of the
+  // prefix at level l of the request's chain (0: outermost), the rest the pieces of
+  // the own tokens.
+  float* o_part; float* lse_part;
+  int* starts;                           // [R + 2]: where each request's cost begins, the total, the run
+  int seg, seg_p, seg_pre;
+  int cp;                                // prefix chunk tokens
+  int tiles_p;                           // column tiles per group
+  int runs;                              // runs of the own tokens' cost, a workgroup each per cache head
+  int min_run;                           // least cost of a run
+  int n_pre;                             // prefix workgroups
 };
 
+// Own tokens are streamed in units of kTreeUnit tokens; a column tile of a request costs
+// its units and kTreeSetup more.
+constexpr int kTreeSetup = 2;
+constexpr int tree_unit(int dtype, int D) { return dtype != kF32 && D == 64 ? 64 : 32; }
+
+// One workgroup per request, cache head and column tile, output written by it.
 hipError_t launch_tree(const TreeArgs& a, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
+// Partial results of prefixes and own tokens, and their combination.
+hipError_t launch_tree_partials(const TreeArgs& a, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
+hipError_t launch_tree_join(const TreeArgs& a, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
 
 }  // namespace parrot

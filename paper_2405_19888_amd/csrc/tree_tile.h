@@ -112,10 +112,11 @@ struct TreeRange {
   int base, end;                    // masked ranges: the drafted tokens are [base, end)
 };
 
-// The tile's state: columns, softmax statistics and output, in registers.
-template <int DT, int D>
+// One wave's part of a tile: its NS column sets' softmax statistics and output, in
+// registers.  Waves of one workgroup may run parts of different NS side by side:
+// every part makes the same loads and barriers.
+template <int DT, int D, int NS>
 struct TreeTile {
-  static constexpr int NS = tree_detail::kSets<DT>;
   static constexpr int EB = Elem<DT>::kBytes;
   static constexpr int ROW_B = D * EB;
   static constexpr int GRAN = ROW_B / 16;                    // 16-byte granules per row
@@ -131,7 +132,7 @@ struct TreeTile {
   int lane, wave, H, h;
   float scale, inv_scale;
   unsigned qsign;
-  bool act[NS];                       // wave-uniform: the set has columns
+  bool act;                           // wave-uniform: the wave has columns
   u32x4 qf[NS][DT == kF32 ? 1 : KS];
   float qs[NS][DT == kF32 ? KS : 1];
   float mref[NS], thr[NS], lsum[NS], lsr[NS];
@@ -152,9 +153,9 @@ struct TreeTile {
   // of heads (row * HQ + query head).
   template <class F>
   PARROT_DEV void load_queries(const void* q, int ncols, F qrow) {
+    act = wave * 16 < ncols;
 #pragma unroll
     for (int c = 0; c < NS; ++c) {
-      act[c] = (wave + 4 * c) * 16 < ncols;
       const int col = column(c);
       const bool ok = col < ncols;
       const char* src = (const char*)q + (size_t)(ok ? qrow(col) : 0) * ROW_B;
@@ -247,9 +248,8 @@ struct TreeTile {
     }
   }
 
-  // One pair of blocks (32 tokens from tok0) of a stage; 16-bit caches.
-  template <bool MASKED>
-  PARROT_DEV void pair(const TreeRange& rg, int span0, int buf, int bl, int tok0) {
+  // One pair of blocks (32 tokens from tok0) of a stage (16-bit caches).
+  PARROT_DEV void pair(const TreeRange& rg, int span0, int buf, int bl, int tok0, bool masked) {
     using namespace prefix_detail;
     const char* kb = lds.ring[buf] + bl * BLK_B;
     const char* vb = kb + kTensorStage;
@@ -266,22 +266,21 @@ struct TreeTile {
         const u32x4 kf = *reinterpret_cast<const u32x4*>(kb + b * BLK_B + off);
 #pragma unroll
         for (int c = 0; c < NS; ++c)
-          if (act[c]) s[c][b] = Mfma<DT>::qk(kf, qf[c][ks], s[c][b]);
+          s[c][b] = Mfma<DT>::qk(kf, qf[c][ks], s[c][b]);
       }
     }
 #pragma unroll
     for (int c = 0; c < NS; ++c) {
-      if (!act[c]) continue;
       float x[8];
 #pragma unroll
       for (int i = 0; i < 4; ++i) { x[i] = s[c][0][i]; x[4 + i] = s[c][1][i]; }
       unsigned vis = 0xFFFFFFFFu;
-      if constexpr (MASKED) {
+      if (masked) {
         if (tok0 >= rg.mask0) vis = lds.mask[(tok0 - rg.mask0) >> 5][column(c)];
         else if (rg.t1 - tok0 < 32) vis = (1u << (rg.t1 - tok0)) - 1u;
       }
       softmax<8>(x, c, vis);
-      if constexpr (MASKED) {
+      if (masked) {
         const unsigned bad = __builtin_amdgcn_readfirstlane(lds.bad[buf][bl >> 1]);
         if (bad) add_cleared<8>(rg, span0, x, c, vis, bad, tok0);
       }
@@ -299,7 +298,6 @@ struct TreeTile {
       const unsigned long long v0 = Mfma<DT>::tr_read(va + off), v1 = Mfma<DT>::tr_read(va + BLK_B + off);
 #pragma unroll
       for (int c = 0; c < NS; ++c) {
-        if (!act[c]) continue;
         const unsigned long long b0 = pw[c][0] | ((unsigned long long)pw[c][1] << 32);
         const unsigned long long b1 = pw[c][2] | ((unsigned long long)pw[c][3] << 32);
         o[c][dt] = Mfma<DT>::pv2(v0, v1, b0, b1, o[c][dt]);
@@ -308,22 +306,20 @@ struct TreeTile {
   }
 
   // One block (16 tokens from tok0) of a stage; fp32 caches.
-  template <bool MASKED>
-  PARROT_DEV void block32(const TreeRange& rg, int span0, int buf, int bl, int tok0) {
+  PARROT_DEV void block32(const TreeRange& rg, int span0, int buf, int bl, int tok0, bool masked) {
     const char* kb = lds.ring[buf] + bl * BLK_B;
     const char* vb = kb + prefix_detail::kTensorStage;
 #pragma unroll
     for (int c = 0; c < NS; ++c) {
-      if (!act[c]) continue;
       const f32x4 s = scores32(kb, c);
       float x[4] = {s[0], s[1], s[2], s[3]};
       unsigned vis = 0xFFFFu;
-      if constexpr (MASKED) {
+      if (masked) {
         if (tok0 >= rg.mask0) vis = (lds.mask[(tok0 - rg.mask0) >> 5][column(c)] >> (tok0 & 16)) & 0xFFFFu;
         else if (rg.t1 - tok0 < 16) vis = (1u << (rg.t1 - tok0)) - 1u;
       }
       softmax<4>(x, c, vis);
-      if constexpr (MASKED) {
+      if (masked) {
         const unsigned bad = __builtin_amdgcn_readfirstlane(lds.bad[buf][bl >> 1]) >> (16 * (bl & 1)) & 0xFFFFu;
         if (bad) add_cleared<4>(rg, span0, x, c, vis, bad, tok0);
       }
@@ -438,22 +434,20 @@ struct TreeTile {
       const int next = buf == 0 ? 2 : buf - 1;               // (st + 2) % 3
       issue(next);
       table(min(st + 3, last));
-      if (act[0]) {
+      if (act) {
         if constexpr (DT == kF32) {
 #pragma unroll 1
           for (int bl = 0; bl < STAGE_BLK; ++bl) {
             const int tok0 = tok_st + bl * kBlock;
             if (tok0 >= rg.t1) break;
-            if (masked) block32<true>(rg, b0, buf, bl, tok0);
-            else block32<false>(rg, b0, buf, bl, tok0);
+            block32(rg, b0, buf, bl, tok0, masked);
           }
         } else {
 #pragma unroll 1
           for (int bl = 0; bl < STAGE_BLK; bl += 2) {
             const int tok0 = tok_st + bl * kBlock;
             if (tok0 >= rg.t1) break;
-            if (masked) pair<true>(rg, b0, buf, bl, tok0);
-            else pair<false>(rg, b0, buf, bl, tok0);
+            pair(rg, b0, buf, bl, tok0, masked);
           }
         }
       }
@@ -462,13 +456,13 @@ struct TreeTile {
     wait_vmcnt<0>();                     // the re-read stages issued by the last iterations
   }
 
-  // The tile's result: f(c, col, value(dt) scaled, lse2) per set with columns; the lane
+  // The tile's result: f(c, col, value(dt) scaled, lse2) per set of a wave with columns; the lane
   // holds elements dt * 16 + 4 (lane / 16) .. + 3 of its column.
   template <class F>
   PARROT_DEV void finish(F f) {
+    if (!act) return;
 #pragma unroll
     for (int c = 0; c < NS; ++c) {
-      if (!act[c]) continue;
       const float lt = sum_xor32(sum_xor16(lsum[c]));
       const float lw = DT == kF32 ? lt : sum_xor32(sum_xor16(lsr[c]));
       f(c, column(c), lw, mref[c] + fast_log2(lt), lt);

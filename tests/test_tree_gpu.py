@@ -10,11 +10,23 @@ from gpu_util import problem_for
 
 pytestmark = pytest.mark.gpu
 
+PATHS = {"one": 0, "split": 1}
 
-def run(plan, batch, q, off, parents, T=None, trees=True, stream=None, use=None):
+
+@pytest.fixture(autouse=True, params=["one", "split"])
+def path(request):
+    """Every test runs on one launch, and on partial results and join."""
+    import paper_2405_19888_amd as parrot
+    force = parrot.load_library().parrot_test_tree_path
+    force(PATHS[request.param])
+    yield request.param
+    force(-1)
+
+
+def run(plan, batch, q, off, parents, T=None, trees=True):
     """One call on poisoned outputs; (out, lse, decoder, device tensors)."""
     import paper_2405_19888_amd as parrot
-    dev = batch.to("cuda") if use is None else use
+    dev = batch.to("cuda")
     dev["q_rows"], dev["query_offsets"] = q.cuda(), torch.from_numpy(off).cuda()
     dev["tree_parents"] = torch.from_numpy(parents).cuda() if trees else None
     rows = parrot.tree_rows_from_host(off, plan.group_ids, plan.num_groups, q.shape[1],
