@@ -205,7 +205,7 @@ namespace {
 struct TreePlan {
   int depth, tiles;
   bool split;                    // partial results and join, else one launch
-  int cp, tiles_p, seg_p, seg_pre, seg, runs, min_run;
+  int cp, tiles_p, seg_p, seg_pre, seg, sets, waves, own_wgs, runs, min_run;
   long n_pre;
   size_t o_bytes, lse_bytes, total_bytes;
 };
@@ -260,13 +260,21 @@ parrot_status check_tree(const parrot_problem* p, const parrot_tree_rows* rows, 
     pl->n_pre = ceil_div((long)p->num_groups * pl->seg_p * H, 8) * 8 * pl->tiles_p;
   }
   pl->seg_pre = pl->depth * pl->seg_p;
-  // own tokens: two workgroups per CU beside prefix work, else three
-  pl->runs = (int)std::max(1L, (pl->n_pre > 0 ? 2 : 3) * cus / H);
+  // own tokens: two workgroups per CU beside prefix work, else three; requests of at
+  // most 32 columns go by waves, each with a run of its own
+  const long most_cols = rows->max_query_rows * G;
+  pl->sets = most_cols <= 16 ? 1 : most_cols <= 32 ? 2 : 0;
+  pl->waves = R * H <= cus ? 8 : 4;
+  const long per_wg = pl->sets ? 4 : 1;
+  // (two column sets a wave: two workgroups per CU in all)
+  const long most_wgs = pl->sets == 2 ? 2 : 3;
+  pl->own_wgs = (int)std::max((pl->n_pre > 0 ? most_wgs - 1 : most_wgs) * cus, ceil_div(H, per_wg));
+  pl->runs = (int)(pl->own_wgs * per_wg / H);
   pl->min_run = kTreeMinRun;
   const long units = ceil_div(p->max_suffix_len, parrot::tree_unit(p->dtype, p->head_dim));
   const long seg = pl->seg_pre + std::min(ceil_div(units, pl->min_run) + 1, (long)pl->runs);
   const double cost = (double)R * pl->tiles * (units + parrot::kTreeSetup);
-  if (pl->runs * H + pl->n_pre > 0x7fffffffL || cost > 2e9 || (double)T * rows->num_query_heads * seg * p->head_dim > 4e18)
+  if ((pl->own_wgs + pl->n_pre) * 256 > 0xffffffffL || ceil_div(R * H, 8) * 8 * pl->tiles * 512 > 0xffffffffL || cost > 2e9 || (double)T * rows->num_query_heads * seg * p->head_dim > 4e18)
     return set_error(PARROT_ERR_UNSUPPORTED, "tree decode: %.3g units of own tokens", cost);
   pl->seg = (int)seg;
   pl->split = g_tree_path >= 0 ? g_tree_path == 1 : true;
@@ -274,7 +282,7 @@ parrot_status check_tree(const parrot_problem* p, const parrot_tree_rows* rows, 
   const size_t slots = (size_t)T * rows->num_query_heads * seg;
   pl->o_bytes = align256(slots * p->head_dim * sizeof(float));
   pl->lse_bytes = align256(slots * sizeof(float));
-  pl->total_bytes = pl->o_bytes + pl->lse_bytes + align256((R + 2) * sizeof(int32_t));
+  pl->total_bytes = pl->o_bytes + pl->lse_bytes + align256((size_t)T * parrot::kTreeDesc * sizeof(int32_t));
   return PARROT_OK;
 }
 
@@ -335,16 +343,16 @@ parrot_status parrot_shared_prefix_tree_decode(
   a.tiles = pl.tiles;
   a.scale_log2 = p->sm_scale * parrot::kLog2e;
   a.cp = pl.cp; a.tiles_p = pl.tiles_p; a.seg = pl.seg; a.seg_p = pl.seg_p; a.seg_pre = pl.seg_pre;
-  a.runs = pl.runs; a.min_run = pl.min_run; a.n_pre = (int)pl.n_pre;
+  a.sets = pl.sets; a.own_wgs = pl.own_wgs; a.runs = pl.runs; a.min_run = pl.min_run; a.n_pre = (int)pl.n_pre;
   a.o_part = reinterpret_cast<float*>(workspace);
   a.lse_part = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + pl.o_bytes);
-  a.starts = reinterpret_cast<int*>(reinterpret_cast<char*>(workspace) + pl.o_bytes + pl.lse_bytes);
+  a.desc = reinterpret_cast<int*>(reinterpret_cast<char*>(workspace) + pl.o_bytes + pl.lse_bytes);
   const parrot_trace none = {nullptr, nullptr, nullptr, nullptr};
   const parrot_trace& tr = trace ? *trace : none;
   const int dt = (int)p->dtype, D = p->head_dim;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (!pl.split) {
-    PARROT_TRY(launched(parrot::launch_tree(a, dt, D, s, ev(tr.partials_start), ev(tr.partials_stop)), "tree kernel"));
+    PARROT_TRY(launched(parrot::launch_tree(a, pl.waves, dt, D, s, ev(tr.partials_start), ev(tr.partials_stop)), "tree kernel"));
     return record_none(tr, s);
   }
   PARROT_TRY(launched(parrot::launch_tree_partials(a, dt, D, s, ev(tr.partials_start), ev(tr.partials_stop)),

@@ -3,7 +3,7 @@
 //
 // One workgroup per (request, cache head, column tile) goes through the prefixes of the
 // request's group chain and its own tokens and writes the output.
-#include "tree_tile.h"
+#include "tree_stream.h"
 
 namespace parrot {
 
@@ -62,7 +62,7 @@ PARROT_DEV void build_masks(const TreeArgs& a, tree_detail::Lds<DT>& lds, const 
 
 // The output rows of a tile that saw its columns' whole contexts.
 template <int DT, int D, int NS, class F>
-PARROT_DEV void write_output(const TreeArgs& a, TreeTile<DT, D, NS>& tile, int ncols, F row_of) {
+PARROT_DEV void write_output(const TreeArgs& a, TreeState<DT, D, NS>& tile, int ncols, F row_of) {
   tile.finish([&](int c, int col, float lw, float lse2, float) {
     if (col >= ncols) return;
     const size_t at = row_of(col);
@@ -83,12 +83,12 @@ PARROT_DEV void tree_item(const TreeArgs& a, tree_detail::Lds<DT>& lds, int r, i
                           int col0, int ncols) {
   const int base = S - rw.count;
   const int HQ = a.H * a.G;
-  TreeTile<DT, D, NS> tile(lds, a.H, h, a.scale_log2);
+  TreeTile<DT, D, NS> tile(lds, a.H, h, a.scale_log2, ncols);
   auto row_of = [&](int col) {                              // in units of heads
     const int x = col0 + col;
     return (size_t)(rw.first + x / a.G) * HQ + h * a.G + x % a.G;
   };
-  tile.load_queries(a.q, ncols, row_of);
+  tile.template load_queries<false>(a.q, ncols, row_of);
 
   int g = ld_uniform(a.gid + r);
   for (int l = 0;; ++l) {                                   // the chain's prefixes, then the own tokens
@@ -109,7 +109,7 @@ PARROT_DEV void tree_item(const TreeArgs& a, tree_detail::Lds<DT>& lds, int r, i
     g = a.parents ? ld_uniform(a.parents + g) : -1;
   }
 
-  write_output<DT, D, NS>(a, tile, ncols, row_of);
+  if (tile.act) write_output<DT, D, NS>(a, tile, ncols, row_of);
 }
 
 template <int DT, int D>
@@ -185,7 +185,7 @@ PARROT_DEV int scan256(int x, int* lds4, int* total) {
 
 // A tile's partial results: slot `slot` of the columns' rows.
 template <int DT, int D, int NS, class F>
-PARROT_DEV void write_partial(const TreeArgs& a, TreeTile<DT, D, NS>& tile, int ncols, int slot, F row_of) {
+PARROT_DEV void write_partial(const TreeArgs& a, TreeState<DT, D, NS>& tile, int ncols, int slot, F row_of) {
   tile.finish([&](int c, int col, float lw, float lse2, float lt) {
     if (col >= ncols) return;
     const size_t at = row_of(col) * (size_t)a.seg + slot;
@@ -197,130 +197,164 @@ PARROT_DEV void write_partial(const TreeArgs& a, TreeTile<DT, D, NS>& tile, int 
   });
 }
 
+// One tile against one key range: columns col0 .. col0 + ncols of the sequence whose rows
+// from row0 on are in lds.rows; slot < 0: the columns' whole context, the output.
+struct TreePiece { TreeRange rg; int h, col0, ncols, row0, slot; };
+
 template <int DT, int D, int NS>
-PARROT_DEV void own_piece(const TreeArgs& a, tree_detail::Lds<DT>& lds, int r, int h, const RowSpan& rw, int S,
-                          int col0, int ncols, int t0, int t1, int slot, bool whole) {
-  const int HQ = a.H * a.G, base = S - rw.count;
-  TreeTile<DT, D, NS> tile(lds, a.H, h, a.scale_log2);
-  auto row_of = [&](int col) {
-    const int x = col0 + col;
-    return (size_t)(rw.first + x / a.G) * HQ + h * a.G + x % a.G;
+PARROT_DEV void tree_piece(const TreeArgs& a, tree_detail::Lds<DT>& lds, const TreePiece& pc) {
+  TreeTile<DT, D, NS> tile(lds, a.H, pc.h, a.scale_log2, pc.ncols);
+  auto row_of = [&](int col) {                              // in units of heads
+    const int x = pc.col0 + col, row = x / a.G;
+    return (size_t)lds.rows[row - pc.row0] * (a.H * a.G) + pc.h * a.G + (x - row * a.G);
   };
-  tile.load_queries(a.q, ncols, row_of);
-  TreeRange rg;
-  rg.pk = a.sk; rg.pv = a.sv; rg.tbl = a.stab + (long)r * a.sstride; rg.npool = a.nsblk;
-  rg.t0 = t0; rg.t1 = t1; rg.mask0 = base & ~31; rg.base = base; rg.end = S;
-  tile.run(rg);
-  if (whole) write_output<DT, D, NS>(a, tile, ncols, row_of);
-  else write_partial<DT, D, NS>(a, tile, ncols, slot, row_of);
+  tile.template load_queries<false>(a.q, pc.ncols, row_of);
+  tile.run(pc.rg);
+  if (!tile.act) return;
+  if (pc.slot < 0) write_output<DT, D, NS>(a, tile, pc.ncols, row_of);
+  else write_partial<DT, D, NS>(a, tile, pc.ncols, pc.slot, row_of);
 }
 
+// The run of an own-role wave (tiles: of all waves of its workgroup), and where it stands.
+struct OwnRun { int u0, u1, q, r, start, tile; };
+
+// What the join needs of the rows of request r, whose cost starts at `start`.
 template <int DT, int D>
-PARROT_DEV void tree_own_role(const TreeArgs& a, tree_detail::Lds<DT>& lds, int wg) {
-  constexpr int COLS = tree_detail::kCols<DT>, UNIT = tree_unit(DT, D);
-  const int tid = threadIdx.x;
-  const int run = wg / a.H, h = wg % a.H;
-  int* scratch = reinterpret_cast<int*>(lds.tbl);
-  // the whole cost, then where this run begins
-  int total = 0;
-  for (int b = 0; b < a.R; b += 256) {
-    int cost = 0, sum;
-    if (b + tid < a.R) {
-      const OwnCost c = own_cost<DT, D>(a, b + tid);
-      cost = c.tiles * (c.units + kTreeSetup);
+PARROT_DEV void write_desc(const TreeArgs& a, int r, const OwnCost& c, int start, int q) {
+  int len[kMaxDepth], nlev = 0;
+  const int gid = a.gid[r];
+  const bool prefixed = a.seg_p > 0 && gid >= 0 && gid < a.NG;
+  for (int g = gid; a.seg_p > 0 && g >= 0 && g < a.NG && nlev < a.depth; g = a.parents ? a.parents[g] : -1) {
+    const int n = min((clampi(a.plen[g], 0, a.max_p) + a.cp - 1) / a.cp, a.seg_p);
+#pragma unroll
+    for (int l = 0; l < kMaxDepth; ++l)
+      if (l == nlev) len[l] = n;
+    ++nlev;
+  }
+  unsigned lo = 0, hi = 0;                                  // outermost level first
+#pragma unroll
+  for (int l = 0; l < kMaxDepth; ++l)
+    if (l < nlev) {
+      const int at = nlev - 1 - l;
+      if (at < 2) lo |= (unsigned)len[l] << (16 * at);
+      else hi |= (unsigned)len[l] << (16 * (at - 2));
     }
-    scan256(cost, scratch, &sum);
+  for (int j = 0; j < c.count; ++j) {
+    int4* d = reinterpret_cast<int4*>(a.desc + (size_t)(c.first + j) * kTreeDesc);
+    d[0] = int4{start + kTreeSetup, c.units + kTreeSetup, c.units, q};
+    d[1] = int4{(int)lo, (int)hi, j, prefixed ? 1 : 0};
+  }
+}
+
+// Finds the runs run_of(wave) of the cost (each wave gets its own); false for a wave whose
+// run is empty.  The first kDescWgs workgroups also write the row descriptors, a share
+// of the requests each.  Every wave of the workgroup calls it.
+constexpr int kDescWgs = 16;
+template <int DT, int D, class F>
+PARROT_DEV bool find_run(const TreeArgs& a, int* scratch, int wg, F run_of, OwnRun* o) {
+  const int tid = threadIdx.x;
+  OwnCost c;
+  auto cost_of = [&](int r) {
+    if (r >= a.R) return 0;
+    c = own_cost<DT, D>(a, r);
+    return c.tiles * (c.units + kTreeSetup);
+  };
+  int total = 0, cost = 0, incl = 0;
+  for (int b = 0; b < a.R; b += 256) {
+    int sum;
+    cost = cost_of(b + tid);
+    incl = scan256(cost, scratch, &sum);
     total += sum;
   }
   const int q = max(a.min_run, (total + a.runs - 1) / a.runs);
-  const int u0 = run * q, u1 = min(total, u0 + q);
-  const bool writes = wg == 0;                    // this workgroup leaves the starts for the join
-  if (u0 >= total && !writes) return;
-  int r = -1, start = 0, before = 0;
-  for (int b = 0; b < a.R && (r < 0 || writes); b += 256) {
-    int cost = 0, sum;
-    if (b + tid < a.R) {
-      const OwnCost c = own_cost<DT, D>(a, b + tid);
-      cost = c.tiles * (c.units + kTreeSetup);
+  if (tid < 4) scratch[8 + 2 * tid] = -1;
+  __syncthreads();
+  const bool writes = wg < kDescWgs;
+  bool all = false;                               // every wave's run was found or is empty
+  for (int b = 0, before = 0; b < a.R && (!all || writes); b += 256) {
+    int sum = total;
+    if (a.R > 256) {                              // (few requests: the first pass stands)
+      cost = cost_of(b + tid);
+      incl = before + scan256(cost, scratch, &sum);
     }
-    const int incl = before + scan256(cost, scratch, &sum);
-    if (writes && b + tid < a.R) a.starts[b + tid] = incl - cost;
-    if (cost > 0 && incl - cost <= u0 && u0 < incl) { scratch[8] = b + tid; scratch[9] = incl - cost; }
-    __syncthreads();
-    if (r < 0 && u0 >= before && u0 < before + sum) { r = scratch[8]; start = scratch[9]; }
+    if (writes && b + tid < a.R && cost > 0 && tid % min(kDescWgs, a.own_wgs) == wg)
+      write_desc<DT, D>(a, b + tid, c, incl - cost, q);
+    all = true;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const int u0 = run_of(w) * q;
+      if (incl - cost <= u0 && u0 < incl) { scratch[8 + 2 * w] = b + tid; scratch[9 + 2 * w] = incl - cost; }
+      all = all && (u0 >= total || u0 < before + sum);
+    }
     before += sum;
   }
-  if (writes && tid == 0) { a.starts[a.R] = total; a.starts[a.R + 1] = q; }
-  if (r < 0 || u0 >= total) return;
-  r = __builtin_amdgcn_readfirstlane(r);
-  start = __builtin_amdgcn_readfirstlane(start);
-
+  __syncthreads();
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  for (; r < a.R && start < u1; ++r) {
-    const int S = clampi(ld_uniform(a.slen + r), 0, a.max_s);
-    const RowSpan rw = row_span(a.qoff, r, a.T, min(S, a.max_q));
-    const int tiles = (rw.count * a.G + COLS - 1) / COLS, units = (S + UNIT - 1) / UNIT;
-    const int g = ld_uniform(a.gid + r);
-    const bool prefixed = a.seg_p > 0 && g >= 0 && g < a.NG;
-    for (int t = 0; t < tiles; ++t, start += units + kTreeSetup) {
-      const int s0 = start + kTreeSetup;          // cost of the first unit
-      const int st0 = max(u0 - s0, 0), st1 = min(u1 - s0, units);
-      if (st1 <= st0) continue;
-      const int piece = run - s0 / q;
-      const bool whole = !prefixed && st0 == 0 && st1 == units;
-      const int col0 = t * COLS, ncols = min(COLS, rw.count * a.G - col0);
-      const int t0 = st0 * UNIT, t1 = min(S, st1 * UNIT);
-      __syncthreads();                            // the ring is free
-      if (t1 > ((S - rw.count) & ~31)) build_masks<DT, D>(a, lds, rw, S - rw.count, col0, ncols);
-      if (tree_detail::kSets<DT> == 2 && (wave + 4) * 16 < ncols)
-        own_piece<DT, D, tree_detail::kSets<DT>>(a, lds, r, h, rw, S, col0, ncols, t0, t1, a.seg_pre + piece, whole);
-      else
-        own_piece<DT, D, 1>(a, lds, r, h, rw, S, col0, ncols, t0, t1, a.seg_pre + piece, whole);
-    }
-  }
+  o->q = q;
+  o->u0 = run_of(wave) * q;
+  o->u1 = min(total, o->u0 + q);
+  o->r = __builtin_amdgcn_readfirstlane(scratch[8 + 2 * wave]);
+  o->start = __builtin_amdgcn_readfirstlane(scratch[9 + 2 * wave]);
+  o->tile = 0;
+  return o->r >= 0 && o->u0 < total;
 }
 
-template <int DT, int D, int NS>
-PARROT_DEV void prefix_piece(const TreeArgs& a, tree_detail::Lds<DT>& lds, int g, int h, int P, int t0, int t1,
-                             int col0, int row0, int ncols, int slot) {
-  const int* rows = reinterpret_cast<const int*>(&lds.mask[0][0]);
-  const int HQ = a.H * a.G;
-  TreeTile<DT, D, NS> tile(lds, a.H, h, a.scale_log2);
-  auto row_of = [&](int col) {
-    const int x = col0 + col;
-    return (size_t)rows[x / a.G - row0] * HQ + h * a.G + x % a.G;
-  };
-  tile.load_queries(a.q, ncols, row_of);
-  TreeRange rg;
-  rg.pk = a.pk; rg.pv = a.pv; rg.tbl = a.ptab + (long)g * a.pstride; rg.npool = a.npblk;
-  rg.t0 = t0; rg.t1 = t1; rg.mask0 = 0x40000000; rg.base = t1; rg.end = t1;
-  tile.run(rg);
-  write_partial<DT, D, NS>(a, tile, ncols, slot, row_of);
-}
-
+// The next piece of an own run; false when the run is done.
 template <int DT, int D>
-PARROT_DEV void tree_prefix_role(const TreeArgs& a, tree_detail::Lds<DT>& lds, int wg) {
+PARROT_DEV bool next_own(const TreeArgs& a, tree_detail::Lds<DT>& lds, int run, OwnRun* o, TreePiece* pc) {
+  constexpr int COLS = tree_detail::kCols<DT>, UNIT = tree_unit(DT, D);
+  while (o->r < a.R && o->start < o->u1) {
+    const int S = clampi(ld_uniform(a.slen + o->r), 0, a.max_s);
+    const int g = ld_uniform(a.gid + o->r);
+    const RowSpan rw = row_span(a.qoff, o->r, a.T, min(S, a.max_q));
+    const int tiles = (rw.count * a.G + COLS - 1) / COLS, units = (S + UNIT - 1) / UNIT;
+    if (o->tile >= tiles) { ++o->r; o->tile = 0; continue; }
+    const int s0 = o->start + kTreeSetup;         // cost of the first unit
+    const int st0 = max(o->u0 - s0, 0), st1 = min(o->u1 - s0, units);
+    const int r = o->r, t = o->tile++;
+    o->start += units + kTreeSetup;
+    if (st1 <= st0) continue;
+    const bool prefixed = a.seg_p > 0 && g >= 0 && g < a.NG;
+    const int base = S - rw.count;
+    pc->rg.pk = a.sk; pc->rg.pv = a.sv; pc->rg.tbl = a.stab + (long)r * a.sstride; pc->rg.npool = a.nsblk;
+    pc->rg.t0 = st0 * UNIT; pc->rg.t1 = min(S, st1 * UNIT);
+    pc->rg.mask0 = base & ~31; pc->rg.base = base; pc->rg.end = S;
+    pc->col0 = t * COLS;
+    pc->ncols = min(COLS, rw.count * a.G - pc->col0);
+    pc->row0 = pc->col0 / a.G;
+    pc->slot = !prefixed && st0 == 0 && st1 == units ? -1 : a.seg_pre + run - s0 / o->q;
+    __syncthreads();                              // the last piece is done with the LDS
+    if (threadIdx.x < COLS) lds.rows[threadIdx.x] = min(rw.first + pc->row0 + (int)threadIdx.x, a.T - 1);
+    if (pc->rg.t1 > pc->rg.mask0) build_masks<DT, D>(a, lds, rw, base, pc->col0, pc->ncols);
+    __syncthreads();
+    return true;
+  }
+  return false;
+}
+
+// The piece of prefix workgroup wg; false if there is none.
+template <int DT, int D>
+PARROT_DEV bool prefix_piece(const TreeArgs& a, tree_detail::Lds<DT>& lds, int wg, TreePiece* pc) {
   constexpr int COLS = tree_detail::kCols<DT>;
   // (group, chunk, head) items; their column tiles are 8 workgroups apart, on one XCD
   const int tile = wg / 8 % a.tiles_p;
   int idx = wg / (8 * a.tiles_p) * 8 + wg % 8;
-  if (idx >= a.NG * a.seg_p * a.H) return;
-  const int h = idx % a.H; idx /= a.H;
+  if (idx >= a.NG * a.seg_p * a.H) return false;
+  pc->h = idx % a.H; idx /= a.H;
   const int c = idx % a.seg_p, g = idx / a.seg_p;
   const int P = clampi(ld_uniform(a.plen + g), 0, a.max_p);
   const int t0 = c * a.cp;
-  if (t0 >= P) return;
-  const int t1 = min(P, t0 + a.cp);
+  if (t0 >= P) return false;
   int lvl = 0;                                            // ancestors of g (< depth)
   if (a.parents)
     for (int x = ld_uniform(a.parents + g); x >= 0 && x < a.NG && lvl < a.depth - 1; x = ld_uniform(a.parents + x)) ++lvl;
   // rows [row0, row0 + COLS] of the stacked list hold this tile's columns
-  const int col0 = tile * COLS, row0 = col0 / a.G;
-  int* rows = reinterpret_cast<int*>(&lds.mask[0][0]);
+  pc->col0 = tile * COLS;
+  pc->row0 = pc->col0 / a.G;
   constexpr int MOST = COLS + 1;
-  static_assert(sizeof(lds.mask) >= (MOST + 1) * sizeof(int), "the row list fits the mask");
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (wave == 0) {
+  const int row0 = pc->row0;
+  if (threadIdx.x < kWave) {
+    const int lane = threadIdx.x;
     int base = 0;
     for (int b = 0; b < a.R && base < row0 + MOST; b += kWave) {
       const int r = b + lane;
@@ -343,166 +377,349 @@ PARROT_DEV void tree_prefix_role(const TreeArgs& a, tree_detail::Lds<DT>& lds, i
         if (lane >= d) incl += v;
       }
       const int first = base + incl - n;
-      for (int x = max(first, row0), e = min(first + n, row0 + MOST); x < e; ++x) rows[x - row0] = oc.first + x - first;
+      for (int x = max(first, row0), e = min(first + n, row0 + MOST); x < e; ++x) lds.rows[x - row0] = oc.first + x - first;
       base += __shfl(incl, kWave - 1);
     }
-    if (lane == 0) rows[MOST] = base;
+    if (lane == 0) lds.rows[MOST] = base;
   }
   __syncthreads();
-  const int ncols = min(COLS, rows[MOST] * a.G - col0);
-  if (ncols <= 0) return;
-  if (tree_detail::kSets<DT> == 2 && (wave + 4) * 16 < ncols)
-    prefix_piece<DT, D, tree_detail::kSets<DT>>(a, lds, g, h, P, t0, t1, col0, row0, ncols, lvl * a.seg_p + c);
-  else
-    prefix_piece<DT, D, 1>(a, lds, g, h, P, t0, t1, col0, row0, ncols, lvl * a.seg_p + c);
+  pc->ncols = __builtin_amdgcn_readfirstlane(min(COLS, lds.rows[MOST] * a.G - pc->col0));
+  if (pc->ncols <= 0) return false;
+  pc->rg.pk = a.pk; pc->rg.pv = a.pv; pc->rg.tbl = a.ptab + (long)g * a.pstride; pc->rg.npool = a.npblk;
+  pc->rg.t0 = t0; pc->rg.t1 = min(P, t0 + a.cp);
+  pc->rg.mask0 = 0x40000000; pc->rg.base = pc->rg.end = pc->rg.t1;
+  pc->slot = lvl * a.seg_p + c;
+  return true;
 }
 
-template <int DT, int D>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3)))
+// Own role by waves (requests of at most kStreamCols columns): wave w of workgroup wg
+// streams run (4 wg + w) / H of cache head (4 wg + w) % H, so the waves of a workgroup
+// read adjacent heads of the same blocks.  No barrier once the runs are found.
+template <int DT, int D, int NS>
+PARROT_DEV void stream_role(const TreeArgs& a, char* lds, int wg) {
+  constexpr int UNIT = tree_unit(DT, D);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int run = (4 * wg + wave) / a.H, h = (4 * wg + wave) % a.H, HQ = a.H * a.G;
+  OwnRun o;
+  if (!find_run<DT, D>(a, reinterpret_cast<int*>(lds), wg, [&](int w) { return (4 * wg + w) / a.H; }, &o)) {
+    __syncthreads();                              // (the others wait below)
+    return;
+  }
+  __syncthreads();                                // the scratch becomes value rows
+  TreeStream<DT, D, NS> st(lds + wave * kStreamLds, a.H, h, a.scale_log2);
+  for (int start = o.start; o.r < a.R && start < o.u1; ++o.r) {
+    const int r = o.r;
+    const int S = clampi(ld_uniform(a.slen + r), 0, a.max_s);
+    const int g = ld_uniform(a.gid + r);
+    const RowSpan rw = row_span(a.qoff, r, a.T, min(S, a.max_q));
+    if (rw.count == 0) continue;
+    const int units = (S + UNIT - 1) / UNIT, s0 = start + kTreeSetup;
+    const int st0 = max(o.u0 - s0, 0), st1 = min(o.u1 - s0, units);
+    start += units + kTreeSetup;
+    if (st1 <= st0) continue;
+    const bool prefixed = a.seg_p > 0 && g >= 0 && g < a.NG;
+    const int base = S - rw.count, ncols = min(rw.count * a.G, 16 * NS);
+    TreeRange rg;
+    rg.pk = a.sk; rg.pv = a.sv; rg.tbl = a.stab + (long)r * a.sstride; rg.npool = a.nsblk;
+    rg.t0 = st0 * UNIT; rg.t1 = min(S, st1 * UNIT);
+    rg.mask0 = base & ~31; rg.base = base; rg.end = S;
+    auto row_of = [&](int col) {
+      const int row = col / a.G;
+      return (size_t)(rw.first + row) * HQ + h * a.G + (col - row * a.G);
+    };
+    st.template load_queries<true>(a.q, ncols, row_of);
+    if (rg.t1 > rg.mask0) st.build_masks(a.tree, rw, base, a.G);
+    st.run(rg);
+    if (!prefixed && st0 == 0 && st1 == units) write_output<DT, D, NS>(a, st, ncols, row_of);
+    else write_partial<DT, D, NS>(a, st, ncols, a.seg_pre + run - s0 / o.q, row_of);
+  }
+}
+
+// SETS 0: own tokens by tiles, else by waves of that many column sets.
+template <int DT, int D, int SETS>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SETS == 2 ? 2 : 3)))
 void k_tree_partials(TreeArgs a) {
   __shared__ __attribute__((aligned(1024))) tree_detail::Lds<DT> lds;
-  const int own = a.runs * a.H;
-  if ((int)blockIdx.x < own) tree_own_role<DT, D>(a, lds, blockIdx.x);
-  else tree_prefix_role<DT, D>(a, lds, blockIdx.x - own);
+  static_assert(sizeof(lds) >= 4 * kStreamLds, "the waves' value rows fit");
+  const int wg = blockIdx.x;
+  const bool own = wg < a.own_wgs;
+  if constexpr (SETS > 0) {
+    if (own) {
+      stream_role<DT, D, SETS>(a, &lds.ring[0][0], wg);
+      return;
+    }
+  }
+  const int run = wg / a.H, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  OwnRun o;
+  TreePiece pc;
+  bool more;
+  if (SETS == 0 && own) {
+    pc.h = wg % a.H;
+    more = find_run<DT, D>(a, lds.tbl, wg, [&](int) { return run; }, &o) && next_own<DT, D>(a, lds, run, &o, &pc);
+  } else {
+    more = prefix_piece<DT, D>(a, lds, wg - a.own_wgs, &pc);
+  }
+  while (more) {                                          // one place for both roles' tiles
+    if (tree_detail::kSets<DT> == 2 && (wave + 4) * 16 < pc.ncols)
+      tree_piece<DT, D, tree_detail::kSets<DT>>(a, lds, pc);
+    else
+      tree_piece<DT, D, 1>(a, lds, pc);
+    more = SETS == 0 && own && next_own<DT, D>(a, lds, run, &o, &pc);
+  }
 }
 
-// Join: a workgroup per row combines the partial results of its query heads.  With
-// base-2 log-sum-exps l_i and normalised outputs o_i of disjoint key sets,
-// l = log2 sum 2^{l_i}, o = sum 2^{l_i - l} o_i.  A wave takes a head at a time; lane i
-// holds the weight of partial i.
-template <int DT, int D>
-__global__ __launch_bounds__(256) void k_tree_join(TreeArgs a) {
+// One launch for a small call of few columns: NW waves share the keys of one request
+// and cache head (the chain's prefixes, then the own tokens: a contiguous share of
+// their units each) and meet in LDS.
+template <int DT, int D, int NS, int NW>
+__global__ __launch_bounds__(NW * 64) void k_tree_small(TreeArgs a) {
   using E = Elem<DT>;
-  constexpr int EPL = D / kWave;
-  const int lane = threadIdx.x & 63;
+  constexpr int UNIT = tree_unit(DT, D), COLS = 16 * NS, STRIDE = D + 4;   // (rows off the same banks)
+  constexpr int O_B = NW * COLS * STRIDE * 4;
+  __shared__ __attribute__((aligned(1024))) char lds[O_B > NW * kStreamLds ? O_B : NW * kStreamLds];
+  __shared__ float s_m[NW][COLS], s_t[NW][COLS], s_w[NW][COLS];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int t = blockIdx.x;
-  const int r = __builtin_amdgcn_readfirstlane(request_of_row(a.qoff, a.R, t, lane));
-  if (r < 0) return;
+  const int r = blockIdx.x / a.H, h = blockIdx.x % a.H, HQ = a.H * a.G;
   const int S = clampi(ld_uniform(a.slen + r), 0, a.max_s);
+  int g = ld_uniform(a.gid + r);
   const RowSpan rw = row_span(a.qoff, r, a.T, min(S, a.max_q));
-  if (t < rw.first || t >= rw.first + rw.count) return;   // padding
-  const int q = ld_uniform(a.starts + a.R + 1), start = ld_uniform(a.starts + r);
-  const int units = (S + tree_unit(DT, D) - 1) / tree_unit(DT, D);
-  // the chunks of the chain's levels, outermost first
-  int np[kMaxDepth] = {0, 0, 0, 0}, len[kMaxDepth];
-  int nlev = 0;
-  const int gid = ld_uniform(a.gid + r);
-  const bool prefixed = a.seg_p > 0 && gid >= 0 && gid < a.NG;
-  for (int g = gid; a.seg_p > 0 && g >= 0 && g < a.NG && nlev < a.depth;
-       g = a.parents ? ld_uniform(a.parents + g) : -1)
-    len[nlev++] = min((clampi(ld_uniform(a.plen + g), 0, a.max_p) + a.cp - 1) / a.cp, a.seg_p);
+  const int ncols = min(rw.count * a.G, COLS), base = S - rw.count;
+  if (ncols == 0) return;
+  TreeStream<DT, D, NS> st(lds + wave * kStreamLds, a.H, h, a.scale_log2);
+  auto row_of = [&](int col) {
+    const int row = col / a.G;
+    return (size_t)(rw.first + row) * HQ + h * a.G + (col - row * a.G);
+  };
+  st.template load_queries<true>(a.q, ncols, row_of);
+  st.build_masks(a.tree, rw, base, a.G);
+  // lengths of the chain's prefixes, innermost first, then the own tokens
+  int grp[kMaxDepth], len[kMaxDepth + 1], total = 0;
 #pragma unroll
-  for (int l = 0; l < kMaxDepth; ++l)
+  for (int l = 0; l < kMaxDepth; ++l) {
+    grp[l] = 0; len[l] = 0;
+    if (l < a.depth && g >= 0 && g < a.NG) {
+      grp[l] = g;
+      len[l] = clampi(ld_uniform(a.plen + g), 0, a.max_p);
+      g = a.parents ? ld_uniform(a.parents + g) : -1;
+    } else {
+      g = -1;
+    }
+    total += (len[l] + UNIT - 1) / UNIT;
+  }
+  len[kMaxDepth] = S;
+  total += (S + UNIT - 1) / UNIT;
+  const int u0 = total * wave / NW, u1 = total * (wave + 1) / NW;
+  int at = 0;
+#pragma unroll 1
+  for (int l = 0; l <= kMaxDepth; ++l) {
+    int n = len[kMaxDepth], gl = 0;
 #pragma unroll
     for (int x = 0; x < kMaxDepth; ++x)
-      if (x == nlev - 1 - l) np[l] = len[x];
-  const int b1 = np[0], b2 = b1 + np[1], b3 = b2 + np[2], b4 = b3 + np[3];
+      if (x == l) { n = len[x]; gl = grp[x]; }
+    const bool pre = l < kMaxDepth;
+    const int units = (n + UNIT - 1) / UNIT;
+    TreeRange rg;
+    rg.pk = pre ? a.pk : a.sk;
+    rg.pv = pre ? a.pv : a.sv;
+    rg.tbl = pre ? a.ptab + (long)gl * a.pstride : a.stab + (long)r * a.sstride;
+    rg.npool = pre ? a.npblk : a.nsblk;
+    rg.t0 = max(u0 - at, 0) * UNIT;
+    rg.t1 = min(n, (u1 - at) * UNIT);
+    rg.mask0 = pre ? 0x40000000 : base & ~31;
+    rg.base = pre ? rg.t1 : base;
+    rg.end = pre ? rg.t1 : S;
+    at += units;
+    if (rg.t0 < rg.t1) st.run(rg);
+  }
+  // the waves' results meet in LDS
+  __syncthreads();
+  float* so = reinterpret_cast<float*>(lds);
+  st.finish([&](int c, int col, float lw, float, float lt) {
+    float* dst = so + ((size_t)wave * COLS + col) * STRIDE + 4 * (st.lane >> 4);
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) *reinterpret_cast<f32x4*>(dst + dt * 16) = st.o[c][dt];
+    if (st.lane < 16) { s_m[wave][col] = st.mref[c]; s_t[wave][col] = lt; s_w[wave][col] = lw; }
+  });
+  __syncthreads();
+  constexpr int EPT = 4;                                  // elements per thread
+  for (int x = threadIdx.x; x < ncols * (D / EPT); x += NW * 64) {
+    const int col = x / (D / EPT), d = x % (D / EPT) * EPT;
+    float mx = s_m[0][col];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) mx = fmaxf(mx, s_m[w][col]);
+    float tot = 0.f, wsum = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float f = fast_exp2(s_m[w][col] - mx);
+      tot = __builtin_fmaf(f, s_t[w][col], tot);
+      wsum = __builtin_fmaf(f, s_w[w][col], wsum);
+      acc += f * *reinterpret_cast<const f32x4*>(so + ((size_t)w * COLS + col) * STRIDE + d);
+    }
+    const size_t row = row_of(col);
+    char* dst = (char*)a.out + (row * D + d) * E::kBytes;
+    const f32x4 v = acc * (1.f / wsum);
+    if constexpr (DT == kF32) *reinterpret_cast<f32x4*>(dst) = v;
+    else store4<DT>(dst, v);
+    if (d == 0) a.lse[row] = (mx + fast_log2(tot)) * kLn2;
+  }
+}
+
+// Join of the partial results of a row's query heads.  With base-2 log-sum-exps l_i and
+// normalised outputs o_i of disjoint key sets, l = log2 sum 2^{l_i}, o = sum 2^{l_i - l} o_i.
+// D / 4 lanes hold a head (16 bytes a lane), so a wave takes two or four heads of a
+// row; lane i of them holds the weight of partial i.  Bound by the round trips of
+// descriptor, log-sum-exps and outputs, and by the partial results' bytes.
+template <int DT, int D>
+__global__ __launch_bounds__(256) void k_tree_join(TreeArgs a) {
+  constexpr int GW = D / 4, HPW = kWave / GW;             // lanes per head, heads per wave
+  constexpr int U = 4;                                    // partial results loaded together
+  const int lane = threadIdx.x & 63;
   const int HQ = a.H * a.G;
-  for (int hq = wave; hq < HQ; hq += 4) {
-    const int col = (t - rw.first) * a.G + hq % a.G;
-    const int s0 = start + col / tree_detail::kCols<DT> * (units + kTreeSetup) + kTreeSetup;
-    const int pieces = (s0 + units - 1) / q - s0 / q + 1;
-    if (!prefixed && pieces == 1) continue;               // written by the piece itself
-    const int n = b4 + pieces;
-    auto slot_of = [&](int i) {
-      int sl = a.seg_pre + (i - b4);
-      sl = i < b4 ? 3 * a.seg_p + (i - b3) : sl;
-      sl = i < b3 ? 2 * a.seg_p + (i - b2) : sl;
-      sl = i < b2 ? a.seg_p + (i - b1) : sl;
-      return i < b1 ? i : sl;
-    };
-    const size_t at = (size_t)t * HQ + hq;
-    const float* lsep = a.lse_part + at * a.seg;
-    const float* op = a.o_part + at * a.seg * D;
-    float mx = -INFINITY;
-    for (int i = lane; i < n; i += kWave) mx = fmaxf(mx, lsep[slot_of(i)]);
-    mx = fmaxf(mx, dpp_f<kDppXor1>(mx));
-    mx = fmaxf(mx, dpp_f<kDppXor2>(mx));
-    mx = fmaxf(mx, dpp_f<kDppHalfMirror>(mx));
-    mx = fmaxf(mx, dpp_f<kDppMirror>(mx));
-    mx = max_xor32(max_xor16(mx));
-    float tot = 0.f, acc[EPL];
+  const unsigned per_row = (HQ + HPW - 1) / HPW;          // (T * HQ is below 2^31)
+  const unsigned w = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int t = (int)(w / per_row);
+  if (t >= a.T) return;
+  const int hq = (int)(w - t * per_row) * HPW + lane / GW, i0 = lane % GW;
+  const int* d = a.desc + (size_t)t * kTreeDesc;
+  const int first = ld_uniform(d), between = ld_uniform(d + 1), units = ld_uniform(d + 2), q = max(1, ld_uniform(d + 3));
+  const unsigned lo = (unsigned)ld_uniform(d + 4), hi = (unsigned)ld_uniform(d + 5);
+  const int j = ld_uniform(d + 6), prefixed = ld_uniform(d + 7);
+  if (t >= ld_uniform(a.qoff + a.R)) return;              // padding (its descriptor holds nothing)
+  const int s0 = first + (j * a.G + hq % a.G) / tree_detail::kCols<DT> * between;
+  const int pieces = (s0 + units - 1) / q - s0 / q + 1;
+  // (clamped, so that a row without a descriptor, in a call that breaks the rules, reads
+  // inside its slots)
+  const int b1 = min((int)(lo & 0xFFFFu), a.seg_p), b2 = b1 + min((int)(lo >> 16), a.seg_p);
+  const int b3 = b2 + min((int)(hi & 0xFFFFu), a.seg_p), b4 = min(b3 + min((int)(hi >> 16), a.seg_p), a.seg_pre);
+  const bool live = hq < HQ && !(prefixed == 0 && pieces == 1);   // one piece: it wrote the output
+  const int n = live ? b4 + min(max(pieces, 0), a.seg - a.seg_pre) : 0;
+  auto slot_of = [&](int i) {
+    int sl = a.seg_pre + (i - b4);
+    sl = i < b4 ? 3 * a.seg_p + (i - b3) : sl;
+    sl = i < b3 ? 2 * a.seg_p + (i - b2) : sl;
+    sl = i < b2 ? a.seg_p + (i - b1) : sl;
+    return i < b1 ? i : sl;
+  };
+  int most = n;
 #pragma unroll
-    for (int e = 0; e < EPL; ++e) acc[e] = 0.f;
-    for (int b = 0; b < n; b += kWave) {
-      // (no guard on mx: logits that are all -inf give NaN)
-      const float w = b + lane < n ? fast_exp2(lsep[slot_of(b + lane)] - mx) : 0.f;
-      tot += w;
-      const int m = min(kWave, n - b);
-      for (int i = 0; i < m; ++i) {
-        const float wi = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), i));
-        const float* src = op + (size_t)slot_of(b + i) * D + lane * EPL;
+  for (int x = GW; x < kWave; x <<= 1) most = max(most, __shfl_xor(most, x));
+  most = __builtin_amdgcn_readfirstlane(most);
+  const size_t at = (size_t)t * HQ + min(hq, HQ - 1);
+  const float* lsep = a.lse_part + at * a.seg;
+  const float* op = a.o_part + at * a.seg * D + i0 * 4;
+  // the lane's first log-sum-exp, and the first outputs beside it
+  const float l0 = i0 < n ? lsep[slot_of(i0)] : -INFINITY;
+  f32x4 v[U];
+  auto load = [&](int i) {                                // partials i .. i + U - 1, those that exist
 #pragma unroll
-        for (int e = 0; e < EPL; ++e) acc[e] = __builtin_fmaf(wi, src[e], acc[e]);
+    for (int u = 0; u < U; ++u) {
+      v[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (i + u < n) v[u] = *reinterpret_cast<const f32x4*>(op + (size_t)slot_of(i + u) * D);
+    }
+  };
+  load(0);
+  float mx = l0;
+#pragma unroll 1
+  for (int i = i0 + GW; i < n; i += GW) mx = fmaxf(mx, lsep[slot_of(i)]);
+  mx = fmaxf(mx, dpp_f<kDppXor1>(mx));
+  mx = fmaxf(mx, dpp_f<kDppXor2>(mx));
+  mx = fmaxf(mx, dpp_f<kDppHalfMirror>(mx));
+  mx = fmaxf(mx, dpp_f<kDppMirror>(mx));
+  if constexpr (GW == 32) mx = max_xor16(mx);
+  float tot = 0.f;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+  for (int b = 0; b < most; b += GW) {
+    // (no guard on mx: logits that are all -inf give NaN)
+    const float wl = b == 0 ? l0 : b + i0 < n ? lsep[slot_of(b + i0)] : -INFINITY;
+    const float wt = b + i0 < n ? fast_exp2(wl - mx) : 0.f;
+    tot += wt;
+    const int end = min(GW, most - b);
+#pragma unroll 1
+    for (int i = 0; i < end; i += U) {
+      if (b + i > 0) load(b + i);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float wi = __shfl(wt, (lane & ~(GW - 1)) + min(i + u, GW - 1));
+        acc += (b + i + u < n ? wi : 0.f) * v[u];
       }
     }
-    tot = group_sum<64>(tot);
-    const float inv = 1.f / tot;
-    char* dst = (char*)a.out + (at * D + lane * EPL) * E::kBytes;
-#pragma unroll
-    for (int e = 0; e < EPL; ++e) E::store1(dst + e * E::kBytes, acc[e] * inv);
-    if (lane == 0) a.lse[at] = (mx + fast_log2(tot)) * kLn2;
+  }
+  tot = group_sum<GW>(tot);
+  if (!live) return;
+  char* dst = (char*)a.out + (at * D + i0 * 4) * Elem<DT>::kBytes;
+  const f32x4 res = acc * (1.f / tot);
+  if constexpr (DT == kF32) *reinterpret_cast<f32x4*>(dst) = res;
+  else store4<DT>(dst, res);
+  if (i0 == 0) a.lse[at] = (mx + fast_log2(tot)) * kLn2;
+}
+
+template <int DT, int D>
+static void launch_tree_t(const TreeArgs& a, int waves, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
+  const dim3 pairs((unsigned)((long)a.R * a.H)), wg(waves * 64);
+  if (a.sets == 0) {
+    const long groups = ((long)a.R * a.H + 7) / 8;
+    hipExtLaunchKernelGGL((k_tree_decode<DT, D>), dim3((unsigned)(groups * 8 * a.tiles)), dim3(256), 0, s, e0, e1, 0, a);
+  } else if (a.sets == 1) {
+    if (waves == 8) hipExtLaunchKernelGGL((k_tree_small<DT, D, 1, 8>), pairs, wg, 0, s, e0, e1, 0, a);
+    else hipExtLaunchKernelGGL((k_tree_small<DT, D, 1, 4>), pairs, wg, 0, s, e0, e1, 0, a);
+  } else {
+    if (waves == 8) hipExtLaunchKernelGGL((k_tree_small<DT, D, 2, 8>), pairs, wg, 0, s, e0, e1, 0, a);
+    else hipExtLaunchKernelGGL((k_tree_small<DT, D, 2, 4>), pairs, wg, 0, s, e0, e1, 0, a);
   }
 }
-
 template <int DT, int D>
-static hipError_t launch_tree_t(const TreeArgs& a, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
-  const long groups = ((long)a.R * a.H + 7) / 8;
-  hipExtLaunchKernelGGL((k_tree_decode<DT, D>), dim3((unsigned)(groups * 8 * a.tiles)), dim3(256), 0, s, e0, e1, 0, a);
-  return hipGetLastError();
-}
-
-hipError_t launch_tree(const TreeArgs& a, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
-  if (a.T < 1 || a.R < 1 || a.H < 1 || a.G < 1 || a.max_q < 1 || a.max_q > kTreeRows || a.tiles < 1 ||
-      (long)a.tiles * tree_cols(dtype) < (long)a.max_q * a.G || a.sstride < 1 || a.nsblk < 1 ||
-      ((long)a.R * a.H + 7) / 8 * 8 * a.tiles > 0x7fffffffL || (a.NG > 0 && (a.npblk < 1 || a.pstride < 1)))
-    return hipErrorInvalidValue;
-  switch (dtype * 1000 + D) {
-    case kF32 * 1000 + 64: return launch_tree_t<kF32, 64>(a, s, e0, e1);
-    case kF32 * 1000 + 128: return launch_tree_t<kF32, 128>(a, s, e0, e1);
-    case kF16 * 1000 + 64: return launch_tree_t<kF16, 64>(a, s, e0, e1);
-    case kF16 * 1000 + 128: return launch_tree_t<kF16, 128>(a, s, e0, e1);
-    case kBF16 * 1000 + 64: return launch_tree_t<kBF16, 64>(a, s, e0, e1);
-    case kBF16 * 1000 + 128: return launch_tree_t<kBF16, 128>(a, s, e0, e1);
-  }
-  return hipErrorInvalidValue;
-}
-
-template <int DT, int D>
-static void launch_partials_t(const TreeArgs& a, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
-  const dim3 grid((unsigned)((long)a.runs * a.H + a.n_pre));
-  hipExtLaunchKernelGGL((k_tree_partials<DT, D>), grid, dim3(256), 0, s, e0, e1, 0, a);
+static void launch_partials_t(const TreeArgs& a, int, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
+  const dim3 grid((unsigned)((long)a.own_wgs + a.n_pre));
+  if (a.sets == 0) hipExtLaunchKernelGGL((k_tree_partials<DT, D, 0>), grid, dim3(256), 0, s, e0, e1, 0, a);
+  else if (a.sets == 1) hipExtLaunchKernelGGL((k_tree_partials<DT, D, 1>), grid, dim3(256), 0, s, e0, e1, 0, a);
+  else hipExtLaunchKernelGGL((k_tree_partials<DT, D, 2>), grid, dim3(256), 0, s, e0, e1, 0, a);
 }
 template <int DT, int D>
-static void launch_join_t(const TreeArgs& a, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
-  hipExtLaunchKernelGGL((k_tree_join<DT, D>), dim3((unsigned)a.T), dim3(256), 0, s, e0, e1, 0, a);
+static void launch_join_t(const TreeArgs& a, int, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
+  const int hpw = kWave / (D / 4), per_row = (a.H * a.G + hpw - 1) / hpw;
+  hipExtLaunchKernelGGL((k_tree_join<DT, D>), dim3((unsigned)(((long)a.T * per_row + 3) / 4)), dim3(256), 0, s, e0, e1, 0, a);
 }
 
-#define PARROT_TREE_LAUNCH(NAME)                                              \
+#define PARROT_TREE_LAUNCH(NAME, WAVES)                                       \
   switch (dtype * 1000 + D) {                                                 \
-    case kF32 * 1000 + 64: NAME<kF32, 64>(a, s, e0, e1); break;               \
-    case kF32 * 1000 + 128: NAME<kF32, 128>(a, s, e0, e1); break;             \
-    case kF16 * 1000 + 64: NAME<kF16, 64>(a, s, e0, e1); break;               \
-    case kF16 * 1000 + 128: NAME<kF16, 128>(a, s, e0, e1); break;             \
-    case kBF16 * 1000 + 64: NAME<kBF16, 64>(a, s, e0, e1); break;             \
-    case kBF16 * 1000 + 128: NAME<kBF16, 128>(a, s, e0, e1); break;           \
+    case kF32 * 1000 + 64: NAME<kF32, 64>(a, WAVES, s, e0, e1); break;        \
+    case kF32 * 1000 + 128: NAME<kF32, 128>(a, WAVES, s, e0, e1); break;      \
+    case kF16 * 1000 + 64: NAME<kF16, 64>(a, WAVES, s, e0, e1); break;        \
+    case kF16 * 1000 + 128: NAME<kF16, 128>(a, WAVES, s, e0, e1); break;      \
+    case kBF16 * 1000 + 64: NAME<kBF16, 64>(a, WAVES, s, e0, e1); break;      \
+    case kBF16 * 1000 + 128: NAME<kBF16, 128>(a, WAVES, s, e0, e1); break;    \
     default: return hipErrorInvalidValue;                                     \
   }                                                                           \
   return hipGetLastError()
 
+// What every launch needs; sets > 0 promises that a request's columns fit them.
+static bool tree_args_ok(const TreeArgs& a) {
+  return a.T >= 1 && a.R >= 1 && a.H >= 1 && a.G >= 1 && a.max_q >= 1 && a.max_q <= kTreeRows && a.sstride >= 1 &&
+         a.nsblk >= 1 && a.depth <= kMaxDepth && (a.NG == 0 || (a.npblk >= 1 && a.pstride >= 1)) && a.sets >= 0 &&
+         a.sets <= 2 && (a.sets == 0 || (long)a.max_q * a.G <= 16 * a.sets);
+}
+
+hipError_t launch_tree(const TreeArgs& a, int waves, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
+  if (!tree_args_ok(a) || a.tiles < 1 || (long)a.tiles * tree_cols(dtype) < (long)a.max_q * a.G ||
+      (waves != 4 && waves != 8) || ((long)a.R * a.H + 7) / 8 * 8 * a.tiles * waves * 64 > 0xffffffffL)
+    return hipErrorInvalidValue;
+  PARROT_TREE_LAUNCH(launch_tree_t, waves);
+}
+
 hipError_t launch_tree_partials(const TreeArgs& a, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
   const long pre = a.n_pre > 0 ? ((long)a.NG * a.seg_p * a.H + 7) / 8 * 8 * a.tiles_p : 0;
-  if (a.T < 1 || a.R < 1 || a.H < 1 || a.G < 1 || a.max_q < 1 || a.max_q > kTreeRows || a.sstride < 1 ||
-      a.nsblk < 1 || a.runs < 1 || a.min_run < 1 || !a.o_part || !a.lse_part || !a.starts || a.n_pre != pre ||
-      (a.n_pre > 0 && (a.npblk < 1 || a.pstride < 1 || a.cp < 64 || a.cp % 64 != 0 || a.depth < 1)) ||
-      (long)a.runs * a.H + a.n_pre > 0x7fffffffL || a.depth > kMaxDepth)
+  if (!tree_args_ok(a) || a.runs < 1 || a.min_run < 1 || a.own_wgs < 1 ||
+      (long)a.own_wgs * (a.sets ? 4 : 1) < (long)a.runs * a.H || !a.o_part || !a.lse_part || !a.desc || a.n_pre != pre ||
+      (a.n_pre > 0 && (a.cp < 64 || a.cp % 64 != 0 || a.depth < 1)) || ((long)a.own_wgs + a.n_pre) * 256 > 0xffffffffL)
     return hipErrorInvalidValue;
-  PARROT_TREE_LAUNCH(launch_partials_t);
+  PARROT_TREE_LAUNCH(launch_partials_t, 0);
 }
 
 hipError_t launch_tree_join(const TreeArgs& a, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
-  PARROT_TREE_LAUNCH(launch_join_t);
+  if (!tree_args_ok(a) || !a.desc || a.seg < 1) return hipErrorInvalidValue;
+  PARROT_TREE_LAUNCH(launch_join_t, 0);
 }
 
 }  // namespace parrot

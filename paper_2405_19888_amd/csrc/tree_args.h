@@ -31,22 +31,31 @@ struct TreeArgs {
   // prefix at level l of the request's chain (0: outermost), the rest the pieces of
   // the own tokens.
   float* o_part; float* lse_part;
-  int* starts;                           // [R + 2]: where each request's cost begins, the total, the run
+  int* desc;                             // [T][kTreeDesc]: what the join needs of each row
   int seg, seg_p, seg_pre;
   int cp;                                // prefix chunk tokens
   int tiles_p;                           // column tiles per group
-  int runs;                              // runs of the own tokens' cost, a workgroup each per cache head
+  int sets;                              // 0: own tokens by tiles, else by waves of that many column sets
+  int own_wgs;                           // workgroups of the own tokens
+  int runs;                              // runs of the own tokens' cost: a workgroup each (by waves: a wave)
+                                         // per cache head
   int min_run;                           // least cost of a run
   int n_pre;                             // prefix workgroups
 };
+
+// Row descriptor: cost of the first unit of the row's first column tile, cost between
+// tiles, units, run length, prefix chunks of the chain's levels (outermost first, 16
+// bits each, two ints), the row within its request, whether it has prefixes.
+constexpr int kTreeDesc = 8;
 
 // Own tokens are streamed in units of kTreeUnit tokens; a column tile of a request costs
 // its units and kTreeSetup more.
 constexpr int kTreeSetup = 2;
 constexpr int tree_unit(int dtype, int D) { return dtype != kF32 && D == 64 ? 64 : 32; }
 
-// One workgroup per request, cache head and column tile, output written by it.
-hipError_t launch_tree(const TreeArgs& a, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
+// One workgroup per request, cache head and column tile, output written by it: a tile,
+// or with sets > 0 `waves` waves that share the keys.
+hipError_t launch_tree(const TreeArgs& a, int waves, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
 // Partial results of prefixes and own tokens, and their combination.
 hipError_t launch_tree_partials(const TreeArgs& a, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
 hipError_t launch_tree_join(const TreeArgs& a, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1);

@@ -49,6 +49,7 @@ struct Lds {
   char ring[kRing3][kStageBytes];
   unsigned mask[kMaskWords][kCols<DT>];   // visible drafted tokens of each column
   int tbl[kTreeSpan];                     // block ids of the current span, clamped
+  int rows[kCols<DT> + 2];                // q rows that hold the tile's columns
   unsigned bad[kRing3][4];                // tokens of a stage with cleared values, a bit each
 };
 // three workgroups of a CU share its 160 KiB, handed out in pieces of 1280 bytes
@@ -112,48 +113,44 @@ struct TreeRange {
   int base, end;                    // masked ranges: the drafted tokens are [base, end)
 };
 
-// One wave's part of a tile: its NS column sets' softmax statistics and output, in
-// registers.  Waves of one workgroup may run parts of different NS side by side:
-// every part makes the same loads and barriers.
+// A wave's columns: NS sets of 16 with their queries, softmax statistics and output, in
+// registers.
 template <int DT, int D, int NS>
-struct TreeTile {
+struct TreeState {
   static constexpr int EB = Elem<DT>::kBytes;
   static constexpr int ROW_B = D * EB;
   static constexpr int GRAN = ROW_B / 16;                    // 16-byte granules per row
   static constexpr int BLK_B = kBlock * ROW_B;               // one block of one head
-  static constexpr int STAGE_BLK = prefix_detail::kTensorStage / BLK_B;
   static constexpr int DT16 = D / 16;
   static constexpr int KS = DT == kF32 ? D / 4 : D / 32;     // MFMA k-steps over D
-  static constexpr int PER_WAVE = prefix_detail::kStageChunks / 4;
   static constexpr float kLazy = 8.f;
-  using L = tree_detail::Lds<DT>;
 
-  L& lds;
-  int lane, wave, H, h;
+  int lane, H, h;
+  int set0, stride;                   // set c is set set0 + stride c of the columns
   float scale, inv_scale;
   unsigned qsign;
-  bool act;                           // wave-uniform: the wave has columns
   u32x4 qf[NS][DT == kF32 ? 1 : KS];
   float qs[NS][DT == kF32 ? KS : 1];
   float mref[NS], thr[NS], lsum[NS], lsr[NS];
   f32x4 o[NS][DT16];
 
-  PARROT_DEV TreeTile(L& l, int heads, int head, float scale_log2) : lds(l), H(heads), h(head) {
+  PARROT_DEV TreeState(int heads, int head, float scale_log2, int first, int step)
+      : H(heads), h(head), set0(first), stride(step) {
     lane = threadIdx.x & 63;
-    wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // a negative scale flips the sign of q (exact); a zero scale is taken as 1e-30
     scale = fmaxf(fabsf(scale_log2), 1e-30f);
     inv_scale = 1.f / scale;
     qsign = scale_log2 < 0.f ? (DT == kF32 ? 0x80000000u : 0x80008000u) : 0u;
   }
-  // column of the tile that this lane holds in set c
-  PARROT_DEV int column(int c) const { return (wave + 4 * c) * 16 + (lane & 15); }
+  // the column that this lane holds in set c
+  PARROT_DEV int column(int c) const { return (set0 + stride * c) * 16 + (lane & 15); }
 
   // Loads the queries of `ncols` columns; qrow(col) is the column's row of q in units
-  // of heads (row * HQ + query head).
-  template <class F>
+  // of heads (row * HQ + query head).  Lane group g of 16 holds, of k-step ks, the
+  // elements 32 ks + 8 g .. + 7 (16-bit), or 4 ks + g (fp32; CHUNKS: 4 g + ks % 4 of
+  // 16-element piece ks / 4, as keys come from 16-byte loads).
+  template <bool CHUNKS, class F>
   PARROT_DEV void load_queries(const void* q, int ncols, F qrow) {
-    act = wave * 16 < ncols;
 #pragma unroll
     for (int c = 0; c < NS; ++c) {
       const int col = column(c);
@@ -162,7 +159,8 @@ struct TreeTile {
       if constexpr (DT == kF32) {
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-          const float x = ok ? reinterpret_cast<const float*>(src)[4 * ks + (lane >> 4)] : 0.f;
+          const int e = CHUNKS ? 16 * (ks >> 2) + 4 * (lane >> 4) + (ks & 3) : 4 * ks + (lane >> 4);
+          const float x = ok ? reinterpret_cast<const float*>(src)[e] : 0.f;
           qs[c][ks] = __uint_as_float(__float_as_uint(x) ^ qsign);
         }
       } else {
@@ -178,6 +176,121 @@ struct TreeTile {
     }
   }
 
+  // NX logits a lane: x[i] is token tok0 + 16 (i / 4) + 4 (lane / 16) + i % 4.  mask: those whose
+  // bit of `vis` (from tok0 on) is clear become -inf.  softmax: x becomes the
+  // probabilities, set c's state moves on.
+  template <int NX>
+  PARROT_DEV void mask(float* x, unsigned vis) const {
+    const unsigned mine = vis >> (4 * (lane >> 4));
+#pragma unroll
+    for (int i = 0; i < NX; ++i) x[i] = (mine >> ((i >> 2) * 16 + (i & 3))) & 1u ? x[i] : -INFINITY;
+  }
+  template <int NX>
+  PARROT_DEV void softmax(float* x, int c) {
+    // (grouped as v_max3 takes them)
+    float lm = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+    if constexpr (NX == 8)
+      lm = fmaxf(fmaxf(fmaxf(fmaxf(x[0], x[1]), x[2]), fmaxf(fmaxf(x[3], x[4]), x[5])), fmaxf(x[6], x[7]));
+    if (__builtin_amdgcn_ballot_w64(lm > thr[c]) != 0) {
+      const float mn = fmaxf(mref[c], max_xor32(max_xor16(lm)) * scale);
+      const float alpha = fast_exp2(mref[c] - mn);
+      lsum[c] *= alpha;
+      lsr[c] *= alpha;
+#pragma unroll
+      for (int i = 0; i < DT16; ++i) o[c][i] *= alpha;
+      mref[c] = mn;
+      thr[c] = (mn + kLazy) * inv_scale;
+    }
+#pragma unroll
+    for (int i = 0; i < NX; ++i) x[i] = fast_exp2(__builtin_fmaf(x[i], scale, -mref[c]));
+    if constexpr (NX == 8) lsum[c] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+    else lsum[c] += (x[0] + x[1]) + (x[2] + x[3]);
+  }
+
+  // Adds the cleared elements of the values (see the head of this file) of the tokens in
+  // `bad` to set c: p are the lane's probabilities, vis its column's bits, value_row(t)
+  // the memory of token t's value.
+  template <int NX, class F>
+  PARROT_DEV void add_cleared(const float* p, int c, unsigned vis, unsigned bad, F value_row) {
+    while (bad) {                                            // wave-uniform
+      const int t = __ffs((int)bad) - 1;
+      bad &= bad - 1;
+      float mine = 0.f;                                      // held by lane group (t % 16) / 4
+#pragma unroll
+      for (int i = 0; i < NX; ++i)
+        if (i == (t >> 4) * 4 + (t & 3)) mine = p[i];
+      const float pt = __shfl(mine, (lane & 15) + 16 * ((t & 15) >> 2));
+      const char* row = value_row(t);
+#pragma unroll
+      for (int dt = 0; dt < DT16; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float v = tree_detail::elem_at<DT>(row + (dt * 16 + 4 * (lane >> 4) + i) * EB);
+          if (!(fabsf(v) <= FLT_MAX) && ((vis >> t) & 1u)) o[c][dt][i] = __builtin_fmaf(pt, v, o[c][dt][i]);
+        }
+    }
+  }
+
+  // The columns' result: f(c, col, weight sum for the output, base-2 lse, weight sum)
+  // per set; the lane holds elements dt * 16 + 4 (lane / 16) .. + 3 of its column.
+  template <class F>
+  PARROT_DEV void finish(F f) {
+#pragma unroll
+    for (int c = 0; c < NS; ++c) {
+      const float lt = sum_xor32(sum_xor16(lsum[c]));
+      const float lw = DT == kF32 ? lt : sum_xor32(sum_xor16(lsr[c]));
+      f(c, column(c), lw, mref[c] + fast_log2(lt), lt);
+    }
+  }
+};
+
+// One wave's part of a tile.  Waves of one workgroup may run parts of different NS side
+// by side: every part makes the same loads and barriers.
+template <int DT, int D, int NS>
+struct TreeTile : TreeState<DT, D, NS> {
+  using Base = TreeState<DT, D, NS>;
+  using Base::lane; using Base::H; using Base::h; using Base::qf; using Base::qs; using Base::o; using Base::lsr;
+  using Base::column;
+  static constexpr int ROW_B = Base::ROW_B, GRAN = Base::GRAN, BLK_B = Base::BLK_B, DT16 = Base::DT16, KS = Base::KS;
+  static constexpr int STAGE_BLK = prefix_detail::kTensorStage / BLK_B;
+  static constexpr int PER_WAVE = prefix_detail::kStageChunks / 4;
+  using L = tree_detail::Lds<DT>;
+
+  L& lds;
+  int wave;
+  bool act;                           // wave-uniform: the wave has columns
+  // 16-bit caches: LDS byte addresses of this lane's K fragment (k-step ks) and V^T
+  // fragment (d tile dt) in block 0 of ring buffer 0; buffers and blocks add constants.
+  // Opaque, so that one register holds each and a read is one instruction.
+  unsigned ka[DT == kF32 ? 1 : KS], va[DT == kF32 ? 1 : DT16];
+
+  PARROT_DEV TreeTile(L& l, int heads, int head, float scale_log2, int ncols)
+      : Base(heads, head, scale_log2, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), 4), lds(l) {
+    wave = this->set0;
+    act = wave * 16 < ncols;
+    if constexpr (DT != kF32) {
+      const unsigned base = lds_addr(&lds.ring[0][0]);
+      const int krow = lane & 15, vrow = 4 * (lane >> 4) + ((lane & 15) >> 2);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        ka[ks] = base + krow * ROW_B + (((4 * ks + (lane >> 4)) ^ tree_detail::swizzle<DT, D>(krow)) << 4);
+        asm volatile("" : "+v"(ka[ks]));
+      }
+#pragma unroll
+      for (int dt = 0; dt < DT16; ++dt) {
+        va[dt] = base + prefix_detail::kTensorStage + vrow * ROW_B + 8 * (lane & 1) +
+                 (((2 * dt + ((lane & 3) >> 1)) ^ tree_detail::swizzle<DT, D>(vrow)) << 4);
+        asm volatile("" : "+v"(va[dt]));
+      }
+    }
+  }
+
+  // memory of the value of token tok of the range
+  PARROT_DEV const char* value_row(const TreeRange& rg, int span0, int tok) const {
+    const int blk = lds.tbl[tok / kBlock - span0];
+    return (const char*)rg.pv + (((size_t)blk * H + h) * kBlock + tok % kBlock) * ROW_B;
+  }
+
   // S^T of one block for set c; kb: the block's K in LDS
   PARROT_DEV f32x4 scores32(const char* kb, int c) const {
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
@@ -191,98 +304,44 @@ struct TreeTile {
     return s;
   }
 
-  // Softmax step of set c over NX logits a lane: token tok0 + 16 (i / 4) + 4 (lane / 16) + i % 4
-  // is visible where its bit of `vis` (from tok0 on) is set.  x becomes the
-  // probabilities.
-  template <int NX>
-  PARROT_DEV void softmax(float* x, int c, unsigned vis) {
-    const unsigned mine = vis >> (4 * (lane >> 4));
-    if (__builtin_amdgcn_ballot_w64(vis != (NX == 8 ? 0xFFFFFFFFu : 0xFFFFu)) != 0) {
-#pragma unroll
-      for (int i = 0; i < NX; ++i) x[i] = (mine >> ((i >> 2) * 16 + (i & 3))) & 1u ? x[i] : -INFINITY;
-    }
-    float lm = x[0];
-#pragma unroll
-    for (int i = 1; i < NX; ++i) lm = fmaxf(lm, x[i]);
-    if (__builtin_amdgcn_ballot_w64(lm > thr[c]) != 0) {
-      const float mn = fmaxf(mref[c], max_xor32(max_xor16(lm)) * scale);
-      const float alpha = fast_exp2(mref[c] - mn);
-      lsum[c] *= alpha;
-      lsr[c] *= alpha;
-#pragma unroll
-      for (int i = 0; i < DT16; ++i) o[c][i] *= alpha;
-      mref[c] = mn;
-      thr[c] = (mn + kLazy) * inv_scale;
-    }
-    float ps = 0.f;
-#pragma unroll
-    for (int i = 0; i < NX; ++i) {
-      x[i] = fast_exp2(__builtin_fmaf(x[i], scale, -mref[c]));
-      ps += x[i];
-    }
-    lsum[c] += ps;
-  }
-
-  // Adds the cleared elements of the values (see the head of this file) of the tokens in
-  // `bad` (from tok0 on) to set c: p are the lane's probabilities, vis its column's bits.
-  template <int NX>
-  PARROT_DEV void add_cleared(const TreeRange& rg, int span0, const float* p, int c, unsigned vis, unsigned bad, int tok0) {
-    while (bad) {                                            // wave-uniform
-      const int t = __ffs((int)bad) - 1;
-      bad &= bad - 1;
-      float mine = 0.f;                                      // held by lane group (t % 16) / 4
-#pragma unroll
-      for (int i = 0; i < NX; ++i)
-        if (i == (t >> 4) * 4 + (t & 3)) mine = p[i];
-      const float pt = __shfl(mine, (lane & 15) + 16 * ((t & 15) >> 2));
-      const int tok = tok0 + t;
-      const int blk = lds.tbl[tok / kBlock - span0];
-      const char* row = (const char*)rg.pv + (((size_t)blk * H + h) * kBlock + tok % kBlock) * ROW_B;
-#pragma unroll
-      for (int dt = 0; dt < DT16; ++dt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float v = tree_detail::elem_at<DT>(row + (dt * 16 + 4 * (lane >> 4) + i) * EB);
-          if (!(fabsf(v) <= FLT_MAX) && ((vis >> t) & 1u)) o[c][dt][i] = __builtin_fmaf(pt, v, o[c][dt][i]);
-        }
-    }
-  }
-
-  // One pair of blocks (32 tokens from tok0) of a stage (16-bit caches).
-  PARROT_DEV void pair(const TreeRange& rg, int span0, int buf, int bl, int tok0, bool masked) {
+  // One pair of blocks (32 tokens from tok0) of a stage, 16-bit caches; `at` is the byte
+  // offset of the pair in the ring (a constant but for masked stages).  K fragments
+  // are read ahead of their products and V^T fragments two d tiles per wait; one at a
+  // time, the LDS round trips took twice the time of the products.
+  template <bool MASKED>
+  PARROT_DEV void pair(const TreeRange& rg, int span0, int at, int tok0, unsigned bad) {
     using namespace prefix_detail;
-    const char* kb = lds.ring[buf] + bl * BLK_B;
-    const char* vb = kb + kTensorStage;
-    const int krow = lane & 15;
-    unsigned pw[NS][4];
     f32x4 s[NS][2];
 #pragma unroll
     for (int c = 0; c < NS; ++c) s[c][0] = s[c][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+    {
+      u32x4 kf[2][KS];
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      const int off = krow * ROW_B + (((4 * ks + (lane >> 4)) ^ tree_detail::swizzle<DT, D>(krow)) << 4);
+      for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const u32x4 kf = *reinterpret_cast<const u32x4*>(kb + b * BLK_B + off);
+        for (int ks = 0; ks < KS; ++ks) kf[b][ks] = lds_read16(ka[ks], at + b * BLK_B);
 #pragma unroll
-        for (int c = 0; c < NS; ++c)
-          s[c][b] = Mfma<DT>::qk(kf, qf[c][ks], s[c][b]);
-      }
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int c = 0; c < NS; ++c) s[c][b] = Mfma<DT>::qk(kf[b][ks], qf[c][ks], s[c][b]);
     }
+    unsigned pw[NS][4];
 #pragma unroll
     for (int c = 0; c < NS; ++c) {
       float x[8];
 #pragma unroll
       for (int i = 0; i < 4; ++i) { x[i] = s[c][0][i]; x[4 + i] = s[c][1][i]; }
       unsigned vis = 0xFFFFFFFFu;
-      if (masked) {
+      if constexpr (MASKED) {
         if (tok0 >= rg.mask0) vis = lds.mask[(tok0 - rg.mask0) >> 5][column(c)];
         else if (rg.t1 - tok0 < 32) vis = (1u << (rg.t1 - tok0)) - 1u;
+        this->template mask<8>(x, vis);
       }
-      softmax<8>(x, c, vis);
-      if (masked) {
-        const unsigned bad = __builtin_amdgcn_readfirstlane(lds.bad[buf][bl >> 1]);
-        if (bad) add_cleared<8>(rg, span0, x, c, vis, bad, tok0);
+      this->template softmax<8>(x, c);
+      if constexpr (MASKED) {
+        if (bad) this->template add_cleared<8>(x, c, vis, bad, [&](int t) { return value_row(rg, span0, tok0 + t); });
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -290,38 +349,44 @@ struct TreeTile {
         lsr[c] = add_pair<DT>(pw[c][i], lsr[c]);
       }
     }
-    const int vrow = 4 * (lane >> 4) + ((lane & 15) >> 2);
-    const char* va = vb + vrow * ROW_B + 8 * (lane & 1);
+    static_assert(DT16 % 2 == 0, "d tiles are read in pairs");
 #pragma unroll
-    for (int dt = 0; dt < DT16; ++dt) {
-      const int off = ((2 * dt + ((lane & 3) >> 1)) ^ tree_detail::swizzle<DT, D>(vrow)) << 4;
-      const unsigned long long v0 = Mfma<DT>::tr_read(va + off), v1 = Mfma<DT>::tr_read(va + BLK_B + off);
+    for (int dt = 0; dt < DT16; dt += 2) {
+      unsigned long long v[2][2];
 #pragma unroll
-      for (int c = 0; c < NS; ++c) {
-        const unsigned long long b0 = pw[c][0] | ((unsigned long long)pw[c][1] << 32);
-        const unsigned long long b1 = pw[c][2] | ((unsigned long long)pw[c][3] << 32);
-        o[c][dt] = Mfma<DT>::pv2(v0, v1, b0, b1, o[c][dt]);
+      for (int u = 0; u < 2; ++u) {
+        v[u][0] = lds_read_tr<DT>(va[dt + u], at);
+        v[u][1] = lds_read_tr<DT>(va[dt + u], at + BLK_B);
       }
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int c = 0; c < NS; ++c) {
+          const unsigned long long b0 = pw[c][0] | ((unsigned long long)pw[c][1] << 32);
+          const unsigned long long b1 = pw[c][2] | ((unsigned long long)pw[c][3] << 32);
+          o[c][dt + u] = Mfma<DT>::pv2(v[u][0], v[u][1], b0, b1, o[c][dt + u]);
+        }
     }
   }
 
   // One block (16 tokens from tok0) of a stage; fp32 caches.
-  PARROT_DEV void block32(const TreeRange& rg, int span0, int buf, int bl, int tok0, bool masked) {
+  template <bool MASKED>
+  PARROT_DEV void block32(const TreeRange& rg, int span0, int buf, int bl, int tok0, unsigned bad) {
     const char* kb = lds.ring[buf] + bl * BLK_B;
     const char* vb = kb + prefix_detail::kTensorStage;
 #pragma unroll
     for (int c = 0; c < NS; ++c) {
       const f32x4 s = scores32(kb, c);
       float x[4] = {s[0], s[1], s[2], s[3]};
-      unsigned vis = 0xFFFFu;
-      if (masked) {
+      if constexpr (MASKED) {
+        unsigned vis = 0xFFFFu;
         if (tok0 >= rg.mask0) vis = (lds.mask[(tok0 - rg.mask0) >> 5][column(c)] >> (tok0 & 16)) & 0xFFFFu;
         else if (rg.t1 - tok0 < 16) vis = (1u << (rg.t1 - tok0)) - 1u;
-      }
-      softmax<4>(x, c, vis);
-      if (masked) {
-        const unsigned bad = __builtin_amdgcn_readfirstlane(lds.bad[buf][bl >> 1]) >> (16 * (bl & 1)) & 0xFFFFu;
-        if (bad) add_cleared<4>(rg, span0, x, c, vis, bad, tok0);
+        this->template mask<4>(x, vis);
+        this->template softmax<4>(x, c);
+        if (bad) this->template add_cleared<4>(x, c, vis, bad, [&](int t) { return value_row(rg, span0, tok0 + t); });
+      } else {
+        this->template softmax<4>(x, c);
       }
       // O^T[d][col] += V^T[d][t] P^T[t][col] with k index kk <-> token 4 kk + kt
 #pragma unroll
@@ -403,70 +468,75 @@ struct TreeTile {
       }
     }
     wait_vmcnt<0>();
-    int buf = 0;
-    for (int st = 0; st < nstages; ++st) {
+    // stages that every column sees whole come first
+    const int full = max(0, min(rg.t1, rg.mask0) - b0 * kBlock) / (STAGE_BLK * kBlock);
+    const int plain = min(full, nstages);
+    // `bufc` carries the ring buffer as a constant: every LDS address of the stage is a
+    // lane constant plus an immediate offset
+    auto step = [&](int st, auto bufc) {
+      constexpr int buf = decltype(bufc)::value;
       wait_vmcnt<PER_WAVE>();            // this stage's loads are the oldest two rounds'
       lds_sync();
+      issue((buf + 2) % 3);
+      table(min(st + 3, last));
+      if (!act) return;
       const int tok_st = (b0 + st * STAGE_BLK) * kBlock;
-      const bool masked = tok_st + STAGE_BLK * kBlock > min(rg.t1, rg.mask0);   // workgroup-uniform
-      if (masked) {
-        // rows past the range end are cleared (0 * NaN), and the values of drafted
-        // tokens that are no finite numbers, with a bit for their token
-        if (tid < 4) lds.bad[buf][tid] = 0u;
-        lds_sync();
-        const int stop = min(rg.t1, rg.end);
-        for (int i = tid; i < kTensorStage / 16; i += 256) {
-          const int row = i / GRAN, tok = tok_st + row;
-          if (tok >= rg.base) {
-            u32x4* at = reinterpret_cast<u32x4*>(lds.ring[buf] + kTensorStage + i * 16);
-            u32x4 v = u32x4{0u, 0u, 0u, 0u};
-            bool write = tok >= stop;
-            if (!write) {
-              v = *at;
-              write = tree_detail::clear_nonfinite<DT>(v);
-              if (write) atomicOr(&lds.bad[buf][row >> 5], 1u << (row & 31));
-            }
-            if (write) *at = v;
-          }
-        }
-        lds_sync();
+      if constexpr (DT == kF32) {
+#pragma unroll 1
+        for (int bl = 0; bl < STAGE_BLK; ++bl) block32<false>(rg, b0, buf, bl, tok_st + bl * kBlock, 0u);
+      } else {
+#pragma unroll
+        for (int bl = 0; bl < STAGE_BLK; bl += 2)
+          pair<false>(rg, b0, buf * kStageBytes + bl * BLK_B, tok_st + bl * kBlock, 0u);
       }
+    };
+    for (int st = 0; st < plain; st += 3) {
+      step(st, std::integral_constant<int, 0>{});
+      if (st + 1 < plain) step(st + 1, std::integral_constant<int, 1>{});
+      if (st + 2 < plain) step(st + 2, std::integral_constant<int, 2>{});
+    }
+#pragma unroll 1
+    for (int st = plain, buf = plain % 3; st < nstages; ++st) {
+      wait_vmcnt<PER_WAVE>();
+      lds_sync();
+      const int tok_st = (b0 + st * STAGE_BLK) * kBlock;
+      // rows past the range end are cleared (0 * NaN), and the values of drafted tokens
+      // that are no finite numbers, with a bit for their token
+      if (tid < 4) lds.bad[buf][tid] = 0u;
+      lds_sync();
+      const int stop = min(rg.t1, rg.end);
+#pragma unroll 1
+      for (int i = tid; i < kTensorStage / 16; i += 256) {
+        const int row = i / GRAN, tok = tok_st + row;
+        if (tok >= rg.base) {
+          u32x4* at = reinterpret_cast<u32x4*>(lds.ring[buf] + kTensorStage + i * 16);
+          u32x4 v = u32x4{0u, 0u, 0u, 0u};
+          bool write = tok >= stop;
+          if (!write) {
+            v = *at;
+            write = tree_detail::clear_nonfinite<DT>(v);
+            if (write) atomicOr(&lds.bad[buf][row >> 5], 1u << (row & 31));
+          }
+          if (write) *at = v;
+        }
+      }
+      lds_sync();
       const int next = buf == 0 ? 2 : buf - 1;               // (st + 2) % 3
       issue(next);
       table(min(st + 3, last));
       if (act) {
-        if constexpr (DT == kF32) {
 #pragma unroll 1
-          for (int bl = 0; bl < STAGE_BLK; ++bl) {
-            const int tok0 = tok_st + bl * kBlock;
-            if (tok0 >= rg.t1) break;
-            block32(rg, b0, buf, bl, tok0, masked);
-          }
-        } else {
-#pragma unroll 1
-          for (int bl = 0; bl < STAGE_BLK; bl += 2) {
-            const int tok0 = tok_st + bl * kBlock;
-            if (tok0 >= rg.t1) break;
-            pair(rg, b0, buf, bl, tok0, masked);
-          }
+        for (int bl = 0; bl < STAGE_BLK; bl += DT == kF32 ? 1 : 2) {
+          const int tok0 = tok_st + bl * kBlock;
+          if (tok0 >= rg.t1) break;
+          const unsigned bad = __builtin_amdgcn_readfirstlane(lds.bad[buf][bl >> 1]);
+          if constexpr (DT == kF32) block32<true>(rg, b0, buf, bl, tok0, bad >> (16 * (bl & 1)) & 0xFFFFu);
+          else pair<true>(rg, b0, buf * kStageBytes + bl * BLK_B, tok0, bad);
         }
       }
       buf = buf == 2 ? 0 : buf + 1;
     }
     wait_vmcnt<0>();                     // the re-read stages issued by the last iterations
-  }
-
-  // The tile's result: f(c, col, value(dt) scaled, lse2) per set of a wave with columns; the lane
-  // holds elements dt * 16 + 4 (lane / 16) .. + 3 of its column.
-  template <class F>
-  PARROT_DEV void finish(F f) {
-    if (!act) return;
-#pragma unroll
-    for (int c = 0; c < NS; ++c) {
-      const float lt = sum_xor32(sum_xor16(lsum[c]));
-      const float lw = DT == kF32 ? lt : sum_xor32(sum_xor16(lsr[c]));
-      f(c, column(c), lw, mref[c] + fast_log2(lt), lt);
-    }
   }
 };
 
