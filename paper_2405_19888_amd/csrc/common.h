@@ -233,6 +233,16 @@ PARROT_DEV void lds_dma16_sbase(const void* base, unsigned voff, unsigned lds_ba
       : "s"(lds_base), "v"(voff), "s"(base)
       : "memory", "m0");
 }
+// ... with the streaming hint, for bytes that nobody reads again.
+PARROT_DEV void lds_dma16_sbase_stream(const void* base, unsigned voff, unsigned lds_base) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %1, %2 nt"
+      :
+      : "s"(lds_base), "v"(voff), "s"(base)
+      : "memory", "m0");
+}
 #pragma clang diagnostic pop
 
 PARROT_DEV unsigned lds_addr(const void* p) {

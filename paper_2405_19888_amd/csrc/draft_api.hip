@@ -215,7 +215,7 @@ struct TreePlan {
 thread_local int g_tree_path = -1;
 
 constexpr int kTreeMinRun = 10;      // cost of a run at least: 8 units and a tile's setup
-constexpr int kTreeChunkMax = 8192, kTreeChunkMin = 256;
+constexpr int kTreeChunkMax = 2560, kTreeChunkMin = 256;
 
 // The row counts of a tree call (or of accept and commit, which have no heads).
 parrot_status check_tree_counts(int32_t requests, const parrot_tree_rows* rows) {
@@ -249,26 +249,35 @@ parrot_status check_tree(const parrot_problem* p, const parrot_tree_rows* rows, 
   const long H = p->num_heads, R = p->num_requests, cus = parrot::device_cus(), cols = parrot::tree_cols(p->dtype);
   if (ceil_div(R * H, 8) * 8 * pl->tiles > 0x7fffffffL)
     return set_error(PARROT_ERR_UNSUPPORTED, "tree decode needs too many workgroups");
-  // the split plan: prefix chunks as long as their workgroups still fill the device
+  // The split plan.  Prefix chunks are as long as their workgroups still fill the device
+  // (a chunk more costs a tile 64 KB of partial results, written and read: 48 rows each on
+  // six prefixes of 2304 tokens take 179 us in one chunk, 199 in two, 237 in five),
+  // but not so long that the last ones run alone (48 rows of 8 requests on 8192 tokens: 126
+  // us in chunks of 4096, 98 of 2048, 111 of 1024).  A group has at most tiles_p tiles, all
+  // of them at most one each beyond their rows'.
   const long mg = p->num_groups > 0 ? rows->max_group_rows : 0;
   pl->tiles_p = (int)ceil_div(mg * G, cols);
   pl->cp = kTreeChunkMax;
   if (pl->tiles_p > 0) {
-    while (pl->cp > kTreeChunkMin && p->num_groups * pl->tiles_p * H * ceil_div(p->max_prefix_len, pl->cp) < 2 * cus)
-      pl->cp /= 2;
+    const long tiles = std::min(p->num_groups * (long)pl->tiles_p, ceil_div(T * pl->depth * G, cols) + p->num_groups);
+    while (pl->cp > kTreeChunkMin && tiles * H * ceil_div(p->max_prefix_len, pl->cp) < cus * 3 / 2) pl->cp /= 2;
+    const long chunks = std::max(1L, ceil_div(p->max_prefix_len, pl->cp));       // of equal length
+    pl->cp = (int)(std::max(1L, ceil_div(p->max_prefix_len, chunks * 64)) * 64);
     pl->seg_p = (int)ceil_div(p->max_prefix_len, pl->cp);
     pl->n_pre = ceil_div((long)p->num_groups * pl->seg_p * H, 8) * 8 * pl->tiles_p;
   }
   pl->seg_pre = pl->depth * pl->seg_p;
-  // own tokens: two workgroups per CU beside prefix work, else three; requests of at
-  // most 32 columns go by waves, each with a run of its own
+  // Own tokens: requests of at most 32 columns go by waves, each with a run of its own.
+  // Four waves a CU read fastest (8 requests of 16 rows on 9600 tokens: 217 us, 235 with
+  // eight, 246 with twelve; with three 212, but 96 requests on 800 tokens 237 for 228).
+  // Tiles: two workgroups per CU (64 and 128 rows on 9600 tokens: 239 and 257 us; 216 and
+  // 280 with one, 261 and 279 with three), three where a request may have several tiles
+  // and the products bound it.
   const long most_cols = rows->max_query_rows * G;
   pl->sets = most_cols <= 16 ? 1 : most_cols <= 32 ? 2 : 0;
   pl->waves = R * H <= cus ? 8 : 4;
   const long per_wg = pl->sets ? 4 : 1;
-  // (two column sets a wave: two workgroups per CU in all)
-  const long most_wgs = pl->sets == 2 ? 2 : 3;
-  pl->own_wgs = (int)std::max((pl->n_pre > 0 ? most_wgs - 1 : most_wgs) * cus, ceil_div(H, per_wg));
+  pl->own_wgs = (int)std::max((pl->sets ? 1 : pl->tiles > 1 ? 3 : 2) * cus, ceil_div(H, per_wg));
   pl->runs = (int)(pl->own_wgs * per_wg / H);
   pl->min_run = kTreeMinRun;
   const long units = ceil_div(p->max_suffix_len, parrot::tree_unit(p->dtype, p->head_dim));

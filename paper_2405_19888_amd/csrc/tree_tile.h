@@ -111,6 +111,7 @@ struct TreeRange {
   int mask0;                        // first token of mask word 0 (a multiple of 32); tokens
                                     // from there on go by the mask.  t1 or more: no mask
   int base, end;                    // masked ranges: the drafted tokens are [base, end)
+  bool once = false;                // tiles: no other tile reads these keys
 };
 
 // A wave's columns: NS sets of 16 with their queries, softmax statistics and output, in
@@ -442,13 +443,19 @@ struct TreeTile : TreeState<DT, D, NS> {
 #pragma unroll
       for (int j = 0; j < PER_WAVE; ++j) tb[j] = lds.tbl[min(st * STAGE_BLK + c_bl[j], nb - 1)];   // past the end: re-read
     };
-    auto issue = [&](int buf) {
+    auto issue_as = [&](int buf, auto once_c) {
 #pragma unroll
       for (int j = 0; j < PER_WAVE; ++j) {
         const unsigned blk = min((unsigned)__builtin_amdgcn_readfirstlane(tb[j]), (unsigned)(rg.npool - 1));
         const char* base = (const char*)(c_v[j] ? rg.pv : rg.pk) + (size_t)blk * blk_stride;
-        lds_dma16_sbase(base, c_src[j], lds_addr(&lds.ring[buf][(wave + j * 4) * 1024]));
+        const unsigned to = lds_addr(&lds.ring[buf][(wave + j * 4) * 1024]);
+        if constexpr (decltype(once_c)::value) lds_dma16_sbase_stream(base, c_src[j], to);
+        else lds_dma16_sbase(base, c_src[j], to);
       }
+    };
+    auto issue = [&](int buf) {
+      if (rg.once) issue_as(buf, std::true_type{});
+      else issue_as(buf, std::false_type{});
     };
     table(0);
     issue(0);
