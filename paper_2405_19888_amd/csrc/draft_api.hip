@@ -203,9 +203,10 @@ extern "C" parrot_status parrot_rotary_fill(
 namespace {
 
 struct TreePlan {
-  int depth, tiles;
+  int depth, max_depth, tiles;   // levels of a chain: this call's, at most
   bool split;                    // partial results and join, else one launch
-  int cp, tiles_p, seg_p, seg_pre, seg, sets, waves, own_wgs, runs, min_run;
+  bool small;                    // the one launch: waves that share the keys, else a tile
+  int cp, tiles_p, seg_p, seg_pre, seg, sets, own_wgs, runs, min_run;
   long n_pre;
   size_t o_bytes, lse_bytes, total_bytes;
 };
@@ -229,6 +230,54 @@ parrot_status check_tree_counts(int32_t requests, const parrot_tree_rows* rows) 
   return PARROT_OK;
 }
 
+// Whether the split plan is the faster one, by estimates of both times in microseconds.
+// Lengths are bounds: the mean is taken as 0.7 of them, the longest as the bound.
+//  * one launch: 8 us and 4 more per round of workgroups (three a CU), and the largest of
+//    a workgroup's latency (0.55 us a 16 KiB stage with one column set a wave, 0.75 with
+//    two, 1.4 with fp32; waves that share the keys 2.4 for 8 steps of 16 KiB, fp32 4), the
+//    bytes (own tokens at 5.6 TB/s, the prefixes that every request reads again at 12
+//    from the caches) and the products at 750 TFLOP/s (fp32 100).
+//  * split plan: by tiles 14 us (fp32 36) and 8 per piece of a workgroup, by waves 12 us and
+//    3 per piece of a wave but 22 at least, 8 for prefixes; the own tokens once per
+//    column tile at 6.0 TB/s (by waves 6.4) or their products (fp32: those of whole tiles),
+//    the prefixes' products, and the partial results, written and read, at 4.7 TB/s.
+// Measured, one launch and split, 16-bit heads of 128: a request of 64 rows on 300, 2000,
+// 8000 tokens and 32 heads 15.5 and 21, 48 and 24, 156 and 50 us; 32 requests of 64 rows,
+// four query heads on each of 8, on 300, 4000 tokens 29 and 75, 180 and 279; 32 requests of
+// 8 rows on one prefix of 300, 4000 tokens and 32 heads 32 and 33, 166 and 57; 128 requests
+// of 4 rows on 1000 tokens and 8 heads 106 and 95.
+bool tree_splits(const parrot_problem* p, const parrot_tree_rows* rows, const TreePlan& pl, long cus) {
+  const double mean = 0.7, R = p->num_requests, H = p->num_heads, HQ = rows->num_query_heads, D = p->head_dim;
+  const double T = rows->num_query_rows, eb = p->dtype == PARROT_DTYPE_F32 ? 4 : 2, kv = 2 * D * eb * H;
+  const bool f32 = p->dtype == PARROT_DTYPE_F32;
+  const double own = p->max_suffix_len, pre = p->num_groups > 0 ? (double)pl.max_depth * p->max_prefix_len : 0;
+  const double flops_own = 4 * D * T * HQ * mean * own, flops_pre = 4 * D * T * HQ * mean * pre;
+  const double rate = f32 ? 1e8 : 7.5e8, qo = 2 * T * HQ * D * eb;
+  double one;
+  const double stage = 16384 / (2 * D * eb), mem = (R * mean * own * kv + qo) / 5.6e6 + R * mean * pre * kv / 12e6;
+  if (pl.small) {
+    one = 8 + std::max((own + pre) / (8 * stage) * (f32 ? 4 : 2.4), mem);
+  } else {
+    const double items = R * H * pl.tiles, rounds = std::ceil(items / (3 * cus));
+    const double lat = f32 ? 1.4 : rows->max_query_rows * HQ / H <= 64 ? 0.55 : 0.75;
+    one = 8 + 4 * rounds + std::max({rounds * (own + pre) / stage * lat, mem, (flops_own + flops_pre) / rate});
+  }
+  const double cuts = std::min(pl.runs / (R * pl.tiles), own / parrot::tree_unit(p->dtype, p->head_dim) / pl.min_run);
+  const double pieces = pre > 0 ? 1 + cuts + pl.max_depth * std::ceil(mean * p->max_prefix_len / pl.cp)
+                                : cuts < 1 ? 2 * cuts : 1 + cuts;
+  const double rest = flops_pre / rate + T * HQ * D * 8 * pieces / 4.7e6 + (pre > 0 ? 8 : 0);
+  double split;
+  if (pl.sets) {
+    const double waves = std::max((R * mean * own * kv + qo) / 6.4e6, flops_own / rate);
+    split = std::max(22.0, 12 + 3 * std::ceil(R * H / (4 * cus)) + waves + rest);
+  } else {
+    const double cols = rows->max_query_rows * HQ / H, fill = f32 ? pl.tiles * parrot::tree_cols(p->dtype) / cols : 1;
+    split = (f32 ? 36 : 14) + 8 * std::ceil(R * H * pl.tiles / pl.own_wgs) +
+            std::max((pl.tiles * R * mean * own * kv + qo) / 6e6, flops_own * fill / rate) + rest;
+  }
+  return split < one;
+}
+
 parrot_status check_tree(const parrot_problem* p, const parrot_tree_rows* rows, bool nested, TreePlan* pl) {
   PARROT_TRY(parrot::check_problem_fields(p));
   PARROT_TRY(check_tree_counts(p->num_requests, rows));
@@ -244,7 +293,9 @@ parrot_status check_tree(const parrot_problem* p, const parrot_tree_rows* rows, 
   if (T * rows->num_query_heads > 0x7fffffffL)
     return set_error(PARROT_ERR_UNSUPPORTED, "num_query_rows * num_query_heads > 2^31 - 1");
   const long G = rows->num_query_heads / p->num_heads;
-  pl->depth = p->num_groups > 0 ? (nested ? std::max(1, (int)p->max_prefix_depth) : 1) : 0;
+  // (the plan is that of nested calls for flat ones too, so that one workspace serves both)
+  pl->max_depth = p->num_groups > 0 ? std::max(1, (int)p->max_prefix_depth) : 0;
+  pl->depth = nested ? pl->max_depth : std::min(pl->max_depth, 1);
   pl->tiles = (int)ceil_div(rows->max_query_rows * G, parrot::tree_cols(p->dtype));
   const long H = p->num_heads, R = p->num_requests, cus = parrot::device_cus(), cols = parrot::tree_cols(p->dtype);
   if (ceil_div(R * H, 8) * 8 * pl->tiles > 0x7fffffffL)
@@ -259,25 +310,29 @@ parrot_status check_tree(const parrot_problem* p, const parrot_tree_rows* rows, 
   pl->tiles_p = (int)ceil_div(mg * G, cols);
   pl->cp = kTreeChunkMax;
   if (pl->tiles_p > 0) {
-    const long tiles = std::min(p->num_groups * (long)pl->tiles_p, ceil_div(T * pl->depth * G, cols) + p->num_groups);
+    const long tiles = std::min(p->num_groups * (long)pl->tiles_p, ceil_div(T * pl->max_depth * G, cols) + p->num_groups);
     while (pl->cp > kTreeChunkMin && tiles * H * ceil_div(p->max_prefix_len, pl->cp) < cus * 3 / 2) pl->cp /= 2;
     const long chunks = std::max(1L, ceil_div(p->max_prefix_len, pl->cp));       // of equal length
     pl->cp = (int)(std::max(1L, ceil_div(p->max_prefix_len, chunks * 64)) * 64);
     pl->seg_p = (int)ceil_div(p->max_prefix_len, pl->cp);
     pl->n_pre = ceil_div((long)p->num_groups * pl->seg_p * H, 8) * 8 * pl->tiles_p;
   }
-  pl->seg_pre = pl->depth * pl->seg_p;
+  if (pl->seg_p > 0xffff) return set_error(PARROT_ERR_UNSUPPORTED, "tree decode: %ld prefix chunks", (long)pl->seg_p);
+  pl->seg_pre = pl->max_depth * pl->seg_p;
   // Own tokens: requests of at most 32 columns go by waves, each with a run of its own.
   // Four waves a CU read fastest (8 requests of 16 rows on 9600 tokens: 217 us, 235 with
   // eight, 246 with twelve; with three 212, but 96 requests on 800 tokens 237 for 228).
   // Tiles: two workgroups per CU (64 and 128 rows on 9600 tokens: 239 and 257 us; 216 and
   // 280 with one, 261 and 279 with three), three where a request may have several tiles
-  // and the products bound it.
+  // and the products bound it, and for fp32 (32 requests of 20 rows on 4000 tokens: 1411 us
+  // with two, 1107 with three).
   const long most_cols = rows->max_query_rows * G;
-  pl->sets = most_cols <= 16 ? 1 : most_cols <= 32 ? 2 : 0;
-  pl->waves = R * H <= cus ? 8 : 4;
+  // (fp32 caches with two column sets spill: 32 requests of 20 rows on 1000 tokens 440 us, by
+  // tiles 351).
+  pl->sets = most_cols <= 16 ? 1 : most_cols <= 32 && p->dtype != PARROT_DTYPE_F32 ? 2 : 0;
+  pl->small = pl->sets == 1 && parrot::tree_small_rows(p->dtype, p->head_dim) && R * H <= cus;
   const long per_wg = pl->sets ? 4 : 1;
-  pl->own_wgs = (int)std::max((pl->sets ? 1 : pl->tiles > 1 ? 3 : 2) * cus, ceil_div(H, per_wg));
+  pl->own_wgs = (int)std::max((pl->sets ? 1 : pl->tiles > 1 || p->dtype == PARROT_DTYPE_F32 ? 3 : 2) * cus, ceil_div(H, per_wg));
   pl->runs = (int)(pl->own_wgs * per_wg / H);
   pl->min_run = kTreeMinRun;
   const long units = ceil_div(p->max_suffix_len, parrot::tree_unit(p->dtype, p->head_dim));
@@ -286,12 +341,12 @@ parrot_status check_tree(const parrot_problem* p, const parrot_tree_rows* rows, 
   if ((pl->own_wgs + pl->n_pre) * 256 > 0xffffffffL || ceil_div(R * H, 8) * 8 * pl->tiles * 512 > 0xffffffffL || cost > 2e9 || (double)T * rows->num_query_heads * seg * p->head_dim > 4e18)
     return set_error(PARROT_ERR_UNSUPPORTED, "tree decode: %.3g units of own tokens", cost);
   pl->seg = (int)seg;
-  pl->split = g_tree_path >= 0 ? g_tree_path == 1 : true;
+  pl->split = g_tree_path >= 0 ? g_tree_path == 1 : tree_splits(p, rows, *pl, cus);
   auto align256 = [](size_t x) { return (x + 255) & ~(size_t)255; };
   const size_t slots = (size_t)T * rows->num_query_heads * seg;
   pl->o_bytes = align256(slots * p->head_dim * sizeof(float));
   pl->lse_bytes = align256(slots * sizeof(float));
-  pl->total_bytes = pl->o_bytes + pl->lse_bytes + align256((size_t)T * parrot::kTreeDesc * sizeof(int32_t));
+  pl->total_bytes = pl->split ? pl->o_bytes + pl->lse_bytes + align256((size_t)T * parrot::kTreeDesc * sizeof(int32_t)) : 256;
   return PARROT_OK;
 }
 
@@ -361,7 +416,7 @@ parrot_status parrot_shared_prefix_tree_decode(
   const int dt = (int)p->dtype, D = p->head_dim;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (!pl.split) {
-    PARROT_TRY(launched(parrot::launch_tree(a, pl.waves, dt, D, s, ev(tr.partials_start), ev(tr.partials_stop)), "tree kernel"));
+    PARROT_TRY(launched(parrot::launch_tree(a, pl.small, dt, D, s, ev(tr.partials_start), ev(tr.partials_stop)), "tree kernel"));
     return record_none(tr, s);
   }
   PARROT_TRY(launched(parrot::launch_tree_partials(a, dt, D, s, ev(tr.partials_start), ev(tr.partials_stop)),

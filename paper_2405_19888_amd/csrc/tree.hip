@@ -464,7 +464,7 @@ PARROT_DEV void stream_role(const TreeArgs& a, char* lds, int wg) {
 
 // SETS 0: own tokens by tiles, else by waves of that many column sets.
 template <int DT, int D, int SETS>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SETS == 2 ? 2 : 3)))
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SETS > 0 ? 2 : 3)))
 void k_tree_partials(TreeArgs a) {
   __shared__ __attribute__((aligned(1024))) tree_detail::Lds<DT> lds;
   static_assert(sizeof(lds) >= 4 * kStreamLds, "the waves' value rows fit");
@@ -495,13 +495,19 @@ void k_tree_partials(TreeArgs a) {
   }
 }
 
-// One launch for a small call of few columns: NW waves share the keys of one request
-// and cache head (the chain's prefixes, then the own tokens: a contiguous share of
-// their units each) and meet in LDS.
-template <int DT, int D, int NS, int NW>
-__global__ __launch_bounds__(NW * 64) void k_tree_small(TreeArgs a) {
+// One launch for a small call of at most 16 columns: kSmallWaves waves share the keys of
+// one request and cache head (the chain's prefixes, then the own tokens: a contiguous
+// share of their units each) and meet in LDS.  Bound by latency, 2.4 us a step of 16 KiB
+// (fp32: 4): one request of 4 rows on 300, 2000 tokens takes 9.6, 26.8 us at 32 16-bit
+// heads of 128 (the tile: 11.6, 41), at fp32 17.8 us on 300 (32).  Rows of 128 bytes, 64
+// tokens a step, leave most waves idle: the tile takes them (8 requests on 1000
+// tokens: 17.6 us, 27 here), and 17 to 32 columns, whose waves meet for longer than they
+// read (32 requests of 20 rows on 300 tokens: 42.6 us, 55.8 here).
+constexpr int kSmallWaves = 8;
+template <int DT, int D>
+__global__ __launch_bounds__(kSmallWaves * 64) void k_tree_small(TreeArgs a) {
   using E = Elem<DT>;
-  constexpr int UNIT = tree_unit(DT, D), COLS = 16 * NS, STRIDE = D + 4;   // (rows off the same banks)
+  constexpr int UNIT = tree_unit(DT, D), NW = kSmallWaves, COLS = 16, STRIDE = D + 4;   // (rows off the same banks)
   constexpr int O_B = NW * COLS * STRIDE * 4;
   __shared__ __attribute__((aligned(1024))) char lds[O_B > NW * kStreamLds ? O_B : NW * kStreamLds];
   __shared__ float s_m[NW][COLS], s_t[NW][COLS], s_w[NW][COLS];
@@ -512,7 +518,7 @@ __global__ __launch_bounds__(NW * 64) void k_tree_small(TreeArgs a) {
   const RowSpan rw = row_span(a.qoff, r, a.T, min(S, a.max_q));
   const int ncols = min(rw.count * a.G, COLS), base = S - rw.count;
   if (ncols == 0) return;
-  TreeStream<DT, D, NS> st(lds + wave * kStreamLds, a.H, h, a.scale_log2);
+  TreeStream<DT, D, 1> st(lds + wave * kStreamLds, a.H, h, a.scale_log2);
   auto row_of = [&](int col) {
     const int row = col / a.G;
     return (size_t)(rw.first + row) * HQ + h * a.G + (col - row * a.G);
@@ -683,25 +689,22 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a) {
 }
 
 template <int DT, int D>
-static void launch_tree_t(const TreeArgs& a, int waves, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
-  const dim3 pairs((unsigned)((long)a.R * a.H)), wg(waves * 64);
-  if (a.sets == 0) {
-    const long groups = ((long)a.R * a.H + 7) / 8;
-    hipExtLaunchKernelGGL((k_tree_decode<DT, D>), dim3((unsigned)(groups * 8 * a.tiles)), dim3(256), 0, s, e0, e1, 0, a);
-  } else if (a.sets == 1) {
-    if (waves == 8) hipExtLaunchKernelGGL((k_tree_small<DT, D, 1, 8>), pairs, wg, 0, s, e0, e1, 0, a);
-    else hipExtLaunchKernelGGL((k_tree_small<DT, D, 1, 4>), pairs, wg, 0, s, e0, e1, 0, a);
-  } else {
-    if (waves == 8) hipExtLaunchKernelGGL((k_tree_small<DT, D, 2, 8>), pairs, wg, 0, s, e0, e1, 0, a);
-    else hipExtLaunchKernelGGL((k_tree_small<DT, D, 2, 4>), pairs, wg, 0, s, e0, e1, 0, a);
+static void launch_tree_t(const TreeArgs& a, bool small, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
+  if constexpr (tree_small_rows(DT, D)) {
+    if (small) {
+      hipExtLaunchKernelGGL((k_tree_small<DT, D>), dim3((unsigned)((long)a.R * a.H)), dim3(kSmallWaves * 64), 0, s, e0, e1, 0, a);
+      return;
+    }
   }
+  const long groups = ((long)a.R * a.H + 7) / 8;
+  hipExtLaunchKernelGGL((k_tree_decode<DT, D>), dim3((unsigned)(groups * 8 * a.tiles)), dim3(256), 0, s, e0, e1, 0, a);
 }
 template <int DT, int D>
 static void launch_partials_t(const TreeArgs& a, int, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
   const dim3 grid((unsigned)((long)a.own_wgs + a.n_pre));
   if (a.sets == 0) hipExtLaunchKernelGGL((k_tree_partials<DT, D, 0>), grid, dim3(256), 0, s, e0, e1, 0, a);
   else if (a.sets == 1) hipExtLaunchKernelGGL((k_tree_partials<DT, D, 1>), grid, dim3(256), 0, s, e0, e1, 0, a);
-  else hipExtLaunchKernelGGL((k_tree_partials<DT, D, 2>), grid, dim3(256), 0, s, e0, e1, 0, a);
+  else if constexpr (DT != kF32) hipExtLaunchKernelGGL((k_tree_partials<DT, D, 2>), grid, dim3(256), 0, s, e0, e1, 0, a);
 }
 template <int DT, int D>
 static void launch_join_t(const TreeArgs& a, int, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
@@ -709,14 +712,14 @@ static void launch_join_t(const TreeArgs& a, int, hipStream_t s, hipEvent_t e0, 
   hipExtLaunchKernelGGL((k_tree_join<DT, D>), dim3((unsigned)(((long)a.T * per_row + 3) / 4)), dim3(256), 0, s, e0, e1, 0, a);
 }
 
-#define PARROT_TREE_LAUNCH(NAME, WAVES)                                       \
+#define PARROT_TREE_LAUNCH(NAME, X)                                       \
   switch (dtype * 1000 + D) {                                                 \
-    case kF32 * 1000 + 64: NAME<kF32, 64>(a, WAVES, s, e0, e1); break;        \
-    case kF32 * 1000 + 128: NAME<kF32, 128>(a, WAVES, s, e0, e1); break;      \
-    case kF16 * 1000 + 64: NAME<kF16, 64>(a, WAVES, s, e0, e1); break;        \
-    case kF16 * 1000 + 128: NAME<kF16, 128>(a, WAVES, s, e0, e1); break;      \
-    case kBF16 * 1000 + 64: NAME<kBF16, 64>(a, WAVES, s, e0, e1); break;      \
-    case kBF16 * 1000 + 128: NAME<kBF16, 128>(a, WAVES, s, e0, e1); break;    \
+    case kF32 * 1000 + 64: NAME<kF32, 64>(a, X, s, e0, e1); break;        \
+    case kF32 * 1000 + 128: NAME<kF32, 128>(a, X, s, e0, e1); break;      \
+    case kF16 * 1000 + 64: NAME<kF16, 64>(a, X, s, e0, e1); break;        \
+    case kF16 * 1000 + 128: NAME<kF16, 128>(a, X, s, e0, e1); break;      \
+    case kBF16 * 1000 + 64: NAME<kBF16, 64>(a, X, s, e0, e1); break;      \
+    case kBF16 * 1000 + 128: NAME<kBF16, 128>(a, X, s, e0, e1); break;    \
     default: return hipErrorInvalidValue;                                     \
   }                                                                           \
   return hipGetLastError()
@@ -728,11 +731,12 @@ static bool tree_args_ok(const TreeArgs& a) {
          a.sets <= 2 && (a.sets == 0 || (long)a.max_q * a.G <= 16 * a.sets);
 }
 
-hipError_t launch_tree(const TreeArgs& a, int waves, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
+hipError_t launch_tree(const TreeArgs& a, bool small, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
   if (!tree_args_ok(a) || a.tiles < 1 || (long)a.tiles * tree_cols(dtype) < (long)a.max_q * a.G ||
-      (waves != 4 && waves != 8) || ((long)a.R * a.H + 7) / 8 * 8 * a.tiles * waves * 64 > 0xffffffffL)
+      ((long)a.R * a.H + 7) / 8 * 8 * a.tiles * kSmallWaves * 64 > 0xffffffffL ||
+      (small && (a.sets != 1 || !tree_small_rows(dtype, D))))
     return hipErrorInvalidValue;
-  PARROT_TREE_LAUNCH(launch_tree_t, waves);
+  PARROT_TREE_LAUNCH(launch_tree_t, small);
 }
 
 hipError_t launch_tree_partials(const TreeArgs& a, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {

@@ -54,8 +54,9 @@ constexpr int kTreeSetup = 2;
 constexpr int tree_unit(int dtype, int D) { return dtype != kF32 && D == 64 ? 64 : 32; }
 
 // One workgroup per request, cache head and column tile, output written by it: a tile,
-// or with sets > 0 `waves` waves that share the keys.
-hipError_t launch_tree(const TreeArgs& a, int waves, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
+// or (small: at most 16 columns, rows of tree_small_rows) waves that share the keys.
+constexpr bool tree_small_rows(int dtype, int D) { return D * (dtype == kF32 ? 4 : 2) >= 256; }
+hipError_t launch_tree(const TreeArgs& a, bool small, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
 // Partial results of prefixes and own tokens, and their combination.
 hipError_t launch_tree_partials(const TreeArgs& a, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
 hipError_t launch_tree_join(const TreeArgs& a, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
