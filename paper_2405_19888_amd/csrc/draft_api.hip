@@ -208,6 +208,7 @@ struct TreePlan {
   bool small;                    // the one launch: waves that share the keys, else a tile
   int cp, tiles_p, seg_p, seg_pre, seg, sets, own_wgs, runs, min_run;
   long n_pre;
+  bool pre_first;                // prefix workgroups before the own tokens'
   size_t o_bytes, lse_bytes, total_bytes;
 };
 
@@ -302,7 +303,8 @@ parrot_status check_tree(const parrot_problem* p, const parrot_tree_rows* rows, 
     return set_error(PARROT_ERR_UNSUPPORTED, "tree decode needs too many workgroups");
   // The split plan.  Prefix chunks are as long as their workgroups still fill the device
   // (a chunk more costs a tile 64 KB of partial results, written and read: 48 rows each on
-  // six prefixes of 2304 tokens take 179 us in one chunk, 199 in two, 237 in five),
+  // six prefixes of 2304 tokens take 167 us in one chunk; before the prefixes went first,
+  // 179 in one, 199 in two, 237 in five),
   // but not so long that the last ones run alone (48 rows of 8 requests on 8192 tokens: 126
   // us in chunks of 4096, 98 of 2048, 111 of 1024).  A group has at most tiles_p tiles, all
   // of them at most one each beyond their rows'.
@@ -336,6 +338,9 @@ parrot_status check_tree(const parrot_problem* p, const parrot_tree_rows* rows, 
   pl->runs = (int)(pl->own_wgs * per_wg / H);
   pl->min_run = kTreeMinRun;
   const long units = ceil_div(p->max_suffix_len, parrot::tree_unit(p->dtype, p->head_dim));
+  // the longer items start first, so that the short ones fill up (48 rows each on six
+  // prefixes of 2304 tokens: 167 us, 182 with the own tokens first)
+  pl->pre_first = (double)R * pl->tiles * units / pl->runs < (double)pl->cp / parrot::tree_unit(p->dtype, p->head_dim);
   const long seg = pl->seg_pre + std::min(ceil_div(units, pl->min_run) + 1, (long)pl->runs);
   const double cost = (double)R * pl->tiles * (units + parrot::kTreeSetup);
   if ((pl->own_wgs + pl->n_pre) * 256 > 0xffffffffL || ceil_div(R * H, 8) * 8 * pl->tiles * 512 > 0xffffffffL || cost > 2e9 || (double)T * rows->num_query_heads * seg * p->head_dim > 4e18)
@@ -408,6 +413,7 @@ parrot_status parrot_shared_prefix_tree_decode(
   a.scale_log2 = p->sm_scale * parrot::kLog2e;
   a.cp = pl.cp; a.tiles_p = pl.tiles_p; a.seg = pl.seg; a.seg_p = pl.seg_p; a.seg_pre = pl.seg_pre;
   a.sets = pl.sets; a.own_wgs = pl.own_wgs; a.runs = pl.runs; a.min_run = pl.min_run; a.n_pre = (int)pl.n_pre;
+  a.first = pl.pre_first ? a.n_pre : 0;
   a.o_part = reinterpret_cast<float*>(workspace);
   a.lse_part = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + pl.o_bytes);
   a.desc = reinterpret_cast<int*>(reinterpret_cast<char*>(workspace) + pl.o_bytes + pl.lse_bytes);

@@ -468,8 +468,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SETS > 0 ? 
 void k_tree_partials(TreeArgs a) {
   __shared__ __attribute__((aligned(1024))) tree_detail::Lds<DT> lds;
   static_assert(sizeof(lds) >= 4 * kStreamLds, "the waves' value rows fit");
-  const int wg = blockIdx.x;
-  const bool own = wg < a.own_wgs;
+  // (all prefix workgroups, a.first of them, come before those of the own tokens, or none)
+  const int at = (int)blockIdx.x - a.first;
+  const bool own = at >= 0 && at < a.own_wgs;
+  const int wg = own ? at : at < 0 ? (int)blockIdx.x : at - a.own_wgs;
   if constexpr (SETS > 0) {
     if (own) {
       stream_role<DT, D, SETS>(a, &lds.ring[0][0], wg);
@@ -484,7 +486,7 @@ void k_tree_partials(TreeArgs a) {
     pc.h = wg % a.H;
     more = find_run<DT, D>(a, lds.tbl, wg, [&](int) { return run; }, &o) && next_own<DT, D>(a, lds, run, &o, &pc);
   } else {
-    more = prefix_piece<DT, D>(a, lds, wg - a.own_wgs, &pc);
+    more = prefix_piece<DT, D>(a, lds, wg, &pc);
   }
   while (more) {                                          // one place for both roles' tiles
     if (tree_detail::kSets<DT> == 2 && (wave + 4) * 16 < pc.ncols)
@@ -742,7 +744,7 @@ hipError_t launch_tree(const TreeArgs& a, bool small, int dtype, int D, hipStrea
 hipError_t launch_tree_partials(const TreeArgs& a, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
   const long pre = a.n_pre > 0 ? ((long)a.NG * a.seg_p * a.H + 7) / 8 * 8 * a.tiles_p : 0;
   if (!tree_args_ok(a) || a.runs < 1 || a.min_run < 1 || a.own_wgs < 1 ||
-      (long)a.own_wgs * (a.sets ? 4 : 1) < (long)a.runs * a.H || !a.o_part || !a.lse_part || !a.desc || a.n_pre != pre ||
+      (long)a.own_wgs * (a.sets ? 4 : 1) < (long)a.runs * a.H || !a.o_part || !a.lse_part || !a.desc || a.n_pre != pre || (a.first != 0 && a.first != a.n_pre) ||
       (a.n_pre > 0 && (a.cp < 64 || a.cp % 64 != 0 || a.depth < 1)) || ((long)a.own_wgs + a.n_pre) * 256 > 0xffffffffL)
     return hipErrorInvalidValue;
   PARROT_TREE_LAUNCH(launch_partials_t, 0);

@@ -41,6 +41,7 @@ struct TreeArgs {
                                          // per cache head
   int min_run;                           // least cost of a run
   int n_pre;                             // prefix workgroups
+  int first;                             // of them before those of the own tokens: all or none
 };
 
 // Row descriptor: cost of the first unit of the row's first column tile, cost between
