@@ -307,7 +307,7 @@ parrot_status check_tree(const parrot_problem* p, const parrot_tree_rows* rows, 
   // 179 in one, 199 in two, 237 in five),
   // but not so long that the last ones run alone (48 rows of 8 requests on 8192 tokens: 126
   // us in chunks of 4096, 98 of 2048, 111 of 1024).  A group has at most tiles_p tiles, all
-  // of them at most one each beyond their rows'.
+  // of them together a tile each beyond what their rows fill.
   const long mg = p->num_groups > 0 ? rows->max_group_rows : 0;
   pl->tiles_p = (int)ceil_div(mg * G, cols);
   pl->cp = kTreeChunkMax;
@@ -343,7 +343,7 @@ parrot_status check_tree(const parrot_problem* p, const parrot_tree_rows* rows, 
   pl->pre_first = (double)R * pl->tiles * units / pl->runs < (double)pl->cp / parrot::tree_unit(p->dtype, p->head_dim);
   const long seg = pl->seg_pre + std::min(ceil_div(units, pl->min_run) + 1, (long)pl->runs);
   const double cost = (double)R * pl->tiles * (units + parrot::kTreeSetup);
-  if ((pl->own_wgs + pl->n_pre) * 256 > 0xffffffffL || ceil_div(R * H, 8) * 8 * pl->tiles * 512 > 0xffffffffL || cost > 2e9 || (double)T * rows->num_query_heads * seg * p->head_dim > 4e18)
+  if ((pl->own_wgs + pl->n_pre) * 256 > 0xffffffffL || ceil_div(R * H, 8) * 8 * pl->tiles * 512 > 0xffffffffL || cost > 1.5e9 || (double)T * rows->num_query_heads * seg * p->head_dim > 4e18)
     return set_error(PARROT_ERR_UNSUPPORTED, "tree decode: %.3g units of own tokens", cost);
   pl->seg = (int)seg;
   pl->split = g_tree_path >= 0 ? g_tree_path == 1 : tree_splits(p, rows, *pl, cus);

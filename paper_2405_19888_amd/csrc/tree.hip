@@ -743,7 +743,7 @@ hipError_t launch_tree(const TreeArgs& a, bool small, int dtype, int D, hipStrea
 
 hipError_t launch_tree_partials(const TreeArgs& a, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
   const long pre = a.n_pre > 0 ? ((long)a.NG * a.seg_p * a.H + 7) / 8 * 8 * a.tiles_p : 0;
-  if (!tree_args_ok(a) || a.runs < 1 || a.min_run < 1 || a.own_wgs < 1 ||
+  if (!tree_args_ok(a) || (a.sets == 2 && dtype == kF32) || a.runs < 1 || a.min_run < 1 || a.own_wgs < 1 ||
       (long)a.own_wgs * (a.sets ? 4 : 1) < (long)a.runs * a.H || !a.o_part || !a.lse_part || !a.desc || a.n_pre != pre || (a.first != 0 && a.first != a.n_pre) ||
       (a.n_pre > 0 && (a.cp < 64 || a.cp % 64 != 0 || a.depth < 1)) || ((long)a.own_wgs + a.n_pre) * 256 > 0xffffffffL)
     return hipErrorInvalidValue;

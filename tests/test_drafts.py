@@ -137,6 +137,25 @@ def test_tree_more_refusals(parrot_lib):
         assert call(parrot_lib, fn, ws=need - 1) == B.PARROT_ERR_WORKSPACE_TOO_SMALL
 
 
+def test_tree_path_by_size(parrot_lib):
+    """Short calls take one launch and no workspace to speak of, few long requests and
+    prefixes of many rows the split plan; a nested problem's flat calls the same one."""
+    def split(prob, rows, nested):
+        return parrot_lib.parrot_test_tree_split(ctypes.byref(prob), ctypes.byref(rows), nested)
+
+    def of(**over):
+        return problem(num_groups=0, max_group_size=0, max_prefix_len=0, num_prefix_blocks=0, **over)
+
+    few = parrot.make_tree_rows(32, 8, 0, 8)
+    short, long = of(), of(max_suffix_len=30000, suffix_table_stride=1875)
+    assert split(short, few, 0) == 0 and split(long, few, 0) == 1
+    assert parrot.parrot_tree_workspace_bytes(short, few) == 256
+    assert parrot.parrot_tree_workspace_bytes(long, few) > 32 * 8 * 128 * 4
+    many = parrot.make_tree_rows(2000, 32, 1000, 8)
+    shared = problem(num_requests=64, max_group_size=32, max_prefix_len=4096, prefix_table_stride=256, max_prefix_depth=2)
+    assert split(shared, many, 0) == split(shared, many, 1) == 1
+
+
 def test_accept_and_commit_refusals(parrot_lib):
     assert call(parrot_lib, "parrot_tree_accept", requests=-1) == B.PARROT_ERR_INVALID_ARGUMENT
     assert call(parrot_lib, "parrot_tree_accept", requests=0, query_offsets=None,

@@ -79,6 +79,15 @@ CASES = {
     "long_own": ("float16", 2, 4, 128, [-1, 0], [2100], [4700, 2049], [13, 30], None),
     "no_rows_between": ("float16", 4, 1, 64, [0, 0, -1, 0], [64], [9, 10, 11, 12], [0, 3, 0, 2], None),
     "f32_long": ("float32", 2, 1, 64, [0], [600], [2500], [40], None),
+    "f32_two_sets": ("float32", 3, 1, 128, [0, -1, 0], [40], [70, 200, 0], [20, 32, 17], None),
+    # few runs of a head, two tiles beside single ones: the tiles are cut at the same tokens
+    "cut_together": ("float16", 40, 8, 128, [-1, -1, -1, -1], [], [1480, 1500, 900, 300], [20, 5, 3, 9], None),
+    # more tiles that share keys than a quarter of the runs: cut where they fall
+    "cut_apart": ("bfloat16", 40, 8, 64, [0, -1, -1, 0], [100], [500, 700, 30, 0], [20, 33, 40, 50], None),
+    # prefix chunks longer than the runs of own tokens, and shorter
+    "prefix_first": ("float16", 2, 2, 128, [0, 0, 1, 1, -1], [900, 257], [20, 0, 31, 64, 3], [40, 33, 3, 40, 20], None),
+    "own_first": ("bfloat16", 1, 1, 64, [0, -1], [80], [9000, 700], [30, 31], None),
+    "heads_odd": ("float16", 7, 3, 128, [0, 1, -1], [15, 333], [130, 65, 2], [11, 22, 33], [-1, 0]),
 }
 
 
@@ -253,3 +262,87 @@ def test_seeded_random_plans():
         q = du.queries(int(off[-1]) + 1, heads * ratio, dim, dtype, seed=i)
         out, lse, _, _ = run(plan, batch, q, off, up)
         check(plan, batch, q, off, up, out, lse, what=f"plan {i} {dtype} {heads}x{ratio}x{dim}")
+
+
+@pytest.mark.parametrize("dtype,dim,most", [("float16", 128, 3), ("float32", 64, 3), ("bfloat16", 64, 30)])
+def test_more_requests_than_threads(dtype, dim, most):
+    """300 requests: lengths and rows are summed in two passes, some bring no rows."""
+    rng = np.random.default_rng(8)
+    rows = [int(x) for x in rng.integers(0, most + 1, 300)]
+    cached = [int(x) for x in rng.integers(0, 90, 300)]
+    groups = [int(x) for x in rng.integers(-1, 3, 300)]
+    cached = [c + 1 if c + n == 0 and g < 0 else c for c, n, g in zip(cached, rows, groups)]
+    plan = du.tree_plan(dtype, 2, dim, groups, [50, 7, 140], cached, rows, [-1, 0, -1])
+    batch, off = du.make_batch(plan), du.offsets_of(rows)
+    up = du.random_trees(rng, rows)
+    q = du.queries(int(off[-1]), 4, dim, dtype)
+    out, lse, _, _ = run(plan, batch, q, off, up)
+    check(plan, batch, q, off, up, out, lse, what=f"300 requests {dtype}")
+
+
+def test_two_calls_at_once():
+    """Two handles on two streams, over the same caches."""
+    import paper_2405_19888_amd as parrot
+    rows, cached = [12, 40, 5], [900, 2000, 64]
+    plan = du.tree_plan("bfloat16", 4, 128, [0, -1, 0], [700], cached, rows)
+    batch, off = du.make_batch(plan), du.offsets_of(rows)
+    up = du.random_trees(np.random.default_rng(3), rows)
+    q = du.queries(57, 8, 128, "bfloat16")
+    want, wlse, first, dev = run(plan, batch, q, off, up)
+    want = want.clone()
+    second = parrot.TreeDecoder(first.problem, first.rows)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for dec, s in zip((first, second), streams):
+            dec(dev, stream=s)
+    torch.cuda.synchronize()
+    assert torch.equal(first.out, want) and torch.equal(second.out, want)
+
+
+def test_two_graphs_of_one_handle():
+    """Graphs of one handle share its workspace; replayed one after the other, with eager
+    calls between them, each gives its own inputs' result."""
+    import paper_2405_19888_amd as parrot
+    rows, cached = [9, 21], [500, 300]
+    plan = du.tree_plan("float16", 2, 128, [0, 0], [260], cached, rows)
+    batch, off = du.make_batch(plan), du.offsets_of(rows)
+    up = du.random_trees(np.random.default_rng(3), rows)
+    qs = [du.queries(30, 8, 128, "float16", seed=i) for i in range(2)]
+    _, _, dec, dev = run(plan, batch, qs[0], off, up)
+    devs, graphs, want = [], [], []
+    for x in qs:
+        devs.append({**dev, "q_rows": x.cuda()})
+        dec(devs[-1])
+        torch.cuda.synchronize()
+        want.append(dec.out.clone())
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            dec(devs[-1])
+    for i in (0, 1, 1, 0, 1):
+        dec(devs[1 - i])
+        torch.cuda.synchronize()
+        dec.out.fill_(float("nan"))
+        graphs[i].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(dec.out, want[i])
+
+
+def test_flat_call_with_a_nested_problem():
+    """A flat call of a problem that allows nested groups uses the same workspace."""
+    import paper_2405_19888_amd as parrot
+    rows, cached = [10, 20, 7], [100, 30, 64]
+    plan = du.tree_plan("float16", 2, 128, [0, 1, -1], [300, 90], cached, rows)
+    batch, off = du.make_batch(plan), du.offsets_of(rows)
+    up = du.random_trees(np.random.default_rng(5), rows)
+    q = du.queries(37, 4, 128, "float16")
+    want, _, dec, dev = run(plan, batch, q, off, up)
+    want = want.clone()
+    prob = problem_for(plan)
+    prob.max_prefix_depth = 4
+    deep = parrot.TreeDecoder(prob, dec.rows)
+    deep.workspace.fill_(0xFF)
+    deep(dev, nested=False)
+    torch.cuda.synchronize()
+    # the same keys in other pieces: each within the rounding of its weights
+    assert (deep.out.double() - want.double()).abs().max() <= 4 * du.UNIT["float16"] * 5
