@@ -1,8 +1,11 @@
 // Attention for trees of drafted tokens over the paged cache (see tree_tile.h for the
 // tile and its mathematics).
 //
-// One workgroup per (request, cache head, column tile) goes through the prefixes of the
-// request's group chain and its own tokens and writes the output.
+// k_tree_decode: a workgroup per (request, cache head, column tile) goes through the
+// prefixes of the request's group chain and its own tokens and writes the output.
+// k_tree_small: the same for at most 16 columns, by waves that share the keys.
+// k_tree_partials, k_tree_join: the split plan, pieces of prefixes and of own tokens, and
+// their combination.
 #include "tree_stream.h"
 
 namespace parrot {
