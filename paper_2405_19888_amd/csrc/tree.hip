@@ -107,7 +107,7 @@ PARROT_DEV void tree_item(const TreeArgs& a, tree_detail::Lds<DT>& lds, int r, i
     rg.mask0 = pre ? 0x40000000 : base & ~31;
     rg.base = pre ? P : base;
     rg.end = rg.t1;
-    tile.run(rg);
+    tile.run(rg, [] {});
     if (!pre) break;
     g = a.parents ? ld_uniform(a.parents + g) : -1;
   }
@@ -211,8 +211,7 @@ PARROT_DEV void tree_piece(const TreeArgs& a, tree_detail::Lds<DT>& lds, const T
     const int x = pc.col0 + col, row = x / a.G;
     return (size_t)lds.rows[row - pc.row0] * (a.H * a.G) + pc.h * a.G + (x - row * a.G);
   };
-  tile.template load_queries<false>(a.q, pc.ncols, row_of);
-  tile.run(pc.rg);
+  tile.run(pc.rg, [&] { tile.template load_queries<false>(a.q, pc.ncols, row_of); });
   if (!tile.act) return;
   if (pc.slot < 0) write_output<DT, D, NS>(a, tile, pc.ncols, row_of);
   else write_partial<DT, D, NS>(a, tile, pc.ncols, pc.slot, row_of);

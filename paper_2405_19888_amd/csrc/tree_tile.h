@@ -167,19 +167,28 @@ struct TreeState {
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
           const int e = CHUNKS ? 16 * (ks >> 2) + 4 * (lane >> 4) + (ks & 3) : 4 * ks + (lane >> 4);
-          const float x = ok ? reinterpret_cast<const float*>(src)[e] : 0.f;
-          qs[c][ks] = __uint_as_float(__float_as_uint(x) ^ qsign);
+          qs[c][ks] = ok ? reinterpret_cast<const float*>(src)[e] : 0.f;
         }
       } else {
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-          const u32x4 x = ok ? ld16(src + (32 * ks + 8 * (lane >> 4)) * 2) : u32x4{0u, 0u, 0u, 0u};
-          qf[c][ks] = x ^ u32x4{qsign, qsign, qsign, qsign};
+          qf[c][ks] = ok ? ld16(src + (32 * ks + 8 * (lane >> 4)) * 2) : u32x4{0u, 0u, 0u, 0u};
         }
       }
       mref[c] = -FLT_MAX; thr[c] = -INFINITY; lsum[c] = 0.f; lsr[c] = 0.f;
 #pragma unroll
       for (int i = 0; i < DT16; ++i) o[c][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    if (qsign) {                        // (a rare branch: it waits for the loads)
+#pragma unroll
+      for (int c = 0; c < NS; ++c)
+        if constexpr (DT == kF32) {
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) qs[c][ks] = -qs[c][ks];
+        } else {
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) qf[c][ks] ^= u32x4{qsign, qsign, qsign, qsign};
+        }
     }
   }
 
@@ -412,14 +421,18 @@ struct TreeTile : TreeState<DT, D, NS> {
 
   // The range's tokens: every wave of the workgroup calls it, whether it has columns
   // or not (all of them load and synchronise).
-  PARROT_DEV void run(const TreeRange& rg) {
+  // first() runs once the first block ids are requested.
+  template <class F>
+  PARROT_DEV void run(const TreeRange& rg, F first) {
     using namespace prefix_detail;
     for (int t = rg.t0; t < rg.t1; t += kTreeSpan * kBlock) {
       const int b0 = t / kBlock;
       const int nb = (min(rg.t1, t + kTreeSpan * kBlock) - t + kBlock - 1) / kBlock;
-      __syncthreads();                                       // the LDS of what ran before is free
-      if ((int)threadIdx.x < nb) lds.tbl[threadIdx.x] = clampi(rg.tbl[b0 + threadIdx.x], 0, rg.npool - 1);
-      __syncthreads();
+      const int id = (int)threadIdx.x < nb ? rg.tbl[b0 + threadIdx.x] : 0;
+      if (t == rg.t0) first();
+      lds_sync();                                            // the LDS of what ran before is free
+      if ((int)threadIdx.x < nb) lds.tbl[threadIdx.x] = clampi(id, 0, rg.npool - 1);
+      lds_sync();
       span(rg, b0, nb);
     }
   }
