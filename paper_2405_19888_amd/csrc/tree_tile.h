@@ -312,10 +312,17 @@ struct TreeTile : TreeState<DT, D, NS> {
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
     const int row = lane & 15;
     const char* krow = kb + row * ROW_B + 4 * (lane >> 4);
+    // (eight reads, then their products: left alone, the compiler waits for each read where
+    // registers are short, and a stage takes 1.4 times as long)
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      const float kv = *reinterpret_cast<const float*>(krow + ((ks ^ tree_detail::swizzle<DT, D>(row)) << 4));
-      s = __builtin_amdgcn_mfma_f32_16x16x4f32(kv, qs[c][ks], s, 0, 0, 0);
+    for (int k0 = 0; k0 < KS; k0 += 8) {
+      float kv[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        kv[i] = *reinterpret_cast<const float*>(krow + (((k0 + i) ^ tree_detail::swizzle<DT, D>(row)) << 4));
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s = __builtin_amdgcn_mfma_f32_16x16x4f32(kv[i], qs[c][k0 + i], s, 0, 0, 0);
     }
     return s;
   }
@@ -409,12 +416,14 @@ struct TreeTile : TreeState<DT, D, NS> {
       for (int kt = 0; kt < 4; ++kt) {
         const int row = 4 * (lane >> 4) + kt;
         const char* vrow = vb + row * ROW_B + 4 * (lane & 3);
+        float v[DT16];
 #pragma unroll
-        for (int dt = 0; dt < DT16; ++dt) {
-          const float v = *reinterpret_cast<const float*>(
+        for (int dt = 0; dt < DT16; ++dt)
+          v[dt] = *reinterpret_cast<const float*>(
               vrow + (((4 * dt + ((lane & 15) >> 2)) ^ tree_detail::swizzle<DT, D>(row)) << 4));
-          o[c][dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, x[kt], o[c][dt], 0, 0, 0);
-        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int dt = 0; dt < DT16; ++dt) o[c][dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[dt], x[kt], o[c][dt], 0, 0, 0);
       }
     }
   }
