@@ -243,10 +243,10 @@ parrot_status check_tree_counts(int32_t requests, const parrot_tree_rows* rows) 
 //    column tile at 6.0 TB/s (by waves 6.4) or their products (fp32: those of whole tiles),
 //    the prefixes' products, and the partial results, written and read, at 4.7 TB/s.
 // Measured, one launch and split, 16-bit heads of 128: a request of 64 rows on 300, 2000,
-// 8000 tokens and 32 heads 15.5 and 21, 48 and 24, 156 and 50 us; 32 requests of 64 rows,
-// four query heads on each of 8, on 300, 4000 tokens 29 and 75, 180 and 279; 32 requests of
-// 8 rows on one prefix of 300, 4000 tokens and 32 heads 32 and 33, 166 and 57; 128 requests
-// of 4 rows on 1000 tokens and 8 heads 106 and 95.
+// 8000 tokens and 32 heads 15 and 20, 47 and 24, 155 and 46 us; 32 requests of 64 rows,
+// four query heads on each of 8, on 300, 4000 tokens 29 and 72, 181 and 284; 32 requests of
+// 8 rows on one prefix of 300, 4000 tokens and 32 heads 33 and 31, 162 and 58; 128 requests
+// of 4 rows on 1000 tokens and 8 heads 103 and 95.
 bool tree_splits(const parrot_problem* p, const parrot_tree_rows* rows, const TreePlan& pl, long cus) {
   const double mean = 0.7, R = p->num_requests, H = p->num_heads, HQ = rows->num_query_heads, D = p->head_dim;
   const double T = rows->num_query_rows, eb = p->dtype == PARROT_DTYPE_F32 ? 4 : 2, kv = 2 * D * eb * H;
@@ -303,8 +303,8 @@ parrot_status check_tree(const parrot_problem* p, const parrot_tree_rows* rows, 
     return set_error(PARROT_ERR_UNSUPPORTED, "tree decode needs too many workgroups");
   // The split plan.  Prefix chunks are as long as their workgroups still fill the device
   // (a chunk more costs a tile 64 KB of partial results, written and read: 48 rows each on
-  // six prefixes of 2304 tokens take 167 us in one chunk; before the prefixes went first,
-  // 179 in one, 199 in two, 237 in five),
+  // six prefixes of 2304 tokens take 156 us in one chunk; at an earlier step 179 in one,
+  // 199 in two, 237 in five),
   // but not so long that the last ones run alone (48 rows of 8 requests on 8192 tokens: 126
   // us in chunks of 4096, 98 of 2048, 111 of 1024).  A group has at most tiles_p tiles, all
   // of them together a tile each beyond what their rows fill.
@@ -327,10 +327,10 @@ parrot_status check_tree(const parrot_problem* p, const parrot_tree_rows* rows, 
   // Tiles: two workgroups per CU (64 and 128 rows on 9600 tokens: 239 and 257 us; 216 and
   // 280 with one, 261 and 279 with three), three where a request may have several tiles
   // and the products bound it, and for fp32 (32 requests of 20 rows on 4000 tokens: 1411 us
-  // with two, 1107 with three).
+  // with two, 1107 with three, 928 since the tile reads ahead).
   const long most_cols = rows->max_query_rows * G;
   // (fp32 caches with two column sets spill: 32 requests of 20 rows on 1000 tokens 440 us, by
-  // tiles 351).
+  // tiles 294).
   pl->sets = most_cols <= 16 ? 1 : most_cols <= 32 && p->dtype != PARROT_DTYPE_F32 ? 2 : 0;
   pl->small = pl->sets == 1 && parrot::tree_small_rows(p->dtype, p->head_dim) && R * H <= cus;
   const long per_wg = pl->sets ? 4 : 1;
@@ -339,7 +339,7 @@ parrot_status check_tree(const parrot_problem* p, const parrot_tree_rows* rows, 
   pl->min_run = kTreeMinRun;
   const long units = ceil_div(p->max_suffix_len, parrot::tree_unit(p->dtype, p->head_dim));
   // the longer items start first, so that the short ones fill up (48 rows each on six
-  // prefixes of 2304 tokens: 167 us, 182 with the own tokens first)
+  // prefixes of 2304 tokens: 167 us, 182 with the own tokens first, at that step)
   pl->pre_first = (double)R * pl->tiles * units / pl->runs < (double)pl->cp / parrot::tree_unit(p->dtype, p->head_dim);
   const long seg = pl->seg_pre + std::min(ceil_div(units, pl->min_run) + 1, (long)pl->runs);
   const double cost = (double)R * pl->tiles * (units + parrot::kTreeSetup);

@@ -257,7 +257,7 @@ PARROT_DEV void write_desc(const TreeArgs& a, int r, const OwnCost& c, int start
 // The tiles of a request read the same keys: with their costs taken up to a multiple of the
 // run length, they are cut at the same tokens, the workgroups that read a token do it
 // at about the same time, and it comes from memory once (6 requests of 96 .. 256 columns
-// on 9000 .. 33000 tokens: 156 us, 180 without).  That costs each such tile half a run of
+// on 9000 .. 33000 tokens: 156 us, 180 without, at that step).  That costs each such tile half a run of
 // idle workgroups, so it is done where they are at most a quarter of the runs.
 
 // Finds the runs run_of(wave) of the cost (each wave gets its own); false for a wave whose
