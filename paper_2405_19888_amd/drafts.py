@@ -68,6 +68,9 @@ def parrot_tree_workspace_bytes(problem: ParrotProblem, rows: ParrotTreeRows) ->
 
 
 # ---------------------------------------------------------------- marshalling
+_TORCH_DTYPES = {v: k for k, v in DTYPE_CODES.items()}
+
+
 def _stream(stream, device: torch.device) -> int:
     if stream is None:
         stream = torch.cuda.current_stream(device)
@@ -100,6 +103,36 @@ def _bound(fn, values, device: torch.device, stream):
     return call
 
 
+def _need(t, name: str, dtype: torch.dtype, least: int, device: torch.device):
+    """Refuses a tensor that the kernels would read or write beyond its end (addresses
+    and None go to the library's own checks; parents are read for real rows alone, whose
+    number only the device knows)."""
+    if not isinstance(t, torch.Tensor):
+        return
+    if t.dtype != dtype or not t.is_contiguous() or t.numel() < least:
+        raise ValueError(f"{name} is not a contiguous {dtype} tensor of at least {least} elements")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+
+
+def _need_cache(p: ParrotProblem, device: torch.device, suffix_k, suffix_v, suffix_tables, suffix_lens):
+    own = p.num_suffix_blocks * p.num_heads * p.block_size * p.head_dim
+    for t, name in ((suffix_k, "suffix_k"), (suffix_v, "suffix_v")):
+        _need(t, name, _TORCH_DTYPES[p.dtype], own, device)
+    _need(suffix_tables, "suffix_tables", torch.int32, p.num_requests * p.suffix_table_stride, device)
+    _need(suffix_lens, "suffix_lens", torch.int32, p.num_requests, device)
+
+
+def _need_rows(x, name: str, rows: int, heads: int, p: ParrotProblem, device: torch.device):
+    """Rows [rows, heads, D] of any row stride."""
+    if not isinstance(x, torch.Tensor):
+        return
+    if x.dtype != _TORCH_DTYPES[p.dtype] or x.dim() != 3 or x.shape[0] < rows or tuple(x.shape[1:]) != (heads, p.head_dim):
+        raise ValueError(f"{name} is not [{rows}, {heads}, {p.head_dim}] of {_TORCH_DTYPES[p.dtype]}")
+    if x.device != device:
+        raise ValueError(f"{name} is on {x.device}, not on {device}")
+
+
 def _row_stride(x: torch.Tensor, name: str) -> int:
     """Elements between the rows of [rows, heads, D] whose heads are adjacent."""
     if x.dim() != 3 or x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != x.shape[2]):
@@ -110,6 +143,15 @@ def _row_stride(x: torch.Tensor, name: str) -> int:
 def _fill_call(problem, num_query_rows, max_query_rows, num_query_heads, rotary, norm_eps, q, k, v, q_norm, k_norm,
                positions, query_offsets, suffix_tables, suffix_lens, q_out, suffix_k, suffix_v, stream):
     fn = load_library().parrot_rotary_fill
+    T, D, dt = int(num_query_rows), problem.head_dim, _TORCH_DTYPES[problem.dtype]
+    for x, name, heads in ((q, "q", int(num_query_heads)), (k, "k", problem.num_heads), (v, "v", problem.num_heads)):
+        _need_rows(x, name, T, heads, problem, k.device)
+    _need(q_out, "q_out", dt, T * int(num_query_heads) * D, k.device)
+    for x, name in ((q_norm, "q_norm"), (k_norm, "k_norm")):
+        _need(x, name, dt, D, k.device)
+    _need(positions, "positions", torch.int32, T, k.device)
+    _need(query_offsets, "query_offsets", torch.int32, problem.num_requests + 1, k.device)
+    _need_cache(problem, k.device, suffix_k, suffix_v, suffix_tables, suffix_lens)
     rows = ParrotFillRows(int(num_query_rows), int(max_query_rows), int(num_query_heads), float(norm_eps),
                           0 if q is None else _row_stride(q, "q"), _row_stride(k, "k"), _row_stride(v, "v"))
     return _bound(fn, (ctypes.byref(problem), ctypes.byref(rows), None if rotary is None else ctypes.byref(rotary), q,
@@ -129,6 +171,20 @@ def parrot_rotary_fill(problem, num_query_rows, max_query_rows, num_query_heads,
 def _tree_call(problem, rows, q, query_offsets, tree_parents, prefix_k, prefix_v, suffix_k, suffix_v, prefix_tables,
                prefix_lens, prefix_parents, suffix_tables, suffix_lens, group_ids, out, lse, workspace, stream):
     fn = load_library().parrot_shared_prefix_tree_decode
+    p, T, HQ, dt, ints = problem, rows.num_query_rows, rows.num_query_heads, _TORCH_DTYPES[problem.dtype], torch.int32
+    pre = p.num_prefix_blocks * p.num_heads * p.block_size * p.head_dim if p.num_groups > 0 else 0
+    for x, name, dtype, least in (
+            (q, "q", dt, T * HQ * p.head_dim), (out, "out", dt, T * HQ * p.head_dim), (lse, "lse", torch.float32, T * HQ),
+            (query_offsets, "query_offsets", ints, p.num_requests + 1), (tree_parents, "tree_parents", ints, 0),
+            (group_ids, "group_ids", ints, p.num_requests)):
+        _need(x, name, dtype, least, q.device)
+    if p.num_groups > 0:
+        for x, name, dtype, least in (
+                (prefix_k, "prefix_k", dt, pre), (prefix_v, "prefix_v", dt, pre), (prefix_lens, "prefix_lens", ints, p.num_groups),
+                (prefix_tables, "prefix_tables", ints, p.num_groups * p.prefix_table_stride),
+                (prefix_parents, "prefix_parents", ints, p.num_groups)):
+            _need(x, name, dtype, least, q.device)
+    _need_cache(p, q.device, suffix_k, suffix_v, suffix_tables, suffix_lens)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     return _bound(fn, (ctypes.byref(problem), ctypes.byref(rows), q, query_offsets, tree_parents, prefix_k, prefix_v,
                        suffix_k, suffix_v, prefix_tables, prefix_lens, prefix_parents, suffix_tables, suffix_lens,
@@ -158,6 +214,12 @@ def parrot_validate_tree_inputs(problem, rows, query_offsets, tree_parents, pref
 def _accept_call(num_requests, rows, query_offsets, tree_parents, draft_tokens, target_tokens, root_tokens,
                  accept_rows, accept_lens, next_tokens, stream):
     fn = load_library().parrot_tree_accept
+    T, R = rows.num_query_rows, int(num_requests)
+    for x, name, least in ((query_offsets, "query_offsets", R + 1), (tree_parents, "tree_parents", 0),
+                           (draft_tokens, "draft_tokens", T), (target_tokens, "target_tokens", T),
+                           (root_tokens, "root_tokens", R), (accept_rows, "accept_rows", T),
+                           (accept_lens, "accept_lens", R), (next_tokens, "next_tokens", R)):
+        _need(x, name, torch.int32, least, query_offsets.device)
     return _bound(fn, (int(num_requests), ctypes.byref(rows), query_offsets, tree_parents, draft_tokens,
                        target_tokens, root_tokens, accept_rows, accept_lens, next_tokens), _device(query_offsets),
                   stream)
@@ -173,6 +235,11 @@ def parrot_tree_accept(num_requests, rows, query_offsets, tree_parents, draft_to
 def _commit_call(problem, rows, query_offsets, accept_rows, accept_lens, suffix_tables, suffix_lens, suffix_k,
                  suffix_v, committed_lens, stream):
     fn = load_library().parrot_tree_commit
+    R = problem.num_requests
+    for x, name, least in ((query_offsets, "query_offsets", R + 1), (accept_rows, "accept_rows", rows.num_query_rows),
+                           (accept_lens, "accept_lens", R), (committed_lens, "committed_lens", R)):
+        _need(x, name, torch.int32, least, suffix_k.device)
+    _need_cache(problem, suffix_k.device, suffix_k, suffix_v, suffix_tables, suffix_lens)
     return _bound(fn, (ctypes.byref(problem), ctypes.byref(rows), query_offsets, accept_rows, accept_lens,
                        suffix_tables, suffix_lens, suffix_k, suffix_v, committed_lens), _device(suffix_k), stream)
 
@@ -185,9 +252,6 @@ def parrot_tree_commit(problem, rows, query_offsets, accept_rows, accept_lens, s
 
 
 # -------------------------------------------------------------------- handles
-_TORCH_DTYPES = {v: k for k, v in DTYPE_CODES.items()}
-
-
 class RotaryFiller:
     """Owns the rotated queries of one fill shape: up to ``num_query_rows`` rows, at
     most ``max_query_rows`` per request.  ``num_query_heads`` 0: keys and values only."""
@@ -315,11 +379,14 @@ def tree_decode(q_rows, query_offsets, tree_parents, prefix_k, prefix_v, suffix_
                                None if prefix_parents is None else prefix_parents.cpu().numpy())
     rows.num_query_rows = q_rows.shape[0]
     dec = TreeDecoder(prob, rows, device=q_rows.device)
-    return dec(dict(q_rows=q_rows, query_offsets=query_offsets, tree_parents=tree_parents, prefix_k=prefix_k,
-                    prefix_v=prefix_v, suffix_k=suffix_k, suffix_v=suffix_v, prefix_tables=prefix_tables,
+    res = dec(dict(q_rows=q_rows, query_offsets=query_offsets, tree_parents=tree_parents, prefix_k=prefix_k,
+                   prefix_v=prefix_v, suffix_k=suffix_k, suffix_v=suffix_v, prefix_tables=prefix_tables,
                     prefix_lens=prefix_lens, suffix_tables=suffix_tables, suffix_lens=suffix_lens,
                     group_ids=group_ids, prefix_parents=prefix_parents),
-               stream=stream, nested=prefix_parents is not None)
+              stream=stream, nested=prefix_parents is not None)
+    if stream is not None:                       # the workspace goes back to the allocator here
+        dec.workspace.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream)))
+    return res
 
 
 def tree_accept(query_offsets, tree_parents, draft_tokens, target_tokens, root_tokens, *, stream=None):

@@ -156,6 +156,51 @@ def test_tree_path_by_size(parrot_lib):
     assert split(shared, many, 0) == split(shared, many, 1) == 1
 
 
+def tensors(dtype=torch.float16):
+    """A tree and fill call's tensors for problem() with 20 rows of 8 query heads."""
+    ints = lambda *n: torch.zeros(n, dtype=torch.int32)
+    pool = torch.zeros((100, 4, 16, 128), dtype=dtype)
+    return dict(q=torch.zeros((20, 8, 128), dtype=dtype), query_offsets=ints(9), tree_parents=ints(20), prefix_k=pool,
+                prefix_v=pool, suffix_k=pool, suffix_v=pool, prefix_block_tables=ints(2, 32), prefix_lens=ints(2),
+                prefix_parents=None, suffix_block_tables=ints(8, 19), suffix_lens=ints(8), group_ids=ints(8),
+                out=torch.zeros((20, 8, 128), dtype=dtype), lse=torch.zeros((20, 8)),
+                workspace=torch.zeros(256, dtype=torch.uint8))
+
+
+@pytest.mark.parametrize("name", ["q", "query_offsets", "tree_parents", "prefix_k", "suffix_v", "prefix_block_tables",
+                                  "prefix_lens", "suffix_block_tables", "suffix_lens", "group_ids", "out", "lse"])
+def test_tensors_that_do_not_fit(parrot_lib, name):
+    """A tensor of another type, too short or with gaps is refused by its name before the
+    library sees its address; fitting ones get as far as the device check."""
+    rows = parrot.make_tree_rows(20, 10, 20, 8)
+    with pytest.raises(ValueError, match="on the GPU"):
+        parrot.parrot_shared_prefix_tree_decode(problem(), rows, **tensors())
+    x = tensors()[name]
+    bads = [x.double()]
+    if name != "tree_parents":                    # (padding rows' parents are not read)
+        bads.append(x[:-1].clone())
+    if x.shape[0] > 1:
+        bads.append(torch.cat([x, x])[::2])
+    for bad in bads:
+        with pytest.raises(ValueError, match=name.replace("_block", "") + " is not a contiguous"):
+            parrot.parrot_shared_prefix_tree_decode(problem(), rows, **{**tensors(), name: bad})
+
+
+def test_fill_tensors_that_do_not_fit(parrot_lib):
+    t = tensors()
+    kv = torch.zeros((20, 4, 128), dtype=torch.float16)
+    good = dict(q=t["q"], k=kv, v=kv, q_norm=None, k_norm=kv[0, 0], positions=t["tree_parents"],
+                query_offsets=t["query_offsets"], suffix_tables=t["suffix_block_tables"], suffix_lens=t["suffix_lens"],
+                q_out=t["out"], suffix_k=t["suffix_k"], suffix_v=t["suffix_v"])
+    with pytest.raises(ValueError, match="on the GPU"):
+        parrot.parrot_rotary_fill(problem(), 20, 10, 8, None, **good)
+    for name, bad, msg in [("q", t["q"][:19], "q is not"), ("k", kv.float(), "k is not"), ("v", kv[:, :3], "v is not"),
+                           ("k_norm", kv[0, 0, :64], "k_norm is not"), ("positions", t["tree_parents"].long(), "positions"),
+                           ("q_out", t["out"][:10], "q_out is not"), ("suffix_k", t["suffix_k"][:99], "suffix_k is not")]:
+        with pytest.raises(ValueError, match=msg):
+            parrot.parrot_rotary_fill(problem(), 20, 10, 8, None, **{**good, name: bad})
+
+
 def test_accept_and_commit_refusals(parrot_lib):
     assert call(parrot_lib, "parrot_tree_accept", requests=-1) == B.PARROT_ERR_INVALID_ARGUMENT
     assert call(parrot_lib, "parrot_tree_accept", requests=0, query_offsets=None,

@@ -239,6 +239,16 @@ def test_one_call_form():
                                   dev["prefix_lens"], dev["suffix_tables"], dev["suffix_lens"], dev["group_ids"])
     torch.cuda.synchronize()
     assert torch.equal(out, want) and torch.equal(lse, wlse)
+    # on another stream, the allocator busy on this one
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    for _ in range(5):
+        got, _ = parrot.tree_decode(dev["q_rows"], dev["query_offsets"], dev["tree_parents"], dev["k_pool"],
+                                    dev["v_pool"], dev["k_pool"], dev["v_pool"], dev["prefix_tables"],
+                                    dev["prefix_lens"], dev["suffix_tables"], dev["suffix_lens"], dev["group_ids"], stream=s)
+        torch.full((1 << 16,), 0xFF, dtype=torch.uint8, device="cuda")
+        s.synchronize()
+        assert torch.equal(got, want)
 
 
 def test_seeded_random_plans():
