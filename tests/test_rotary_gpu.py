@@ -202,3 +202,27 @@ def test_graph_and_one_call_form():
                                  dev["k_pool"], dev["v_pool"], dev["suffix_tables"], dev["suffix_lens"], rotary=rot)
         torch.cuda.synchronize()
         assert torch.equal(out, got) and torch.equal(torch.nan_to_num(gk), torch.nan_to_num(dev["k_pool"]))
+
+
+@pytest.mark.parametrize("dtype,dim,interleaved,rd", [("float16", 128, False, 128), ("bfloat16", 128, False, 96),
+                                                      ("float32", 128, False, 20), ("float16", 64, True, 64),
+                                                      ("bfloat16", 64, False, 12)])
+@pytest.mark.parametrize("requests", [2, 300])
+def test_in_place_over_many_heads(dtype, dim, interleaved, rd, requests):
+    """Queries rotated in place, several steps of a row's heads requested ahead, by few rows
+    (a row's heads over several workgroups) and by many."""
+    import paper_2405_19888_amd as parrot
+    rows = [5] * requests
+    plan, batch, off = setup(dtype, 8, dim, [3] * requests, rows)
+    T = 5 * requests
+    q, k, v = (rows_of(i, T, h, dim, dtype) for i, h in ((1, 72), (2, 8), (3, 8)))
+    w = 1 + 0.1 * rows_of(9, 1, 1, dim, dtype)[0, 0]
+    rot = parrot.make_rotary(rd, interleaved=interleaved)
+    positions = [int(x) for x in np.random.default_rng(0).integers(0, 9000, T)]
+    want, dev = fill(plan, batch, off, q, k, v, positions, rot, q_norm=w, k_norm=w)
+    x = q.cuda()
+    parrot.parrot_rotary_fill(want.problem, T, 5, 72, rot, x, k.cuda(), v.cuda(), dev["q_norm"], dev["k_norm"],
+                              dev["positions"], dev["query_offsets"], dev["suffix_tables"], dev["suffix_lens"], x,
+                              dev["k_pool"], dev["v_pool"], norm_eps=EPS)
+    torch.cuda.synchronize()
+    assert torch.equal(x, want.q_out)
