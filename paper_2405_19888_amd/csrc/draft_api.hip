@@ -445,11 +445,18 @@ parrot_status parrot_validate_tree_inputs(
 }
 
 // Test hooks (not in parrot_attn.h): the path of this thread's tree calls (see
-// g_tree_path; -1 gives the choice back), and the path these arguments take (-1: invalid).
+// g_tree_path; -1 gives the choice back), the path these arguments take (-1: invalid), and
+// the kernel: one launch by a tile (0) or by waves that share the keys (1), partial results
+// by tiles (2) or by waves of one or two column sets (3, 4).
 void parrot_test_tree_path(int path) { g_tree_path = path == 0 || path == 1 ? path : -1; }
 int parrot_test_tree_split(const parrot_problem* p, const parrot_tree_rows* rows, int nested) {
   TreePlan pl;
   return check_tree(p, rows, nested != 0, &pl) == PARROT_OK ? pl.split : -1;
+}
+int parrot_test_tree_kernel(const parrot_problem* p, const parrot_tree_rows* rows, int nested) {
+  TreePlan pl;
+  if (check_tree(p, rows, nested != 0, &pl) != PARROT_OK) return -1;
+  return pl.split ? 2 + pl.sets : pl.small ? 1 : 0;
 }
 
 // --------------------------------------------------------- accept and commit

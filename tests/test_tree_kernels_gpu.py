@@ -1,0 +1,102 @@
+"""Every kernel that a tree call may take, by type, head size and columns: which one runs,
+parity over nested prefixes and real trees with several steps a wave, and what drafted
+tokens hold that a row does not see."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import drafts_util as du
+from drafts_util import oracle
+from gpu_util import problem_for
+from test_tree_gpu import check, run
+
+pytestmark = pytest.mark.gpu
+
+TYPES = [("float16", 128), ("float16", 64), ("bfloat16", 128), ("bfloat16", 64), ("float32", 128), ("float32", 64)]
+COLUMNS = {"16": 8, "32": 16, "more": 37}              # rows of the longest tree, two query heads each
+PATHS = {"one": 0, "split": 1}
+
+
+def kernel_of(dtype, dim, columns, path):
+    """The kernel as parrot_test_tree_kernel names it."""
+    few = columns == "16"
+    if path == "one":                                  # rows of 256 bytes and more are shared by waves
+        return 1 if few and (dim == 128 or dtype == "float32") else 0
+    if columns == "32" and dtype != "float32":
+        return 4
+    return 3 if few else 2
+
+
+@pytest.fixture(params=["one", "split"])
+def path(request):
+    import paper_2405_19888_amd as parrot
+    force = parrot.load_library().parrot_test_tree_path
+    force(PATHS[request.param])
+    yield request.param
+    force(-1)
+
+
+def batch_of(dtype, dim, columns, seed):
+    """Three requests on chains of four, one and no prefixes, drafted tokens at odd offsets."""
+    most = COLUMNS[columns]
+    rows, cached = [most, max(1, most - 3), most], [1203, 45, 310]
+    plan = du.tree_plan(dtype, 2, dim, [3, 0, -1], [130, 33, 70, 45], cached, rows, [-1, 0, 1, 2], seed=seed)
+    up = du.random_trees(np.random.default_rng(seed + 50), rows, spread=4, roots=2)
+    off = du.offsets_of(rows)
+    return plan, du.make_batch(plan, seed=seed), off, up, du.queries(int(off[-1]) + 2, 4, dim, dtype, seed=seed), rows, cached
+
+
+def takes(dec, plan):
+    import paper_2405_19888_amd as parrot
+    return parrot.load_library().parrot_test_tree_kernel(ctypes.byref(dec.problem), ctypes.byref(dec.rows), int(plan.nested))
+
+
+@pytest.mark.parametrize("columns", COLUMNS)
+@pytest.mark.parametrize("dtype,dim", TYPES)
+def test_parity(path, dtype, dim, columns):
+    plan, batch, off, up, q, _, _ = batch_of(dtype, dim, columns, seed=len(columns) + dim)
+    out, lse, dec, _ = run(plan, batch, q, off, up)
+    assert takes(dec, plan) == kernel_of(dtype, dim, columns, path)
+    check(plan, batch, q, off, up, out, lse, what=f"{path} {dtype} {dim} columns {columns}")
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("columns", COLUMNS)
+@pytest.mark.parametrize("dtype,dim", TYPES)
+def test_masked_tokens_hold_anything(path, dtype, dim, columns, value):
+    """Drafted tokens whose values (one element of a head, neighbouring tokens, the last one
+    whole) and then whose keys are no finite numbers: rows that do not see them keep every
+    bit, rows that do get them where they stand."""
+    plan, batch, off, up, q, rows, cached = batch_of(dtype, dim, columns, seed=3)
+    clean, clse, dec, _ = run(plan, batch, q, off, up)
+    assert takes(dec, plan) == kernel_of(dtype, dim, columns, path)
+    n, last = int(off[-1]), rows[0] - 1
+    held = {(0, 2): [5], (0, 3): [5, dim - 1], (0, last): list(range(dim)), (2, 0): [17]}    # (request, token): elements
+    slot = lambda r, t: (int(plan.suffix_tables[r][(cached[r] + t) // 16]), (cached[r] + t) % 16)
+    hits = torch.zeros((n, dim), dtype=torch.bool)                             # by query heads 2, 3
+    sees = torch.zeros(n, dtype=torch.bool)
+    for (r, t), elements in held.items():
+        blk, at = slot(r, t)
+        batch.v_pool[blk, 1, at, elements] = value
+        for j in range(rows[r]):
+            if t in oracle.tree_path(up[off[r]:off[r + 1]], j):
+                hits[int(off[r]) + j, elements] = True
+                sees[int(off[r]) + j] = True
+    assert sees.any() and not sees.all()
+    got, glse, _, _ = run(plan, batch, q, off, up)
+    got, clean = got[:n].cpu(), clean[:n].cpu()
+    assert torch.equal(glse[:n], clse[:n])
+    assert torch.equal(got[:, :2], clean[:, :2])
+    for head in (2, 3):
+        assert torch.equal(got[:, head][~hits], clean[:, head][~hits])
+        hit = got[:, head][hits]
+        assert torch.isnan(hit).all() if value != value else (hit == value).all()
+    for r, t in held:
+        blk, at = slot(r, t)
+        batch.k_pool[blk, 1, at, :] = value
+    got, glse, _, _ = run(plan, batch, q, off, up)
+    got, glse = got[:n].cpu(), glse[:n].cpu()
+    assert torch.equal(got[~sees], clean[~sees]) and torch.equal(glse[~sees], clse[:n].cpu()[~sees])
+    assert torch.equal(got[:, :2], clean[:, :2])
