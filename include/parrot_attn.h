@@ -508,7 +508,8 @@ parrot_status parrot_rotary_fill(
  *                        (each row follows the one before)
  * Row j attends to the prefixes of r's group chain, r's own tokens before the
  * drafted ones, the ancestors of j and j itself:
- *   out, lse             the decode formula over those keys.
+ *   out, lse             the decode formula over those keys; both NaN for a row
+ *                        with a logit of NaN or +inf, or whose logits are all -inf.
  * Keys and values of tokens a row does not see never reach its result, whatever
  * they hold (NaN and infinities too).
  *

@@ -63,13 +63,15 @@ PARROT_DEV void build_masks(const TreeArgs& a, tree_detail::Lds<DT>& lds, const 
   static_assert(NW + 1 == tree_detail::kMaskWords, "rows shifted by up to 31 bits");
 }
 
-// The output rows of a tile that saw its columns' whole contexts.
+// The output rows of a tile that saw its columns' whole contexts.  Every row sees itself, so a
+// weight sum of 0 means that each logit is -inf: output and log-sum-exp are NaN then, as the
+// join gives them (-inf is left to contexts without keys, which no row has).
 template <int DT, int D, int NS, class F>
 PARROT_DEV void write_output(const TreeArgs& a, TreeState<DT, D, NS>& tile, int ncols, F row_of) {
-  tile.finish([&](int c, int col, float lw, float lse2, float) {
+  tile.finish([&](int c, int col, float lw, float lse2, float lt) {
     if (col >= ncols) return;
     const size_t at = row_of(col);
-    const float inv = 1.f / lw;            // (0 only where every logit is -inf: the result is NaN)
+    const float inv = 1.f / lw;
     char* dst = (char*)a.out + (at * D + 4 * (tile.lane >> 4)) * Elem<DT>::kBytes;
 #pragma unroll
     for (int dt = 0; dt < D / 16; ++dt) {
@@ -77,7 +79,7 @@ PARROT_DEV void write_output(const TreeArgs& a, TreeState<DT, D, NS>& tile, int 
       if constexpr (DT == kF32) *reinterpret_cast<f32x4*>(dst + dt * 64) = v;
       else store4<DT>(dst + dt * 32, v);
     }
-    if (tile.lane < 16) a.lse[at] = lse2 * kLn2;
+    if (tile.lane < 16) a.lse[at] = lt == 0.f ? __builtin_nanf("") : lse2 * kLn2;
   });
 }
 
@@ -598,7 +600,7 @@ __global__ __launch_bounds__(kSmallWaves * 64) void k_tree_small(TreeArgs a) {
     const f32x4 v = acc * (1.f / wsum);
     if constexpr (DT == kF32) *reinterpret_cast<f32x4*>(dst) = v;
     else store4<DT>(dst, v);
-    if (d == 0) a.lse[row] = (mx + fast_log2(tot)) * kLn2;
+    if (d == 0) a.lse[row] = tot == 0.f ? __builtin_nanf("") : (mx + fast_log2(tot)) * kLn2;   // (as write_output)
   }
 }
 

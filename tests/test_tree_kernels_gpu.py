@@ -100,3 +100,51 @@ def test_masked_tokens_hold_anything(path, dtype, dim, columns, value):
     got, glse = got[:n].cpu(), glse[:n].cpu()
     assert torch.equal(got[~sees], clean[~sees]) and torch.equal(glse[~sees], clse[:n].cpu()[~sees])
     assert torch.equal(got[:, :2], clean[:, :2])
+
+
+@pytest.mark.parametrize("columns", COLUMNS)
+@pytest.mark.parametrize("dtype,dim", TYPES)
+def test_logits_that_are_no_finite_numbers(path, dtype, dim, columns):
+    """Queries of infinities and NaN, and logits that are all -inf, give NaN in output and
+    lse on every kernel; single logits of -inf are weights of 0; other rows keep every bit."""
+    plan, batch, off, up, q, rows, cached = batch_of(dtype, dim, columns, seed=7)
+    q = q.abs() + 0.125
+    clean, clse, dec, _ = run(plan, batch, q, off, up)
+    assert takes(dec, plan) == kernel_of(dtype, dim, columns, path)
+    n = int(off[-1])
+    clean, clse = clean[:n].cpu(), clse[:n].cpu()
+    x = q.clone()
+    x[0, 1], x[2, 3], x[n - 1] = float("inf"), float("nan"), -float("inf")
+    got, glse, _, _ = run(plan, batch, x, off, up)
+    got, glse = got[:n].cpu(), glse[:n].cpu()
+    bad = torch.zeros((n, 4), dtype=torch.bool)
+    bad[0, 1] = bad[2, 3] = bad[n - 1] = True
+    assert torch.isnan(got[bad]).all() and torch.isnan(glse[bad]).all()
+    assert torch.equal(got[~bad], clean[~bad]) and torch.equal(glse[~bad], clse[~bad])
+
+    # request 2 has no prefix: the keys of its cached tokens, then all its keys, in cache head 1
+    def clear(lo, hi):
+        for p in range(lo, hi):
+            batch.k_pool[int(plan.suffix_tables[2][p // 16]), 1, p % 16] = -float("inf")
+    clear(0, cached[2])
+    got, glse, _, _ = run(plan, batch, q, off, up)
+    got, glse = got[:n].cpu(), glse[:n].cpu()
+    mine = torch.zeros((n, 4), dtype=torch.bool)
+    mine[int(off[2]):, 2:] = True
+    assert torch.equal(got[~mine], clean[~mine]) and torch.equal(glse[~mine], clse[~mine])
+    ref, rlse, spread, _ = oracle.shared_prefix_tree(
+        q, off, up, batch.k_pool, batch.v_pool, batch.k_pool, batch.v_pool, plan.prefix_tables, plan.prefix_lens,
+        plan.suffix_tables, plan.suffix_lens, plan.group_ids, plan.sm_scale, plan.prefix_parents)
+    finite = batch.k_pool.double()
+    finite = float(finite[finite.isfinite()].abs().max())
+    noise = plan.sm_scale * finite * q[:n].double().abs().sum(-1).numpy()          # no logit has more
+    tol = du.out_tolerance(dtype, ref[:n], spread[:n], noise, cached[2] + rows[2], dim)
+    ltol = du.lse_tolerance(rlse[:n], noise, cached[2] + rows[2], dim)
+    at = mine.numpy()
+    assert (np.abs(got.double().numpy() - ref[:n])[at] <= tol[at]).all()
+    assert (np.abs(glse.double().numpy() - rlse[:n])[at] <= ltol[at]).all()
+    clear(cached[2], cached[2] + rows[2])
+    got, glse, _, _ = run(plan, batch, q, off, up)
+    got, glse = got[:n].cpu(), glse[:n].cpu()
+    assert torch.isnan(got[mine]).all() and torch.isnan(glse[mine]).all()
+    assert torch.equal(got[~mine], clean[~mine]) and torch.equal(glse[~mine], clse[~mine])
