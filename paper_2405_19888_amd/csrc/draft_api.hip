@@ -446,7 +446,7 @@ parrot_status parrot_validate_tree_inputs(
 
 // Test hooks (not in parrot_attn.h): the path of this thread's tree calls (see
 // g_tree_path; -1 gives the choice back), the path these arguments take (-1: invalid), and
-// the kernel: one launch by a tile (0) or by waves that share the keys (1), partial results
+// their kernel: one launch by a tile (0) or by waves that share the keys (1), partial results
 // by tiles (2) or by waves of one or two column sets (3, 4).
 void parrot_test_tree_path(int path) { g_tree_path = path == 0 || path == 1 ? path : -1; }
 int parrot_test_tree_split(const parrot_problem* p, const parrot_tree_rows* rows, int nested) {
@@ -457,6 +457,12 @@ int parrot_test_tree_kernel(const parrot_problem* p, const parrot_tree_rows* row
   TreePlan pl;
   if (check_tree(p, rows, nested != 0, &pl) != PARROT_OK) return -1;
   return pl.split ? 2 + pl.sets : pl.small ? 1 : 0;
+}
+// The slots that the join reads for a row's descriptor into out[0 .. most): how many.
+int parrot_test_tree_slots(uint32_t lo, uint32_t hi, int own, int seg_p, int seg_pre, int seg, int* out, int most) {
+  const parrot::TreeSlots s = parrot::tree_slots(lo, hi, own, seg_p, seg_pre, seg);
+  for (int i = 0; i < s.n && i < most; ++i) out[i] = s.slot(i);
+  return s.n;
 }
 
 // --------------------------------------------------------- accept and commit

@@ -627,19 +627,9 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a) {
   if (t >= ld_uniform(a.qoff + a.R)) return;              // padding (its descriptor holds nothing)
   const int s0 = first + (j * a.G + hq % a.G) / tree_detail::kCols<DT> * between;
   const int pieces = (s0 + units - 1) / q - s0 / q + 1;
-  // (clamped, so that a row without a descriptor, in a call that breaks the rules, reads
-  // inside its slots)
-  const int b1 = min((int)(lo & 0xFFFFu), a.seg_p), b2 = b1 + min((int)(lo >> 16), a.seg_p);
-  const int b3 = b2 + min((int)(hi & 0xFFFFu), a.seg_p), b4 = min(b3 + min((int)(hi >> 16), a.seg_p), a.seg_pre);
   const bool live = hq < HQ && !(prefixed == 0 && pieces == 1);   // one piece: it wrote the output
-  const int n = live ? b4 + min(max(pieces, 0), a.seg - a.seg_pre) : 0;
-  auto slot_of = [&](int i) {
-    int sl = a.seg_pre + (i - b4);
-    sl = i < b4 ? 3 * a.seg_p + (i - b3) : sl;
-    sl = i < b3 ? 2 * a.seg_p + (i - b2) : sl;
-    sl = i < b2 ? a.seg_p + (i - b1) : sl;
-    return i < b1 ? i : sl;
-  };
+  const TreeSlots slots = tree_slots(lo, hi, pieces, a.seg_p, a.seg_pre, a.seg);
+  const int n = live ? slots.n : 0;
   int most = n;
 #pragma unroll
   for (int x = GW; x < kWave; x <<= 1) most = max(most, __shfl_xor(most, x));
@@ -648,19 +638,19 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a) {
   const float* lsep = a.lse_part + at * a.seg;
   const float* op = a.o_part + at * a.seg * D + i0 * 4;
   // the lane's first log-sum-exp, and the first outputs beside it
-  const float l0 = i0 < n ? lsep[slot_of(i0)] : -INFINITY;
+  const float l0 = i0 < n ? lsep[slots.slot(i0)] : -INFINITY;
   f32x4 v[U];
   auto load = [&](int i) {                                // partials i .. i + U - 1, those that exist
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       v[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (i + u < n) v[u] = *reinterpret_cast<const f32x4*>(op + (size_t)slot_of(i + u) * D);
+      if (i + u < n) v[u] = *reinterpret_cast<const f32x4*>(op + (size_t)slots.slot(i + u) * D);
     }
   };
   load(0);
   float mx = l0;
 #pragma unroll 1
-  for (int i = i0 + GW; i < n; i += GW) mx = fmaxf(mx, lsep[slot_of(i)]);
+  for (int i = i0 + GW; i < n; i += GW) mx = fmaxf(mx, lsep[slots.slot(i)]);
   mx = fmaxf(mx, dpp_f<kDppXor1>(mx));
   mx = fmaxf(mx, dpp_f<kDppXor2>(mx));
   mx = fmaxf(mx, dpp_f<kDppHalfMirror>(mx));
@@ -671,7 +661,7 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a) {
 #pragma unroll 1
   for (int b = 0; b < most; b += GW) {
     // (no guard on mx: logits that are all -inf give NaN)
-    const float wl = b == 0 ? l0 : b + i0 < n ? lsep[slot_of(b + i0)] : -INFINITY;
+    const float wl = b == 0 ? l0 : b + i0 < n ? lsep[slots.slot(b + i0)] : -INFINITY;
     const float wt = b + i0 < n ? fast_exp2(wl - mx) : 0.f;
     tot += wt;
     const int end = min(GW, most - b);

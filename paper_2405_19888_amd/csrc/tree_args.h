@@ -49,6 +49,36 @@ struct TreeArgs {
 // bits each, two ints), the row within its request, whether it has prefixes.
 constexpr int kTreeDesc = 8;
 
+// The partial results of a row: its prefix chunks, outermost level first (lo, hi: their
+// counts, as the descriptor holds them), then `own` pieces of its own tokens.  Index i is
+// slot slot(i) of the row's seg slots.  Counts are clamped so that any descriptor (that of a row
+// which no request holds was never written) stays inside them.
+struct TreeSlots {
+  int b1, b2, b3, b4, n, seg_p, seg_pre;
+  __host__ __device__ int slot(int i) const {
+    int sl = seg_pre + (i - b4);
+    sl = i < b4 ? 3 * seg_p + (i - b3) : sl;
+    sl = i < b3 ? 2 * seg_p + (i - b2) : sl;
+    sl = i < b2 ? seg_p + (i - b1) : sl;
+    return i < b1 ? i : sl;
+  }
+};
+__host__ __device__ inline TreeSlots tree_slots(unsigned lo, unsigned hi, int own, int seg_p, int seg_pre, int seg) {
+  auto least = [](int x, int y) { return x < y ? x : y; };
+  auto chunks = [&](unsigned count, int level) {               // (the row has slots for seg_pre / seg_p levels)
+    return least((int)count, least(seg_p, seg_pre - level * seg_p < 0 ? 0 : seg_pre - level * seg_p));
+  };
+  TreeSlots s;
+  s.b1 = chunks(lo & 0xFFFFu, 0);
+  s.b2 = s.b1 + chunks(lo >> 16, 1);
+  s.b3 = s.b2 + chunks(hi & 0xFFFFu, 2);
+  s.b4 = s.b3 + chunks(hi >> 16, 3);
+  s.n = s.b4 + least(own < 0 ? 0 : own, seg - seg_pre);
+  s.seg_p = seg_p;
+  s.seg_pre = seg_pre;
+  return s;
+}
+
 // Own tokens are streamed in units of kTreeUnit tokens; a column tile of a request costs
 // its units and kTreeSetup more.
 constexpr int kTreeSetup = 2;

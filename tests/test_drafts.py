@@ -156,6 +156,28 @@ def test_tree_path_by_size(parrot_lib):
     assert split(shared, many, 0) == split(shared, many, 1) == 1
 
 
+@pytest.mark.parametrize("levels", [0, 1, 2, 3, 4])
+def test_join_stays_inside_a_row(parrot_lib, levels):
+    """The join's slots: chunks of every level and pieces where they stand, and inside the
+    row's slots whatever a descriptor that nobody wrote holds."""
+    rng = np.random.default_rng(levels)
+    out = (ctypes.c_int * 4096)()
+    slots = lambda *a: out[:parrot_lib.parrot_test_tree_slots(*a, out, len(out))]
+    for _ in range(200):
+        chunks = int(rng.integers(1, 9)) if levels else 0
+        before, pieces = levels * chunks, int(rng.integers(1, 9))
+        seg = before + pieces
+        n = [int(x) for x in rng.integers(0, chunks + 1, levels)]
+        own = int(rng.integers(0, pieces + 1))
+        want = [l * chunks + c for l in range(levels) for c in range(n[l])] + [before + i for i in range(own)]
+        n += [0] * (4 - levels)
+        assert slots(n[0] | n[1] << 16, n[2] | n[3] << 16, own, chunks, before, seg) == want
+        for lo, hi, some in ((0xFFFFFFFF, 0xFFFFFFFF, 1 << 30), (0x00010001, 0x7FFF0003, -5),
+                             *[(int(a), int(b), int(c)) for a, b, c in rng.integers(0, 1 << 31, (5, 3))]):
+            got = slots(lo, hi, some, chunks, before, seg)
+            assert len(got) <= seg and all(0 <= x < seg for x in got), (lo, hi, some, chunks, before, seg)
+
+
 def tensors(dtype=torch.float16):
     """A tree and fill call's tensors for problem() with 20 rows of 8 query heads."""
     ints = lambda *n: torch.zeros(n, dtype=torch.int32)
