@@ -537,7 +537,10 @@ typedef struct {
 } parrot_tree_rows;
 
 /* Bytes of workspace parrot_shared_prefix_tree_decode needs (0 when T = 0); depends
- * on the current device's compute-unit count like parrot_workspace_bytes.
+ * on the current device's compute-unit count like parrot_workspace_bytes.  For the
+ * same heads, head_dim and dtype it never decreases as num_requests, num_groups,
+ * max_prefix_len, max_suffix_len, max_prefix_depth or the row counts grow, so a
+ * workspace for an engine's largest step serves every smaller one.
  * (size_t)-1 if the arguments are invalid. */
 size_t parrot_tree_workspace_bytes(const parrot_problem* p, const parrot_tree_rows* rows);
 

@@ -209,7 +209,11 @@ struct TreePlan {
   int cp, tiles_p, seg_p, seg_pre, seg, sets, own_wgs, runs, min_run;
   long n_pre;
   bool pre_first;                // prefix workgroups before the own tokens'
-  size_t o_bytes, lse_bytes, total_bytes;
+  int pieces, piece_cols;        // of a cache head's own tokens, columns of each
+  size_t own0, slots;            // first slot of the own tokens' partial results, slots in all
+  size_t o_bytes, lse_bytes;
+  size_t used_bytes;             // of workspace, by this call
+  size_t total_bytes;            // what no call of at most these sizes exceeds
 };
 
 // Overrides the estimate below for tests and tuning (per thread, set through
@@ -217,7 +221,37 @@ struct TreePlan {
 thread_local int g_tree_path = -1;
 
 constexpr int kTreeMinRun = 10;      // cost of a run at least: 8 units and a tile's setup
-constexpr int kTreeChunkMax = 2560, kTreeChunkMin = 256;
+constexpr int kTreeChunkMax = 2560, kTreeChunkMin = 256;   // prefix chunks are halved while above the second
+constexpr int kTreeChunkLeast = 160;
+constexpr double kTreeSplitLeast = 22;   // microseconds of a split call, at least
+
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// How own tokens are cut for requests of at most `cols` columns: by waves of `sets` column
+// sets, else (0) by tiles.
+struct OwnRole { int sets, wgs, runs, tiles, piece_cols; };
+OwnRole own_role(int dtype, long H, long cols, long cus) {
+  const bool f32 = dtype == PARROT_DTYPE_F32;
+  OwnRole o;
+  o.sets = cols <= 16 ? 1 : cols <= 32 && !f32 ? 2 : 0;
+  o.tiles = (int)ceil_div(cols, parrot::tree_cols(dtype));
+  const long per_wg = o.sets ? 4 : 1;
+  o.wgs = (int)std::max((o.sets ? 1 : o.tiles > 1 || f32 ? 3 : 2) * cus, ceil_div(H, per_wg));
+  o.runs = (int)(o.wgs * per_wg / H);
+  o.piece_cols = o.sets ? 16 * o.sets : parrot::tree_cols(dtype);
+  return o;
+}
+
+// Slots of the prefixes' partial results that no call of at most these sizes exceeds: a row
+// has one per level and chunk, and chunks are halved only while all of them are at most
+// `cap`, or what the longest chunks take.  Where all rows read prefixes the chunk rule stays
+// below `cap` by itself.
+double prefix_slot_bound(const parrot_problem* p, const parrot_tree_rows* rows, int levels, long cus) {
+  if (levels == 0 || rows->max_group_rows == 0) return 0;
+  const double each = (double)rows->num_query_rows * rows->num_query_heads * levels, cap = 4.0 * cus * parrot::tree_cols(p->dtype);
+  return std::min(each * ceil_div(p->max_prefix_len, kTreeChunkLeast),
+                  std::max(each * ceil_div(p->max_prefix_len, kTreeChunkMax), cap));
+}
 
 // The row counts of a tree call (or of accept and commit, which have no heads).
 parrot_status check_tree_counts(int32_t requests, const parrot_tree_rows* rows) {
@@ -241,13 +275,16 @@ parrot_status check_tree_counts(int32_t requests, const parrot_tree_rows* rows) 
 //  * split plan: by tiles 14 us (fp32 36) and 8 per piece of a workgroup, by waves 12 us and
 //    3 per piece of a wave but 22 at least, 8 for prefixes; the own tokens once per
 //    column tile at 6.0 TB/s (by waves 6.4) or their products (fp32: those of whole tiles),
-//    the prefixes' products, and the partial results, written and read, at 4.7 TB/s.
+//    the prefixes' products, and the partial results, written and read, at 4.7 TB/s;
+//    kTreeSplitLeast at least.
+// The first grows with every size, and the second has a least value: `never` is set where no
+// call of at most these sizes splits.
 // Measured, one launch and split, 16-bit heads of 128: a request of 64 rows on 300, 2000,
 // 8000 tokens and 32 heads 15 and 20, 47 and 24, 155 and 46 us; 32 requests of 64 rows,
 // four query heads on each of 8, on 300, 4000 tokens 29 and 72, 181 and 284; 32 requests of
 // 8 rows on one prefix of 300, 4000 tokens and 32 heads 33 and 31, 162 and 58; 128 requests
 // of 4 rows on 1000 tokens and 8 heads 103 and 95.
-bool tree_splits(const parrot_problem* p, const parrot_tree_rows* rows, const TreePlan& pl, long cus) {
+bool tree_splits(const parrot_problem* p, const parrot_tree_rows* rows, const TreePlan& pl, long cus, bool* never) {
   const double mean = 0.7, R = p->num_requests, H = p->num_heads, HQ = rows->num_query_heads, D = p->head_dim;
   const double T = rows->num_query_rows, eb = p->dtype == PARROT_DTYPE_F32 ? 4 : 2, kv = 2 * D * eb * H;
   const bool f32 = p->dtype == PARROT_DTYPE_F32;
@@ -270,13 +307,14 @@ bool tree_splits(const parrot_problem* p, const parrot_tree_rows* rows, const Tr
   double split;
   if (pl.sets) {
     const double waves = std::max((R * mean * own * kv + qo) / 6.4e6, flops_own / rate);
-    split = std::max(22.0, 12 + 3 * std::ceil(R * H / (4 * cus)) + waves + rest);
+    split = std::max(kTreeSplitLeast, 12 + 3 * std::ceil(R * H / (4 * cus)) + waves + rest);
   } else {
     const double cols = rows->max_query_rows * HQ / H, fill = f32 ? pl.tiles * parrot::tree_cols(p->dtype) / cols : 1;
     split = (f32 ? 36 : 14) + 8 * std::ceil(R * H * pl.tiles / pl.own_wgs) +
             std::max((pl.tiles * R * mean * own * kv + qo) / 6e6, flops_own * fill / rate) + rest;
   }
-  return split < one;
+  *never = one <= kTreeSplitLeast;
+  return std::max(split, kTreeSplitLeast) < one;
 }
 
 parrot_status check_tree(const parrot_problem* p, const parrot_tree_rows* rows, bool nested, TreePlan* pl) {
@@ -313,7 +351,10 @@ parrot_status check_tree(const parrot_problem* p, const parrot_tree_rows* rows, 
   pl->cp = kTreeChunkMax;
   if (pl->tiles_p > 0) {
     const long tiles = std::min(p->num_groups * (long)pl->tiles_p, ceil_div(T * pl->max_depth * G, cols) + p->num_groups);
-    while (pl->cp > kTreeChunkMin && tiles * H * ceil_div(p->max_prefix_len, pl->cp) < cus * 3 / 2) pl->cp /= 2;
+    const double each = (double)T * rows->num_query_heads * pl->max_depth, most = prefix_slot_bound(p, rows, pl->max_depth, cus);
+    while (pl->cp > kTreeChunkMin && tiles * H * ceil_div(p->max_prefix_len, pl->cp) < cus * 3 / 2 &&
+           each * ceil_div(p->max_prefix_len, pl->cp / 2) <= most)
+      pl->cp /= 2;
     const long chunks = std::max(1L, ceil_div(p->max_prefix_len, pl->cp));       // of equal length
     pl->cp = (int)(std::max(1L, ceil_div(p->max_prefix_len, chunks * 64)) * 64);
     pl->seg_p = (int)ceil_div(p->max_prefix_len, pl->cp);
@@ -331,11 +372,12 @@ parrot_status check_tree(const parrot_problem* p, const parrot_tree_rows* rows, 
   const long most_cols = rows->max_query_rows * G;
   // (fp32 caches with two column sets spill: 32 requests of 20 rows on 1000 tokens 440 us, by
   // tiles 294).
-  pl->sets = most_cols <= 16 ? 1 : most_cols <= 32 && p->dtype != PARROT_DTYPE_F32 ? 2 : 0;
+  const OwnRole own = own_role((int)p->dtype, H, most_cols, cus);
+  pl->sets = own.sets;
   pl->small = pl->sets == 1 && parrot::tree_small_rows(p->dtype, p->head_dim) && R * H <= cus;
-  const long per_wg = pl->sets ? 4 : 1;
-  pl->own_wgs = (int)std::max((pl->sets ? 1 : pl->tiles > 1 || p->dtype == PARROT_DTYPE_F32 ? 3 : 2) * cus, ceil_div(H, per_wg));
-  pl->runs = (int)(pl->own_wgs * per_wg / H);
+  pl->own_wgs = own.wgs;
+  pl->runs = own.runs;
+  pl->piece_cols = own.piece_cols;
   pl->min_run = kTreeMinRun;
   const long units = ceil_div(p->max_suffix_len, parrot::tree_unit(p->dtype, p->head_dim));
   // the longer items start first, so that the short ones fill up (48 rows each on six
@@ -343,15 +385,30 @@ parrot_status check_tree(const parrot_problem* p, const parrot_tree_rows* rows, 
   pl->pre_first = (double)R * pl->tiles * units / pl->runs < (double)pl->cp / parrot::tree_unit(p->dtype, p->head_dim);
   const long seg = pl->seg_pre + std::min(ceil_div(units, pl->min_run) + 1, (long)pl->runs);
   const double cost = (double)R * pl->tiles * (units + parrot::kTreeSetup);
-  if ((pl->own_wgs + pl->n_pre) * 256 > 0xffffffffL || ceil_div(R * H, 8) * 8 * pl->tiles * 512 > 0xffffffffL || cost > 1.5e9 || (double)T * rows->num_query_heads * seg * p->head_dim > 4e18)
+  // slots of the own tokens, by this call's columns and by fewer
+  const auto own_slots = [&](const OwnRole& o) { return (double)H * (o.runs + (double)R * o.tiles) * o.piece_cols; };
+  double own_most = own_slots(own);
+  for (const long c : {16L, 32L, cols})
+    if (c < most_cols) own_most = std::max(own_most, own_slots(own_role((int)p->dtype, H, c, cus)));
+  const double pre_slots = (double)T * rows->num_query_heads * pl->seg_pre, pre_most = prefix_slot_bound(p, rows, pl->max_depth, cus);
+  if ((pl->own_wgs + pl->n_pre) * 256 > 0xffffffffL || ceil_div(R * H, 8) * 8 * pl->tiles * 512 > 0xffffffffL || cost > 1.5e9 || (own_most + std::max(pre_slots, pre_most)) * p->head_dim > 1e18)
     return set_error(PARROT_ERR_UNSUPPORTED, "tree decode: %.3g units of own tokens", cost);
   pl->seg = (int)seg;
-  pl->split = g_tree_path >= 0 ? g_tree_path == 1 : tree_splits(p, rows, *pl, cus);
-  auto align256 = [](size_t x) { return (x + 255) & ~(size_t)255; };
-  const size_t slots = (size_t)T * rows->num_query_heads * seg;
-  pl->o_bytes = align256(slots * p->head_dim * sizeof(float));
-  pl->lse_bytes = align256(slots * sizeof(float));
-  pl->total_bytes = pl->split ? pl->o_bytes + pl->lse_bytes + align256((size_t)T * parrot::kTreeDesc * sizeof(int32_t)) : 256;
+  pl->pieces = (int)(pl->runs + R * pl->tiles);
+  pl->own0 = (size_t)pre_slots;
+  pl->slots = pl->own0 + (size_t)own_slots(own);
+  bool never = false;
+  pl->split = tree_splits(p, rows, *pl, cus, &never);
+  if (g_tree_path >= 0) { pl->split = g_tree_path == 1; never = !pl->split; }
+  const auto bytes = [&](size_t slots) {
+    return align256(slots * p->head_dim * sizeof(float)) + align256(slots * sizeof(float)) + align256((size_t)T * parrot::kTreeDesc * sizeof(int32_t));
+  };
+  pl->o_bytes = align256(pl->slots * p->head_dim * sizeof(float));
+  pl->lse_bytes = align256(pl->slots * sizeof(float));
+  pl->total_bytes = never ? 256 : bytes((size_t)own_most + (size_t)pre_most);
+  pl->used_bytes = pl->split ? bytes(pl->slots) : 0;
+  if (pl->used_bytes > pl->total_bytes)
+    return set_error(PARROT_ERR_UNSUPPORTED, "tree decode: the plan needs %zu bytes of %zu", pl->used_bytes, pl->total_bytes);
   return PARROT_OK;
 }
 
@@ -417,6 +474,7 @@ parrot_status parrot_shared_prefix_tree_decode(
   a.o_part = reinterpret_cast<float*>(workspace);
   a.lse_part = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + pl.o_bytes);
   a.desc = reinterpret_cast<int*>(reinterpret_cast<char*>(workspace) + pl.o_bytes + pl.lse_bytes);
+  a.own0 = pl.own0; a.pieces = pl.pieces; a.piece_cols = pl.piece_cols;
   const parrot_trace none = {nullptr, nullptr, nullptr, nullptr};
   const parrot_trace& tr = trace ? *trace : none;
   const int dt = (int)p->dtype, D = p->head_dim;
@@ -457,6 +515,11 @@ int parrot_test_tree_kernel(const parrot_problem* p, const parrot_tree_rows* row
   TreePlan pl;
   if (check_tree(p, rows, nested != 0, &pl) != PARROT_OK) return -1;
   return pl.split ? 2 + pl.sets : pl.small ? 1 : 0;
+}
+// Bytes of workspace that the plan of these arguments writes.
+size_t parrot_test_tree_used_bytes(const parrot_problem* p, const parrot_tree_rows* rows, int nested) {
+  TreePlan pl;
+  return check_tree(p, rows, nested != 0, &pl) == PARROT_OK ? pl.used_bytes : (size_t)-1;
 }
 // The slots that the join reads for a row's descriptor into out[0 .. most): how many.
 int parrot_test_tree_slots(uint32_t lo, uint32_t hi, int own, int seg_p, int seg_pre, int seg, int* out, int most) {

@@ -188,12 +188,17 @@ PARROT_DEV int scan256(int x, int* lds4, int* total) {
   return x + before;
 }
 
-// A tile's partial results: slot `slot` of the columns' rows.
+// The first slot of an own piece: its columns follow.
+PARROT_DEV size_t piece_slot(const TreeArgs& a, int h, int piece) {
+  return a.own0 + ((size_t)h * a.pieces + piece) * a.piece_cols;
+}
+
+// A tile's partial results, each column's at slot slot_of(col).
 template <int DT, int D, int NS, class F>
-PARROT_DEV void write_partial(const TreeArgs& a, TreeState<DT, D, NS>& tile, int ncols, int slot, F row_of) {
+PARROT_DEV void write_partial(const TreeArgs& a, TreeState<DT, D, NS>& tile, int ncols, F slot_of) {
   tile.finish([&](int c, int col, float lw, float lse2, float lt) {
     if (col >= ncols) return;
-    const size_t at = row_of(col) * (size_t)a.seg + slot;
+    const size_t at = slot_of(col);
     const float inv = lw == 0.f ? 0.f : 1.f / lw;           // a piece may hold no key the row sees
     float* dst = a.o_part + at * D + 4 * (tile.lane >> 4);
 #pragma unroll
@@ -203,11 +208,12 @@ PARROT_DEV void write_partial(const TreeArgs& a, TreeState<DT, D, NS>& tile, int
 }
 
 // One tile against one key range: columns col0 .. col0 + ncols of the sequence whose rows
-// from row0 on are in lds.rows; slot < 0: the columns' whole context, the output.
+// from row0 on are in lds.rows.  slot: the chunk's entry of each row (own: the piece's
+// number); < 0: the columns' whole context, the output.
 struct TreePiece { TreeRange rg; int h, col0, ncols, row0, slot; };
 
 template <int DT, int D, int NS>
-PARROT_DEV void tree_piece(const TreeArgs& a, tree_detail::Lds<DT>& lds, const TreePiece& pc) {
+PARROT_DEV void tree_piece(const TreeArgs& a, tree_detail::Lds<DT>& lds, const TreePiece& pc, bool own) {
   TreeTile<DT, D, NS> tile(lds, a.H, pc.h, a.scale_log2, pc.ncols);
   auto row_of = [&](int col) {                              // in units of heads
     const int x = pc.col0 + col, row = x / a.G;
@@ -216,7 +222,8 @@ PARROT_DEV void tree_piece(const TreeArgs& a, tree_detail::Lds<DT>& lds, const T
   tile.run(pc.rg, [&] { tile.template load_queries<false>(a.q, pc.ncols, row_of); });
   if (!tile.act) return;
   if (pc.slot < 0) write_output<DT, D, NS>(a, tile, pc.ncols, row_of);
-  else write_partial<DT, D, NS>(a, tile, pc.ncols, pc.slot, row_of);
+  else if (own) write_partial<DT, D, NS>(a, tile, pc.ncols, [&](int col) { return piece_slot(a, pc.h, pc.slot) + col; });
+  else write_partial<DT, D, NS>(a, tile, pc.ncols, [&](int col) { return row_of(col) * (size_t)a.seg_pre + pc.slot; });
 }
 
 // The run of an own-role wave (tiles: of all waves of its workgroup), and where it stands.
@@ -252,7 +259,7 @@ PARROT_DEV void write_desc(const TreeArgs& a, int r, const OwnCost& c, int start
   for (int j = 0; j < c.count; ++j) {
     int4* d = reinterpret_cast<int4*>(a.desc + (size_t)(c.first + j) * kTreeDesc);
     d[0] = int4{start + kTreeSetup, tile_cost(c.units, c.tiles, pad), c.units, q};
-    d[1] = int4{(int)lo, (int)hi, j, prefixed ? 1 : 0};
+    d[1] = int4{(int)lo, (int)hi, j, 2 * r + (prefixed ? 1 : 0)};
   }
 }
 
@@ -353,7 +360,7 @@ PARROT_DEV bool next_own(const TreeArgs& a, tree_detail::Lds<DT>& lds, int run, 
     pc->col0 = t * COLS;
     pc->ncols = min(COLS, rw.count * a.G - pc->col0);
     pc->row0 = pc->col0 / a.G;
-    pc->slot = !prefixed && st0 == 0 && st1 == units ? -1 : a.seg_pre + run - s0 / o->q;
+    pc->slot = !prefixed && st0 == 0 && st1 == units ? -1 : run + r * a.tiles + t;
     __syncthreads();                              // the last piece is done with the LDS
     if (threadIdx.x < COLS) lds.rows[threadIdx.x] = min(rw.first + pc->row0 + (int)threadIdx.x, a.T - 1);
     if (pc->rg.t1 > pc->rg.mask0) build_masks<DT, D>(a, lds, rw, base, pc->col0, pc->ncols);
@@ -462,7 +469,7 @@ PARROT_DEV void stream_role(const TreeArgs& a, char* lds, int wg) {
     if (rg.t1 > rg.mask0) st.build_masks(a.tree, rw, base, a.G);
     st.run(rg);
     if (!prefixed && st0 == 0 && st1 == units) write_output<DT, D, NS>(a, st, ncols, row_of);
-    else write_partial<DT, D, NS>(a, st, ncols, a.seg_pre + run - s0 / o.q, row_of);
+    else write_partial<DT, D, NS>(a, st, ncols, [&](int col) { return piece_slot(a, h, run + r) + col; });
   }
 }
 
@@ -494,9 +501,9 @@ void k_tree_partials(TreeArgs a) {
   }
   while (more) {                                          // one place for both roles' tiles
     if (tree_detail::kSets<DT> == 2 && (wave + 4) * 16 < pc.ncols)
-      tree_piece<DT, D, tree_detail::kSets<DT>>(a, lds, pc);
+      tree_piece<DT, D, tree_detail::kSets<DT>>(a, lds, pc, SETS == 0 && own);
     else
-      tree_piece<DT, D, 1>(a, lds, pc);
+      tree_piece<DT, D, 1>(a, lds, pc, SETS == 0 && own);
     more = SETS == 0 && own && next_own<DT, D>(a, lds, run, &o, &pc);
   }
 }
@@ -623,34 +630,43 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a) {
   const int* d = a.desc + (size_t)t * kTreeDesc;
   const int first = ld_uniform(d), between = ld_uniform(d + 1), units = ld_uniform(d + 2), q = max(1, ld_uniform(d + 3));
   const unsigned lo = (unsigned)ld_uniform(d + 4), hi = (unsigned)ld_uniform(d + 5);
-  const int j = ld_uniform(d + 6), prefixed = ld_uniform(d + 7);
+  const int j = ld_uniform(d + 6), of = ld_uniform(d + 7), prefixed = of & 1;
   if (t >= ld_uniform(a.qoff + a.R)) return;              // padding (its descriptor holds nothing)
-  const int s0 = first + (j * a.G + hq % a.G) / tree_detail::kCols<DT> * between;
+  const int x = j * a.G + hq % a.G, tile = x / tree_detail::kCols<DT>;
+  const int s0 = first + tile * between;
   const int pieces = (s0 + units - 1) / q - s0 / q + 1;
   const bool live = hq < HQ && !(prefixed == 0 && pieces == 1);   // one piece: it wrote the output
   const TreeSlots slots = tree_slots(lo, hi, pieces, a.seg_p, a.seg_pre, a.seg);
   const int n = live ? slots.n : 0;
   int most = n;
 #pragma unroll
-  for (int x = GW; x < kWave; x <<= 1) most = max(most, __shfl_xor(most, x));
+  for (int m = GW; m < kWave; m <<= 1) most = max(most, __shfl_xor(most, m));
   most = __builtin_amdgcn_readfirstlane(most);
   const size_t at = (size_t)t * HQ + min(hq, HQ - 1);
-  const float* lsep = a.lse_part + at * a.seg;
-  const float* op = a.o_part + at * a.seg * D + i0 * 4;
+  // the row's first own piece, and its column (clamped as the slots are)
+  const int piece = s0 / q + (of >> 1) * a.tiles + tile;
+  const int col = (int)min((unsigned)(x - tile * tree_detail::kCols<DT>), (unsigned)a.piece_cols - 1u);
+  auto place = [&](int i) {                               // slot of partial i
+    const int sl = slots.slot(i);
+    if (sl < a.seg_pre) return at * a.seg_pre + sl;
+    const unsigned pc = min((unsigned)(piece + (sl - a.seg_pre)), (unsigned)a.pieces - 1u);
+    return piece_slot(a, min(hq, HQ - 1) / a.G, (int)pc) + col;
+  };
+  const float* op = a.o_part + i0 * 4;
   // the lane's first log-sum-exp, and the first outputs beside it
-  const float l0 = i0 < n ? lsep[slots.slot(i0)] : -INFINITY;
+  const float l0 = i0 < n ? a.lse_part[place(i0)] : -INFINITY;
   f32x4 v[U];
   auto load = [&](int i) {                                // partials i .. i + U - 1, those that exist
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       v[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (i + u < n) v[u] = *reinterpret_cast<const f32x4*>(op + (size_t)slots.slot(i + u) * D);
+      if (i + u < n) v[u] = *reinterpret_cast<const f32x4*>(op + place(i + u) * D);
     }
   };
   load(0);
   float mx = l0;
 #pragma unroll 1
-  for (int i = i0 + GW; i < n; i += GW) mx = fmaxf(mx, lsep[slots.slot(i)]);
+  for (int i = i0 + GW; i < n; i += GW) mx = fmaxf(mx, a.lse_part[place(i)]);
   mx = fmaxf(mx, dpp_f<kDppXor1>(mx));
   mx = fmaxf(mx, dpp_f<kDppXor2>(mx));
   mx = fmaxf(mx, dpp_f<kDppHalfMirror>(mx));
@@ -661,7 +677,7 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a) {
 #pragma unroll 1
   for (int b = 0; b < most; b += GW) {
     // (no guard on mx: logits that are all -inf give NaN)
-    const float wl = b == 0 ? l0 : b + i0 < n ? lsep[slots.slot(b + i0)] : -INFINITY;
+    const float wl = b == 0 ? l0 : b + i0 < n ? a.lse_part[place(b + i0)] : -INFINITY;
     const float wt = b + i0 < n ? fast_exp2(wl - mx) : 0.f;
     tot += wt;
     const int end = min(GW, most - b);
@@ -738,14 +754,15 @@ hipError_t launch_tree(const TreeArgs& a, bool small, int dtype, int D, hipStrea
 hipError_t launch_tree_partials(const TreeArgs& a, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
   const long pre = a.n_pre > 0 ? ((long)a.NG * a.seg_p * a.H + 7) / 8 * 8 * a.tiles_p : 0;
   if (!tree_args_ok(a) || (a.sets == 2 && dtype == kF32) || a.runs < 1 || a.min_run < 1 || a.own_wgs < 1 ||
-      (long)a.own_wgs * (a.sets ? 4 : 1) < (long)a.runs * a.H || !a.o_part || !a.lse_part || !a.desc || a.n_pre != pre || (a.first != 0 && a.first != a.n_pre) ||
+      (long)a.own_wgs * (a.sets ? 4 : 1) < (long)a.runs * a.H || !a.o_part || !a.lse_part || !a.desc || a.n_pre != pre ||
+      a.pieces < a.runs + a.R * (long)a.tiles || a.piece_cols < (a.sets ? 16 * a.sets : tree_cols(dtype)) || a.own0 != (size_t)a.T * a.H * a.G * a.seg_pre || (a.first != 0 && a.first != a.n_pre) ||
       (a.n_pre > 0 && (a.cp < 64 || a.cp % 64 != 0 || a.depth < 1)) || ((long)a.own_wgs + a.n_pre) * 256 > 0xffffffffL)
     return hipErrorInvalidValue;
   PARROT_TREE_LAUNCH(launch_partials_t, 0);
 }
 
 hipError_t launch_tree_join(const TreeArgs& a, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
-  if (!tree_args_ok(a) || !a.desc || a.seg < 1) return hipErrorInvalidValue;
+  if (!tree_args_ok(a) || !a.o_part || !a.lse_part || !a.desc || a.seg < 1 || a.pieces < 1 || a.piece_cols < 1) return hipErrorInvalidValue;
   PARROT_TREE_LAUNCH(launch_join_t, 0);
 }
 

@@ -26,13 +26,18 @@ struct TreeArgs {
   int tiles;                             // column tiles per request
   float scale_log2;
 
-  // Split plan only.  Partial results o_part [T][HQ][seg][D] (normalised) and lse_part
-  // [T][HQ][seg] (base 2): slots [l * seg_p, (l + 1) * seg_p) hold the chunks of the
-  // prefix at level l of the request's chain (0: outermost), the rest the pieces of
-  // the own tokens.
+  // Split plan only.  Partial results: outputs o_part [slot][D] (normalised) and log-sum-exps
+  // lse_part [slot] (base 2).  The first [T][HQ][seg_pre] slots are the prefixes': entry
+  // l * seg_p + c is chunk c of the prefix at level l of the request's chain (0: outermost).
+  // From own0 on, [H][pieces][piece_cols] are the own tokens': tile t of request r, cut by run
+  // u, is piece u + r * tiles + t.  Along the cost each next piece takes the next run or the
+  // next tile, so no two share a number, and their bytes go with the runs and the tiles,
+  // not with the rows times the pieces a row may have.
   float* o_part; float* lse_part;
+  size_t own0;
+  int pieces, piece_cols;
   int* desc;                             // [T][kTreeDesc]: what the join needs of each row
-  int seg, seg_p, seg_pre;
+  int seg, seg_p, seg_pre;               // seg: partial results of a row, at most
   int cp;                                // prefix chunk tokens
   int tiles_p;                           // column tiles per group
   int sets;                              // 0: own tokens by tiles, else by waves of that many column sets
@@ -46,12 +51,13 @@ struct TreeArgs {
 
 // Row descriptor: cost of the first unit of the row's first column tile, cost between
 // tiles, units, run length, prefix chunks of the chain's levels (outermost first, 16
-// bits each, two ints), the row within its request, whether it has prefixes.
+// bits each, two ints), the row within its request, its request and (bit 0) whether that has
+// prefixes.
 constexpr int kTreeDesc = 8;
 
 // The partial results of a row: its prefix chunks, outermost level first (lo, hi: their
 // counts, as the descriptor holds them), then `own` pieces of its own tokens.  Index i is
-// slot slot(i) of the row's seg slots.  Counts are clamped so that any descriptor (that of a row
+// entry slot(i): below seg_pre of the row's prefix slots, from there on its pieces.  Counts are clamped so that any descriptor (that of a row
 // which no request holds was never written) stays inside them.
 struct TreeSlots {
   int b1, b2, b3, b4, n, seg_p, seg_pre;

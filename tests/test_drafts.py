@@ -156,6 +156,48 @@ def test_tree_path_by_size(parrot_lib):
     assert split(shared, many, 0) == split(shared, many, 1) == 1
 
 
+def drawn_sizes(rng):
+    """Sizes of a tree call: [requests, groups, prefix, own tokens, depth, rows, most, group rows]."""
+    log = lambda lo, hi: int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+    R, most, own = log(1, 300), log(1, 128), log(128, 40000)
+    T = int(rng.integers(1, R * most + 1))
+    return [R, int(rng.integers(0, 12)), log(1, 100000), own, int(rng.integers(0, 5)), T, most, int(rng.integers(0, T + 1))]
+
+
+def tree_sizes(sizes, heads, ratio, dim, dtype):
+    R, ng, pre, own, depth, T, most, group = sizes
+    prob = problem(num_requests=R, num_heads=heads, head_dim=dim, num_groups=ng, max_group_size=min(R, 1 if ng else 0),
+                   max_prefix_len=pre if ng else 0, max_suffix_len=own, prefix_table_stride=-(-pre // 16),
+                   suffix_table_stride=-(-own // 16), max_prefix_depth=depth, dtype=dtype)
+    return prob, parrot.make_tree_rows(T, most, group if ng else 0, heads * ratio)
+
+
+@pytest.mark.parametrize("heads,ratio", [(8, 4), (32, 1), (1, 8), (5, 3), (300, 1), (700, 1)])
+@pytest.mark.parametrize("dim,dtype", [(128, 1), (64, 2), (128, 0), (64, 0)])
+def test_tree_workspace_never_decreases(parrot_lib, heads, ratio, dim, dtype):
+    """One workspace for the largest call serves every smaller one, whichever plan each takes."""
+    used = parrot_lib.parrot_test_tree_used_bytes
+    used.restype = ctypes.c_size_t
+    rng = np.random.default_rng(heads * dim + dtype)
+    changes = 0
+    for _ in range(300):
+        big = drawn_sizes(rng)
+        prob, rows = tree_sizes(big, heads, ratio, dim, dtype)
+        most = parrot.parrot_tree_workspace_bytes(prob, rows)
+        for nested in (0, 1):
+            assert used(ctypes.byref(prob), ctypes.byref(rows), nested) <= most
+        for _ in range(8):
+            small = [x if rng.random() < 0.4 else int(rng.integers(min(x, i not in (1, 4, 7)), x + 1)) for i, x in enumerate(big)]
+            small[3], small[7] = max(small[3], small[6]), min(small[7], small[5])
+            if small[3] > big[3]:
+                continue
+            prob, rows = tree_sizes(small, heads, ratio, dim, dtype)
+            less = parrot.parrot_tree_workspace_bytes(prob, rows)
+            assert less <= most, (big, small)
+            changes += used(ctypes.byref(prob), ctypes.byref(rows), 0) > 0
+    assert changes > 100                          # many of them take the split plan
+
+
 @pytest.mark.parametrize("levels", [0, 1, 2, 3, 4])
 def test_join_stays_inside_a_row(parrot_lib, levels):
     """The join's slots: chunks of every level and pieces where they stand, and inside the

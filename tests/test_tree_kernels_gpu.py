@@ -148,3 +148,38 @@ def test_logits_that_are_no_finite_numbers(path, dtype, dim, columns):
     got, glse = got[:n].cpu(), glse[:n].cpu()
     assert torch.isnan(got[mine]).all() and torch.isnan(glse[mine]).all()
     assert torch.equal(got[~mine], clean[~mine]) and torch.equal(glse[~mine], clse[~mine])
+
+
+def test_one_workspace_serves_smaller_batches():
+    """A workspace sized for the largest batch, which takes one launch, holds the partial
+    results of a part of it, which does not."""
+    import paper_2405_19888_amd as parrot
+    rows, cached = [64] * 16, [936 - 7 * r for r in range(16)]
+    plan = du.tree_plan("float16", 2, 128, [-1] * 16, [], cached, rows)
+    batch = du.make_batch(plan)
+    up = du.random_trees(np.random.default_rng(1), rows)
+    q = du.queries(16 * 64, 16, 128, "float16")
+    _, _, big, dev = run(plan, batch, q, du.offsets_of(rows), up)
+    takes = parrot.load_library().parrot_test_tree_kernel
+    assert takes(ctypes.byref(big.problem), ctypes.byref(big.rows), 0) == 0
+    for n in (8, 3, 1):
+        prob = problem_for(plan)
+        prob.num_requests = n
+        counts = parrot.make_tree_rows(64 * n, 64, 0, 16)
+        assert takes(ctypes.byref(prob), ctypes.byref(counts), 0) == 2
+        small = parrot.TreeDecoder(prob, counts)
+        assert small.workspace.numel() <= big.workspace.numel()
+        want, wlse = small(dev)
+        big.workspace.fill_(0xFF)
+        big.out.fill_(7.0)
+        parrot.parrot_shared_prefix_tree_decode(
+            prob, counts, dev["q_rows"], dev["query_offsets"], dev["tree_parents"], None, None, dev["k_pool"], dev["v_pool"],
+            None, None, None, dev["suffix_tables"], dev["suffix_lens"], dev["group_ids"], big.out, big.lse, big.workspace)
+        torch.cuda.synchronize()
+        assert torch.equal(big.out[:64 * n], want) and torch.equal(big.lse[:64 * n], wlse)
+        assert (big.out[64 * n:] == 7.0).all()
+        part = [x[:64 * n] for x in (q, up)]
+        few = du.tree_plan("float16", 2, 128, [-1] * n, [], cached[:n], rows[:n])
+        few.suffix_tables, few.suffix_lens = plan.suffix_tables[:n], plan.suffix_lens[:n]
+        if n == 1:
+            check(few, batch, part[0], du.offsets_of(rows[:n]), part[1], want, wlse, what="one of sixteen")
