@@ -105,8 +105,7 @@ def _bound(fn, values, device: torch.device, stream):
 
 def _need(t, name: str, dtype: torch.dtype, least: int, device: torch.device):
     """Refuses a tensor that the kernels would read or write beyond its end (addresses
-    and None go to the library's own checks; parents are read for real rows alone, whose
-    number only the device knows)."""
+    and None go to the library's own checks)."""
     if not isinstance(t, torch.Tensor):
         return
     if t.dtype != dtype or not t.is_contiguous() or t.numel() < least:
@@ -131,6 +130,16 @@ def _need_rows(x, name: str, rows: int, heads: int, p: ParrotProblem, device: to
         raise ValueError(f"{name} is not [{rows}, {heads}, {p.head_dim}] of {_TORCH_DTYPES[p.dtype]}")
     if x.device != device:
         raise ValueError(f"{name} is on {x.device}, not on {device}")
+
+
+def _within_parents(rows: ParrotTreeRows, tree_parents) -> ParrotTreeRows:
+    """The row counts of a call whose parents may stop where its padding begins: only the
+    device knows where that is, so rows behind the tensor's end are taken as padding, and
+    nothing is read there whatever the offsets say."""
+    if not isinstance(tree_parents, torch.Tensor) or tree_parents.numel() >= rows.num_query_rows:
+        return rows
+    n = tree_parents.numel()
+    return make_tree_rows(n, rows.max_query_rows, min(rows.max_group_rows, n), rows.num_query_heads)
 
 
 def _row_stride(x: torch.Tensor, name: str) -> int:
@@ -178,6 +187,7 @@ def _tree_call(problem, rows, q, query_offsets, tree_parents, prefix_k, prefix_v
             (query_offsets, "query_offsets", ints, p.num_requests + 1), (tree_parents, "tree_parents", ints, 0),
             (group_ids, "group_ids", ints, p.num_requests)):
         _need(x, name, dtype, least, q.device)
+    rows = _within_parents(rows, tree_parents)
     if p.num_groups > 0:
         for x, name, dtype, least in (
                 (prefix_k, "prefix_k", dt, pre), (prefix_v, "prefix_v", dt, pre), (prefix_lens, "prefix_lens", ints, p.num_groups),
@@ -195,7 +205,7 @@ def parrot_shared_prefix_tree_decode(problem, rows, q, query_offsets, tree_paren
                                      suffix_v, prefix_block_tables, prefix_lens, prefix_parents, suffix_block_tables,
                                      suffix_lens, group_ids, out, lse, workspace, stream=None, trace=None):
     """Attention of drafted trees (see the C header); tree_parents None: chains,
-    prefix_parents None: flat groups."""
+    prefix_parents None: flat groups.  Rows behind the end of tree_parents are padding."""
     _tree_call(problem, rows, q, query_offsets, tree_parents, prefix_k, prefix_v, suffix_k, suffix_v,
                prefix_block_tables, prefix_lens, prefix_parents, suffix_block_tables, suffix_lens, group_ids, out,
                lse, workspace, stream)(trace)
@@ -204,6 +214,7 @@ def parrot_shared_prefix_tree_decode(problem, rows, q, query_offsets, tree_paren
 def parrot_validate_tree_inputs(problem, rows, query_offsets, tree_parents, prefix_block_tables, prefix_lens,
                                 prefix_parents, suffix_block_tables, suffix_lens, group_ids, scratch, stream=None):
     """Device-side content check of a tree call's inputs (synchronises)."""
+    rows = _within_parents(rows, tree_parents)
     with torch.cuda.device(_device(suffix_lens)):
         _check(load_library().parrot_validate_tree_inputs(
             ctypes.byref(problem), ctypes.byref(rows), _ptr(query_offsets), _ptr(tree_parents),
@@ -220,6 +231,7 @@ def _accept_call(num_requests, rows, query_offsets, tree_parents, draft_tokens, 
                            (root_tokens, "root_tokens", R), (accept_rows, "accept_rows", T),
                            (accept_lens, "accept_lens", R), (next_tokens, "next_tokens", R)):
         _need(x, name, torch.int32, least, query_offsets.device)
+    rows = _within_parents(rows, tree_parents)
     return _bound(fn, (int(num_requests), ctypes.byref(rows), query_offsets, tree_parents, draft_tokens,
                        target_tokens, root_tokens, accept_rows, accept_lens, next_tokens), _device(query_offsets),
                   stream)

@@ -250,6 +250,25 @@ def test_tensors_that_do_not_fit(parrot_lib, name):
             parrot.parrot_shared_prefix_tree_decode(problem(), rows, **{**tensors(), name: bad})
 
 
+def test_parents_shorter_than_the_rows(parrot_lib, monkeypatch):
+    """The library is told of no row whose parent the tensor does not hold."""
+    from paper_2405_19888_amd import drafts
+    told = []
+    monkeypatch.setattr(drafts, "_bound", lambda fn, values, *_: lambda *_: told.append(values[1]._obj))
+    monkeypatch.setattr(drafts, "_device", lambda t: t.device)
+    counts = parrot.make_tree_rows(20, 10, 18, 8)
+    t, ints = tensors(), [torch.zeros(n, dtype=torch.int32) for n in (20, 20, 8, 20, 8, 8)]
+    for n in (25, 20, 19, 12, 0):
+        parents = torch.full((n,), -1, dtype=torch.int32)
+        parrot.parrot_shared_prefix_tree_decode(problem(), counts, **{**t, "tree_parents": parents})
+        parrot.parrot_tree_accept(8, counts, t["query_offsets"], parents, *ints)
+        for rows in told[-2:]:
+            assert (rows.num_query_rows, rows.max_query_rows, rows.num_query_heads) == (min(n, 20), 10, 8)
+            assert rows.max_group_rows == min(n, 18)
+    parrot.parrot_shared_prefix_tree_decode(problem(), counts, **{**t, "tree_parents": None})
+    assert told[-1].num_query_rows == 20 and counts.num_query_rows == 20 and counts.max_group_rows == 18
+
+
 def test_fill_tensors_that_do_not_fit(parrot_lib):
     t = tensors()
     kv = torch.zeros((20, 4, 128), dtype=torch.float16)

@@ -183,3 +183,26 @@ def test_one_workspace_serves_smaller_batches():
         few.suffix_tables, few.suffix_lens = plan.suffix_tables[:n], plan.suffix_lens[:n]
         if n == 1:
             check(few, batch, part[0], du.offsets_of(rows[:n]), part[1], want, wlse, what="one of sixteen")
+
+
+def test_parents_that_stop_early(path):
+    """Rows behind the end of the parents tensor are padding: left as they were, by tree
+    decode and accept; requests before them are not touched by that."""
+    import paper_2405_19888_amd as parrot
+    plan, batch, off, up, q, rows, _ = batch_of("float16", 128, "32", seed=2)
+    out, lse, dec, dev = run(plan, batch, q, off, up)
+    want, n = out.clone(), int(off[2])
+    held = dev["tree_parents"][:n].clone()
+    dec.out.fill_(7.0)
+    dec.bind({**dev, "tree_parents": held}, nested=True)()
+    torch.cuda.synchronize()
+    # (fewer rows may be cut otherwise: each result within the rounding of its weights)
+    assert (dec.out[:n].double() - want[:n].double()).abs().max() <= 4 * du.UNIT["float16"] * 5
+    assert (dec.out[n:] == 7.0).all()
+    tokens = [torch.arange(off[-1], dtype=torch.int32).cuda() for _ in range(2)]
+    ver = parrot.TreeVerifier(dec.problem, parrot.make_tree_rows(int(off[-1]), 16, 0, 4))
+    ver.accept_rows.fill_(-77)
+    ver.bind_accept({**dev, "tree_parents": held, "draft_tokens": tokens[0], "target_tokens": tokens[1],
+                     "root_tokens": torch.zeros(3, dtype=torch.int32).cuda()})()
+    torch.cuda.synchronize()
+    assert (ver.accept_rows[n:] == -77).all() and (ver.accept_rows[:n] >= -1).all() and ver.accept_lens[2] == 0
