@@ -122,6 +122,19 @@ def _need_cache(p: ParrotProblem, device: torch.device, suffix_k, suffix_v, suff
     _need(suffix_lens, "suffix_lens", torch.int32, p.num_requests, device)
 
 
+def _need_tree(p: ParrotProblem, device: torch.device, query_offsets, tree_parents, prefix_tables, prefix_lens,
+               prefix_parents, suffix_tables, suffix_lens, group_ids):
+    """The int arrays of a tree call."""
+    arrays = [(query_offsets, "query_offsets", p.num_requests + 1), (tree_parents, "tree_parents", 0),
+              (group_ids, "group_ids", p.num_requests), (suffix_lens, "suffix_lens", p.num_requests),
+              (suffix_tables, "suffix_tables", p.num_requests * p.suffix_table_stride)]
+    if p.num_groups > 0:
+        arrays += [(prefix_lens, "prefix_lens", p.num_groups), (prefix_parents, "prefix_parents", p.num_groups),
+                   (prefix_tables, "prefix_tables", p.num_groups * p.prefix_table_stride)]
+    for x, name, least in arrays:
+        _need(x, name, torch.int32, least, device)
+
+
 def _need_rows(x, name: str, rows: int, heads: int, p: ParrotProblem, device: torch.device):
     """Rows [rows, heads, D] of any row stride."""
     if not isinstance(x, torch.Tensor):
@@ -180,20 +193,18 @@ def parrot_rotary_fill(problem, num_query_rows, max_query_rows, num_query_heads,
 def _tree_call(problem, rows, q, query_offsets, tree_parents, prefix_k, prefix_v, suffix_k, suffix_v, prefix_tables,
                prefix_lens, prefix_parents, suffix_tables, suffix_lens, group_ids, out, lse, workspace, stream):
     fn = load_library().parrot_shared_prefix_tree_decode
-    p, T, HQ, dt, ints = problem, rows.num_query_rows, rows.num_query_heads, _TORCH_DTYPES[problem.dtype], torch.int32
-    pre = p.num_prefix_blocks * p.num_heads * p.block_size * p.head_dim if p.num_groups > 0 else 0
-    for x, name, dtype, least in (
-            (q, "q", dt, T * HQ * p.head_dim), (out, "out", dt, T * HQ * p.head_dim), (lse, "lse", torch.float32, T * HQ),
-            (query_offsets, "query_offsets", ints, p.num_requests + 1), (tree_parents, "tree_parents", ints, 0),
-            (group_ids, "group_ids", ints, p.num_requests)):
+    p, T, HQ, dt = problem, rows.num_query_rows, rows.num_query_heads, _TORCH_DTYPES[problem.dtype]
+    for x, name, dtype, least in ((q, "q", dt, T * HQ * p.head_dim), (out, "out", dt, T * HQ * p.head_dim),
+                                  (lse, "lse", torch.float32, T * HQ)):
         _need(x, name, dtype, least, q.device)
-    rows = _within_parents(rows, tree_parents)
+    _need_tree(p, q.device, query_offsets, tree_parents, prefix_tables, prefix_lens, prefix_parents, suffix_tables,
+               suffix_lens, group_ids)
     if p.num_groups > 0:
-        for x, name, dtype, least in (
-                (prefix_k, "prefix_k", dt, pre), (prefix_v, "prefix_v", dt, pre), (prefix_lens, "prefix_lens", ints, p.num_groups),
-                (prefix_tables, "prefix_tables", ints, p.num_groups * p.prefix_table_stride),
-                (prefix_parents, "prefix_parents", ints, p.num_groups)):
-            _need(x, name, dtype, least, q.device)
+        for x, name in ((prefix_k, "prefix_k"), (prefix_v, "prefix_v")):
+            _need(x, name, dt, p.num_prefix_blocks * p.num_heads * p.block_size * p.head_dim, q.device)
+    if isinstance(workspace, torch.Tensor):          # (its size is the library's to check)
+        _need(workspace, "workspace", workspace.dtype, 0, q.device)
+    rows = _within_parents(rows, tree_parents)
     _need_cache(p, q.device, suffix_k, suffix_v, suffix_tables, suffix_lens)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     return _bound(fn, (ctypes.byref(problem), ctypes.byref(rows), q, query_offsets, tree_parents, prefix_k, prefix_v,
@@ -214,6 +225,9 @@ def parrot_shared_prefix_tree_decode(problem, rows, q, query_offsets, tree_paren
 def parrot_validate_tree_inputs(problem, rows, query_offsets, tree_parents, prefix_block_tables, prefix_lens,
                                 prefix_parents, suffix_block_tables, suffix_lens, group_ids, scratch, stream=None):
     """Device-side content check of a tree call's inputs (synchronises)."""
+    _need_tree(problem, suffix_lens.device, query_offsets, tree_parents, prefix_block_tables, prefix_lens,
+               prefix_parents, suffix_block_tables, suffix_lens, group_ids)
+    _need(scratch, "scratch", torch.int32, 16, suffix_lens.device)
     rows = _within_parents(rows, tree_parents)
     with torch.cuda.device(_device(suffix_lens)):
         _check(load_library().parrot_validate_tree_inputs(

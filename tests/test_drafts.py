@@ -250,6 +250,30 @@ def test_tensors_that_do_not_fit(parrot_lib, name):
             parrot.parrot_shared_prefix_tree_decode(problem(), rows, **{**tensors(), name: bad})
 
 
+def test_workspace_and_checked_tensors_that_do_not_fit(parrot_lib):
+    """A workspace with gaps or on another device, and every array and the scratch of the
+    content check, are refused by name."""
+    rows = parrot.make_tree_rows(20, 10, 20, 8)
+    for bad in (torch.zeros(1, dtype=torch.uint8).expand(1 << 20), torch.zeros(512, dtype=torch.uint8)[::2],
+                torch.zeros((16, 32)).t()):
+        with pytest.raises(ValueError, match="workspace is not a contiguous"):
+            parrot.parrot_shared_prefix_tree_decode(problem(), rows, **{**tensors(), "workspace": bad})
+    with pytest.raises(ValueError, match="workspace is on meta"):
+        parrot.parrot_shared_prefix_tree_decode(
+            problem(), rows, **{**tensors(), "workspace": torch.zeros(512, dtype=torch.uint8, device="meta")})
+    names = ["query_offsets", "tree_parents", "prefix_block_tables", "prefix_lens", "prefix_parents",
+             "suffix_block_tables", "suffix_lens", "group_ids"]
+    good = {n: tensors()[n] for n in names}
+    good.update(prefix_parents=torch.zeros(2, dtype=torch.int32), scratch=torch.zeros(16, dtype=torch.int32))
+    with pytest.raises(ValueError, match="on the GPU"):
+        parrot.parrot_validate_tree_inputs(problem(), rows, **good)
+    for name, x in good.items():
+        bads = [x.long(), torch.cat([x, x])[::2]] + ([x[:-1].clone()] if name != "tree_parents" else [])
+        for bad in bads:
+            with pytest.raises(ValueError, match=name.replace("_block", "") + " is not a contiguous"):
+                parrot.parrot_validate_tree_inputs(problem(), rows, **{**good, name: bad})
+
+
 def test_parents_shorter_than_the_rows(parrot_lib, monkeypatch):
     """The library is told of no row whose parent the tensor does not hold."""
     from paper_2405_19888_amd import drafts
