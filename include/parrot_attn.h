@@ -404,8 +404,9 @@ parrot_status parrot_validate_prefill_inputs(
  *   a' = amplitude * (a cos - b sin),  b' = amplitude * (b cos + a sin).
  * parrot_rotary_init (or parrot_rotary_from_frequencies) fills the struct; it is
  * plain host data, may be copied, and holds no pointer.  Angles are kept as 64-bit
- * binary fractions of a turn, so n * f_i is exact modulo a turn to 2^-32 at any
- * int32 position (negative ones turn backwards).
+ * binary fractions of a turn, right to 1.5 * 2^-64, and n * f_i modulo a turn is cut to
+ * 2^-32, so an angle is right to 2^-31 turns at any int32 position (negative ones
+ * turn backwards).
  */
 #define PARROT_ROTARY_MAX_PAIRS 64
 typedef struct {

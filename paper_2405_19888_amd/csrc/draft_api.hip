@@ -28,13 +28,33 @@ parrot_status launched(hipError_t e, const char* what) {
 static_assert(PARROT_ROTARY_MAX_PAIRS == parrot::kRotaryPairs && PARROT_MAX_TREE_ROWS == parrot::kTreeRows,
               "header and kernels agree");
 
-constexpr double kTwoPi = 6.283185307179586476925286766559;
+constexpr long double kTwoPi = 6.283185307179586476925286766559005768L;
 
 parrot_status check_rotary(int32_t rotary_dim, int32_t interleaved) {
   if (rotary_dim < 2 || rotary_dim > 2 * PARROT_ROTARY_MAX_PAIRS || rotary_dim % 2 != 0)
     return bad("rotary_dim %ld is not even and in [2, %ld]", rotary_dim, 2 * PARROT_ROTARY_MAX_PAIRS);
   if (interleaved != 0 && interleaved != 1) return bad("interleaved %ld is not 0 or 1", interleaved);
   return PARROT_OK;
+}
+
+// Frequencies are computed with the 64 bits that x86-64's long double has: what a fraction of a turn is off
+// by comes n times at position n, and those of a double (2^-53 of it) are off by 2^-25 turns at
+// the last position.
+parrot_status store_rotary(parrot_rotary* rotary, int32_t rotary_dim, int32_t interleaved,
+                           const long double* radians, double amplitude) {
+  if (!(amplitude > 0) || !std::isfinite((float)amplitude)) return bad("amplitude is not positive and finite");
+  parrot_rotary out{};
+  out.rotary_dim = rotary_dim;
+  out.interleaved = interleaved;
+  out.amplitude = (float)amplitude;
+  for (int i = 0; i < rotary_dim / 2; ++i) {
+    const long double turns = radians[i] / kTwoPi;
+    if (!(turns >= 0.0L && turns < 1.0L)) return bad("frequency %ld is not in [0, 2 pi)", i);
+    // the nearest multiple of 2^-64 (it fits: turns < 1 is at most 1 - 2^-64)
+    out.turns[i] = (uint64_t)std::round(std::ldexp(turns, 64));
+  }
+  *rotary = out;
+  return set_error(PARROT_OK, "");
 }
 
 }  // namespace
@@ -47,19 +67,9 @@ parrot_status parrot_rotary_from_frequencies(parrot_rotary* rotary, int32_t rota
                                              double amplitude) {
   if (!rotary || !radians) return bad(rotary ? "radians is NULL" : "rotary is NULL");
   PARROT_TRY(check_rotary(rotary_dim, interleaved));
-  if (!(amplitude > 0) || !std::isfinite((float)amplitude)) return bad("amplitude is not positive and finite");
-  parrot_rotary out{};
-  out.rotary_dim = rotary_dim;
-  out.interleaved = interleaved;
-  out.amplitude = (float)amplitude;
-  for (int i = 0; i < rotary_dim / 2; ++i) {
-    const double turns = radians[i] / kTwoPi;
-    if (!(turns >= 0.0 && turns < 1.0)) return bad("frequency %ld is not in [0, 2 pi)", i);
-    // the nearest multiple of 2^-64; turns < 1 is at most 1 - 2^-53, so this fits
-    out.turns[i] = (uint64_t)std::ldexp(turns, 64);
-  }
-  *rotary = out;
-  return set_error(PARROT_OK, "");
+  long double wide[PARROT_ROTARY_MAX_PAIRS];
+  std::copy(radians, radians + rotary_dim / 2, wide);
+  return store_rotary(rotary, rotary_dim, interleaved, wide, amplitude);
 }
 
 parrot_status parrot_rotary_init(parrot_rotary* rotary, const parrot_rotary_config* c) {
@@ -80,28 +90,31 @@ parrot_status parrot_rotary_init(parrot_rotary* rotary, const parrot_rotary_conf
   }
   if (c->scaling == PARROT_ROTARY_SCALE_NTK && c->rotary_dim < 4) return bad("NTK scaling needs rotary_dim >= 4");
   if (!(c->amplitude >= 0.0)) return bad("amplitude is negative");
-  const double rd = c->rotary_dim;
-  const double base = c->scaling == PARROT_ROTARY_SCALE_NTK ? c->base * std::pow(s, rd / (rd - 2.0)) : c->base;
+  const long double rd = c->rotary_dim;
+  const long double base = c->scaling == PARROT_ROTARY_SCALE_NTK ? c->base * std::pow((long double)s, rd / (rd - 2)) : c->base;
   // YaRN: the pairs that turn `high` and `low` times in the trained length, rounded
   // outwards, bound the blend
   double first = 0.0, last = 0.0;
   if (yarn) {
-    auto pair_of = [&](double turns) { return rd * std::log(c->original_length / (turns * kTwoPi)) / (2.0 * std::log(c->base)); };
+    auto pair_of = [&](double turns) {
+      return c->rotary_dim * std::log(c->original_length / (turns * (double)kTwoPi)) / (2.0 * std::log(c->base));
+    };
     first = std::max(std::floor(pair_of(high)), 0.0);
-    last = std::min(std::ceil(pair_of(low)), rd - 1.0);
+    last = std::min(std::ceil(pair_of(low)), c->rotary_dim - 1.0);
   }
-  double radians[PARROT_ROTARY_MAX_PAIRS];
+  const auto share = [](long double x) { return std::min(1.0L, std::max(0.0L, x)); };
+  long double radians[PARROT_ROTARY_MAX_PAIRS];
   for (int i = 0; i < c->rotary_dim / 2; ++i) {
-    const double f = std::pow(base, -2.0 * i / rd);
-    double keep = 1.0;                                      // share of the unscaled frequency
-    if (c->scaling == PARROT_ROTARY_SCALE_LINEAR) keep = 0.0;
-    if (yarn) keep = 1.0 - std::min(1.0, std::max(0.0, (i - first) / std::max(last - first, 1e-3)));
+    const long double f = std::pow(base, -2 * i / rd);
+    long double keep = 1;                                    // share of the unscaled frequency
+    if (c->scaling == PARROT_ROTARY_SCALE_LINEAR) keep = 0;
+    if (yarn) keep = 1 - share((i - first) / std::max((long double)(last - first), 1e-3L));
     if (c->scaling == PARROT_ROTARY_SCALE_WAVELENGTH)
-      keep = std::min(1.0, std::max(0.0, (c->original_length * f / kTwoPi - low) / (high - low)));
-    radians[i] = c->scaling == PARROT_ROTARY_SCALE_NTK ? f : f * keep + f / s * (1.0 - keep);
+      keep = share((c->original_length * f / kTwoPi - low) / (high - low));
+    radians[i] = c->scaling == PARROT_ROTARY_SCALE_NTK ? f : f * keep + f / s * (1 - keep);
   }
   const double amplitude = c->amplitude > 0.0 ? c->amplitude : yarn ? 0.1 * std::log(s) + 1.0 : 1.0;
-  return parrot_rotary_from_frequencies(rotary, c->rotary_dim, c->interleaved, radians, amplitude);
+  return store_rotary(rotary, c->rotary_dim, c->interleaved, radians, amplitude);
 }
 
 }  // extern "C"

@@ -341,6 +341,26 @@ def test_rotary_frequencies(parrot_lib, scaling, kw, rd, base):
     assert all(abs(same.turns[i] - rot.turns[i]) <= 16 * 2.0 ** -53 * rot.turns[i] + 1 for i in range(rd // 2))
 
 
+@pytest.mark.parametrize("rd,base", [(128, 10000.0), (64, 500000.0), (20, 7.5)])
+@pytest.mark.parametrize("scaling,factor", [("none", 1.0), ("linear", 4.0), ("ntk", 8.0)])
+def test_rotary_turns_hold_at_far_positions(parrot_lib, rd, base, scaling, factor):
+    """The stored fraction of a turn is the exact one's to 1.5 * 2^-64, so 2^31 positions keep
+    the angle to 2^-32 turns (and its lower 32 bits, cut off, are another 2^-32)."""
+    from decimal import Decimal, getcontext
+    getcontext().prec = 60
+    pi = Decimal("3.14159265358979323846264338327950288419716939937510582097494")
+    exact = Decimal(base)
+    if scaling == "ntk":
+        exact *= Decimal(factor) ** (Decimal(rd) / (rd - 2))
+    rot = parrot.make_rotary(rd, base=base, scaling=scaling, factor=factor)
+    for i in range(rd // 2):
+        f = exact ** (Decimal(-2 * i) / rd) / (Decimal(factor) if scaling == "linear" else 1)
+        assert abs(Decimal(rot.turns[i]) - f / (2 * pi) * 2 ** 64) <= Decimal("1.5"), i
+    for f in (0.0, 1.0, 0.1, 6.283185307179586, 2.0 ** -60):
+        turns = parrot.rotary_from_frequencies([f]).turns[0]
+        assert abs(Decimal(turns) - Decimal(f) / (2 * pi) * 2 ** 64) <= Decimal("1.5"), f
+
+
 @pytest.mark.parametrize("kw", [
     dict(rotary_dim=0), dict(rotary_dim=7), dict(rotary_dim=130), dict(base=1.0), dict(base=float("nan")),
     dict(scaling="linear", factor=0.5), dict(scaling="yarn", factor=4.0), dict(scaling="ntk", rotary_dim=2, factor=2.0),
