@@ -42,7 +42,7 @@ parrot_status check_rotary(int32_t rotary_dim, int32_t interleaved) {
 // the last position.
 parrot_status store_rotary(parrot_rotary* rotary, int32_t rotary_dim, int32_t interleaved,
                            const long double* radians, double amplitude) {
-  if (!(amplitude > 0) || !std::isfinite((float)amplitude)) return bad("amplitude is not positive and finite");
+  if (!((float)amplitude > 0.f) || !std::isfinite((float)amplitude)) return bad("amplitude is not positive and finite in fp32");
   parrot_rotary out{};
   out.rotary_dim = rotary_dim;
   out.interleaved = interleaved;

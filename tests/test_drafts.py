@@ -371,6 +371,16 @@ def test_rotary_refusals(parrot_lib, kw):
         parrot.make_rotary(**{"rotary_dim": 64, **kw})
 
 
+def test_amplitude_that_is_no_positive_float(parrot_lib):
+    """An amplitude below the least float would scale every rotated pair by zero."""
+    for bad in (1e-50, 5e-324):
+        with pytest.raises(B.ParrotError, match="amplitude"):
+            parrot.make_rotary(64, amplitude=bad)
+        with pytest.raises(B.ParrotError, match="amplitude"):
+            parrot.rotary_from_frequencies([0.1], amplitude=bad)
+    assert parrot.make_rotary(64, amplitude=2.0 ** -149).amplitude == 2.0 ** -149
+
+
 def test_rotary_from_frequencies_refusals(parrot_lib):
     for bad in ([-0.1], [7.0], [float("nan")], [0.1] * 65, []):
         with pytest.raises(B.ParrotError):
