@@ -7,6 +7,7 @@ library is missing or a call fails, an exception says so.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Optional
@@ -247,6 +248,20 @@ def _stream_handle(stream) -> Optional[int]:
     if stream is None:
         stream = torch.cuda.current_stream()
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _on_stream(stream, device: torch.device):
+    """Makes ``stream`` (a torch stream, another object with a handle, or a handle; None: the
+    current one) current for the body of a one-call form: its copies of lengths wait for what
+    the stream holds, and what it allocates belongs to the stream."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = _stream_handle(stream)
+        stream = torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)
+    if stream.device != device:
+        raise ValueError(f"stream is on {stream.device}, not on {device}")
+    return torch.cuda.stream(stream)
 
 
 def _decode(fn_name, problem, q, prefix_k, prefix_v, suffix_k, suffix_v, prefix_block_tables,

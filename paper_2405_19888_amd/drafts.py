@@ -20,7 +20,7 @@ from typing import Optional
 import torch
 
 from .binding import (DTYPE_CODES, PARROT_ERR_INVALID_ARGUMENT, ParrotError, ParrotFillRows, ParrotProblem,
-                      ParrotRotary, ParrotRotaryConfig, ParrotTrace, ParrotTreeRows, _check, _ptr,
+                      ParrotRotary, ParrotRotaryConfig, ParrotTrace, ParrotTreeRows, _check, _on_stream, _ptr,
                       _sizes_from_tensors, load_library, make_problem, parrot_last_error)
 
 _SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3, "wavelength": 4}
@@ -364,6 +364,8 @@ class TreeVerifier:
 
 
 # ------------------------------------------------------------- one-call forms
+# With ``stream``, the host copies of lengths, the results' memory and the call itself are that
+# stream's: inputs may come from work that it holds, and a result may be dropped at once.
 def _cache_problem(suffix_k, suffix_tables, suffix_lens) -> ParrotProblem:
     """ParrotProblem of a call that touches own tokens only (one device-to-host copy
     of the lengths, for their maximum)."""
@@ -385,12 +387,13 @@ def rotary_fill(q_rows, k_rows, v_rows, positions, query_offsets, suffix_k, suff
     """One fill on torch tensors: returns the rotated queries [T, HQ, D] (None without
     q_rows) and writes keys and values into the pools.  Sizes the call from host copies
     of the offsets and lengths; engines that know them reuse a RotaryFiller."""
-    prob = _cache_problem(suffix_k, suffix_tables, suffix_lens)
-    fill = RotaryFiller(prob, k_rows.shape[0], _most_rows(query_offsets), 0 if q_rows is None else q_rows.shape[1],
-                        rotary=rotary, norm_eps=norm_eps, device=k_rows.device)
-    return fill(dict(q_rows=q_rows, k_rows=k_rows, v_rows=v_rows, positions=positions, query_offsets=query_offsets,
-                     suffix_k=suffix_k, suffix_v=suffix_v, suffix_tables=suffix_tables, suffix_lens=suffix_lens,
-                     q_norm=q_norm, k_norm=k_norm), stream=stream)
+    with _on_stream(stream, k_rows.device):
+        prob = _cache_problem(suffix_k, suffix_tables, suffix_lens)
+        fill = RotaryFiller(prob, k_rows.shape[0], _most_rows(query_offsets), 0 if q_rows is None else q_rows.shape[1],
+                            rotary=rotary, norm_eps=norm_eps, device=k_rows.device)
+        return fill(dict(q_rows=q_rows, k_rows=k_rows, v_rows=v_rows, positions=positions, query_offsets=query_offsets,
+                         suffix_k=suffix_k, suffix_v=suffix_v, suffix_tables=suffix_tables, suffix_lens=suffix_lens,
+                         q_norm=q_norm, k_norm=k_norm), stream=stream)
 
 
 def tree_decode(q_rows, query_offsets, tree_parents, prefix_k, prefix_v, suffix_k, suffix_v, prefix_tables,
@@ -398,40 +401,39 @@ def tree_decode(q_rows, query_offsets, tree_parents, prefix_k, prefix_v, suffix_
     """One tree-decode call on torch tensors (see TreeDecoder); q_rows [T, HQ, D] with HQ
     a multiple of the pools' heads.  Returns (out, lse)."""
     sm_scale = 1.0 / math.sqrt(q_rows.shape[-1]) if sm_scale is None else sm_scale
-    prob = _sizes_from_tensors(suffix_k.transpose(1, 2), prefix_k, suffix_k, prefix_tables, suffix_tables, group_ids,
-                               prefix_lens, suffix_lens, sm_scale, prefix_parents)
-    off = query_offsets.cpu().numpy()
-    rows = tree_rows_from_host(off, group_ids.cpu().numpy(), prob.num_groups, q_rows.shape[1],
-                               None if prefix_parents is None else prefix_parents.cpu().numpy())
-    rows.num_query_rows = q_rows.shape[0]
-    dec = TreeDecoder(prob, rows, device=q_rows.device)
-    res = dec(dict(q_rows=q_rows, query_offsets=query_offsets, tree_parents=tree_parents, prefix_k=prefix_k,
-                   prefix_v=prefix_v, suffix_k=suffix_k, suffix_v=suffix_v, prefix_tables=prefix_tables,
-                    prefix_lens=prefix_lens, suffix_tables=suffix_tables, suffix_lens=suffix_lens,
-                    group_ids=group_ids, prefix_parents=prefix_parents),
-              stream=stream, nested=prefix_parents is not None)
-    if stream is not None:                       # the workspace goes back to the allocator here
-        dec.workspace.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream)))
-    return res
+    with _on_stream(stream, q_rows.device):
+        prob = _sizes_from_tensors(suffix_k.transpose(1, 2), prefix_k, suffix_k, prefix_tables, suffix_tables, group_ids,
+                                   prefix_lens, suffix_lens, sm_scale, prefix_parents)
+        rows = tree_rows_from_host(query_offsets.cpu().numpy(), group_ids.cpu().numpy(), prob.num_groups, q_rows.shape[1],
+                                   None if prefix_parents is None else prefix_parents.cpu().numpy())
+        rows.num_query_rows = q_rows.shape[0]
+        dec = TreeDecoder(prob, rows, device=q_rows.device)
+        return dec(dict(q_rows=q_rows, query_offsets=query_offsets, tree_parents=tree_parents, prefix_k=prefix_k,
+                        prefix_v=prefix_v, suffix_k=suffix_k, suffix_v=suffix_v, prefix_tables=prefix_tables,
+                        prefix_lens=prefix_lens, suffix_tables=suffix_tables, suffix_lens=suffix_lens,
+                        group_ids=group_ids, prefix_parents=prefix_parents),
+                   stream=stream, nested=prefix_parents is not None)
 
 
 def tree_accept(query_offsets, tree_parents, draft_tokens, target_tokens, root_tokens, *, stream=None):
     """One walk on torch int32 tensors; returns (accept_rows, accept_lens, next_tokens)."""
     dev = _device(query_offsets)
     T, R = draft_tokens.shape[0], root_tokens.shape[0]
-    rows = make_tree_rows(T, _most_rows(query_offsets), 0, 1)
-    taken, lens, follow = (torch.empty(n, dtype=torch.int32, device=dev) for n in (T, R, R))
-    parrot_tree_accept(R, rows, query_offsets, tree_parents, draft_tokens, target_tokens, root_tokens, taken, lens,
-                       follow, stream=stream)
+    with _on_stream(stream, dev):
+        rows = make_tree_rows(T, _most_rows(query_offsets), 0, 1)
+        taken, lens, follow = (torch.empty(n, dtype=torch.int32, device=dev) for n in (T, R, R))
+        parrot_tree_accept(R, rows, query_offsets, tree_parents, draft_tokens, target_tokens, root_tokens, taken, lens,
+                           follow, stream=stream)
     return taken, lens, follow
 
 
 def tree_commit(query_offsets, accept_rows, accept_lens, suffix_k, suffix_v, suffix_tables, suffix_lens, *,
                 stream=None):
     """One move in a layer's pools; returns the committed own lengths."""
-    prob = _cache_problem(suffix_k, suffix_tables, suffix_lens)
-    rows = make_tree_rows(accept_rows.shape[0], _most_rows(query_offsets), 0, 1)
-    out = torch.empty(accept_lens.shape[0], dtype=torch.int32, device=suffix_k.device)
-    parrot_tree_commit(prob, rows, query_offsets, accept_rows, accept_lens, suffix_tables, suffix_lens, suffix_k,
-                       suffix_v, out, stream=stream)
+    with _on_stream(stream, suffix_k.device):
+        prob = _cache_problem(suffix_k, suffix_tables, suffix_lens)
+        rows = make_tree_rows(accept_rows.shape[0], _most_rows(query_offsets), 0, 1)
+        out = torch.empty(accept_lens.shape[0], dtype=torch.int32, device=suffix_k.device)
+        parrot_tree_commit(prob, rows, query_offsets, accept_rows, accept_lens, suffix_tables, suffix_lens, suffix_k,
+                           suffix_v, out, stream=stream)
     return out
