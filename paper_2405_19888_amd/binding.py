@@ -614,13 +614,14 @@ def shared_prefix_decode(q, prefix_k, prefix_v, suffix_k, suffix_v, prefix_table
     ``per_request`` runs the baseline that reads each request's prefix itself.
     Engines that know the maxima on the host should build a ParrotProblem and
     reuse a Decoder instead (no copy, no allocation per call)."""
-    prob = _sizes_from_tensors(q, prefix_k, suffix_k, prefix_tables, suffix_tables, group_ids,
-                               prefix_lens, suffix_lens, sm_scale, prefix_parents)
-    dec = Decoder(prob, device=q.device)
-    t = dict(q=q, prefix_k=prefix_k, prefix_v=prefix_v, suffix_k=suffix_k, suffix_v=suffix_v,
-             prefix_tables=prefix_tables, prefix_lens=prefix_lens, suffix_tables=suffix_tables,
-             suffix_lens=suffix_lens, group_ids=group_ids, prefix_parents=prefix_parents)
-    return dec(t, shared=not per_request, stream=stream, nested=prefix_parents is not None)
+    with _on_stream(stream, q.device):
+        prob = _sizes_from_tensors(q, prefix_k, suffix_k, prefix_tables, suffix_tables, group_ids,
+                                   prefix_lens, suffix_lens, sm_scale, prefix_parents)
+        dec = Decoder(prob, device=q.device)
+        t = dict(q=q, prefix_k=prefix_k, prefix_v=prefix_v, suffix_k=suffix_k, suffix_v=suffix_v,
+                 prefix_tables=prefix_tables, prefix_lens=prefix_lens, suffix_tables=suffix_tables,
+                 suffix_lens=suffix_lens, group_ids=group_ids, prefix_parents=prefix_parents)
+        return dec(t, shared=not per_request, stream=stream, nested=prefix_parents is not None)
 
 
 def shared_prefix_prefill(q_rows, query_offsets, prefix_k, prefix_v, suffix_k, suffix_v,
@@ -631,14 +632,15 @@ def shared_prefix_prefill(q_rows, query_offsets, prefix_k, prefix_v, suffix_k, s
     Sizes the problem and the row counts from host copies of the int arrays,
     allocates out, lse and the workspace, and runs on ``stream``.  Returns
     (out, lse)."""
-    prob = _sizes_from_tensors(q_rows, prefix_k, suffix_k, prefix_tables, suffix_tables, group_ids,
-                               prefix_lens, suffix_lens, sm_scale, prefix_parents)
-    rows = prefill_rows_from_host(query_offsets.cpu().numpy(), group_ids.cpu().numpy(),
-                                  prob.num_groups,
-                                  None if prefix_parents is None else prefix_parents.cpu().numpy())
-    pre = Prefiller(prob, rows, device=q_rows.device)
-    t = dict(q_rows=q_rows, query_offsets=query_offsets, prefix_k=prefix_k, prefix_v=prefix_v,
-             suffix_k=suffix_k, suffix_v=suffix_v, prefix_tables=prefix_tables,
-             prefix_lens=prefix_lens, suffix_tables=suffix_tables, suffix_lens=suffix_lens,
-             group_ids=group_ids, prefix_parents=prefix_parents)
-    return pre(t, stream=stream, nested=prefix_parents is not None)
+    with _on_stream(stream, q_rows.device):
+        prob = _sizes_from_tensors(q_rows, prefix_k, suffix_k, prefix_tables, suffix_tables, group_ids,
+                                   prefix_lens, suffix_lens, sm_scale, prefix_parents)
+        rows = prefill_rows_from_host(query_offsets.cpu().numpy(), group_ids.cpu().numpy(),
+                                      prob.num_groups,
+                                      None if prefix_parents is None else prefix_parents.cpu().numpy())
+        pre = Prefiller(prob, rows, device=q_rows.device)
+        t = dict(q_rows=q_rows, query_offsets=query_offsets, prefix_k=prefix_k, prefix_v=prefix_v,
+                 suffix_k=suffix_k, suffix_v=suffix_v, prefix_tables=prefix_tables,
+                 prefix_lens=prefix_lens, suffix_tables=suffix_tables, suffix_lens=suffix_lens,
+                 group_ids=group_ids, prefix_parents=prefix_parents)
+        return pre(t, stream=stream, nested=prefix_parents is not None)

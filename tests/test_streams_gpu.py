@@ -21,14 +21,16 @@ def late(s, targets):
             x = (x @ x).clamp_(-1, 1)
         for t, h in zip(targets, held):
             t.copy_(h)
+    return held                                        # (read when the stream gets there)
 
 
 def on_stream(call, targets, handle):
     """The call's results on a busy side stream, given as a stream or by its handle."""
     s = torch.cuda.Stream()
-    late(s, targets)
+    held = late(s, targets)
     got = call(s.cuda_stream if handle else s)
     s.synchronize()
+    del held
     return got
 
 
@@ -55,12 +57,14 @@ def forms(d):
                                              rotary=parrot.make_rotary(64), stream=s),
         "tree": lambda s: parrot.tree_decode(d["q"], d["off"], d["up"], *pools, stream=s),
         "accept": lambda s: parrot.tree_accept(d["off"], d["up"], d["tokens"], d["tokens"], d["roots"], stream=s),
+        "decode": lambda s: parrot.shared_prefix_decode(d["q"][:2, :2].contiguous(), *pools, sm_scale=0.125, stream=s),
+        "prefill": lambda s: parrot.shared_prefix_prefill(d["q"][:, :2].contiguous(), d["off"], *pools, sm_scale=0.125, stream=s),
         "commit": lambda s: parrot.tree_commit(d["off"], d["rows"], d["lens"], *cache, stream=s),
     }
 
 
 @pytest.mark.parametrize("handle", [False, True])
-@pytest.mark.parametrize("name", ["fill", "tree", "accept", "commit"])
+@pytest.mark.parametrize("name", ["fill", "tree", "accept", "commit", "decode", "prefill"])
 def test_sizes_and_memory_are_the_streams(name, handle):
     d, fresh = step(), step()
     want = forms(fresh)[name](None)
