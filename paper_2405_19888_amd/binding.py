@@ -393,10 +393,12 @@ def prefill_rows_from_host(query_offsets, group_ids, num_groups, prefix_parents=
     q = np.diff(off)
     per_group = np.zeros(max(int(num_groups), 1), dtype=np.int64)
     par = None if prefix_parents is None else np.asarray(prefix_parents)
+    # (walks stop after num_groups steps: parents that the validator rejects cannot loop them)
     for r, g in enumerate(np.asarray(group_ids)):
-        x = int(g)
-        while x >= 0:
+        x, n = int(g), 0
+        while 0 <= x < int(num_groups) and n < int(num_groups):
             per_group[x] += q[r]
+            n += 1
             x = int(par[x]) if par is not None else -1
     return make_prefill_rows(int(off[-1]), max(int(q.max()) if q.size else 0, 1),
                              int(per_group.max()) if num_groups else 0)

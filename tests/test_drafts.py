@@ -220,6 +220,16 @@ def test_join_stays_inside_a_row(parrot_lib, levels):
             assert len(got) <= seg and all(0 <= x < seg for x in got), (lo, hi, some, chunks, before, seg)
 
 
+@pytest.mark.timeout(20)
+def test_row_counts_of_bad_groups(parrot_lib):
+    """Parents in a ring and group ids out of range, which the content check refuses, neither
+    hang nor break the row counts on the host."""
+    rows = parrot.tree_rows_from_host([0, 3, 5, 9], [1, 0, 7], 2, 8, prefix_parents=[1, 0])
+    assert (rows.num_query_rows, rows.max_query_rows, rows.max_group_rows) == (9, 4, 5)
+    rows = parrot.tree_rows_from_host([0, 3, 5], [1, 0], 2, 8, prefix_parents=[5, 0])
+    assert rows.max_group_rows == 5
+
+
 def tensors(dtype=torch.float16):
     """A tree and fill call's tensors for problem() with 20 rows of 8 query heads."""
     ints = lambda *n: torch.zeros(n, dtype=torch.int32)
