@@ -636,37 +636,43 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a) {
   const int s0 = first + tile * between;
   const int pieces = (s0 + units - 1) / q - s0 / q + 1;
   const bool live = hq < HQ && !(prefixed == 0 && pieces == 1);   // one piece: it wrote the output
-  const TreeSlots slots = tree_slots(lo, hi, pieces, a.seg_p, a.seg_pre, a.seg);
+  // the row's first own piece and its column there (clamped as the slots are)
+  const int piece = clampi(s0 / q + (of >> 1) * a.tiles + tile, 0, a.pieces - 1);
+  const int col = clampi(x - tile * tree_detail::kCols<DT>, 0, a.piece_cols - 1);
+  const TreeSlots slots = tree_slots(lo, hi, min(pieces, a.pieces - piece), a.seg_p, a.seg_pre, a.seg);
   const int n = live ? slots.n : 0;
   int most = n;
 #pragma unroll
   for (int m = GW; m < kWave; m <<= 1) most = max(most, __shfl_xor(most, m));
   most = __builtin_amdgcn_readfirstlane(most);
   const size_t at = (size_t)t * HQ + min(hq, HQ - 1);
-  // the row's first own piece, and its column (clamped as the slots are)
-  const int piece = s0 / q + (of >> 1) * a.tiles + tile;
-  const int col = (int)min((unsigned)(x - tile * tree_detail::kCols<DT>), (unsigned)a.piece_cols - 1u);
-  auto place = [&](int i) {                               // slot of partial i
+  const size_t pre = at * a.seg_pre, own = piece_slot(a, min(hq, HQ - 1) / a.G, piece) + col;
+  const float* l_pre = a.lse_part + pre;
+  const float* l_own = a.lse_part + own;
+  const float* o_pre = a.o_part + pre * D + i0 * 4;
+  const float* o_own = a.o_part + own * D + i0 * 4;
+  auto lse_of = [&](int i) {                              // of partial i
     const int sl = slots.slot(i);
-    if (sl < a.seg_pre) return at * a.seg_pre + sl;
-    const unsigned pc = min((unsigned)(piece + (sl - a.seg_pre)), (unsigned)a.pieces - 1u);
-    return piece_slot(a, min(hq, HQ - 1) / a.G, (int)pc) + col;
+    return sl < a.seg_pre ? l_pre[sl] : l_own[(sl - a.seg_pre) * a.piece_cols];
   };
-  const float* op = a.o_part + i0 * 4;
+  auto out_of = [&](int i) {
+    const int sl = slots.slot(i);
+    return sl < a.seg_pre ? o_pre + sl * D : o_own + (sl - a.seg_pre) * a.piece_cols * D;
+  };
   // the lane's first log-sum-exp, and the first outputs beside it
-  const float l0 = i0 < n ? a.lse_part[place(i0)] : -INFINITY;
+  const float l0 = i0 < n ? lse_of(i0) : -INFINITY;
   f32x4 v[U];
   auto load = [&](int i) {                                // partials i .. i + U - 1, those that exist
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       v[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (i + u < n) v[u] = *reinterpret_cast<const f32x4*>(op + place(i + u) * D);
+      if (i + u < n) v[u] = *reinterpret_cast<const f32x4*>(out_of(i + u));
     }
   };
   load(0);
   float mx = l0;
 #pragma unroll 1
-  for (int i = i0 + GW; i < n; i += GW) mx = fmaxf(mx, a.lse_part[place(i)]);
+  for (int i = i0 + GW; i < n; i += GW) mx = fmaxf(mx, lse_of(i));
   mx = fmaxf(mx, dpp_f<kDppXor1>(mx));
   mx = fmaxf(mx, dpp_f<kDppXor2>(mx));
   mx = fmaxf(mx, dpp_f<kDppHalfMirror>(mx));
@@ -677,7 +683,7 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a) {
 #pragma unroll 1
   for (int b = 0; b < most; b += GW) {
     // (no guard on mx: logits that are all -inf give NaN)
-    const float wl = b == 0 ? l0 : b + i0 < n ? a.lse_part[place(b + i0)] : -INFINITY;
+    const float wl = b == 0 ? l0 : b + i0 < n ? lse_of(b + i0) : -INFINITY;
     const float wt = b + i0 < n ? fast_exp2(wl - mx) : 0.f;
     tot += wt;
     const int end = min(GW, most - b);
