@@ -511,6 +511,8 @@ parrot_status parrot_rotary_fill(
  * drafted ones, the ancestors of j and j itself:
  *   out, lse             the decode formula over those keys; both NaN for a row
  *                        with a logit of NaN or +inf, or whose logits are all -inf.
+ *                        16-bit caches: the weights are rounded to dtype for their
+ *                        product with V and divided by the rounded ones' sum.
  * Keys and values of tokens a row does not see never reach its result, whatever
  * they hold (NaN and infinities too).
  *

@@ -292,11 +292,11 @@ parrot_status check_tree_counts(int32_t requests, const parrot_tree_rows* rows) 
 //    kTreeSplitLeast at least.
 // The first grows with every size, and the second has a least value: `never` is set where no
 // call of at most these sizes splits.
-// Measured, one launch and split, 16-bit heads of 128: a request of 64 rows on 300, 2000,
+// Measured, one launch and split, bfloat16 heads of 128: a request of 64 rows on 300, 2000,
 // 8000 tokens and 32 heads 15 and 20, 47 and 24, 155 and 46 us; 32 requests of 64 rows,
 // four query heads on each of 8, on 300, 4000 tokens 29 and 72, 181 and 284; 32 requests of
-// 8 rows on one prefix of 300, 4000 tokens and 32 heads 33 and 31, 162 and 58; 128 requests
-// of 4 rows on 1000 tokens and 8 heads 103 and 95.
+// 8 rows on 100 own tokens and one prefix of 300, 4000 tokens and 32 heads 33 and 31, 162 and
+// 58; 128 requests of 4 rows on 1000 tokens and 8 heads 103 and 95.
 bool tree_splits(const parrot_problem* p, const parrot_tree_rows* rows, const TreePlan& pl, long cus, bool* never) {
   const double mean = 0.7, R = p->num_requests, H = p->num_heads, HQ = rows->num_query_heads, D = p->head_dim;
   const double T = rows->num_query_rows, eb = p->dtype == PARROT_DTYPE_F32 ? 4 : 2, kv = 2 * D * eb * H;
@@ -352,11 +352,12 @@ parrot_status check_tree(const parrot_problem* p, const parrot_tree_rows* rows, 
   const long H = p->num_heads, R = p->num_requests, cus = parrot::device_cus(), cols = parrot::tree_cols(p->dtype);
   if (ceil_div(R * H, 8) * 8 * pl->tiles > 0x7fffffffL)
     return set_error(PARROT_ERR_UNSUPPORTED, "tree decode needs too many workgroups");
-  // The split plan.  Prefix chunks are as long as their workgroups still fill the device
-  // (a chunk more costs a tile 64 KB of partial results, written and read: 48 rows each on
-  // six prefixes of 2304 tokens take 156 us in one chunk; at an earlier step 179 in one,
+  // The split plan (figures here and below: 32 heads of 128 in bfloat16 but where it says
+  // fp32, no other tokens, a query head for each).  Prefix chunks are as long as their workgroups still fill the device
+  // (a chunk more costs a tile 64 KB of partial results, written and read: 48 requests of 48 rows,
+  // eight on each of six prefixes of 2304 tokens, take 156 us in one chunk; at an earlier step 179 in one,
   // 199 in two, 237 in five),
-  // but not so long that the last ones run alone (48 rows of 8 requests on 8192 tokens: 126
+  // but not so long that the last ones run alone (8 requests of 48 rows on one of 8192 tokens: 126
   // us in chunks of 4096, 98 of 2048, 111 of 1024).  A group has at most tiles_p tiles, all
   // of them together a tile each beyond what their rows fill.
   const long mg = p->num_groups > 0 ? rows->max_group_rows : 0;
@@ -378,13 +379,13 @@ parrot_status check_tree(const parrot_problem* p, const parrot_tree_rows* rows, 
   // Own tokens: requests of at most 32 columns go by waves, each with a run of its own.
   // Four waves a CU read fastest (8 requests of 16 rows on 9600 tokens: 217 us, 235 with
   // eight, 246 with twelve; with three 212, but 96 requests on 800 tokens 237 for 228).
-  // Tiles: two workgroups per CU (64 and 128 rows on 9600 tokens: 239 and 257 us; 216 and
-  // 280 with one, 261 and 279 with three), three where a request may have several tiles
-  // and the products bound it, and for fp32 (32 requests of 20 rows on 4000 tokens: 1411 us
-  // with two, 1107 with three, 928 since the tile reads ahead).
+  // Tiles: two workgroups per CU (8 requests of 64 and 128 rows on 9600 tokens: 239 and 257
+  // us; 216 and 280 with one, 261 and 279 with three), three where a request may have several
+  // tiles and the products bound it, and for fp32 (32 requests of 20 rows on 4000 tokens: 1411
+  // us with two, 1107 with three; one launch, which such calls take, 845).
   const long most_cols = rows->max_query_rows * G;
   // (fp32 caches with two column sets spill: 32 requests of 20 rows on 1000 tokens 440 us, by
-  // tiles 294).
+  // tiles 295).
   const OwnRole own = own_role((int)p->dtype, H, most_cols, cus);
   pl->sets = own.sets;
   pl->small = pl->sets == 1 && parrot::tree_small_rows(p->dtype, p->head_dim) && R * H <= cus;
@@ -393,8 +394,8 @@ parrot_status check_tree(const parrot_problem* p, const parrot_tree_rows* rows, 
   pl->piece_cols = own.piece_cols;
   pl->min_run = kTreeMinRun;
   const long units = ceil_div(p->max_suffix_len, parrot::tree_unit(p->dtype, p->head_dim));
-  // the longer items start first, so that the short ones fill up (48 rows each on six
-  // prefixes of 2304 tokens: 167 us, 182 with the own tokens first, at that step)
+  // the longer items start first, so that the short ones fill up (those
+  // on six prefixes of 2304 tokens: 167 us, 182 with the own tokens first, at that step)
   pl->pre_first = (double)R * pl->tiles * units / pl->runs < (double)pl->cp / parrot::tree_unit(p->dtype, p->head_dim);
   const long seg = pl->seg_pre + std::min(ceil_div(units, pl->min_run) + 1, (long)pl->runs);
   const double cost = (double)R * pl->tiles * (units + parrot::kTreeSetup);

@@ -4,10 +4,10 @@
 // Per head x of a query or key row, with g the norm's weight (or 1) and c_e, s_e
 // the amplitude times cosine and sine of the angle of element e's pair,
 //   y_e = (x_e g_e c_e -/+ x_p g_p s_e) / sqrt(mean(x^2) + eps),  p the pair's other element
-// in fp32, rounded once.  Everything is read once and written once, so the call is
-// bound by memory: 7500 rows of 96 16-bit heads of 128, normalised and rotated in halves,
+// in fp32, rounded once.  Everything is read once and written once (but for halves whose
+// partners no 16 bytes line up with, below), so the call is bound by memory: 7500 rows of 96 16-bit heads of 128, normalised and rotated in halves,
 // 369 MB, take 73 us (5.1 TB/s; a large copy reaches 4.7, without the 256 MB cache
-// that holds part of what was just written).
+// that holds part of what was just written); fp32, 738 MB, 147 us.
 //
 // Angles: position n turns pair i by n f_i.  In fp32 that product is off by 0.006
 // radians at n = 100000, so f_i / (2 pi) comes as a 64-bit binary fraction of a turn:
@@ -26,6 +26,11 @@
 // registers left five waves a SIMD, and those rows took 113 us, 139 with three steps ahead
 // and four waves; 1500 rows of 48 heads 14.7 and 17.9 us for 11.0.  Two rows a
 // workgroup: as long, and 12.3 us.)
+//
+// kRotaryHalfScalar (half layout, RD / 2 no multiple of a lane's 16 bytes: RD = 20, 50): a lane
+// reads each partner, and its weight, again from the caches, 2 or 4 bytes at a time: the rows
+// above take 197 us with RD = 20 and 175 with RD = 50, 78 with 128; 1500 rows of 48 heads 27
+// for 12.
 #include "draft_args.h"
 
 namespace parrot {

@@ -266,7 +266,7 @@ PARROT_DEV void write_desc(const TreeArgs& a, int r, const OwnCost& c, int start
 // The tiles of a request read the same keys: with their costs taken up to a multiple of the
 // run length, they are cut at the same tokens, the workgroups that read a token do it
 // at about the same time, and it comes from memory once (6 requests of 96 .. 256 columns
-// on 9000 .. 33000 tokens: 156 us, 180 without, at that step).  That costs each such tile half a run of
+// on 9000 .. 33000 tokens, 8 heads of 128 in fp16: 156 us, 180 without, at that step).  That costs each such tile half a run of
 // idle workgroups, so it is done where they are at most a quarter of the runs.
 
 // Finds the runs run_of(wave) of the cost (each wave gets its own); false for a wave whose
@@ -513,9 +513,9 @@ void k_tree_partials(TreeArgs a) {
 // share of their units each) and meet in LDS.  Bound by latency, 2.4 us a step of 16 KiB
 // (fp32: 4): one request of 4 rows on 300, 2000 tokens takes 9.6, 26.8 us at 32 16-bit
 // heads of 128 (the tile: 11.6, 41), at fp32 17.8 us on 300 (32).  Rows of 128 bytes, 64
-// tokens a step, leave most waves idle: the tile takes them (8 requests on 1000
-// tokens: 17.6 us, 27 here), and 17 to 32 columns, whose waves meet for longer than they
-// read (32 requests of 20 rows on 300 tokens: 42.6 us, 55.8 here).
+// tokens a step, leave most waves idle: the tile takes them (8 requests of 4 rows on 1000
+// tokens, 32 heads of 64: 17.6 us, 27 here), and 17 to 32 columns, whose waves meet for longer than they
+// read (32 requests of 20 rows on 300 tokens, 32 heads of 128: 42.6 us, 55.8 here).
 constexpr int kSmallWaves = 8;
 template <int DT, int D>
 __global__ __launch_bounds__(kSmallWaves * 64) void k_tree_small(TreeArgs a) {

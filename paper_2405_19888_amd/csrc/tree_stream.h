@@ -7,8 +7,8 @@
 // for but its loads: 8 KiB of K (as the QK operand wants it, 64 contiguous bytes of
 // 16 token rows an instruction) and 8 KiB of V (contiguous) come into registers one step
 // ahead; V goes through 8 KiB of the wave's own LDS, swizzled, to be read transposed.
-// Four waves a CU keep 64 KiB in flight.  Bound by memory: 8 requests of 16 rows on 9600
-// tokens, 1.26 GB, take 211 us with the join (6.0 TB/s; a plain read 7.06), of 32 rows
+// Four waves a CU keep 64 KiB in flight.  Bound by memory (32 heads of 128 in bfloat16):
+// 8 requests of 16 rows on 9600 tokens, 1.26 GB, take 211 us with the join (6.0 TB/s; a plain read 7.06), of 32 rows
 // 222, eight waves a CU 235 and 240, a shared tile 246 and more; 96 requests of 16 rows
 // on 800 tokens 222 (185 at that rate: queries, masks and first keys of each piece have
 // nothing to hide behind).  All waits are the compiler's.

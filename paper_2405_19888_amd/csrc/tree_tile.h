@@ -9,8 +9,11 @@
 // with an online softmax in fp32 whose reference moves only when a column's logits
 // exceed it by more than 2^8 (as the prefill tile's), so most blocks need no
 // cross-lane maximum.  Probabilities are rounded to the cache's type for the product
-// (16-bit caches), and the output is divided by the sum of the rounded ones, so a
-// dominant weight's rounding cancels; the lse keeps the sum of the unrounded ones.
+// (16-bit caches: the matrix cores take both factors in one type, and high and low halves
+// would double the second product), and the output is divided by the sum of the rounded
+// ones, so a dominant weight's rounding cancels; the lse keeps the sum of the unrounded ones.
+// Against 64 bits the output is off by 1.3 to 1.4 times its own rounding (fp16 2.9e-4 for
+// 2.1e-4, bf16 2.3e-3 for 1.7e-3 of its norm).
 //
 // Keys and values pass through LDS in 16 KiB stages (8 of each: 32 tokens of 128
 // 16-bit elements) by direct-to-LDS loads into a ring of three, two stages ahead.
@@ -21,7 +24,9 @@
 // 1.28 us for a 32-token stage of 128 columns each (1.25 PFLOP/s; a large bf16 product
 // reaches 1.12), one alone 0.74.  What a piece costs beside its stages, 17 us (queries
 // and masks after the row lists, the first stages, the masked ones, the partial results,
-// instructions fetched for the first time), bounds the short ones.
+// instructions fetched for the first time), bounds the short ones.  The 16-bit instances for
+// heads of 128 keep three waves a SIMD by spilling: k_tree_partials 31 vector and 167 scalar
+// registers, k_tree_decode 2 and 49, stored and loaded outside the stage loops, once a piece.
 //
 // Mask: drafted tokens follow the cached ones, from own position `base` on.  The
 // bits of the tokens a column sees are kept per 32-token word counted from base
