@@ -222,6 +222,7 @@ struct TreePlan {
   int cp, tiles_p, seg_p, seg_pre, seg, sets, own_wgs, runs, min_run;
   long n_pre;
   bool pre_first;                // prefix workgroups before the own tokens'
+  long held;                     // rows with prefixes, at most
   int pieces, piece_cols;        // of a cache head's own tokens, columns of each
   size_t own0, slots;            // first slot of the own tokens' partial results, slots in all
   size_t o_bytes, lse_bytes;
@@ -255,15 +256,16 @@ OwnRole own_role(int dtype, long H, long cols, long cus) {
   return o;
 }
 
-// Slots of the prefixes' partial results that no call of at most these sizes exceeds: a row
-// has one per level and chunk, and chunks are halved only while all of them are at most
-// `cap`, or what the longest chunks take.  Where all rows read prefixes the chunk rule stays
-// below `cap` by itself.
-double prefix_slot_bound(const parrot_problem* p, const parrot_tree_rows* rows, int levels, long cus) {
-  if (levels == 0 || rows->max_group_rows == 0) return 0;
-  const double each = (double)rows->num_query_rows * rows->num_query_heads * levels, cap = 4.0 * cus * parrot::tree_cols(p->dtype);
+// Slots of the prefixes' partial results that no call of at most these sizes exceeds: each
+// of `held` rows has one per query head, level and chunk.  Chunks are halved only while their
+// workgroups, one per cache head, chunk and column tile, are fewer than 3/2 a CU, so after that
+// there are less than 3 a CU, of tree_cols slots at most per level: those tiles hold every row
+// that has prefixes.
+double prefix_slot_bound(const parrot_problem* p, const parrot_tree_rows* rows, long held, int levels, long cus) {
+  if (levels == 0 || held == 0) return 0;
+  const double each = (double)held * rows->num_query_heads * levels;
   return std::min(each * ceil_div(p->max_prefix_len, kTreeChunkLeast),
-                  std::max(each * ceil_div(p->max_prefix_len, kTreeChunkMax), cap));
+                  std::max(each * ceil_div(p->max_prefix_len, kTreeChunkMax), 3.0 * cus * parrot::tree_cols(p->dtype) * levels));
 }
 
 // The row counts of a tree call (or of accept and commit, which have no heads).
@@ -365,10 +367,7 @@ parrot_status check_tree(const parrot_problem* p, const parrot_tree_rows* rows, 
   pl->cp = kTreeChunkMax;
   if (pl->tiles_p > 0) {
     const long tiles = std::min(p->num_groups * (long)pl->tiles_p, ceil_div(T * pl->max_depth * G, cols) + p->num_groups);
-    const double each = (double)T * rows->num_query_heads * pl->max_depth, most = prefix_slot_bound(p, rows, pl->max_depth, cus);
-    while (pl->cp > kTreeChunkMin && tiles * H * ceil_div(p->max_prefix_len, pl->cp) < cus * 3 / 2 &&
-           each * ceil_div(p->max_prefix_len, pl->cp / 2) <= most)
-      pl->cp /= 2;
+    while (pl->cp > kTreeChunkMin && tiles * H * ceil_div(p->max_prefix_len, pl->cp) < cus * 3 / 2) pl->cp /= 2;
     const long chunks = std::max(1L, ceil_div(p->max_prefix_len, pl->cp));       // of equal length
     pl->cp = (int)(std::max(1L, ceil_div(p->max_prefix_len, chunks * 64)) * 64);
     pl->seg_p = (int)ceil_div(p->max_prefix_len, pl->cp);
@@ -404,7 +403,8 @@ parrot_status check_tree(const parrot_problem* p, const parrot_tree_rows* rows, 
   double own_most = own_slots(own);
   for (const long c : {16L, 32L, cols})
     if (c < most_cols) own_most = std::max(own_most, own_slots(own_role((int)p->dtype, H, c, cus)));
-  const double pre_slots = (double)T * rows->num_query_heads * pl->seg_pre, pre_most = prefix_slot_bound(p, rows, pl->max_depth, cus);
+  pl->held = pl->seg_pre > 0 ? std::min(T, p->num_groups * mg) : 0;
+  const double pre_slots = (double)pl->held * rows->num_query_heads * pl->seg_pre, pre_most = prefix_slot_bound(p, rows, pl->held, pl->max_depth, cus);
   if ((pl->own_wgs + pl->n_pre) * 256 > 0xffffffffL || ceil_div(R * H, 8) * 8 * pl->tiles * 512 > 0xffffffffL || cost > 1.5e9 || (own_most + std::max(pre_slots, pre_most)) * p->head_dim > 1e18)
     return set_error(PARROT_ERR_UNSUPPORTED, "tree decode: %.3g units of own tokens", cost);
   pl->seg = (int)seg;
@@ -488,7 +488,7 @@ parrot_status parrot_shared_prefix_tree_decode(
   a.o_part = reinterpret_cast<float*>(workspace);
   a.lse_part = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + pl.o_bytes);
   a.desc = reinterpret_cast<int*>(reinterpret_cast<char*>(workspace) + pl.o_bytes + pl.lse_bytes);
-  a.own0 = pl.own0; a.pieces = pl.pieces; a.piece_cols = pl.piece_cols;
+  a.own0 = pl.own0; a.held = (int)pl.held; a.pieces = pl.pieces; a.piece_cols = pl.piece_cols;
   const parrot_trace none = {nullptr, nullptr, nullptr, nullptr};
   const parrot_trace& tr = trace ? *trace : none;
   const int dt = (int)p->dtype, D = p->head_dim;

@@ -223,7 +223,10 @@ PARROT_DEV void tree_piece(const TreeArgs& a, tree_detail::Lds<DT>& lds, const T
   if (!tile.act) return;
   if (pc.slot < 0) write_output<DT, D, NS>(a, tile, pc.ncols, row_of);
   else if (own) write_partial<DT, D, NS>(a, tile, pc.ncols, [&](int col) { return piece_slot(a, pc.h, pc.slot) + col; });
-  else write_partial<DT, D, NS>(a, tile, pc.ncols, [&](int col) { return row_of(col) * (size_t)a.seg_pre + pc.slot; });
+  else write_partial<DT, D, NS>(a, tile, pc.ncols, [&](int col) {
+    const int x = pc.col0 + col, row = x / a.G;
+    return ((size_t)lds.held[row - pc.row0] * (a.H * a.G) + pc.h * a.G + (x - row * a.G)) * a.seg_pre + pc.slot;
+  });
 }
 
 // The run of an own-role wave (tiles: of all waves of its workgroup), and where it stands.
@@ -235,12 +238,16 @@ PARROT_DEV int tile_cost(int units, int tiles, int pad) {
   return tiles > 1 && pad > 0 ? (cost + pad - 1) / pad * pad : cost;
 }
 
-// What the join needs of the rows of request r, whose cost starts at `start`.
+// Whether request r has prefixes that the prefix role reads.
+PARROT_DEV bool has_prefixes(const TreeArgs& a, int gid) { return a.seg_p > 0 && gid >= 0 && gid < a.NG; }
+
+// What the join needs of the rows of request r, whose cost starts at `start` and whose rows
+// are numbers held0, held0 + 1 .. of those with prefixes.
 template <int DT, int D>
-PARROT_DEV void write_desc(const TreeArgs& a, int r, const OwnCost& c, int start, int q, int pad) {
+PARROT_DEV void write_desc(const TreeArgs& a, int r, const OwnCost& c, int start, int held0, int q, int pad) {
   int len[kMaxDepth], nlev = 0;
   const int gid = a.gid[r];
-  const bool prefixed = a.seg_p > 0 && gid >= 0 && gid < a.NG;
+  const bool prefixed = has_prefixes(a, gid);
   for (int g = gid; a.seg_p > 0 && g >= 0 && g < a.NG && nlev < a.depth; g = a.parents ? a.parents[g] : -1) {
     const int n = min((clampi(a.plen[g], 0, a.max_p) + a.cp - 1) / a.cp, a.seg_p);
 #pragma unroll
@@ -260,6 +267,7 @@ PARROT_DEV void write_desc(const TreeArgs& a, int r, const OwnCost& c, int start
     int4* d = reinterpret_cast<int4*>(a.desc + (size_t)(c.first + j) * kTreeDesc);
     d[0] = int4{start + kTreeSetup, tile_cost(c.units, c.tiles, pad), c.units, q};
     d[1] = int4{(int)lo, (int)hi, j, 2 * r + (prefixed ? 1 : 0)};
+    d[2] = int4{held0 + j, 0, 0, 0};
   }
 }
 
@@ -307,14 +315,23 @@ PARROT_DEV bool find_run(const TreeArgs& a, int* scratch, int wg, F run_of, OwnR
   __syncthreads();
   const bool writes = wg < kDescWgs;
   bool all = false;                               // every wave's run was found or is empty
-  for (int b = 0, before = 0; b < a.R && (!all || writes); b += 256) {
+  for (int b = 0, before = 0, held = 0; b < a.R && (!all || writes); b += 256) {
     int sum = total;
     if (a.R > 256) {                              // (few requests: the first pass stands)
       cost = cost_of(b + tid);
       incl = before + scan256(cost, scratch, &sum);
     }
-    if (writes && b + tid < a.R && cost > 0 && tid % min(kDescWgs, a.own_wgs) == wg)
-      write_desc<DT, D>(a, b + tid, c, incl - cost, q, pad);
+    if (writes) {
+      int rows = 0, held0 = 0;
+      if (a.seg_p > 0) {                          // rows with prefixes before the request's
+        int here;
+        rows = b + tid < a.R && has_prefixes(a, a.gid[b + tid]) ? c.count : 0;
+        held0 = held + scan256(rows, scratch, &here) - rows;
+        held += here;
+      }
+      if (b + tid < a.R && cost > 0 && tid % min(kDescWgs, a.own_wgs) == wg)
+        write_desc<DT, D>(a, b + tid, c, incl - cost, held0, q, pad);
+    }
     all = true;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
@@ -393,30 +410,35 @@ PARROT_DEV bool prefix_piece(const TreeArgs& a, tree_detail::Lds<DT>& lds, int w
   const int row0 = pc->row0;
   if (threadIdx.x < kWave) {
     const int lane = threadIdx.x;
-    int base = 0;
+    int base = 0, held = 0;                               // rows of the list, rows with prefixes
     for (int b = 0; b < a.R && base < row0 + MOST; b += kWave) {
       const int r = b + lane;
-      bool reads = false;
+      bool reads = false, any = false;
       OwnCost oc;
       oc.count = 0; oc.first = 0;
       if (r < a.R) {
         int x = a.gid[r];
         oc = own_cost<DT, D>(a, r);
+        any = has_prefixes(a, x);
         for (int d = 0; d < a.depth && x >= 0 && x < a.NG; ++d) {
           if (x == g) { reads = true; break; }
           x = a.parents ? a.parents[x] : -1;
         }
       }
-      const int n = reads ? oc.count : 0;
-      int incl = n;
+      const int n = reads ? oc.count : 0, m = any ? oc.count : 0;
+      int incl = n, among = m;
 #pragma unroll
       for (int d = 1; d < kWave; d <<= 1) {
-        const int v = __shfl_up(incl, d);
-        if (lane >= d) incl += v;
+        const int v = __shfl_up(incl, d), u = __shfl_up(among, d);
+        if (lane >= d) { incl += v; among += u; }
       }
-      const int first = base + incl - n;
-      for (int x = max(first, row0), e = min(first + n, row0 + MOST); x < e; ++x) lds.rows[x - row0] = oc.first + x - first;
+      const int first = base + incl - n, held0 = held + among - m;
+      for (int x = max(first, row0), e = min(first + n, row0 + MOST); x < e; ++x) {
+        lds.rows[x - row0] = oc.first + x - first;
+        lds.held[x - row0] = clampi(held0 + x - first, 0, a.held - 1);
+      }
       base += __shfl(incl, kWave - 1);
+      held += __shfl(among, kWave - 1);
     }
     if (lane == 0) lds.rows[MOST] = base;
   }
@@ -631,6 +653,7 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a) {
   const int first = ld_uniform(d), between = ld_uniform(d + 1), units = ld_uniform(d + 2), q = max(1, ld_uniform(d + 3));
   const unsigned lo = (unsigned)ld_uniform(d + 4), hi = (unsigned)ld_uniform(d + 5);
   const int j = ld_uniform(d + 6), of = ld_uniform(d + 7), prefixed = of & 1;
+  const int held = clampi(ld_uniform(d + 8), 0, max(a.held - 1, 0));
   if (t >= ld_uniform(a.qoff + a.R)) return;              // padding (its descriptor holds nothing)
   const int x = j * a.G + hq % a.G, tile = x / tree_detail::kCols<DT>;
   const int s0 = first + tile * between;
@@ -646,7 +669,7 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a) {
   for (int m = GW; m < kWave; m <<= 1) most = max(most, __shfl_xor(most, m));
   most = __builtin_amdgcn_readfirstlane(most);
   const size_t at = (size_t)t * HQ + min(hq, HQ - 1);
-  const size_t pre = at * a.seg_pre, own = piece_slot(a, min(hq, HQ - 1) / a.G, piece) + col;
+  const size_t pre = ((size_t)held * HQ + min(hq, HQ - 1)) * a.seg_pre, own = piece_slot(a, min(hq, HQ - 1) / a.G, piece) + col;
   const float* l_pre = a.lse_part + pre;
   const float* l_own = a.lse_part + own;
   const float* o_pre = a.o_part + pre * D + i0 * 4;
@@ -761,7 +784,7 @@ hipError_t launch_tree_partials(const TreeArgs& a, int dtype, int D, hipStream_t
   const long pre = a.n_pre > 0 ? ((long)a.NG * a.seg_p * a.H + 7) / 8 * 8 * a.tiles_p : 0;
   if (!tree_args_ok(a) || (a.sets == 2 && dtype == kF32) || a.runs < 1 || a.min_run < 1 || a.own_wgs < 1 ||
       (long)a.own_wgs * (a.sets ? 4 : 1) < (long)a.runs * a.H || !a.o_part || !a.lse_part || !a.desc || a.n_pre != pre ||
-      a.pieces < a.runs + a.R * (long)a.tiles || a.piece_cols < (a.sets ? 16 * a.sets : tree_cols(dtype)) || a.own0 != (size_t)a.T * a.H * a.G * a.seg_pre || (a.first != 0 && a.first != a.n_pre) ||
+      a.pieces < a.runs + a.R * (long)a.tiles || a.piece_cols < (a.sets ? 16 * a.sets : tree_cols(dtype)) || a.own0 != (size_t)a.held * a.H * a.G * a.seg_pre || (a.n_pre > 0 && a.held < 1) || (a.first != 0 && a.first != a.n_pre) ||
       (a.n_pre > 0 && (a.cp < 64 || a.cp % 64 != 0 || a.depth < 1)) || ((long)a.own_wgs + a.n_pre) * 256 > 0xffffffffL)
     return hipErrorInvalidValue;
   PARROT_TREE_LAUNCH(launch_partials_t, 0);

@@ -27,7 +27,8 @@ struct TreeArgs {
   float scale_log2;
 
   // Split plan only.  Partial results: outputs o_part [slot][D] (normalised) and log-sum-exps
-  // lse_part [slot] (base 2).  The first [T][HQ][seg_pre] slots are the prefixes': entry
+  // lse_part [slot] (base 2).  The first [held][HQ][seg_pre] slots are the prefixes': for each
+  // row of a request that has any, counted in request order (`held` bounds them), entry
   // l * seg_p + c is chunk c of the prefix at level l of the request's chain (0: outermost).
   // From own0 on, [H][pieces][piece_cols] are the own tokens': tile t of request r, cut by run
   // u, is piece u + r * tiles + t.  Along the cost each next piece takes the next run or the
@@ -35,7 +36,7 @@ struct TreeArgs {
   // not with the rows times the pieces a row may have.
   float* o_part; float* lse_part;
   size_t own0;
-  int pieces, piece_cols;
+  int held, pieces, piece_cols;
   int* desc;                             // [T][kTreeDesc]: what the join needs of each row
   int seg, seg_p, seg_pre;               // seg: partial results of a row, at most
   int cp;                                // prefix chunk tokens
@@ -52,8 +53,8 @@ struct TreeArgs {
 // Row descriptor: cost of the first unit of the row's first column tile, cost between
 // tiles, units, run length, prefix chunks of the chain's levels (outermost first, 16
 // bits each, two ints), the row within its request, its request and (bit 0) whether that has
-// prefixes.
-constexpr int kTreeDesc = 8;
+// prefixes, the row's number among those that have.
+constexpr int kTreeDesc = 12;
 
 // The partial results of a row: its prefix chunks, outermost level first (lo, hi: their
 // counts, as the descriptor holds them), then `own` pieces of its own tokens.  Index i is

@@ -25,7 +25,7 @@
 // reaches 1.12), one alone 0.74.  What a piece costs beside its stages, 17 us (queries
 // and masks after the row lists, the first stages, the masked ones, the partial results,
 // instructions fetched for the first time), bounds the short ones.  The 16-bit instances for
-// heads of 128 keep three waves a SIMD by spilling: k_tree_partials 31 vector and 167 scalar
+// heads of 128 keep three waves a SIMD by spilling: k_tree_partials 31 vector and 147 scalar
 // registers, k_tree_decode 2 and 49, stored and loaded outside the stage loops, once a piece.
 //
 // Mask: drafted tokens follow the cached ones, from own position `base` on.  The
@@ -61,6 +61,7 @@ struct Lds {
   unsigned mask[kMaskWords][kCols<DT>];   // visible drafted tokens of each column
   int tbl[kTreeSpan];                     // block ids of the current span, clamped
   int rows[kCols<DT> + 2];                // q rows that hold the tile's columns
+  int held[kCols<DT> + 1];                // prefix tiles: their numbers among rows with prefixes
   unsigned bad[kRing3][4];                // tokens of a stage with cleared values, a bit each
 };
 // three workgroups of a CU share its 160 KiB, handed out in pieces of 1280 bytes

@@ -206,3 +206,21 @@ def test_parents_that_stop_early(path):
                      "root_tokens": torch.zeros(3, dtype=torch.int32).cuda()})()
     torch.cuda.synchronize()
     assert (ver.accept_rows[n:] == -77).all() and (ver.accept_rows[:n] >= -1).all() and ver.accept_lens[2] == 0
+
+
+@pytest.mark.parametrize("dtype,dim,most", [("float16", 128, 5), ("bfloat16", 64, 12), ("float32", 128, 9)])
+def test_few_rows_with_prefixes(path, dtype, dim, most):
+    """Two requests of seventy read long prefixes, in many chunks: the partial results of those
+    rows alone are kept, and the others' stand elsewhere."""
+    rng = np.random.default_rng(most)
+    rows = [int(x) for x in rng.integers(0, most + 1, 70)]
+    rows[9], rows[66] = most, most - 1
+    cached = [int(x) for x in rng.integers(1, 60, 70)]
+    groups = [-1] * 70
+    groups[9], groups[66] = 1, 0
+    plan = du.tree_plan(dtype, 2, dim, groups, [2900, 333], cached, rows, [-1, 0], seed=1)
+    batch, off = du.make_batch(plan, seed=2), du.offsets_of(rows)
+    up = du.random_trees(rng, rows)
+    q = du.queries(int(off[-1]) + 4, 4, dim, dtype)
+    out, lse, _, _ = run(plan, batch, q, off, up)
+    check(plan, batch, q, off, up, out, lse, what=f"{path} {dtype} {dim} few rows with prefixes")
