@@ -610,6 +610,120 @@ parrot_status parrot_tree_commit(
     void* stream, const parrot_trace* trace);
 
 /*
+ * Caches held in 8 bits.  A block holds 16 tokens of each cache head as codes (OCP e4m3) with one
+ * scale for the head's keys and one for its values:
+ *   scales               uint8 [num_blocks][H][2] (keys, values): byte b, 1 .. 254, stands for
+ *                        2^(b - 127) (OCP e8m0); 0 is the scale of a block of zeros.  4-byte
+ *                        aligned, readable up to the next multiple of 4 bytes
+ *   k                    uint8 [num_blocks][H][16][D], 16-byte aligned
+ *   v                    uint8 [num_blocks][H][D / 64][4][16][4][4], 16-byte aligned: token
+ *                        4 g + t, element 64 x + 4 c + d of the head at [x][g][c][d][t] (the order
+ *                        in which the matrix cores take them)
+ * and an element's value is its code times the scale.  p->dtype is the type of rows, queries
+ * and outputs.  Blocks, tables and lengths are as for the other caches.
+ */
+typedef struct { void* k; void* v; void* scales; } parrot_cache8;
+
+/*
+ * parrot_rotary_fill into a cache held in 8 bits: the rows are normalised, rotated and assigned
+ * as there, queries written to q_out in dtype.  Of each block and head that new rows go to, with y
+ * their keys (or values) in fp32:
+ *   need   the least power of two, at least 2^-126, with |y| <= 448 need for every finite y
+ *          (0 when all of them are zero),
+ *   scale  need when the rows hold the block's first slot, else the larger of need and the
+ *          block's scale so far,
+ *   codes  y / scale rounded to the nearest, ties to even; NaN for a y that is no finite number.
+ * Where a scale grows, the tokens that the block held before are brought to it by the same
+ * rounding (a code's bits stay unless it falls below 2^-6 of the scale).  Slots behind a block's
+ * last row stay as they were.  No two requests may share a block that new rows go to.  Other
+ * arguments, padding and errors as parrot_rotary_fill.
+ */
+parrot_status parrot_cache8_fill(
+    const parrot_problem* p, const parrot_fill_rows* rows, const parrot_rotary* rotary,
+    const void* q, const void* k, const void* v,
+    const void* q_norm, const void* k_norm,
+    const int32_t* positions, const int32_t* query_offsets,
+    const int32_t* suffix_block_tables, const int32_t* suffix_lens,
+    void* q_out, const parrot_cache8* suffix,
+    void* stream, const parrot_trace* trace);
+
+/*
+ * Attention over caches held in 8 bits, for single tokens, chains of drafted tokens and prompts
+ * (Section 5.3 for the sharing; Section 7, Fill and Generate).  Request r's last Q_r own tokens are
+ * its rows, as in parrot_shared_prefix_prefill: row query_offsets[r] + j is own position
+ * S_r - Q_r + j and attends to the prefixes of r's group chain and r's own tokens up to itself.
+ * Query heads may outnumber the cache's heads (query head i reads cache head i / (HQ / H)).
+ *   out, lse             the decode formula over those keys; both NaN for a row with a logit of NaN
+ *                        or +inf, or whose logits are all -inf.  16-bit types: the weights
+ *                        are rounded to dtype for their product with V and divided by the
+ *                        rounded ones' sum.  float32: weights and logits in fp32
+ * Keys and values of tokens a row does not see never reach its result, whatever they hold.
+ *
+ * What a step reads is laid out by parrot_cache8_plan, once for all layers of the step: it depends on
+ * the row offsets, lengths and groups alone, and on the problem's and rows' fields but for
+ * sm_scale and the block counts.  Neither call synchronises, and both may be captured into a graph.
+ *   rows                 (host) as for a tree call, but max_query_rows may reach max_suffix_len
+ *   plan                 >= parrot_cache8_plan_bytes(p, rows) bytes, 256-byte aligned: written by
+ *                        parrot_cache8_plan, only read by parrot_cache8_attention (calls
+ *                        on several streams may share it).  A call with a plan of other rows,
+ *                        lengths or groups gives unspecified values, and no access leaves the
+ *                        buffers that p and rows describe
+ *   prefix_parents       as parrot_nested_prefix_decode, or NULL for flat groups
+ *   prefix               (may be NULL when num_groups = 0)
+ *   q, out               [T][HQ][D] dtype, 16-byte aligned;  lse float32 [T][HQ]
+ *   workspace            >= parrot_cache8_workspace_bytes(p, rows) bytes, 256-byte aligned;
+ *                        contents on entry are ignored
+ * Rows from query_offsets[R] on are padding: their out and lse are left as they were (so one
+ * captured graph serves batches of fewer rows).  Both sizes depend on the current device's compute
+ * units, like parrot_workspace_bytes.  For the same heads, head_dim and dtype they never decrease as
+ * num_requests, num_groups, max_prefix_len, max_suffix_len, max_prefix_depth or the row counts
+ * grow.  (size_t)-1 if the arguments are invalid, 0 when T = 0.
+ */
+size_t parrot_cache8_plan_bytes(const parrot_problem* p, const parrot_tree_rows* rows);
+size_t parrot_cache8_workspace_bytes(const parrot_problem* p, const parrot_tree_rows* rows);
+
+parrot_status parrot_cache8_plan(
+    const parrot_problem* p, const parrot_tree_rows* rows,
+    const int32_t* query_offsets, const int32_t* prefix_lens, const int32_t* prefix_parents,
+    const int32_t* suffix_lens, const int32_t* group_ids,
+    void* plan, size_t plan_bytes, void* stream);
+
+parrot_status parrot_cache8_attention(
+    const parrot_problem* p, const parrot_tree_rows* rows,
+    const void* q, const parrot_cache8* prefix, const parrot_cache8* suffix,
+    const int32_t* prefix_block_tables, const int32_t* suffix_block_tables,
+    const void* plan, size_t plan_bytes,
+    void* out, float* lse,
+    void* workspace, size_t workspace_bytes,
+    void* stream, const parrot_trace* trace);
+
+/* parrot_validate_tree_inputs (without parents of rows) for a call over 8 bits. */
+parrot_status parrot_validate_cache8_inputs(
+    const parrot_problem* p, const parrot_tree_rows* rows, const int32_t* query_offsets,
+    const int32_t* prefix_block_tables, const int32_t* prefix_lens,
+    const int32_t* prefix_parents,
+    const int32_t* suffix_block_tables, const int32_t* suffix_lens,
+    const int32_t* group_ids, int32_t* scratch, void* stream);
+
+/*
+ * Copies cache blocks: block dst[i] of every pool becomes block src[i] of it, for
+ * i < num_copies, in one launch (a fork's last block, blocks moved together; the lists come from
+ * parrot_store_take_copies).  Any cache: a pool is an array of blocks of block_bytes bytes each.
+ *   pools                (host) [num_pools]; base 16-byte aligned where block_bytes is a
+ *                        multiple of 16, else 2-byte; block_bytes even
+ *   num_blocks           blocks of every pool (of the smallest)
+ *   src, dst             int32 [num_copies] block ids.  Pairs with an id outside
+ *                        [0, num_blocks) are skipped (pad with -1).  No dst may be
+ *                        another pair's src or dst
+ */
+typedef struct { void* base; int64_t block_bytes; } parrot_block_pool;
+
+parrot_status parrot_copy_blocks(
+    const parrot_block_pool* pools, int32_t num_pools, int32_t num_blocks,
+    const int32_t* src, const int32_t* dst, int32_t num_copies,
+    void* stream, const parrot_trace* trace);
+
+/*
  * Measurement aid: the device's attainable HBM read bandwidth, the ceiling of
  * the bandwidth-bound decode kernels (Section 8.3: token generation is bound
  * by memory bandwidth).  Reads every byte of

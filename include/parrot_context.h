@@ -63,6 +63,29 @@ parrot_status parrot_store_truncate(parrot_context_store* st, int32_t ctx, int32
 /* FreeContext: release the context's own blocks and its references. */
 parrot_status parrot_store_free(parrot_context_store* st, int32_t ctx);
 
+/* Fork: a new context with the tokens of `ctx` (Section 7: contexts forked from contexts; sampling
+ * several continuations of one context).  Prefixes and own blocks are shared; the own ones
+ * until one of the sharers appends into the last one, which gets a copy of it then
+ * (parrot_store_take_copies), or truncates and appends.  Fork a context whose tokens are all in the
+ * cache.  Returns the new context id (>= 0); -1 without host memory; -2 for an unknown context. */
+int32_t parrot_store_fork(parrot_context_store* st, int32_t ctx);
+
+/* Compaction: moves blocks in use from the highest ids to the lowest free ones, `most` blocks at
+ * most, so that the tail of the pools falls free.  The moves are copies to take
+ * (parrot_store_take_copies); tables built from here on hold the new ids.  Returns the number
+ * of blocks moved; -1 without host memory, -2 on bad arguments. */
+int32_t parrot_store_compact(parrot_context_store* st, int32_t most);
+
+/* The block copies that appends after a fork and compactions owe, as parrot_copy_blocks takes them: no
+ * destination is another copy's source or destination.  Take them and enqueue their copy before the next call
+ * that writes the cache; blocks that they read are not handed out before.  take_copies gives
+ * all of them (PARROT_ERR_WORKSPACE_TOO_SMALL when there are more than `most`) and forgets them. */
+int32_t parrot_store_num_copies(const parrot_context_store* st);
+parrot_status parrot_store_take_copies(parrot_context_store* st, int32_t* src, int32_t* dst, int32_t most);
+
+/* One past the highest block id in use. */
+int32_t parrot_store_block_end(const parrot_context_store* st);
+
 int32_t parrot_store_free_blocks(const parrot_context_store* st);
 int32_t parrot_store_num_prefixes(const parrot_context_store* st);   /* cached trie nodes */
 /* Tokens of a context: cached prefix tokens of its path and own tokens

@@ -114,6 +114,14 @@ class ParrotTreeRows(ctypes.Structure):
     ]
 
 
+class ParrotCache8(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
+
+
+class ParrotBlockPool(ctypes.Structure):
+    _fields_ = [("base", ctypes.c_void_p), ("block_bytes", ctypes.c_int64)]
+
+
 EXPORTED = (
     "parrot_workspace_bytes", "parrot_shared_prefix_decode", "parrot_per_request_decode",
     "parrot_nested_prefix_decode", "parrot_shared_prefix_decode_append",
@@ -124,6 +132,8 @@ EXPORTED = (
     "parrot_rotary_init", "parrot_rotary_from_frequencies", "parrot_rotary_fill",
     "parrot_tree_workspace_bytes", "parrot_shared_prefix_tree_decode", "parrot_validate_tree_inputs",
     "parrot_tree_accept", "parrot_tree_commit",
+    "parrot_cache8_fill", "parrot_cache8_plan_bytes", "parrot_cache8_workspace_bytes", "parrot_cache8_plan",
+    "parrot_cache8_attention", "parrot_validate_cache8_inputs", "parrot_copy_blocks",
 )
 
 STATIC_SCRATCH_BYTES = 64 << 20   # PARROT_STATIC_SCRATCH_BYTES
@@ -194,6 +204,21 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     for name, args in drafting.items():
         getattr(lib, name).argtypes = args
         getattr(lib, name).restype = ctypes.c_int
+    cache8_p = ctypes.POINTER(ParrotCache8)
+    cache8 = {
+        "parrot_cache8_fill": [prob_p, ctypes.POINTER(ParrotFillRows), rotary_p] + [vp] * 10 + [cache8_p, vp, trace_p],
+        "parrot_cache8_plan": [prob_p, tree_p] + [vp] * 6 + [sz, vp],
+        "parrot_cache8_attention": [prob_p, tree_p, vp, cache8_p, cache8_p] + [vp] * 3 + [sz] + [vp] * 3 + [sz, vp, trace_p],
+        "parrot_validate_cache8_inputs": [prob_p, tree_p] + [vp] * 9,
+        "parrot_copy_blocks": [ctypes.POINTER(ParrotBlockPool), ctypes.c_int32, ctypes.c_int32, vp, vp, ctypes.c_int32,
+                               vp, trace_p],
+    }
+    for name, args in cache8.items():
+        getattr(lib, name).argtypes = args
+        getattr(lib, name).restype = ctypes.c_int
+    for name in ("parrot_cache8_plan_bytes", "parrot_cache8_workspace_bytes"):
+        getattr(lib, name).argtypes = [prob_p, tree_p]
+        getattr(lib, name).restype = sz
     lib.parrot_tree_workspace_bytes.argtypes = [prob_p, tree_p]
     lib.parrot_tree_workspace_bytes.restype = sz
     lib.parrot_last_error.argtypes = []

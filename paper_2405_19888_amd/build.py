@@ -22,6 +22,7 @@ LIB_PATH = os.path.join(PKG, LIB_NAME)
 
 SOURCES = ["api.hip", "partials.hip", "direct.hip", "prefill.hip", "merge.hip", "ceiling.hip",
            "draft_api.hip", "rotary.hip", "tree.hip", "accept.hip",
+           "cache8_api.hip", "cache8_fill.hip", "cache8_attend.hip", "blocks.hip",
            "context_store.cpp"]
 
 # Packed fp32 arithmetic is disabled: the kernels write only scalar float code.

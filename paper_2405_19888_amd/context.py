@@ -18,7 +18,8 @@ STORE_EXPORTED = (
     "parrot_store_create", "parrot_store_destroy", "parrot_store_fill", "parrot_store_append",
     "parrot_store_truncate", "parrot_store_free", "parrot_store_free_blocks", "parrot_store_num_prefixes",
     "parrot_store_prefix_tokens", "parrot_store_own_tokens", "parrot_store_batch_shape",
-    "parrot_store_build_batch",
+    "parrot_store_build_batch", "parrot_store_fork", "parrot_store_compact", "parrot_store_num_copies",
+    "parrot_store_take_copies", "parrot_store_block_end",
 )
 
 
@@ -46,7 +47,13 @@ def _lib():
     lib.parrot_store_truncate.restype = ctypes.c_int
     lib.parrot_store_free.argtypes = [vp, i32]
     lib.parrot_store_free.restype = ctypes.c_int
-    for name in ("parrot_store_free_blocks", "parrot_store_num_prefixes"):
+    for name in ("parrot_store_fork", "parrot_store_compact"):
+        getattr(lib, name).argtypes = [vp, i32]
+        getattr(lib, name).restype = i32
+    lib.parrot_store_take_copies.argtypes = [vp, ip, ip, i32]
+    lib.parrot_store_take_copies.restype = ctypes.c_int
+    for name in ("parrot_store_free_blocks", "parrot_store_num_prefixes", "parrot_store_num_copies",
+                 "parrot_store_block_end"):
         getattr(lib, name).argtypes = [vp]
         getattr(lib, name).restype = i32
     for name in ("parrot_store_prefix_tokens", "parrot_store_own_tokens"):
@@ -120,6 +127,42 @@ class ContextStore:
 
     def free(self, ctx: int):
         _check(self._lib.parrot_store_free(self._h, int(ctx)))
+
+    def fork(self, ctx: int) -> int:
+        """A new context with the same tokens, sharing the blocks until one of them appends
+        into the last one (see take_copies)."""
+        c = self._lib.parrot_store_fork(self._h, int(ctx))
+        if c == -1:
+            raise MemoryError("no host memory for a context")
+        if c < 0:
+            raise ValueError(f"unknown context {ctx}")
+        return int(c)
+
+    def compact(self, most: int | None = None) -> int:
+        """Move blocks in use from the highest ids to the lowest free ones (at most
+        `most`); returns how many.  See take_copies."""
+        n = self._lib.parrot_store_compact(self._h, self.num_blocks if most is None else int(most))
+        if n == -1:
+            raise MemoryError("no host memory to compact")
+        if n < 0:
+            raise ValueError("most is negative")
+        return int(n)
+
+    @property
+    def num_copies(self) -> int:
+        return int(self._lib.parrot_store_num_copies(self._h))
+
+    def take_copies(self):
+        """(src, dst) int32 arrays of the block copies owed since the last call, for
+        copy_blocks: enqueue them before the next call that writes the cache."""
+        src, dst = np.zeros(self.num_copies, np.int32), np.zeros(self.num_copies, np.int32)
+        _check(self._lib.parrot_store_take_copies(self._h, _iptr(src), _iptr(dst), len(src)))
+        return src, dst
+
+    @property
+    def block_end(self) -> int:
+        """One past the highest block id in use."""
+        return int(self._lib.parrot_store_block_end(self._h))
 
     @property
     def free_blocks(self) -> int:

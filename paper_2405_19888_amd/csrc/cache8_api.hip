@@ -1,0 +1,296 @@
+// C ABI of caches held in 8 bits: fill of new rows, plan and attention; and copies of cache blocks.
+// Argument checks, sizing and launches; host scalars only.
+#include <algorithm>
+#include <cmath>
+
+#include "cache8_args.h"
+#include "host.h"
+
+using parrot::set_error;
+
+namespace {
+
+#define PARROT_TRY(x) do { parrot_status _s = (x); if (_s != PARROT_OK) return _s; } while (0)
+
+long ceil_div(long a, long b) { return (a + b - 1) / b; }
+hipEvent_t ev(void* p) { return reinterpret_cast<hipEvent_t>(p); }
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+parrot_status bad(const char* fmt, long a = 0, long b = 0) {
+  return set_error(PARROT_ERR_INVALID_ARGUMENT, fmt, a, b);
+}
+
+parrot_status launched(hipError_t e, const char* what) {
+  if (e != hipSuccess) return set_error(PARROT_ERR_HIP, "%s launch failed: %s", what, hipGetErrorString(e));
+  return set_error(PARROT_OK, "");
+}
+
+parrot_status check_pool(const parrot_cache8* c, const char* name) {
+  if (!c) return set_error(PARROT_ERR_INVALID_ARGUMENT, "%s is NULL", name);
+  char k[32], v[32], s[32];
+  snprintf(k, sizeof k, "%s->k", name);
+  snprintf(v, sizeof v, "%s->v", name);
+  snprintf(s, sizeof s, "%s->scales", name);
+  const parrot::PtrCheck need[] = {{c->k, k, 16}, {c->v, v, 16}, {c->scales, s, 4}};
+  return parrot::check_pointers(need);
+}
+parrot::Pool8 pool(const parrot_cache8* c) { return {c->k, c->v, c->scales}; }
+
+// ----------------------------------------------------------------- attention
+struct Plan8 {
+  int depth;                       // levels of prefixes that the plan has room for
+  int sets, cols, runs, min_run;
+  bool wide;                       // neighbouring waves take runs of one head, else neighbouring heads
+  int max_entries;
+  long slots;
+  parrot::Plan8Layout at;
+  size_t plan_bytes, o_bytes, lse_bytes;
+};
+
+constexpr int kMinRun = 6;         // cost of a run at least: four units and a tile's setup
+
+parrot_status check_attend(const parrot_problem* p, const parrot_tree_rows* rows, Plan8* pl) {
+  PARROT_TRY(parrot::check_problem_fields(p));
+  if (!rows) return bad("rows is NULL");
+  *pl = Plan8{};
+  const long T = rows->num_query_rows, R = p->num_requests, H = p->num_heads, NG = p->num_groups;
+  if (T < 0) return bad("num_query_rows %ld < 0", T);
+  if (T == 0) return PARROT_OK;
+  if (R == 0) return bad("num_query_rows %ld > 0 with no requests", T);
+  if (rows->max_query_rows < 1 || rows->max_query_rows > p->max_suffix_len)
+    return bad("max_query_rows %ld not in [1, max_suffix_len = %ld]", rows->max_query_rows, p->max_suffix_len);
+  if (rows->num_query_heads < 1 || rows->num_query_heads % H != 0)
+    return bad("num_query_heads %ld is not a multiple of num_heads %ld", rows->num_query_heads, H);
+  if (NG > 0 && (rows->max_group_rows < 0 || rows->max_group_rows > T))
+    return bad("max_group_rows %ld not in [0, num_query_rows]", rows->max_group_rows);
+  if (T * rows->num_query_heads > 0x7fffffffL)
+    return set_error(PARROT_ERR_UNSUPPORTED, "num_query_rows * num_query_heads > 2^31 - 1");
+  const long G = rows->num_query_heads / H, cus = parrot::device_cus();
+  const bool f32 = p->dtype == PARROT_DTYPE_F32;
+  pl->depth = NG > 0 ? std::max(1, (int)p->max_prefix_depth) : 0;
+  const long most = G * std::max((long)rows->max_query_rows, NG > 0 ? (long)rows->max_group_rows : 0L);
+  pl->sets = most <= 16 ? 1 : most <= 32 || f32 ? 2 : 4;
+  pl->cols = 16 * pl->sets;
+  pl->wide = most > pl->cols;
+  // four waves a CU hold 64 KiB on their way, and a tile of 64 columns leaves room for no more
+  const long waves = cus * (pl->sets > 2 || (f32 && pl->sets > 1) ? 4 : 8);
+  pl->runs = (int)std::max(1L, waves / H);
+  pl->min_run = kMinRun;
+  // column tiles: those that columns fill, and one more for each sequence (sizes as for the
+  // narrowest tiles and the most slots of calls of fewer columns, so that they never decrease)
+  const long tiles = (1 + pl->depth) * T * G / 16 + R + NG;
+  const long units = ceil_div(std::max(p->max_suffix_len, NG > 0 ? p->max_prefix_len : 0), parrot::kUnit);
+  long spread = 16 * std::max(1L, cus * 8 / H);
+  if (pl->sets > 1) spread = std::max(spread, 32 * std::max(1L, cus * (f32 ? 4 : 8) / H));
+  if (pl->sets > 2) spread = std::max(spread, 64 * std::max(1L, cus * 4 / H));
+  pl->slots = (1 + pl->depth) * T * G + spread;
+  const double ints = (double)tiles * (1 + parrot::kEntryInts) + (double)T * (parrot::kRowInts + pl->depth) +
+                      (NG + R) * (1.0 + parrot::kMaxDepth) + (parrot::kPlanWaves + 1.0) * NG;
+  if (((1.0 + pl->depth) * T * G / pl->cols + R + NG) * (units + parrot::kPieceSetup) > 1.5e9 || pl->slots > 0x7fffffffL || ints > 1.0e9 ||
+      R + NG > 0x3fffffffL || pl->runs * H * 64 > 0xffffffffL || T * ceil_div(rows->num_query_heads, 2) * 256 > 0xffffffffL)
+    return set_error(PARROT_ERR_UNSUPPORTED, "attention over 8 bits: %ld rows in %ld column tiles of %ld units", T, tiles, units);
+  pl->max_entries = (int)tiles;
+  auto& at = pl->at;
+  long n = parrot::kPlanHead;
+  auto take = [&n](long ints) { const long first = n; n = (n + ints + 3) & ~3L; return first; };
+  at.head = 0;
+  at.cost = take(tiles);
+  at.entry = take(tiles * parrot::kEntryInts);
+  at.row = take(T * parrot::kRowInts);
+  at.list = take(T * std::max(pl->depth, 1));
+  at.seq = take(NG + R + 1);
+  at.pos = take(R * parrot::kMaxDepth);
+  at.count = take((parrot::kPlanWaves + 1) * NG + 1);
+  at.total = n;
+  pl->plan_bytes = align256((size_t)n * sizeof(int32_t));
+  pl->o_bytes = align256((size_t)H * pl->slots * p->head_dim * sizeof(float));
+  pl->lse_bytes = align256((size_t)H * pl->slots * sizeof(float));
+  return PARROT_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+parrot_status parrot_cache8_fill(
+    const parrot_problem* p, const parrot_fill_rows* rows, const parrot_rotary* rotary, const void* q, const void* k,
+    const void* v, const void* q_norm, const void* k_norm, const int32_t* positions, const int32_t* query_offsets,
+    const int32_t* suffix_block_tables, const int32_t* suffix_lens, void* q_out, const parrot_cache8* suffix, void* stream,
+    const parrot_trace* trace) {
+  PARROT_TRY(parrot::check_fill(p, rows));
+  if (rows->num_query_rows == 0) return set_error(PARROT_OK, "");
+  parrot::Fill8Args a{};
+  int partner;
+  PARROT_TRY(parrot::fill_args(p, rows, rotary, q, k, v, q_norm, k_norm, positions, query_offsets, suffix_block_tables,
+                               suffix_lens, q_out, &a.f, &partner));
+  PARROT_TRY(check_pool(suffix, "suffix"));
+  if (suffix->k == suffix->v) return bad("suffix->k and suffix->v are the same pool");
+  a.f.sk = suffix->k; a.f.sv = suffix->v; a.scales = suffix->scales;
+  const long elt = p->dtype == PARROT_DTYPE_F32 ? 4 : 2;
+  const long units = rows->max_query_rows == 1 ? p->num_requests : rows->num_query_rows / 16 + 2L * p->num_requests;
+  parrot::fill_slabs(&a.f, 4096 / (p->head_dim * elt), std::max(1L, std::min((long)rows->num_query_rows, units)));
+  if (units * a.f.slabs * 256 > 0xffffffffL)
+    return set_error(PARROT_ERR_UNSUPPORTED, "fill needs %ld workgroups", units * a.f.slabs);
+  a.units = (int)units;
+  return launched(parrot::launch_fill8(a, partner, (int)p->dtype, p->head_dim, reinterpret_cast<hipStream_t>(stream),
+                                       trace ? ev(trace->partials_start) : nullptr,
+                                       trace ? ev(trace->partials_stop) : nullptr),
+                  "8-bit fill kernel");
+}
+
+size_t parrot_cache8_plan_bytes(const parrot_problem* p, const parrot_tree_rows* rows) {
+  Plan8 pl;
+  if (check_attend(p, rows, &pl) != PARROT_OK) return (size_t)-1;
+  set_error(PARROT_OK, "");
+  return pl.plan_bytes;
+}
+
+size_t parrot_cache8_workspace_bytes(const parrot_problem* p, const parrot_tree_rows* rows) {
+  Plan8 pl;
+  if (check_attend(p, rows, &pl) != PARROT_OK) return (size_t)-1;
+  set_error(PARROT_OK, "");
+  return pl.o_bytes + pl.lse_bytes;
+}
+
+parrot_status parrot_cache8_plan(
+    const parrot_problem* p, const parrot_tree_rows* rows, const int32_t* query_offsets, const int32_t* prefix_lens,
+    const int32_t* prefix_parents, const int32_t* suffix_lens, const int32_t* group_ids, void* plan, size_t plan_bytes,
+    void* stream) {
+  Plan8 pl;
+  PARROT_TRY(check_attend(p, rows, &pl));
+  if (rows->num_query_rows == 0) return set_error(PARROT_OK, "");
+  const parrot::PtrCheck need[] = {{query_offsets, "query_offsets", 4}, {suffix_lens, "suffix_lens", 4},
+                                   {group_ids, "group_ids", 4}, {plan, "plan", 256}};
+  PARROT_TRY(parrot::check_pointers(need));
+  if (p->num_groups > 0) {
+    const parrot::PtrCheck pre[] = {{prefix_lens, "prefix_lens", 4}};
+    PARROT_TRY(parrot::check_pointers(pre));
+    if (prefix_parents && reinterpret_cast<uintptr_t>(prefix_parents) % 4)
+      return bad("prefix_parents is not 4-byte aligned");
+  }
+  if (plan_bytes < pl.plan_bytes)
+    return set_error(PARROT_ERR_WORKSPACE_TOO_SMALL, "plan is %zu bytes, need %zu", plan_bytes, pl.plan_bytes);
+  parrot::Plan8Args a{};
+  a.qoff = query_offsets; a.plen = prefix_lens; a.slen = suffix_lens; a.gid = group_ids;
+  a.parents = p->num_groups > 0 ? prefix_parents : nullptr;
+  a.plan = reinterpret_cast<int*>(plan);
+  a.at = pl.at;
+  a.T = rows->num_query_rows; a.R = p->num_requests; a.NG = p->num_groups;
+  a.G = rows->num_query_heads / p->num_heads;
+  a.depth = a.parents ? pl.depth : std::min(pl.depth, 1);
+  a.max_p = p->max_prefix_len; a.max_s = p->max_suffix_len; a.max_q = rows->max_query_rows;
+  a.cols = pl.cols; a.runs = pl.runs; a.min_run = pl.min_run;
+  a.max_entries = pl.max_entries; a.max_slots = pl.slots;
+  return launched(parrot::launch_plan8(a, reinterpret_cast<hipStream_t>(stream)), "plan kernel");
+}
+
+parrot_status parrot_cache8_attention(
+    const parrot_problem* p, const parrot_tree_rows* rows, const void* q, const parrot_cache8* prefix,
+    const parrot_cache8* suffix, const int32_t* prefix_block_tables, const int32_t* suffix_block_tables, const void* plan,
+    size_t plan_bytes, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream,
+    const parrot_trace* trace) {
+  Plan8 pl;
+  PARROT_TRY(check_attend(p, rows, &pl));
+  if (rows->num_query_rows == 0) return set_error(PARROT_OK, "");
+  const parrot::PtrCheck need[] = {{q, "q", 16}, {suffix_block_tables, "suffix_block_tables", 4}, {plan, "plan", 256},
+                                   {out, "out", 16}, {lse, "lse", 4}, {workspace, "workspace", 256}};
+  PARROT_TRY(parrot::check_pointers(need));
+  PARROT_TRY(check_pool(suffix, "suffix"));
+  if (p->num_groups > 0) {
+    PARROT_TRY(check_pool(prefix, "prefix"));
+    const parrot::PtrCheck pre[] = {{prefix_block_tables, "prefix_block_tables", 4}};
+    PARROT_TRY(parrot::check_pointers(pre));
+  }
+  if (q == out) return bad("out is q");
+  if (plan_bytes < pl.plan_bytes)
+    return set_error(PARROT_ERR_WORKSPACE_TOO_SMALL, "plan is %zu bytes, need %zu", plan_bytes, pl.plan_bytes);
+  if (workspace_bytes < pl.o_bytes + pl.lse_bytes)
+    return set_error(PARROT_ERR_WORKSPACE_TOO_SMALL, "workspace is %zu bytes, need %zu", workspace_bytes, pl.o_bytes + pl.lse_bytes);
+  parrot::Attend8Args a{};
+  a.q = q; a.out = out; a.lse = lse;
+  a.own = pool(suffix);
+  if (p->num_groups > 0) a.pre = pool(prefix);
+  a.ptab = prefix_block_tables; a.stab = suffix_block_tables;
+  a.plan = reinterpret_cast<const int*>(plan);
+  a.at = pl.at;
+  a.o_part = reinterpret_cast<float*>(workspace);
+  a.lse_part = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + pl.o_bytes);
+  a.slots = pl.slots;
+  a.T = rows->num_query_rows; a.R = p->num_requests; a.H = p->num_heads; a.NG = p->num_groups;
+  a.G = rows->num_query_heads / p->num_heads; a.depth = pl.depth;
+  a.pstride = p->prefix_table_stride; a.sstride = p->suffix_table_stride;
+  a.max_p = p->num_groups > 0 ? p->max_prefix_len : 0; a.max_s = p->max_suffix_len;
+  a.npblk = p->num_groups > 0 ? p->num_prefix_blocks : 1; a.nsblk = p->num_suffix_blocks;
+  a.runs = pl.runs; a.sets = pl.sets; a.wide = pl.wide; a.max_entries = pl.max_entries;
+  a.flip = p->sm_scale < 0.f;
+  a.scale_log2 = std::fabs(p->sm_scale) * parrot::kLog2e;
+  const parrot_trace none = {nullptr, nullptr, nullptr, nullptr};
+  const parrot_trace& tr = trace ? *trace : none;
+  const int dt = (int)p->dtype, D = p->head_dim;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  PARROT_TRY(launched(parrot::launch_attend8(a, dt, D, s, ev(tr.partials_start), ev(tr.partials_stop)), "8-bit attention kernel"));
+  return launched(parrot::launch_join8(a, dt, D, s, ev(tr.merge_start), ev(tr.merge_stop)), "8-bit join kernel");
+}
+
+parrot_status parrot_validate_cache8_inputs(
+    const parrot_problem* p, const parrot_tree_rows* rows, const int32_t* query_offsets,
+    const int32_t* prefix_block_tables, const int32_t* prefix_lens, const int32_t* prefix_parents,
+    const int32_t* suffix_block_tables, const int32_t* suffix_lens, const int32_t* group_ids, int32_t* scratch,
+    void* stream) {
+  Plan8 pl;
+  PARROT_TRY(check_attend(p, rows, &pl));
+  if (rows->num_query_rows == 0) return set_error(PARROT_OK, "");
+  const parrot_prefill_rows as_prefill = {rows->num_query_rows, rows->max_query_rows, rows->max_group_rows};
+  const parrot::ValidateTree tree = {nullptr};
+  return parrot::validate_inputs(p, prefix_block_tables, prefix_lens, prefix_parents, suffix_block_tables,
+                                 suffix_lens, group_ids, scratch, stream, &as_prefill, query_offsets, &tree);
+}
+
+// -------------------------------------------------------------------- blocks
+parrot_status parrot_copy_blocks(const parrot_block_pool* pools, int32_t num_pools, int32_t num_blocks, const int32_t* src,
+                                 const int32_t* dst, int32_t num_copies, void* stream, const parrot_trace* trace) {
+  if (num_pools < 0) return bad("num_pools %ld < 0", num_pools);
+  if (num_copies < 0) return bad("num_copies %ld < 0", num_copies);
+  if (num_blocks < 1) return bad("num_blocks %ld < 1", num_blocks);
+  if (num_pools > 0 && !pools) return bad("pools is NULL");
+  if (num_pools == 0 || num_copies == 0) return set_error(PARROT_OK, "");
+  const parrot::PtrCheck need[] = {{src, "src", 4}, {dst, "dst", 4}};
+  PARROT_TRY(parrot::check_pointers(need));
+  if (src == dst) return bad("src and dst are the same array");
+  for (int32_t i = 0; i < num_pools; ++i) {
+    const parrot_block_pool& x = pools[i];
+    if (!x.base) return bad("pool %ld is NULL", i);
+    if (x.block_bytes < 2 || x.block_bytes % 2 != 0 || x.block_bytes > (1LL << 31))
+      return bad("block_bytes of pool %ld is not even and in [2, 2^31]", i);
+    if (reinterpret_cast<uintptr_t>(x.base) % (x.block_bytes % 16 ? 2 : 16)) return bad("pool %ld is not aligned", i);
+  }
+  // pools whose blocks have one size go together
+  int32_t done = 0;
+  while (done < num_pools) {
+    parrot::CopyArgs a{};
+    a.src = src; a.dst = dst; a.blocks = num_blocks;
+    const int32_t first = done;
+    for (; done < num_pools && done - first < parrot::kCopyPools; ++done) {
+      a.base[done - first] = pools[done].base;
+      a.bytes[done - first] = (unsigned)pools[done].block_bytes;
+    }
+    a.pools = done - first;
+    // a launch holds less than 2^32 threads
+    long most = 0;
+    for (int i = 0; i < a.pools; ++i) most = std::max(most, (long)a.bytes[i]);
+    const long each = ceil_div(most, 16384) * a.pools * 256, at_once = std::max(1L, 0xf0000000L / each);
+    if (each > 0xf0000000L) return set_error(PARROT_ERR_UNSUPPORTED, "blocks of %ld bytes", most);
+    for (long i = 0; i < num_copies; i += at_once) {
+      a.n = (int)std::min(at_once, num_copies - i);
+      a.src = src + i; a.dst = dst + i;
+      PARROT_TRY(launched(parrot::launch_copy_blocks(a, reinterpret_cast<hipStream_t>(stream),
+                                                     trace && first == 0 && i == 0 ? ev(trace->partials_start) : nullptr,
+                                                     trace && done == num_pools && i + at_once >= num_copies
+                                                         ? ev(trace->partials_stop) : nullptr),
+                          "copy kernel"));
+    }
+  }
+  return set_error(PARROT_OK, "");
+}
+
+}  // extern "C"

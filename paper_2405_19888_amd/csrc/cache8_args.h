@@ -1,0 +1,85 @@
+// Arguments of the kernels of a cache held in 8 bits, shared by the kernels and the host
+// code, and the format itself.
+//
+// A block-head is 16 tokens of one head of one block: 16 * D codes (e4m3) of keys and as many of
+// values, and a byte each for their scales: b stands for 2^(b - 127), and a value is its code
+// times that.  Keys are row-major, [16][D].  Values are [D / 64][4][16][4][4]: token
+// 4 g + t, element 64 x + 4 c + d at [x][g][c][d][t].
+#pragma once
+
+#include "draft_args.h"
+
+namespace parrot {
+
+constexpr int kBlockTokens = 16;
+constexpr int kUnit = 32;                // tokens of a unit: two blocks, one k step of the PV product
+
+struct Pool8 { const void* k; const void* v; const void* scales; };
+
+struct Fill8Args {
+  FillArgs f;                            // sk, sv: the code pools
+  void* scales;                          // [nsblk][H][2]
+  int units;                             // (request, block) pairs, at most
+};
+hipError_t launch_fill8(const Fill8Args& a, int partner, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
+
+// Where a plan holds what, in ints from its start.  Entries are the column tiles of sequences:
+// the groups first (their columns are the rows of all requests that read the group's prefix, times
+// the query heads of a cache head), then the requests (their own rows' columns), in order.
+struct Plan8Layout {
+  long head, cost, entry, row, list, seq, pos, count, total;
+};
+constexpr int kPlanHead = 16;            // ints of the head: entries, run length, total cost, slots
+constexpr int kEntryInts = 12;
+constexpr int kRowInts = 12;
+constexpr int kPlanWaves = 16;           // waves of the planning workgroup
+constexpr int kPieceSetup = 2;           // cost of a tile beside its units
+
+// An entry: sequence (request r, or ~g), its columns [col0, col0 + ncols), cost at which it
+// starts, units, first slot of its partial results (-1: it writes the output), pieces, keys,
+// keys that every column sees, first row (group: first place in the row list).
+enum Entry8 { kEntSeq, kEntCol0, kEntCols, kEntCost, kEntUnits, kEntSlot, kEntPieces, kEntKeys, kEntBase, kEntFirst };
+// A row: entry of its request's first tile, its place in the request, levels of prefixes, then
+// for each level the entry of the group's first tile and the row's place in the group's list.
+enum Row8 { kRowEntry, kRowPlace, kRowLevels, kRowUnused, kRowGroup };
+
+struct Plan8Args {
+  const int* qoff; const int* plen; const int* parents; const int* slen; const int* gid;
+  int* plan;
+  Plan8Layout at;
+  int T, R, NG, G, depth, max_p, max_s, max_q;   // depth: levels of this call's chains
+  int cols;                              // columns of a tile
+  int runs, min_run;
+  int max_entries; long max_slots;
+};
+hipError_t launch_plan8(const Plan8Args& a, hipStream_t s);
+
+struct Attend8Args {
+  const void* q;                         // [T][HQ][D]
+  Pool8 pre, own;
+  const int* ptab; const int* stab;
+  const int* plan;
+  Plan8Layout at;
+  void* out; float* lse;                 // [T][HQ][D] dtype, [T][HQ]
+  float* o_part; float* lse_part;        // [H][slots][D] normalised, [H][slots] base 2
+  long slots;
+  int T, R, H, G, NG, depth;             // depth: levels that the plan has room for
+  int pstride, sstride, max_p, max_s, npblk, nsblk;
+  int runs, sets, wide, max_entries;     // sets: column sets of a tile; wide: a workgroup's waves take runs of one head
+  int flip;                              // sm_scale < 0: queries change sign
+  float scale_log2;                      // |sm_scale| log2(e)
+};
+hipError_t launch_attend8(const Attend8Args& a, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
+hipError_t launch_join8(const Attend8Args& a, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
+
+// A copy of blocks of several pools, each with its block's bytes (a multiple of 2).
+constexpr int kCopyPools = 128;          // pools of one launch
+struct CopyArgs {
+  void* base[kCopyPools];
+  unsigned bytes[kCopyPools];
+  const int* src; const int* dst;
+  int n, pools, blocks;
+};
+hipError_t launch_copy_blocks(const CopyArgs& a, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
+
+}  // namespace parrot

@@ -1,0 +1,381 @@
+// A wave's attention over a range of keys held in 8 bits, for up to 16 * NS columns.
+//
+// A column is a (row, query head) pair that reads the wave's cache head.  Per unit of 32
+// tokens (two blocks), with c_b the block's key scale times sm_scale log2(e):
+//   S^T = K Q^T        (tokens x columns) on the matrix cores, codes widened to the queries' type
+//   p   = 2^(c_b s - m), m a reference no more than 8 below the column's largest logit
+//   O^T += V^T P       (elements x columns), values widened and scaled by their block's 2^e
+// Widening is exact (a code has four significant bits), so the operands are the values the
+// cache stands for; the only roundings are those of P and of the fp32 sums.
+//
+// No LDS and no lane exchange: a lane's S^T values (tokens 4 g .. 4 g + 3 of a block for
+// g = lane / 16, column lane % 16) are the PV operand's k group g, and the layout of the
+// values holds the same four tokens side by side (cache8_args.h).  So a wave needs nothing but
+// its own loads, 16 bytes a lane, which come into registers 16 KiB ahead.
+//
+// Types: bfloat16 and float16 round P once, and the output is divided by the sum of the rounded
+// weights (a dominant weight's rounding cancels).  float32 queries and weights are cut into
+// three bfloat16 parts, which hold all 24 bits: three products for one, at 16 times the rate of
+// the fp32 ones.  float16 does not hold every scale: values are taken relative to 2^vexp, raised as
+// blocks need it, exact down to 2^-15 of it, and smaller blocks pass the rest to their weights.
+#pragma once
+
+#include "cache8_args.h"
+
+namespace parrot {
+
+template <int DT> struct Wide8;
+template <> struct Wide8<kF16> {
+  typedef f16x8 v8;
+  PARROT_DEV static unsigned two(unsigned w, float s, bool hi) {
+    return __builtin_bit_cast(unsigned, hi ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, s, true)
+                                           : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, s, false));
+  }
+  PARROT_DEV static f32x4 mma(const u32x4& a, const u32x4& b, const f32x4& c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
+  }
+  PARROT_DEV static unsigned pack(float x, float y) { return __builtin_bit_cast(unsigned, f16x2{(_Float16)x, (_Float16)y}); }
+  PARROT_DEV static float add(unsigned p, float acc) {
+    return __builtin_amdgcn_fdot2(as_f16x2(p), f16x2{(_Float16)1.f, (_Float16)1.f}, acc, false);
+  }
+};
+struct WideBf16 {
+  typedef bf16x8 v8;
+  PARROT_DEV static unsigned two(unsigned w, float s, bool hi) {
+    return __builtin_bit_cast(unsigned, hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, true)
+                                           : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, false));
+  }
+  PARROT_DEV static f32x4 mma(const u32x4& a, const u32x4& b, const f32x4& c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
+  }
+  PARROT_DEV static unsigned pack(float x, float y) { return __builtin_bit_cast(unsigned, bf16x2{(__bf16)x, (__bf16)y}); }
+  PARROT_DEV static float add(unsigned p, float acc) {
+    return __builtin_amdgcn_fdot2_f32_bf16(as_bf16x2(p), bf16x2{(__bf16)1.f, (__bf16)1.f}, acc, false);
+  }
+};
+template <> struct Wide8<kBF16> : WideBf16 {};
+template <> struct Wide8<kF32> : WideBf16 {};
+
+// The high 16 bits of two floats, the first in the low half.
+PARROT_DEV unsigned high_halves(float x, float y) {
+  return __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
+}
+PARROT_DEV float high_part(float x) { return __uint_as_float(__float_as_uint(x) & 0xFFFF0000u); }
+
+// One range of keys for the columns of one tile.
+struct Range8 {
+  Pool8 pool;
+  const int* tbl;
+  int npool;                             // blocks of the pool
+  int u0, u1;                            // units
+  int end;                               // keys; from here on slots hold anything
+  int plain;                             // keys before it are seen by every column
+};
+
+template <int DT, int D, int NS>
+struct Tile8 {
+  using W = Wide8<DT>;
+  static constexpr int X = D / 64;                    // 16-byte loads of each tensor, per block and lane
+  static constexpr int NU = 4 / X;                    // units on their way: 16 KiB
+  static constexpr int PARTS = DT == kF32 ? 3 : 1;
+  static constexpr int BLK_B = kBlockTokens * D;
+  static constexpr float kNoKey = -3.0e38f;           // a reference that every finite logit moves
+
+  int lane, h, H;
+  u32x4 qf[NS][PARTS][2 * X];
+  f32x4 o[NS][4 * X];
+  float mref[NS], lt[NS], lw[NS];
+  int lim[NS];                                        // keys the lane's column sees
+  int vexp;                                           // float16: o is in units of 2^(vexp - 127)
+
+  PARROT_DEV Tile8(int heads, int head) : lane(threadIdx.x & 63), h(head), H(heads) {
+#pragma unroll
+    for (int c = 0; c < NS; ++c) {
+      mref[c] = kNoKey; lt[c] = 0.f; lw[c] = 0.f; lim[c] = 0;
+#pragma unroll
+      for (int t = 0; t < 4 * X; ++t) o[c][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    vexp = 0;
+  }
+  PARROT_DEV int column(int c) const { return 16 * c + (lane & 15); }
+
+  // Queries of the tile's columns; at(c) is the column's place in [T][HQ], or -1.
+  template <class F>
+  PARROT_DEV void load_queries(const void* q, bool flip, F at) {
+    const int g = lane >> 4;
+#pragma unroll
+    for (int c = 0; c < NS; ++c) {
+      const long row = at(c);
+      const char* src = (const char*)q + (row < 0 ? 0 : row) * (D * Elem<DT>::kBytes);
+      const bool on = row >= 0;
+#pragma unroll
+      for (int s = 0; s < 2 * X; ++s) {
+        const int d = (s >> 1) * 64 + g * 16 + (s & 1) * 8;
+        if constexpr (DT == kF32) {
+          u32x4 lo = ld16(src + d * 4), hi = ld16(src + d * 4 + 16);
+          const unsigned w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+          unsigned p[3][4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float x = on ? __uint_as_float(w[2 * i]) : 0.f, y = on ? __uint_as_float(w[2 * i + 1]) : 0.f;
+            x = flip ? -x : x;
+            y = flip ? -y : y;
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+              p[k][i] = high_halves(x, y);
+              x -= high_part(x);
+              y -= high_part(y);
+            }
+          }
+#pragma unroll
+          for (int k = 0; k < 3; ++k) qf[c][k][s] = u32x4{p[k][0], p[k][1], p[k][2], p[k][3]};
+        } else {
+          u32x4 v = ld16(src + d * 2);
+          const unsigned f = flip ? 0x80008000u : 0u;
+          qf[c][0][s] = on ? u32x4{v.x ^ f, v.y ^ f, v.z ^ f, v.w ^ f} : u32x4{0u, 0u, 0u, 0u};
+        }
+      }
+    }
+  }
+
+  PARROT_DEV void scale_outputs(float f, int c) {
+#pragma unroll
+    for (int t = 0; t < 4 * X; ++t) o[c][t] *= f;
+  }
+
+  PARROT_DEV void run(const Range8& rg, float scale_log2) {
+    const int g = lane >> 4;
+    const int last = max((rg.end - 1) / kBlockTokens, 0);
+    // keys: row lane % 16, 16 bytes at 16 g of each 64; values: 16 bytes a lane
+    const unsigned koff = (lane & 15) * D + g * 16, voff = lane * 16;
+    u32x4 kr[NU][2][X], vr[NU][2][X];
+    unsigned sc[NU][2];                               // a block's scale bytes: keys, values
+    int nid[2];
+    auto ids = [&](int u) {                           // of unit u (past the end: the last block)
+#pragma unroll
+      for (int b = 0; b < 2; ++b) nid[b] = ld_uniform(rg.tbl + min(2 * u + b, last));
+    };
+    auto issue = [&](int n, int u) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int id = (int)min((unsigned)nid[b], (unsigned)(rg.npool - 1));
+        const size_t bh = (size_t)id * H + h;
+        const char* kp = (const char*)rg.pool.k + bh * BLK_B;
+        const char* vp = (const char*)rg.pool.v + bh * BLK_B;
+#pragma unroll
+        for (int x = 0; x < X; ++x) kr[n][b][x] = ld16(kp + koff + x * 64);
+#pragma unroll
+        for (int x = 0; x < X; ++x) vr[n][b][x] = ld16(vp + voff + x * 1024);
+        const unsigned word = (unsigned)ld_uniform((const int*)((const char*)rg.pool.scales + ((bh * 2) & ~(size_t)3)));
+        sc[n][b] = (bh & 1 ? word >> 16 : word) & 0xFFFFu;
+      }
+      ids(u + 1);
+    };
+    ids(rg.u0);
+#pragma unroll
+    for (int n = 0; n < NU; ++n)
+      if (rg.u0 + n < rg.u1) issue(n, rg.u0 + n);
+#pragma unroll 1
+    for (int ub = rg.u0; ub < rg.u1; ub += NU) {
+#pragma unroll
+      for (int n = 0; n < NU; ++n) {
+        const int u = ub + n;
+        if (u >= rg.u1) break;
+        unit(rg, u * kUnit, kr[n], vr[n], sc[n], scale_log2);
+        __builtin_amdgcn_sched_barrier(0);            // (the next loads take this unit's registers)
+        if (u + NU < rg.u1) issue(n, u + NU);
+      }
+    }
+  }
+
+  // Output of column c and its log-sum-exp: f(c, column, factor of o, log2 of the sum, rounded sum).
+  template <class F>
+  PARROT_DEV void finish(F f) {
+#pragma unroll
+    for (int c = 0; c < NS; ++c) {
+      const float t = sum_xor32(sum_xor16(lt[c]));
+      float w = t;
+      if constexpr (DT != kF32) w = sum_xor32(sum_xor16(lw[c]));
+      float inv = w == 0.f ? 0.f : 1.f / w;
+      if constexpr (DT == kF16) inv *= vexp > 0 ? __uint_as_float((unsigned)vexp << 23) : 1.f;
+      f(c, column(c), inv, t == 0.f ? -INFINITY : mref[c] + fast_log2(t));
+    }
+  }
+  // Elements 64 x + 16 (lane / 16) + 4 i .. + 3 of column c.
+  PARROT_DEV f32x4 four(int c, int x, int i) const {
+    return f32x4{o[c][4 * x][i], o[c][4 * x + 1][i], o[c][4 * x + 2][i], o[c][4 * x + 3][i]};
+  }
+
+ private:
+  PARROT_DEV void unit(const Range8& rg, int tok0, u32x4 (&k)[2][X], u32x4 (&v)[2][X], unsigned (&sc)[2], float scale_log2) {
+    const int g = lane >> 4;
+    f32x4 s[NS][2];
+#pragma unroll
+    for (int c = 0; c < NS; ++c) s[c][0] = s[c][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int st = 0; st < 2 * X; ++st)
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const unsigned w0 = k[b][st >> 1][2 * (st & 1)], w1 = k[b][st >> 1][2 * (st & 1) + 1];
+        const u32x4 kf = {W::two(w0, 1.f, false), W::two(w0, 1.f, true), W::two(w1, 1.f, false), W::two(w1, 1.f, true)};
+#pragma unroll
+        for (int c = 0; c < NS; ++c)
+#pragma unroll
+          for (int p = PARTS - 1; p >= 0; --p) s[c][b] = W::mma(kf, qf[c][p][st], s[c][b]);
+      }
+    const bool masked = tok0 + kUnit > rg.plain;
+    bool bad = false;                                  // a value that some columns see is no number
+    if (masked) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int left = rg.end - (tok0 + 16 * b + 4 * g);
+        const unsigned keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+        unsigned any = 0;
+#pragma unroll
+        for (int x = 0; x < X; ++x)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const unsigned w = v[b][x][i] & keep;
+            v[b][x][i] = w;
+            any |= (w & 0x7F7F7F7Fu) + 0x01010101u;
+          }
+        bad = bad || (any & 0x80808080u) != 0;
+      }
+      bad = __ballot(bad) != 0;
+    }
+    float cb[2], vs[2], rest[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      cb[b] = __uint_as_float((sc[b] & 0xFFu) << 23) * scale_log2;
+      vs[b] = __uint_as_float((sc[b] >> 8) << 23);
+      rest[b] = 1.f;
+    }
+    if constexpr (DT == kF16) {
+      // (up to 2^7 above vexp: 448 * 2^7 is a float16)
+      const int e0 = sc[0] >> 8, e1 = sc[1] >> 8, top = max(e0, e1);
+      if (top > vexp + 7 || vexp == 0) {
+        if (vexp > 0) {
+          const float f = ldexpf(1.f, vexp - top);
+#pragma unroll
+          for (int c = 0; c < NS; ++c) scale_outputs(f, c);
+        }
+        vexp = top;
+      }
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int rel = (b ? e1 : e0) - vexp;
+        vs[b] = __uint_as_float((unsigned)(127 + max(rel, -15)) << 23);
+        rest[b] = rel < -15 ? ldexpf(1.f, max(rel + 15, -30)) : 1.f;
+      }
+    }
+    unsigned pw[NS][PARTS][4];
+#pragma unroll
+    for (int c = 0; c < NS; ++c) {
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = s[c][i >> 2][i & 3] * cb[i >> 2];
+      if (masked) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (tok0 + 16 * (i >> 2) + 4 * g + (i & 3) >= lim[c]) x[i] = -INFINITY;
+      }
+      const float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+      if (__ballot(mx > mref[c] + 8.f)) {
+        const float m = fmaxf(mref[c], max_xor32(max_xor16(mx)));
+        const float f = fast_exp2(mref[c] - m);
+        mref[c] = m;
+        lt[c] *= f;
+        lw[c] *= f;
+        scale_outputs(f, c);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[i] = fast_exp2(x[i] - mref[c]);
+        lt[c] += x[i];
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (DT == kF32) {
+          float y0 = x[2 * i], y1 = x[2 * i + 1];
+#pragma unroll
+          for (int p = 0; p < 3; ++p) {
+            pw[c][p][i] = high_halves(y0, y1);
+            y0 -= high_part(y0);
+            y1 -= high_part(y1);
+          }
+        } else {
+          pw[c][0][i] = W::pack(x[2 * i], x[2 * i + 1]);
+          lw[c] = W::add(pw[c][0][i], lw[c]);
+        }
+      }
+      if constexpr (DT == kF16) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+          if (rest[b] != 1.f) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              f16x2 y = as_f16x2(pw[c][0][2 * b + i]);
+              y *= f16x2{(_Float16)rest[b], (_Float16)rest[b]};
+              pw[c][0][2 * b + i] = __builtin_bit_cast(unsigned, y);
+            }
+          }
+      }
+    }
+    if (bad) mark_bad(v, x_seen(tok0));
+#pragma unroll
+    for (int x = 0; x < X; ++x)
+#pragma unroll
+      for (int dd = 0; dd < 4; ++dd) {
+        const unsigned w0 = v[0][x][dd], w1 = v[1][x][dd];
+        const u32x4 vf = {W::two(w0, vs[0], false), W::two(w0, vs[0], true), W::two(w1, vs[1], false), W::two(w1, vs[1], true)};
+#pragma unroll
+        for (int c = 0; c < NS; ++c)
+#pragma unroll
+          for (int p = PARTS - 1; p >= 0; --p)
+            o[c][4 * x + dd] = W::mma(vf, u32x4{pw[c][p][0], pw[c][p][1], pw[c][p][2], pw[c][p][3]}, o[c][4 * x + dd]);
+      }
+  }
+
+  // 1 where the lane's column sees the token of its P operand, as that operand.
+  struct Seen { u32x4 w[NS]; };
+  PARROT_DEV Seen x_seen(int tok0) const {
+    Seen r;
+    const int g = lane >> 4;
+#pragma unroll
+    for (int c = 0; c < NS; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int t = tok0 + 16 * (i >> 1) + 4 * g + 2 * (i & 1);
+        r.w[c][i] = W::pack(t < lim[c] ? 1.f : 0.f, t + 1 < lim[c] ? 1.f : 0.f);
+      }
+    return r;
+  }
+  // Values that are no numbers, in a unit that not all columns see whole: they make NaN of the
+  // element in the columns that see their token, and are cleared for the others.
+  PARROT_DEV void mark_bad(u32x4 (&v)[2][X], const Seen& seen) {
+#pragma unroll
+    for (int x = 0; x < X; ++x)
+#pragma unroll
+      for (int dd = 0; dd < 4; ++dd) {
+        u32x4 one;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const unsigned w = v[b][x][dd];
+          const unsigned nan = (((w & 0x7F7F7F7Fu) + 0x01010101u) >> 7) & 0x01010101u;     // 1 in such bytes
+          v[b][x][dd] = w & ~(nan * 255u);
+          const unsigned code = nan * 0x38u;                                               // 1.0 in e4m3
+          one[2 * b] = W::two(code, 1.f, false);
+          one[2 * b + 1] = W::two(code, 1.f, true);
+        }
+#pragma unroll
+        for (int c = 0; c < NS; ++c) {
+          const f32x4 n = W::mma(one, seen.w[c], f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (n[i] > 0.f) o[c][4 * x + dd][i] = __builtin_nanf("");
+        }
+      }
+  }
+};
+
+}  // namespace parrot

@@ -3,6 +3,8 @@
 // and the batch arrays of parrot_nested_prefix_decode.  Host code only.
 #include <algorithm>
 #include <cstdint>
+#include <functional>
+#include <new>
 #include <unordered_map>
 #include <vector>
 
@@ -54,6 +56,9 @@ struct parrot_context_store {
   // (parent node + 1, hash of the prefix) -> child node
   std::unordered_map<uint64_t, std::vector<int32_t>> children;
   int32_t live_nodes = 0;
+  std::vector<int32_t> users;                     // per block: nodes and contexts that hold it
+  std::vector<int32_t> holds;                     // per block: copies not taken yet that read it
+  std::vector<std::pair<int32_t, int32_t>> copies;   // (source, destination), not taken yet
 
   static uint64_t key(int32_t parent, uint64_t h) {
     return h ^ (0x9e3779b97f4a7c15ull * static_cast<uint64_t>(parent + 1));
@@ -74,11 +79,41 @@ struct parrot_context_store {
   int32_t take_block() {
     int32_t b = free_list.back();
     free_list.pop_back();
+    users[b] = 1;
     return b;
+  }
+  // (the free list has room for every block: nothing here allocates)
+  void free_if_unused(int32_t b) {
+    if (users[b] == 0 && holds[b] == 0) free_list.push_back(b);
+  }
+  void drop_block(int32_t b) {
+    if (--users[b] > 0) return;
+    // a copy into a block that nobody holds any more is not owed; nothing reads such a block
+    for (size_t i = 0; i < copies.size(); ++i)
+      if (copies[i].second == b) {
+        const int32_t from = copies[i].first;
+        copies.erase(copies.begin() + i);
+        --holds[from];
+        free_if_unused(from);
+        break;
+      }
+    free_if_unused(b);
+  }
+  // What block b will hold is in this one: where b itself is still to be copied to, its source.
+  size_t copy_into(int32_t b) const {
+    size_t i = 0;
+    while (i < copies.size() && copies[i].second != b) ++i;
+    return i;
+  }
+  void owe_copy(int32_t from, int32_t to) {
+    const size_t i = copy_into(from);
+    if (i < copies.size()) from = copies[i].first;
+    copies.emplace_back(from, to);
+    ++holds[from];
   }
   void release_node(int32_t id) {
     Node& nd = nodes[id];
-    for (int32_t b : nd.blocks) free_list.push_back(b);
+    for (int32_t b : nd.blocks) drop_block(b);
     auto it = children.find(key(nd.parent, nd.hash));
     if (it != children.end()) {
       auto& v = it->second;
@@ -104,6 +139,8 @@ parrot_context_store* parrot_store_create(int32_t block_size, int32_t num_blocks
   st->free_list.resize(num_blocks);
   // hand out low block ids first
   for (int32_t i = 0; i < num_blocks; ++i) st->free_list[i] = num_blocks - 1 - i;
+  st->users.resize(num_blocks);
+  st->holds.resize(num_blocks);
   return st;
 }
 
@@ -184,6 +221,19 @@ parrot_status parrot_store_append(parrot_context_store* st, int32_t ctx, int32_t
     if (st->free_list.empty())
       return parrot::set_error(PARROT_ERR_WORKSPACE_TOO_SMALL, "no free KV block for context %d", ctx);
     c.blocks.push_back(st->take_block());
+  } else if (const int32_t last = c.blocks.back(); st->users[last] > 1) {
+    // the new token goes into a block that other contexts read: this one gets its own
+    if (st->free_list.empty())
+      return parrot::set_error(PARROT_ERR_WORKSPACE_TOO_SMALL, "no free KV block for context %d", ctx);
+    try {
+      st->copies.reserve(st->copies.size() + 1);
+    } catch (const std::bad_alloc&) {
+      return parrot::set_error(PARROT_ERR_WORKSPACE_TOO_SMALL, "no host memory for a copy");
+    }
+    const int32_t mine = st->take_block();
+    st->owe_copy(last, mine);
+    --st->users[last];
+    c.blocks.back() = mine;
   }
   ++c.own;
   return parrot::set_error(PARROT_OK, "");
@@ -197,7 +247,7 @@ parrot_status parrot_store_truncate(parrot_context_store* st, int32_t ctx, int32
   const size_t keep = st->blocks_for(own_tokens);
   // (the free list was made with room for every block: nothing here allocates)
   while (c.blocks.size() > keep) {
-    st->free_list.push_back(c.blocks.back());
+    st->drop_block(c.blocks.back());
     c.blocks.pop_back();
   }
   c.own = own_tokens;
@@ -207,7 +257,7 @@ parrot_status parrot_store_truncate(parrot_context_store* st, int32_t ctx, int32
 parrot_status parrot_store_free(parrot_context_store* st, int32_t ctx) {
   if (!st || !st->context(ctx)) return parrot::set_error(PARROT_ERR_INVALID_ARGUMENT, "unknown context %d", ctx);
   Context& c = st->ctxs[ctx];
-  for (int32_t b : c.blocks) st->free_list.push_back(b);
+  for (int32_t b : c.blocks) st->drop_block(b);
   for (int32_t x = c.node; x >= 0;) {
     const int32_t parent = st->nodes[x].parent;
     if (--st->nodes[x].refs == 0) st->release_node(x);
@@ -216,6 +266,97 @@ parrot_status parrot_store_free(parrot_context_store* st, int32_t ctx) {
   c = Context();
   st->free_ctxs.push_back(ctx);
   return parrot::set_error(PARROT_OK, "");
+}
+
+int32_t parrot_store_fork(parrot_context_store* st, int32_t ctx) {
+  if (!st || !st->context(ctx)) {
+    parrot::set_error(PARROT_ERR_INVALID_ARGUMENT, "unknown context %d", ctx);
+    return -2;
+  }
+  try {
+    Context twin = st->ctxs[ctx];
+    int32_t id;
+    if (!st->free_ctxs.empty()) { id = st->free_ctxs.back(); st->free_ctxs.pop_back(); }
+    else { id = static_cast<int32_t>(st->ctxs.size()); st->ctxs.emplace_back(); }
+    for (int32_t b : twin.blocks) ++st->users[b];
+    for (int32_t x = twin.node; x >= 0; x = st->nodes[x].parent) ++st->nodes[x].refs;
+    st->ctxs[id] = std::move(twin);
+    return id;
+  } catch (const std::bad_alloc&) {
+    parrot::set_error(PARROT_ERR_WORKSPACE_TOO_SMALL, "no host memory for a context");
+    return -1;
+  }
+}
+
+int32_t parrot_store_compact(parrot_context_store* st, int32_t most) {
+  if (!st || most < 0) {
+    parrot::set_error(PARROT_ERR_INVALID_ARGUMENT, "%s", st ? "most is negative" : "store is NULL");
+    return -2;
+  }
+  const int32_t n = static_cast<int32_t>(st->users.size());
+  std::vector<int32_t> now;
+  try {
+    now.resize(n);
+    st->copies.reserve(st->copies.size() + n);
+  } catch (const std::bad_alloc&) {
+    parrot::set_error(PARROT_ERR_WORKSPACE_TOO_SMALL, "no host memory to compact");
+    return -1;
+  }
+  for (int32_t b = 0; b < n; ++b) now[b] = b;
+  int32_t to = 0, moved = 0;
+  for (int32_t from = n - 1; moved < most; --from) {
+    while (from >= 0 && st->users[from] == 0) --from;
+    while (to < from && (st->users[to] > 0 || st->holds[to] > 0)) ++to;
+    if (to >= from) break;
+    // a block that is still to be copied to is copied to its new place instead
+    const size_t i = st->copy_into(from);
+    if (i < st->copies.size()) {
+      st->copies[i].second = to;
+    } else {
+      st->copies.emplace_back(from, to);
+      ++st->holds[from];
+    }
+    st->users[to] = st->users[from];
+    st->users[from] = 0;
+    now[from] = to;
+    ++moved;
+  }
+  for (Node& nd : st->nodes)
+    for (int32_t& b : nd.blocks) b = now[b];
+  for (Context& c : st->ctxs)
+    for (int32_t& b : c.blocks) b = now[b];
+  st->free_list.clear();                           // (lowest ids are handed out first)
+  for (int32_t b = n - 1; b >= 0; --b) st->free_if_unused(b);
+  return moved;
+}
+
+int32_t parrot_store_num_copies(const parrot_context_store* st) {
+  return st ? static_cast<int32_t>(st->copies.size()) : -1;
+}
+
+parrot_status parrot_store_take_copies(parrot_context_store* st, int32_t* src, int32_t* dst, int32_t most) {
+  if (!st) return parrot::set_error(PARROT_ERR_INVALID_ARGUMENT, "store is NULL");
+  const int32_t n = static_cast<int32_t>(st->copies.size());
+  if (most < n) return parrot::set_error(PARROT_ERR_WORKSPACE_TOO_SMALL, "%d copies, room for %d", n, most);
+  if (n > 0 && (!src || !dst)) return parrot::set_error(PARROT_ERR_INVALID_ARGUMENT, "src or dst is NULL");
+  const size_t freed = st->free_list.size();
+  for (int32_t i = 0; i < n; ++i) {
+    src[i] = st->copies[i].first;
+    dst[i] = st->copies[i].second;
+    --st->holds[src[i]];
+    st->free_if_unused(src[i]);
+  }
+  st->copies.clear();
+  // (lowest ids first, so that a compacted pool stays so; in place)
+  if (st->free_list.size() > freed) std::sort(st->free_list.begin(), st->free_list.end(), std::greater<int32_t>());
+  return parrot::set_error(PARROT_OK, "");
+}
+
+int32_t parrot_store_block_end(const parrot_context_store* st) {
+  if (!st) return -1;
+  int32_t n = static_cast<int32_t>(st->users.size());
+  while (n > 0 && st->users[n - 1] == 0 && st->holds[n - 1] == 0) --n;
+  return n;
 }
 
 int32_t parrot_store_free_blocks(const parrot_context_store* st) {

@@ -136,31 +136,30 @@ parrot_status check_fill_rows(const parrot_problem* p, const parrot_fill_rows* r
 
 }  // namespace
 
-extern "C" parrot_status parrot_rotary_fill(
-    const parrot_problem* p, const parrot_fill_rows* rows, const parrot_rotary* rotary, const void* q,
-    const void* k, const void* v, const void* q_norm, const void* k_norm, const int32_t* positions,
-    const int32_t* query_offsets, const int32_t* suffix_block_tables, const int32_t* suffix_lens,
-    void* q_out, void* suffix_k, void* suffix_v, void* stream, const parrot_trace* trace) {
-  PARROT_TRY(check_fill_rows(p, rows));
-  if (rows->num_query_rows == 0) return set_error(PARROT_OK, "");
+namespace parrot {
+
+// The checks of a fill's arguments but for its cache, and the kernels' arguments.
+parrot_status fill_args(const parrot_problem* p, const parrot_fill_rows* rows, const parrot_rotary* rotary, const void* q,
+                        const void* k, const void* v, const void* q_norm, const void* k_norm, const int32_t* positions,
+                        const int32_t* query_offsets, const int32_t* suffix_block_tables, const int32_t* suffix_lens,
+                        void* q_out, FillArgs* out, int* partner) {
   if ((q == nullptr) != (q_out == nullptr)) return bad(q ? "q_out is NULL and q is not" : "q is NULL and q_out is not");
-  const parrot::PtrCheck need[] = {
+  const PtrCheck need[] = {
       {k, "k", 16}, {v, "v", 16}, {query_offsets, "query_offsets", 4},
-      {suffix_block_tables, "suffix_block_tables", 4}, {suffix_lens, "suffix_lens", 4},
-      {suffix_k, "suffix_k", 16}, {suffix_v, "suffix_v", 16}};
-  PARROT_TRY(parrot::check_pointers(need));
+      {suffix_block_tables, "suffix_block_tables", 4}, {suffix_lens, "suffix_lens", 4}};
+  PARROT_TRY(check_pointers(need));
   const long T = rows->num_query_rows, D = p->head_dim, H = p->num_heads;
   const long elt = p->dtype == PARROT_DTYPE_F32 ? 4 : 2;
   const long HQ = q ? rows->num_query_heads : 0;
   if (q) {
     if (HQ < 1) return bad("num_query_heads %ld < 1", HQ);
-    const parrot::PtrCheck qs[] = {{q, "q", 16}, {q_out, "q_out", 16}};
-    PARROT_TRY(parrot::check_pointers(qs));
+    const PtrCheck qs[] = {{q, "q", 16}, {q_out, "q_out", 16}};
+    PARROT_TRY(check_pointers(qs));
   }
-  for (const parrot::PtrCheck& c : {parrot::PtrCheck{q_norm, "q_norm", 16}, parrot::PtrCheck{k_norm, "k_norm", 16}})
+  for (const PtrCheck& c : {PtrCheck{q_norm, "q_norm", 16}, PtrCheck{k_norm, "k_norm", 16}})
     if (c.ptr) {
-      const parrot::PtrCheck one[] = {c};
-      PARROT_TRY(parrot::check_pointers(one));
+      const PtrCheck one[] = {c};
+      PARROT_TRY(check_pointers(one));
     }
   struct { const char* name; int64_t stride; long width; } strides[] = {
       {"q_stride", rows->q_stride, HQ * D}, {"k_stride", rows->k_stride, H * D}, {"v_stride", rows->v_stride, H * D}};
@@ -177,36 +176,63 @@ extern "C" parrot_status parrot_rotary_fill(
   if (rotary) {
     PARROT_TRY(check_rotary(rotary->rotary_dim, rotary->interleaved));
     if (rotary->rotary_dim > D) return bad("rotary_dim %ld > head_dim %ld", rotary->rotary_dim, D);
-    const parrot::PtrCheck pos[] = {{positions, "positions", 4}};
-    PARROT_TRY(parrot::check_pointers(pos));
+    const PtrCheck pos[] = {{positions, "positions", 4}};
+    PARROT_TRY(check_pointers(pos));
   }
 
-  parrot::FillArgs a{};
+  FillArgs a{};
   a.q = q; a.k = k; a.v = v;
   a.q_stride = rows->q_stride * elt; a.k_stride = rows->k_stride * elt; a.v_stride = rows->v_stride * elt;
   a.q_norm = q ? q_norm : nullptr; a.k_norm = k_norm;
   a.positions = positions; a.qoff = query_offsets; a.stab = suffix_block_tables; a.slen = suffix_lens;
-  a.q_out = q_out; a.sk = suffix_k; a.sv = suffix_v;
+  a.q_out = q_out;
   a.T = (int)T; a.R = p->num_requests; a.HQ = (int)HQ; a.H = (int)H;
   a.sstride = p->suffix_table_stride; a.max_s = p->max_suffix_len; a.max_q = rows->max_query_rows;
   a.nsblk = p->num_suffix_blocks;
   a.eps = rows->norm_eps; a.amplitude = 1.f;
-  int partner = parrot::kRotaryNone;
+  *partner = kRotaryNone;
   if (rotary) {
     a.rd = rotary->rotary_dim;
     a.amplitude = rotary->amplitude;
     std::copy(rotary->turns, rotary->turns + PARROT_ROTARY_MAX_PAIRS, a.turns);
     const int per_lane = 16 / (int)elt;
-    partner = rotary->interleaved ? parrot::kRotaryInterleaved
-              : a.rd / 2 % per_lane == 0 ? parrot::kRotaryHalfVector : parrot::kRotaryHalfScalar;
+    *partner = rotary->interleaved ? kRotaryInterleaved : a.rd / 2 % per_lane == 0 ? kRotaryHalfVector : kRotaryHalfScalar;
   }
-  // a row's heads over several workgroups where rows alone do not fill the device
-  const long heads = HQ + 2 * H, step = 4096 / (D * elt);
-  const long slabs = std::max(1L, std::min(ceil_div(heads, step), ceil_div(4L * parrot::device_cus(), T)));
-  a.slab_heads = (int)(ceil_div(ceil_div(heads, slabs), step) * step);
-  a.slabs = (int)ceil_div(heads, a.slab_heads);
+  *out = a;
+  return PARROT_OK;
+}
+
+// The heads of a row or unit, `step` of them at a time, over several workgroups where the
+// `items` of a launch alone do not fill the device.
+void fill_slabs(FillArgs* a, long step, long items) {
+  const long heads = a->HQ + 2L * a->H;
+  const long slabs = std::max(1L, std::min(ceil_div(heads, step), ceil_div(4L * device_cus(), items)));
+  a->slab_heads = (int)(ceil_div(ceil_div(heads, slabs), step) * step);
+  a->slabs = (int)ceil_div(heads, a->slab_heads);
+}
+
+parrot_status check_fill(const parrot_problem* p, const parrot_fill_rows* rows) { return check_fill_rows(p, rows); }
+
+}  // namespace parrot
+
+extern "C" parrot_status parrot_rotary_fill(
+    const parrot_problem* p, const parrot_fill_rows* rows, const parrot_rotary* rotary, const void* q,
+    const void* k, const void* v, const void* q_norm, const void* k_norm, const int32_t* positions,
+    const int32_t* query_offsets, const int32_t* suffix_block_tables, const int32_t* suffix_lens,
+    void* q_out, void* suffix_k, void* suffix_v, void* stream, const parrot_trace* trace) {
+  PARROT_TRY(check_fill_rows(p, rows));
+  if (rows->num_query_rows == 0) return set_error(PARROT_OK, "");
+  parrot::FillArgs a;
+  int partner;
+  PARROT_TRY(parrot::fill_args(p, rows, rotary, q, k, v, q_norm, k_norm, positions, query_offsets, suffix_block_tables,
+                               suffix_lens, q_out, &a, &partner));
+  const parrot::PtrCheck pools[] = {{suffix_k, "suffix_k", 16}, {suffix_v, "suffix_v", 16}};
+  PARROT_TRY(parrot::check_pointers(pools));
+  a.sk = suffix_k; a.sv = suffix_v;
+  const long T = a.T;
+  parrot::fill_slabs(&a, 4096 / (p->head_dim * (p->dtype == PARROT_DTYPE_F32 ? 4 : 2)), T);
   if (T * a.slabs > 0x7fffffffL) return set_error(PARROT_ERR_UNSUPPORTED, "fill needs %ld workgroups", T * a.slabs);
-  return launched(parrot::launch_fill(a, partner, (int)p->dtype, (int)D, reinterpret_cast<hipStream_t>(stream),
+  return launched(parrot::launch_fill(a, partner, (int)p->dtype, p->head_dim, reinterpret_cast<hipStream_t>(stream),
                                       trace ? ev(trace->partials_start) : nullptr,
                                       trace ? ev(trace->partials_stop) : nullptr),
                   "fill kernel");

@@ -33,4 +33,14 @@ parrot_status validate_inputs(const parrot_problem* p, const int32_t* prefix_blo
                               const parrot_prefill_rows* rows, const int32_t* query_offsets,
                               const ValidateTree* tree);
 
+// Fills of new rows: the checks of their counts, those of the other arguments but for the
+// cache with the kernels' arguments and how partners come, and the split of their heads.
+struct FillArgs;
+parrot_status check_fill(const parrot_problem* p, const parrot_fill_rows* rows);
+parrot_status fill_args(const parrot_problem* p, const parrot_fill_rows* rows, const parrot_rotary* rotary, const void* q,
+                        const void* k, const void* v, const void* q_norm, const void* k_norm, const int32_t* positions,
+                        const int32_t* query_offsets, const int32_t* suffix_block_tables, const int32_t* suffix_lens,
+                        void* q_out, FillArgs* out, int* partner);
+void fill_slabs(FillArgs* a, long step, long items);
+
 }  // namespace parrot

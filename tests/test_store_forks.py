@@ -1,0 +1,269 @@
+"""Forks, copies owed and compaction of the host context store (CPU), against a model of the
+cache's contents: what every context reads through its tables, whoever shares its blocks."""
+import numpy as np
+import pytest
+
+from paper_2405_19888_amd.binding import ParrotError
+from paper_2405_19888_amd.context import ContextStore
+
+
+class Cache:
+    """Blocks of tokens, written as an engine writes them: copies taken before every write."""
+
+    def __init__(self, st):
+        self.st = st
+        self.blocks = [[None] * st.block_size for _ in range(st.num_blocks)]
+        self.want = {}
+
+    def settle(self):
+        src, dst = self.st.take_copies()
+        assert self.st.num_copies == 0
+        assert len(set(dst.tolist())) == len(dst) and not set(dst.tolist()) & set(src.tolist())
+        was = [list(b) for b in self.blocks]
+        for a, b in zip(src, dst):
+            self.blocks[b] = list(was[a])
+
+    def own_row(self, ctx):
+        return self.st.build_batch([ctx]).suffix_tables[0]
+
+    def fill(self, tokens, bounds=()):
+        c = self.st.fill(tokens, bounds)
+        self.settle()
+        own = tokens[bounds[-1]:] if len(bounds) else tokens
+        row = self.own_row(c)
+        for i, t in enumerate(own):
+            self.blocks[row[i // self.st.block_size]][i % self.st.block_size] = t
+        self.want[c] = list(own)
+        return c
+
+    def append(self, ctx, token):
+        self.st.append(ctx, token)
+        self.settle()
+        i = len(self.want[ctx])
+        self.blocks[self.own_row(ctx)[i // self.st.block_size]][i % self.st.block_size] = token
+        self.want[ctx].append(token)
+
+    def fork(self, ctx):
+        c = self.st.fork(ctx)
+        self.want[c] = list(self.want[ctx])
+        return c
+
+    def truncate(self, ctx, n):
+        self.st.truncate(ctx, n)
+        del self.want[ctx][n:]
+
+    def free(self, ctx):
+        self.st.free(ctx)
+        del self.want[ctx]
+
+    def check(self):
+        B = self.st.block_size
+        used = set()
+        for c, want in self.want.items():
+            assert self.st.own_tokens(c) == len(want)
+            row = self.own_row(c)
+            got = [self.blocks[row[i // B]][i % B] for i in range(len(want))]
+            assert got == want, c
+            used |= set(int(x) for x in row[:-(-len(want) // B)])
+        return used
+
+
+def test_forks_share_until_they_append():
+    st = ContextStore(4, 20)
+    m = Cache(st)
+    a = m.fill([1, 2, 3, 4, 5, 6], ())
+    assert st.free_blocks == 18
+    b, c = m.fork(a), m.fork(a)
+    assert st.free_blocks == 18 and st.num_copies == 0
+    m.append(b, 70)
+    assert st.free_blocks == 17              # b's last block is its own now
+    m.append(c, 80)
+    assert st.free_blocks == 16
+    m.append(a, 90)                          # nobody else reads it any more
+    assert st.free_blocks == 16
+    m.check()
+    m.append(a, 91)
+    d = m.fork(a)                            # a full block: nothing to copy
+    m.append(d, 92)
+    m.append(a, 93)
+    assert m.check()
+    for x in (a, b, c, d):
+        m.free(x)
+    assert st.free_blocks == 20
+
+
+def test_truncating_into_a_shared_block():
+    st = ContextStore(4, 20)
+    m = Cache(st)
+    a = m.fill(list(range(10)))
+    b = m.fork(a)
+    m.truncate(b, 6)                         # block 1 is shared, and partly b's
+    m.append(b, 50)
+    m.check()
+    m.truncate(a, 0)
+    m.check()
+    m.append(a, 60)
+    m.check()
+
+
+def test_forks_of_contexts_with_prefixes():
+    st = ContextStore(16, 50)
+    a = st.fill(list(range(60)), [40])
+    b = st.fork(a)
+    st.free(a)
+    assert st.num_prefixes == 1 and st.prefix_tokens(b) == 40 and st.own_tokens(b) == 20
+    c = st.fork(b)
+    batch = st.build_batch([b, c])
+    assert batch.group_ids.tolist() == [0, 0] and batch.shape.max_group_size == 2
+    assert batch.suffix_tables[0].tolist() == batch.suffix_tables[1].tolist()
+    st.free(b)
+    st.free(c)
+    assert st.free_blocks == 50 and st.num_prefixes == 0
+
+
+def test_untaken_copies():
+    """Copies owed but not taken: sources are not handed out, dropped destinations owe nothing,
+    and copies of copies come from the first source."""
+    st = ContextStore(4, 6)
+    a = st.fill([1, 2], ())
+    b = st.fork(a)
+    st.append(b)                             # owes last block of a -> new block
+    assert st.num_copies == 1
+    st.free(a)
+    assert st.free_blocks == 4               # its block is still to be read
+    st.free(b)
+    assert st.num_copies == 0 and st.free_blocks == 6
+    a = st.fill([1, 2], ())
+    b = st.fork(a)
+    st.append(b)
+    c = st.fork(b)
+    st.append(c)
+    src, dst = st.take_copies()
+    assert src[0] == src[1] and dst[0] != dst[1]
+    for x in (a, b, c):
+        st.free(x)
+    assert st.free_blocks == 6
+
+
+def test_no_blocks_left_changes_nothing():
+    st = ContextStore(4, 2)
+    a = st.fill([1, 2, 3, 4, 5], ())
+    b = st.fork(a)
+    with pytest.raises(ParrotError):
+        st.append(b)
+    assert st.own_tokens(b) == 5 and st.num_copies == 0
+    st.free(a)
+    st.append(b)                             # alone: writes in place
+    assert st.num_copies == 0 and st.own_tokens(b) == 6
+
+
+def test_compaction():
+    st = ContextStore(4, 40)
+    m = Cache(st)
+    ids = [m.fill(list(range(100 * i, 100 * i + 7))) for i in range(12)]
+    for i in (0, 2, 3, 5, 6, 9):
+        m.free(ids[i])
+    f = m.fork(ids[10])
+    assert st.block_end == 24
+    n = st.compact(3)
+    assert n == 3
+    m.settle()
+    m.check()
+    n = st.compact()
+    assert n > 0 and st.num_copies == n
+    assert st.block_end == 21                # (24 but for the three moved before) what the copies read is still there
+    m.settle()
+    assert m.check() == set(range(12)) and st.block_end == 12
+    m.append(f, 5)
+    m.append(ids[10], 6)
+    m.check()
+    assert st.block_end == 13                # (the lowest free ids are handed out)
+    assert st.compact() == 0
+
+
+def test_compaction_moves_prefixes():
+    st = ContextStore(4, 30)
+    a = st.fill(list(range(16)), [8])
+    b = st.fill(list(range(8)) + [50] * 6, [8])
+    st.free(a)
+    before = st.build_batch([b])
+    assert st.compact() >= 1
+    src, dst = st.take_copies()
+    moved = dict(zip(src.tolist(), dst.tolist()))
+    after = st.build_batch([b])
+    to = lambda rows: [[moved.get(int(x), int(x)) for x in r] for r in rows]
+    assert after.prefix_tables.tolist() == to(before.prefix_tables)
+    assert after.suffix_tables.tolist() == to(before.suffix_tables)
+    assert st.block_end == 4
+
+
+def test_bad_arguments():
+    st = ContextStore(4, 8)
+    with pytest.raises(ValueError):
+        st.fork(0)
+    with pytest.raises(ValueError):
+        st.compact(-1)
+    a = st.fill([1, 2], ())
+    b = st.fork(a)
+    st.append(b)
+    assert st._lib.parrot_store_take_copies(st._h, None, None, 0) == 3          # room for none
+    assert st._lib.parrot_store_take_copies(st._h, None, None, 1) == 1
+    assert st.num_copies == 1
+    assert st._lib.parrot_store_num_copies(None) == -1 and st._lib.parrot_store_block_end(None) == -1
+    assert st._lib.parrot_store_fork(None, 0) == -2 and st._lib.parrot_store_compact(None, 1) == -2
+
+
+@pytest.mark.parametrize("seed", range(8))
+def test_random_operations(seed):
+    rng = np.random.default_rng(seed)
+    st = ContextStore([4, 16][seed % 2], 60)
+    m = Cache(st)
+    token = 1000
+    for step in range(300):
+        op = rng.random()
+        live = list(m.want)
+        token += 1
+        pick = live[int(rng.integers(0, len(live)))] if live else None
+        try:
+            if op < 0.2 or not live:
+                m.fill([token * 100 + i for i in range(int(rng.integers(1, 40)))])
+            elif op < 0.35 and len(live) < 30:
+                m.fork(pick)
+            elif op < 0.75:
+                m.append(pick, token)
+            elif op < 0.85:
+                m.truncate(pick, int(rng.integers(0, len(m.want[pick]) + 1)))
+            elif op < 0.93:
+                m.free(pick)
+            else:
+                st.compact(int(rng.integers(0, 20)))
+                m.settle()
+        except (MemoryError, ParrotError):
+            continue
+        used = m.check()
+        assert st.free_blocks == 60 - len(used), step
+    for c in list(m.want):
+        m.free(c)
+    assert st.free_blocks == 60 and st.block_end == 0
+
+
+def test_under_sanitizers(tmp_path):
+    import os
+    import shutil
+    import subprocess
+    import sys
+    from test_store_sanitized import ROOT, RUNNER, _runtime
+    asan, ubsan = (_runtime("libasan.so"), _runtime("libubsan.so")) if shutil.which("g++") else (None, None)
+    if not (asan and ubsan) or os.environ.get("PARROT_STORE_SANITIZED"):
+        pytest.skip("no sanitizer runtimes, or running under them")
+    lib = str(tmp_path / "libstore_sanitized.so")
+    csrc = os.path.join(ROOT, "paper_2405_19888_amd", "csrc")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-omit-frame-pointer",
+                    "-fno-sanitize-recover=undefined", "-shared", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", csrc,
+                    os.path.join(csrc, "context_store.cpp"), os.path.join(ROOT, "tests", "sanitizer_stub.cpp"), "-o", lib],
+                   check=True)
+    env = dict(os.environ, LD_PRELOAD=f"{asan}:{ubsan}", ASAN_OPTIONS="detect_leaks=0", PARROT_STORE_SANITIZED="1")
+    code = RUNNER.format(root=ROOT, lib=lib, tests=os.path.abspath(__file__))
+    p = subprocess.run([sys.executable, "-c", code], env=env, capture_output=True, text=True, timeout=600)
+    assert p.returncode == 0, p.stdout[-3000:] + p.stderr[-3000:]
+    assert "passed" in p.stdout
