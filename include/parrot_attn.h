@@ -661,20 +661,23 @@ parrot_status parrot_cache8_fill(
  *
  * What a step reads is laid out by parrot_cache8_plan, once for all layers of the step: it depends on
  * the row offsets, lengths and groups alone, and on the problem's and rows' fields but for
- * sm_scale and the block counts.  Neither call synchronises, and both may be captured into a graph.
+ * sm_scale and the block counts.  Small calls run as one kernel that needs no plan, where an estimate
+ * from p and rows expects that to be faster (the same p and rows always decide the same way);
+ * parrot_cache8_plan enqueues nothing then.  Neither call synchronises, and both may be captured
+ * into a graph.
  *   rows                 (host) as for a tree call, but max_query_rows may reach max_suffix_len
  *   plan                 >= parrot_cache8_plan_bytes(p, rows) bytes, 256-byte aligned: written by
  *                        parrot_cache8_plan, only read by parrot_cache8_attention (calls
- *                        on several streams may share it).  A call with a plan of other rows,
- *                        lengths or groups gives unspecified values, and no access leaves the
- *                        buffers that p and rows describe
- *   prefix_parents       as parrot_nested_prefix_decode, or NULL for flat groups
+ *                        on several streams may share it).  A call whose plan is of other rows,
+ *                        lengths or groups than its arrays gives unspecified values, and no access
+ *                        leaves the buffers that p and rows describe
  *   prefix               (may be NULL when num_groups = 0)
  *   q, out               [T][HQ][D] dtype, 16-byte aligned;  lse float32 [T][HQ]
  *   workspace            >= parrot_cache8_workspace_bytes(p, rows) bytes, 256-byte aligned;
  *                        contents on entry are ignored
  * Rows from query_offsets[R] on are padding: their out and lse are left as they were (so one
- * captured graph serves batches of fewer rows).  Both sizes depend on the current device's compute
+ * captured graph serves batches of fewer rows).  Other arguments as
+ * parrot_shared_prefix_tree_decode.  Both sizes depend on the current device's compute
  * units, like parrot_workspace_bytes.  For the same heads, head_dim and dtype they never decrease as
  * num_requests, num_groups, max_prefix_len, max_suffix_len, max_prefix_depth or the row counts
  * grow.  (size_t)-1 if the arguments are invalid, 0 when T = 0.
@@ -690,8 +693,12 @@ parrot_status parrot_cache8_plan(
 
 parrot_status parrot_cache8_attention(
     const parrot_problem* p, const parrot_tree_rows* rows,
-    const void* q, const parrot_cache8* prefix, const parrot_cache8* suffix,
-    const int32_t* prefix_block_tables, const int32_t* suffix_block_tables,
+    const void* q, const int32_t* query_offsets,
+    const parrot_cache8* prefix, const parrot_cache8* suffix,
+    const int32_t* prefix_block_tables, const int32_t* prefix_lens,
+    const int32_t* prefix_parents,
+    const int32_t* suffix_block_tables, const int32_t* suffix_lens,
+    const int32_t* group_ids,
     const void* plan, size_t plan_bytes,
     void* out, float* lse,
     void* workspace, size_t workspace_bytes,

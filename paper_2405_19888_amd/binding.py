@@ -208,7 +208,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     cache8 = {
         "parrot_cache8_fill": [prob_p, ctypes.POINTER(ParrotFillRows), rotary_p] + [vp] * 10 + [cache8_p, vp, trace_p],
         "parrot_cache8_plan": [prob_p, tree_p] + [vp] * 6 + [sz, vp],
-        "parrot_cache8_attention": [prob_p, tree_p, vp, cache8_p, cache8_p] + [vp] * 3 + [sz] + [vp] * 3 + [sz, vp, trace_p],
+        "parrot_cache8_attention": [prob_p, tree_p, vp, vp, cache8_p, cache8_p] + [vp] * 7 + [sz] + [vp] * 3 + [sz, vp, trace_p],
         "parrot_validate_cache8_inputs": [prob_p, tree_p] + [vp] * 9,
         "parrot_copy_blocks": [ctypes.POINTER(ParrotBlockPool), ctypes.c_int32, ctypes.c_int32, vp, vp, ctypes.c_int32,
                                vp, trace_p],

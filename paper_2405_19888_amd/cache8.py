@@ -151,33 +151,33 @@ def parrot_cache8_plan(problem, rows, query_offsets, prefix_lens, prefix_parents
     _plan_call(problem, rows, query_offsets, prefix_lens, prefix_parents, suffix_lens, group_ids, plan, stream)()
 
 
-def _attend_call(problem, rows, q, prefix, suffix, prefix_tables, suffix_tables, plan, out, lse, workspace, stream):
+def _attend_call(problem, rows, q, query_offsets, prefix, suffix, prefix_tables, prefix_lens, prefix_parents, suffix_tables,
+                 suffix_lens, group_ids, plan, out, lse, workspace, stream):
     p, T, HQ, dt = problem, rows.num_query_rows, rows.num_query_heads, _TORCH_DTYPES[problem.dtype]
     for x, name, dtype, least in ((q, "q", dt, T * HQ * p.head_dim), (out, "out", dt, T * HQ * p.head_dim),
-                                  (lse, "lse", torch.float32, T * HQ), (plan, "plan", torch.int32, 0),
-                                  (suffix_tables, "suffix_tables", torch.int32, p.num_requests * p.suffix_table_stride)):
+                                  (lse, "lse", torch.float32, T * HQ), (plan, "plan", torch.int32, 0)):
         _need(x, name, dtype, least, q.device)
-    if isinstance(workspace, torch.Tensor):
+    _need_tree(p, q.device, query_offsets, None, prefix_tables, prefix_lens, prefix_parents, suffix_tables, suffix_lens,
+               group_ids)
+    if isinstance(workspace, torch.Tensor):          # (its size is the library's to check)
         _need(workspace, "workspace", workspace.dtype, 0, q.device)
     own = _pool(suffix, "suffix", p.num_suffix_blocks, p, q.device)
-    pre = None
-    if p.num_groups > 0:
-        pre = _pool(prefix, "prefix", p.num_prefix_blocks, p, q.device)
-        _need(prefix_tables, "prefix_tables", torch.int32, p.num_groups * p.prefix_table_stride, q.device)
+    pre = _pool(prefix, "prefix", p.num_prefix_blocks, p, q.device) if p.num_groups > 0 else None
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     call = _bound(load_library().parrot_cache8_attention,
-                  (ctypes.byref(p), ctypes.byref(rows), q, None if pre is None else ctypes.byref(pre), ctypes.byref(own),
-                   prefix_tables, suffix_tables, plan, 0 if plan is None else plan.numel() * 4, out, lse, workspace, ws_bytes),
-                  _device(q), stream)
+                  (ctypes.byref(p), ctypes.byref(rows), q, query_offsets, None if pre is None else ctypes.byref(pre),
+                   ctypes.byref(own), prefix_tables, prefix_lens, prefix_parents, suffix_tables, suffix_lens, group_ids, plan,
+                   0 if plan is None else plan.numel() * 4, out, lse, workspace, ws_bytes), _device(q), stream)
     call.pools = (prefix, suffix)                # (the structs hold addresses only)
     return call
 
 
-def parrot_cache8_attention(problem, rows, q, prefix, suffix, prefix_block_tables, suffix_block_tables, plan, out, lse,
-                            workspace, stream=None, trace=None):
-    """Attention of a step's rows over a layer's 8-bit pools (see the C header)."""
-    _attend_call(problem, rows, q, prefix, suffix, prefix_block_tables, suffix_block_tables, plan, out, lse, workspace,
-                 stream)(trace)
+def parrot_cache8_attention(problem, rows, q, query_offsets, prefix, suffix, prefix_block_tables, prefix_lens, prefix_parents,
+                            suffix_block_tables, suffix_lens, group_ids, plan, out, lse, workspace, stream=None, trace=None):
+    """Attention of a step's rows over a layer's 8-bit pools (see the C header);
+    prefix_parents None: flat groups."""
+    _attend_call(problem, rows, q, query_offsets, prefix, suffix, prefix_block_tables, prefix_lens, prefix_parents,
+                 suffix_block_tables, suffix_lens, group_ids, plan, out, lse, workspace, stream)(trace)
 
 
 def parrot_validate_cache8_inputs(problem, rows, query_offsets, prefix_block_tables, prefix_lens, prefix_parents,
@@ -284,11 +284,13 @@ class Cache8Decoder:
 
     def bind(self, t: dict, stream=None):
         """Marshal once; the returned callable re-issues the same call, with what the plan
-        holds then.  ``t`` holds q_rows, suffix_tables, the layer's pools ``suffix`` and, with
-        groups, prefix_tables and ``prefix``."""
+        holds then.  ``t`` holds the planner's int arrays, q_rows, suffix_tables, the layer's
+        pools ``suffix`` and, with groups, prefix_tables and ``prefix``."""
         pl = self.planner
-        return _attend_call(pl.problem, pl.rows, t["q_rows"], t.get("prefix"), t["suffix"], t.get("prefix_tables"),
-                            t["suffix_tables"], pl.plan, self.out, self.lse, self.workspace, stream)
+        return _attend_call(pl.problem, pl.rows, t["q_rows"], t["query_offsets"], t.get("prefix"), t["suffix"],
+                            t.get("prefix_tables"), t.get("prefix_lens"), t["prefix_parents"] if pl.nested else None,
+                            t["suffix_tables"], t["suffix_lens"], t["group_ids"], pl.plan, self.out, self.lse,
+                            self.workspace, stream)
 
     def __call__(self, t: dict, stream=None, trace=None):
         self.bind(t, stream=stream)(trace)

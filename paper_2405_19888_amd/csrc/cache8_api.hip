@@ -39,6 +39,8 @@ parrot::Pool8 pool(const parrot_cache8* c) { return {c->k, c->v, c->scales}; }
 // ----------------------------------------------------------------- attention
 struct Plan8 {
   int depth;                       // levels of prefixes that the plan has room for
+  bool direct;                     // one launch without a plan
+  int tiles;                       // its column tiles per request
   int sets, cols, runs, min_run;
   bool wide;                       // neighbouring waves take runs of one head, else neighbouring heads
   int max_entries;
@@ -47,7 +49,15 @@ struct Plan8 {
   size_t plan_bytes, o_bytes, lse_bytes;
 };
 
+// Overrides the rule below for tests and tuning (per thread, set through
+// parrot_test_cache8_path): 0 one launch, 1 plan, partial results and join.
+thread_local int g_path = -1;
+
 constexpr int kMinRun = 6;         // cost of a run at least: four units and a tile's setup
+
+bool takes_one_launch(const parrot_problem* p, const parrot_tree_rows* rows, int depth, int tiles, long cus) {
+  return false;
+}
 
 parrot_status check_attend(const parrot_problem* p, const parrot_tree_rows* rows, Plan8* pl) {
   PARROT_TRY(parrot::check_problem_fields(p));
@@ -69,43 +79,76 @@ parrot_status check_attend(const parrot_problem* p, const parrot_tree_rows* rows
   const bool f32 = p->dtype == PARROT_DTYPE_F32;
   pl->depth = NG > 0 ? std::max(1, (int)p->max_prefix_depth) : 0;
   const long most = G * std::max((long)rows->max_query_rows, NG > 0 ? (long)rows->max_group_rows : 0L);
-  pl->sets = most <= 16 ? 1 : most <= 32 || f32 ? 2 : 4;
+  pl->sets = most <= 16 ? 1 : 2;
   pl->cols = 16 * pl->sets;
   pl->wide = most > pl->cols;
-  // four waves a CU hold 64 KiB on their way, and a tile of 64 columns leaves room for no more
-  const long waves = cus * (pl->sets > 2 || (f32 && pl->sets > 1) ? 4 : 8);
-  pl->runs = (int)std::max(1L, waves / H);
+  const auto waves = [&](int sets) { return cus * (f32 && sets > 1 ? 4 : 8); };
+  pl->runs = (int)std::max(1L, waves(pl->sets) / H);
   pl->min_run = kMinRun;
   // column tiles: those that columns fill, and one more for each sequence (sizes as for the
   // narrowest tiles and the most slots of calls of fewer columns, so that they never decrease)
   const long tiles = (1 + pl->depth) * T * G / 16 + R + NG;
-  const long units = ceil_div(std::max(p->max_suffix_len, NG > 0 ? p->max_prefix_len : 0), parrot::kUnit);
-  long spread = 16 * std::max(1L, cus * 8 / H);
-  if (pl->sets > 1) spread = std::max(spread, 32 * std::max(1L, cus * (f32 ? 4 : 8) / H));
-  if (pl->sets > 2) spread = std::max(spread, 64 * std::max(1L, cus * 4 / H));
+  const long units = ceil_div(p->max_suffix_len, parrot::kUnit) +
+                     (NG > 0 ? pl->depth * ceil_div(p->max_prefix_len, parrot::kUnit) : 0);
+  long spread = 16 * std::max(1L, waves(1) / H);
+  if (pl->sets > 1) spread = std::max(spread, 32 * std::max(1L, waves(2) / H));
   pl->slots = (1 + pl->depth) * T * G + spread;
-  const double ints = (double)tiles * (1 + parrot::kEntryInts) + (double)T * (parrot::kRowInts + pl->depth) +
-                      (NG + R) * (1.0 + parrot::kMaxDepth) + (parrot::kPlanWaves + 1.0) * NG;
+  const double ints = (double)tiles * (1 + parrot::kEntryInts) + (double)T * (1 + parrot::kRowInts + pl->depth) + waves(1) +
+                      (NG + R) * (1.0 + parrot::kMaxDepth + parrot::kReqInts) + (parrot::kPlanWaves + 1.0) * NG;
   if (((1.0 + pl->depth) * T * G / pl->cols + R + NG) * (units + parrot::kPieceSetup) > 1.5e9 || pl->slots > 0x7fffffffL || ints > 1.0e9 ||
-      R + NG > 0x3fffffffL || pl->runs * H * 64 > 0xffffffffL || T * ceil_div(rows->num_query_heads, 2) * 256 > 0xffffffffL)
+      R + NG > 0x3fffffffL || pl->runs * H * 64 > 0xffffffffL)
     return set_error(PARROT_ERR_UNSUPPORTED, "attention over 8 bits: %ld rows in %ld column tiles of %ld units", T, tiles, units);
   pl->max_entries = (int)tiles;
   auto& at = pl->at;
   long n = parrot::kPlanHead;
   auto take = [&n](long ints) { const long first = n; n = (n + ints + 3) & ~3L; return first; };
-  at.head = 0;
   at.cost = take(tiles);
   at.entry = take(tiles * parrot::kEntryInts);
+  at.run = take(waves(1));
   at.row = take(T * parrot::kRowInts);
+  at.join = take(T);
   at.list = take(T * std::max(pl->depth, 1));
   at.seq = take(NG + R + 1);
+  at.req = take(R * parrot::kReqInts);
   at.pos = take(R * parrot::kMaxDepth);
   at.count = take((parrot::kPlanWaves + 1) * NG + 1);
   at.total = n;
   pl->plan_bytes = align256((size_t)n * sizeof(int32_t));
   pl->o_bytes = align256((size_t)H * pl->slots * p->head_dim * sizeof(float));
   pl->lse_bytes = align256((size_t)H * pl->slots * sizeof(float));
+  pl->tiles = (int)ceil_div(rows->max_query_rows * G, 16);
+  const bool fits = R * H * pl->tiles <= 1L << 22;
+  pl->direct = fits && (g_path >= 0 ? g_path == 0 : takes_one_launch(p, rows, pl->depth, pl->tiles, cus));
   return PARROT_OK;
+}
+
+// The int arrays of a step: checks, and as the kernels take them.
+parrot_status step_arrays(const parrot_problem* p, const parrot_tree_rows* rows, const Plan8& pl, const int32_t* query_offsets,
+                          const int32_t* prefix_lens, const int32_t* prefix_parents, const int32_t* suffix_lens,
+                          const int32_t* group_ids, parrot::Step8* st) {
+  const parrot::PtrCheck need[] = {{query_offsets, "query_offsets", 4}, {suffix_lens, "suffix_lens", 4},
+                                   {group_ids, "group_ids", 4}};
+  PARROT_TRY(parrot::check_pointers(need));
+  if (p->num_groups > 0) {
+    const parrot::PtrCheck pre[] = {{prefix_lens, "prefix_lens", 4}};
+    PARROT_TRY(parrot::check_pointers(pre));
+    if (prefix_parents && reinterpret_cast<uintptr_t>(prefix_parents) % 4)
+      return bad("prefix_parents is not 4-byte aligned");
+  }
+  st->qoff = query_offsets; st->plen = prefix_lens; st->slen = suffix_lens; st->gid = group_ids;
+  st->parents = p->num_groups > 0 ? prefix_parents : nullptr;
+  st->T = rows->num_query_rows; st->R = p->num_requests; st->NG = p->num_groups;
+  st->G = rows->num_query_heads / p->num_heads;
+  st->depth = st->parents ? pl.depth : std::min(pl.depth, 1);
+  st->max_p = p->num_groups > 0 ? p->max_prefix_len : 0;
+  st->max_s = p->max_suffix_len; st->max_q = rows->max_query_rows;
+  return PARROT_OK;
+}
+
+parrot_status record_none(const parrot_trace& tr, hipStream_t s) {
+  for (void* e : {tr.merge_start, tr.merge_stop})
+    if (e && hipEventRecord(ev(e), s) != hipSuccess) return set_error(PARROT_ERR_HIP, "hipEventRecord failed");
+  return set_error(PARROT_OK, "");
 }
 
 }  // namespace
@@ -159,39 +202,32 @@ parrot_status parrot_cache8_plan(
   Plan8 pl;
   PARROT_TRY(check_attend(p, rows, &pl));
   if (rows->num_query_rows == 0) return set_error(PARROT_OK, "");
-  const parrot::PtrCheck need[] = {{query_offsets, "query_offsets", 4}, {suffix_lens, "suffix_lens", 4},
-                                   {group_ids, "group_ids", 4}, {plan, "plan", 256}};
+  parrot::Plan8Args a{};
+  PARROT_TRY(step_arrays(p, rows, pl, query_offsets, prefix_lens, prefix_parents, suffix_lens, group_ids, &a.st));
+  const parrot::PtrCheck need[] = {{plan, "plan", 256}};
   PARROT_TRY(parrot::check_pointers(need));
-  if (p->num_groups > 0) {
-    const parrot::PtrCheck pre[] = {{prefix_lens, "prefix_lens", 4}};
-    PARROT_TRY(parrot::check_pointers(pre));
-    if (prefix_parents && reinterpret_cast<uintptr_t>(prefix_parents) % 4)
-      return bad("prefix_parents is not 4-byte aligned");
-  }
   if (plan_bytes < pl.plan_bytes)
     return set_error(PARROT_ERR_WORKSPACE_TOO_SMALL, "plan is %zu bytes, need %zu", plan_bytes, pl.plan_bytes);
-  parrot::Plan8Args a{};
-  a.qoff = query_offsets; a.plen = prefix_lens; a.slen = suffix_lens; a.gid = group_ids;
-  a.parents = p->num_groups > 0 ? prefix_parents : nullptr;
+  if (pl.direct) return set_error(PARROT_OK, "");
   a.plan = reinterpret_cast<int*>(plan);
   a.at = pl.at;
-  a.T = rows->num_query_rows; a.R = p->num_requests; a.NG = p->num_groups;
-  a.G = rows->num_query_heads / p->num_heads;
-  a.depth = a.parents ? pl.depth : std::min(pl.depth, 1);
-  a.max_p = p->max_prefix_len; a.max_s = p->max_suffix_len; a.max_q = rows->max_query_rows;
-  a.cols = pl.cols; a.runs = pl.runs; a.min_run = pl.min_run;
+  a.cols = pl.cols; a.chain_cols = parrot::kChainTiles * pl.cols;
+  a.runs = pl.runs; a.min_run = pl.min_run;
   a.max_entries = pl.max_entries; a.max_slots = pl.slots;
   return launched(parrot::launch_plan8(a, reinterpret_cast<hipStream_t>(stream)), "plan kernel");
 }
 
 parrot_status parrot_cache8_attention(
-    const parrot_problem* p, const parrot_tree_rows* rows, const void* q, const parrot_cache8* prefix,
-    const parrot_cache8* suffix, const int32_t* prefix_block_tables, const int32_t* suffix_block_tables, const void* plan,
-    size_t plan_bytes, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream,
+    const parrot_problem* p, const parrot_tree_rows* rows, const void* q, const int32_t* query_offsets,
+    const parrot_cache8* prefix, const parrot_cache8* suffix, const int32_t* prefix_block_tables, const int32_t* prefix_lens,
+    const int32_t* prefix_parents, const int32_t* suffix_block_tables, const int32_t* suffix_lens, const int32_t* group_ids,
+    const void* plan, size_t plan_bytes, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream,
     const parrot_trace* trace) {
   Plan8 pl;
   PARROT_TRY(check_attend(p, rows, &pl));
   if (rows->num_query_rows == 0) return set_error(PARROT_OK, "");
+  parrot::Attend8Args a{};
+  PARROT_TRY(step_arrays(p, rows, pl, query_offsets, prefix_lens, prefix_parents, suffix_lens, group_ids, &a.st));
   const parrot::PtrCheck need[] = {{q, "q", 16}, {suffix_block_tables, "suffix_block_tables", 4}, {plan, "plan", 256},
                                    {out, "out", 16}, {lse, "lse", 4}, {workspace, "workspace", 256}};
   PARROT_TRY(parrot::check_pointers(need));
@@ -206,7 +242,6 @@ parrot_status parrot_cache8_attention(
     return set_error(PARROT_ERR_WORKSPACE_TOO_SMALL, "plan is %zu bytes, need %zu", plan_bytes, pl.plan_bytes);
   if (workspace_bytes < pl.o_bytes + pl.lse_bytes)
     return set_error(PARROT_ERR_WORKSPACE_TOO_SMALL, "workspace is %zu bytes, need %zu", workspace_bytes, pl.o_bytes + pl.lse_bytes);
-  parrot::Attend8Args a{};
   a.q = q; a.out = out; a.lse = lse;
   a.own = pool(suffix);
   if (p->num_groups > 0) a.pre = pool(prefix);
@@ -217,19 +252,31 @@ parrot_status parrot_cache8_attention(
   a.lse_part = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + pl.o_bytes);
   a.slots = pl.slots;
   a.T = rows->num_query_rows; a.R = p->num_requests; a.H = p->num_heads; a.NG = p->num_groups;
-  a.G = rows->num_query_heads / p->num_heads; a.depth = pl.depth;
+  a.G = a.st.G; a.depth = pl.depth;
   a.pstride = p->prefix_table_stride; a.sstride = p->suffix_table_stride;
-  a.max_p = p->num_groups > 0 ? p->max_prefix_len : 0; a.max_s = p->max_suffix_len;
+  a.max_p = a.st.max_p; a.max_s = p->max_suffix_len;
   a.npblk = p->num_groups > 0 ? p->num_prefix_blocks : 1; a.nsblk = p->num_suffix_blocks;
-  a.runs = pl.runs; a.sets = pl.sets; a.wide = pl.wide; a.max_entries = pl.max_entries;
+  a.runs = pl.runs; a.sets = pl.sets; a.wide = pl.wide; a.max_entries = pl.max_entries; a.tiles = pl.tiles;
   a.flip = p->sm_scale < 0.f;
   a.scale_log2 = std::fabs(p->sm_scale) * parrot::kLog2e;
   const parrot_trace none = {nullptr, nullptr, nullptr, nullptr};
   const parrot_trace& tr = trace ? *trace : none;
   const int dt = (int)p->dtype, D = p->head_dim;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  if (pl.direct) {
+    PARROT_TRY(launched(parrot::launch_direct8(a, dt, D, s, ev(tr.partials_start), ev(tr.partials_stop)), "8-bit attention kernel"));
+    return record_none(tr, s);
+  }
   PARROT_TRY(launched(parrot::launch_attend8(a, dt, D, s, ev(tr.partials_start), ev(tr.partials_stop)), "8-bit attention kernel"));
   return launched(parrot::launch_join8(a, dt, D, s, ev(tr.merge_start), ev(tr.merge_stop)), "8-bit join kernel");
+}
+
+// Test hooks (not in parrot_attn.h): the path of this thread's calls (see g_path; -1 gives the
+// choice back), and the one these arguments take (-1: invalid).
+void parrot_test_cache8_path(int path) { g_path = path == 0 || path == 1 ? path : -1; }
+int parrot_test_cache8_planned(const parrot_problem* p, const parrot_tree_rows* rows) {
+  Plan8 pl;
+  return check_attend(p, rows, &pl) == PARROT_OK ? !pl.direct : -1;
 }
 
 parrot_status parrot_validate_cache8_inputs(

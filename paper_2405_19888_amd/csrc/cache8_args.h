@@ -26,29 +26,45 @@ hipError_t launch_fill8(const Fill8Args& a, int partner, int dtype, int D, hipSt
 // Where a plan holds what, in ints from its start.  Entries are the column tiles of sequences:
 // the groups first (their columns are the rows of all requests that read the group's prefix, times
 // the query heads of a cache head), then the requests (their own rows' columns), in order.
+// A request whose own columns fill kChainTiles tiles goes through its group chain by itself, in
+// one piece with its own tokens, and is no reader of the groups.
 struct Plan8Layout {
-  long head, cost, entry, row, list, seq, pos, count, total;
+  long cost, entry, run, row, join, list, seq, req, pos, count, total;
 };
-constexpr int kPlanHead = 16;            // ints of the head: entries, run length, total cost, slots
+constexpr int kPlanHead = 16;            // ints of the head, see Head8
 constexpr int kEntryInts = 12;
 constexpr int kRowInts = 12;
+constexpr int kReqInts = 12;
 constexpr int kPlanWaves = 16;           // waves of the planning workgroup
 constexpr int kPieceSetup = 2;           // cost of a tile beside its units
+constexpr int kChainTiles = 4;
 
-// An entry: sequence (request r, or ~g), its columns [col0, col0 + ncols), cost at which it
-// starts, units, first slot of its partial results (-1: it writes the output), pieces, keys,
-// keys that every column sees, first row (group: first place in the row list).
-enum Entry8 { kEntSeq, kEntCol0, kEntCols, kEntCost, kEntUnits, kEntSlot, kEntPieces, kEntKeys, kEntBase, kEntFirst };
+// The head: entries, run length, total cost, rows to join.
+enum Head8 { kHeadEntries, kHeadRun, kHeadCost, kHeadJoins };
+// An entry: sequence (request r, or ~g for group), its columns [col0, col0 + ncols), cost at which it
+// starts, units, first slot of its partial results (-1: it writes the output), pieces, own keys (of a
+// group: its prefix's), keys that every column sees, first row (group: first place in the row
+// list), flags: the chain's prefixes come first; no other tile reads the keys.
+enum Entry8 { kEntSeq, kEntCol0, kEntCols, kEntCost, kEntUnits, kEntSlot, kEntPieces, kEntKeys, kEntBase, kEntFirst, kEntFlags };
+constexpr int kEntChained = 1, kEntOnce = 2;
 // A row: entry of its request's first tile, its place in the request, levels of prefixes, then
 // for each level the entry of the group's first tile and the row's place in the group's list.
 enum Row8 { kRowEntry, kRowPlace, kRowLevels, kRowUnused, kRowGroup };
+// A request: first row, rows, own tokens, its group where it reads groups' results (-1), then
+// its chain's groups and their tokens, innermost first.
+enum Req8 { kReqFirst, kReqCount, kReqKeys, kReqReads, kReqChain };
 
-struct Plan8Args {
+// The int arrays of a step.
+struct Step8 {
   const int* qoff; const int* plen; const int* parents; const int* slen; const int* gid;
+  int T, R, NG, G, depth, max_p, max_s, max_q;   // depth: levels of this call's chains
+};
+struct Plan8Args {
+  Step8 st;
   int* plan;
   Plan8Layout at;
-  int T, R, NG, G, depth, max_p, max_s, max_q;   // depth: levels of this call's chains
   int cols;                              // columns of a tile
+  int chain_cols;                        // own columns from which a request is no reader of groups
   int runs, min_run;
   int max_entries; long max_slots;
 };
@@ -60,17 +76,21 @@ struct Attend8Args {
   const int* ptab; const int* stab;
   const int* plan;
   Plan8Layout at;
+  Step8 st;                              // the one launch without a plan
   void* out; float* lse;                 // [T][HQ][D] dtype, [T][HQ]
   float* o_part; float* lse_part;        // [H][slots][D] normalised, [H][slots] base 2
   long slots;
   int T, R, H, G, NG, depth;             // depth: levels that the plan has room for
   int pstride, sstride, max_p, max_s, npblk, nsblk;
   int runs, sets, wide, max_entries;     // sets: column sets of a tile; wide: a workgroup's waves take runs of one head
+  int tiles;                             // one launch: column tiles of a request
   int flip;                              // sm_scale < 0: queries change sign
   float scale_log2;                      // |sm_scale| log2(e)
 };
 hipError_t launch_attend8(const Attend8Args& a, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
 hipError_t launch_join8(const Attend8Args& a, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
+// One launch, without a plan: a workgroup per request, cache head and column tile.
+hipError_t launch_direct8(const Attend8Args& a, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
 
 // A copy of blocks of several pools, each with its block's bytes (a multiple of 2).
 constexpr int kCopyPools = 128;          // pools of one launch

@@ -1,5 +1,5 @@
 // Attention over a cache held in 8 bits (cache8_args.h has the format, cache8_tile.h the
-// wave's mathematics): plan, partial results, join.
+// wave's mathematics): plan, partial results and join, or one launch for small calls.
 //
 // What a step has to read is laid end to end as one list of costs: column tiles of the groups'
 // prefixes (the rows of all requests below a group, stacked, so that a prefix is read once per tile
@@ -38,7 +38,7 @@ PARROT_DEV int scan1024(int x, int* lds, int* total) {
 
 // The rows of request r, and its own tokens.
 struct Own8 { int first, count, keys; };
-PARROT_DEV Own8 own_rows(const Plan8Args& a, int r) {
+PARROT_DEV Own8 own_rows(const Step8& a, int r) {
   Own8 o;
   o.keys = clampi(a.slen[r], 0, a.max_s);
   const int begin = a.qoff[r], end = a.qoff[r + 1];
@@ -51,20 +51,19 @@ PARROT_DEV Own8 own_rows(const Plan8Args& a, int r) {
 
 // Rows of each of the wave's requests that read groups, by level of the chain: counts of the
 // wave's rows per group (assign false), or each request's place in the group's list.
-PARROT_DEV void walk_groups(const Plan8Args& a, int* count, bool assign) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int r0 = (int)((long)a.R * wave / kPlanWaves), r1 = (int)((long)a.R * (wave + 1) / kPlanWaves);
-  int* mine = count + (long)wave * a.NG;
-  int* pos = a.plan + a.at.pos;
+PARROT_DEV void walk_groups(const Plan8Args& a, const int* req, int* pos, int* count, bool assign) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, NG = a.st.NG;
+  const int r0 = (int)((long)a.st.R * wave / kPlanWaves), r1 = (int)((long)a.st.R * (wave + 1) / kPlanWaves);
+  int* mine = count + (long)wave * NG;
   for (int b = r0; b < r1; b += kWave) {
     const int r = b + lane;
     int n = 0, grp = -1;
     if (r < r1) {
-      n = own_rows(a, r).count;
-      grp = a.gid[r];
+      n = req[(long)r * kReqInts + kReqCount];
+      grp = req[(long)r * kReqInts + kReqReads];
     }
-    for (int l = 0; l < a.depth; ++l) {
-      const bool on = n > 0 && grp >= 0 && grp < a.NG;
+    for (int l = 0; l < a.st.depth; ++l) {
+      const bool on = n > 0 && grp >= 0;
       unsigned long long todo = __ballot(on);
       if (!todo) break;
       while (todo) {
@@ -83,62 +82,90 @@ PARROT_DEV void walk_groups(const Plan8Args& a, int* count, bool assign) {
         const int sum = __shfl(incl, kWave - 1);
         if (lane == leader) mine[gl] = base + sum;
         todo &= ~all;
-        // (a wave's own writes come back in order)
-        __threadfence_block();
+        __threadfence_block();                          // (a wave's own writes come back in order)
       }
-      grp = on && a.parents ? a.parents[grp] : -1;
+      grp = on && l + 1 < kMaxDepth ? req[(long)r * kReqInts + kReqChain + 2 * (l + 1)] : -1;
     }
   }
 }
 
-// One workgroup: a few round trips and scans for a usual batch, 1024 requests, groups or entries a round.
+// One workgroup: a few round trips and scans for a usual batch, 1024 requests, groups or entries a
+// round.  What it looks up again and again is in LDS where it fits.
+constexpr int kPlanReqs = 1024, kPlanCounts = 4096, kPlanSeqs = 2048;
 __global__ __launch_bounds__(1024) void k_cache8_plan(Plan8Args a) {
-  __shared__ int lds[kPlanWaves];
+  __shared__ int lds[kPlanWaves + 2];
+  __shared__ __attribute__((aligned(16))) int l_req[kPlanReqs * kReqInts];
+  __shared__ int l_count[kPlanCounts], l_seq[kPlanSeqs], l_cost[kPlanSeqs];
   const int tid = threadIdx.x;
-  int* head = a.plan;
-  int* cost = a.plan + a.at.cost;
+  const Step8& st = a.st;
   int* ent = a.plan + a.at.entry;
   int* rows = a.plan + a.at.row;
   int* list = a.plan + a.at.list;
-  int* seq = a.plan + a.at.seq;
-  int* count = a.plan + a.at.count;
-  int* off = count + (long)kPlanWaves * a.NG;           // first place of each group's rows
-  const int* pos = a.plan + a.at.pos;
+  int* joins = a.plan + a.at.join;
+  int* pos = a.plan + a.at.pos;
+  const int nseq = st.NG + st.R;
+  int* const g_req = a.plan + a.at.req;
+  int* req = st.R <= kPlanReqs ? l_req : g_req;
+  int* count = (long)(kPlanWaves + 1) * st.NG + 1 <= kPlanCounts ? l_count : a.plan + a.at.count;
+  int* seq = nseq < kPlanSeqs ? l_seq : a.plan + a.at.seq;
+  int* off = count + (long)kPlanWaves * st.NG;          // first place of each group's rows
 
+  // the requests
+  for (int r = tid; r < st.R; r += 1024) {
+    const Own8 o = own_rows(st, r);
+    int v[kReqInts] = {o.first, o.count, o.keys, -1, -1, 0, -1, 0, -1, 0, -1, 0};
+    int grp = st.gid[r];
+    const bool chained = (long)o.count * st.G >= a.chain_cols;
+#pragma unroll
+    for (int l = 0; l < kMaxDepth; ++l)
+      if (l < st.depth && grp >= 0 && grp < st.NG) {
+        v[kReqChain + 2 * l] = grp;
+        v[kReqChain + 2 * l + 1] = clampi(st.plen[grp], 0, st.max_p);
+        if (l == 0 && !chained) v[kReqReads] = grp;
+        grp = st.parents ? st.parents[grp] : -1;
+      } else {
+        grp = -1;
+      }
+    // (the attention reads the requests from the plan)
+#pragma unroll
+    for (int i = 0; i < kReqInts; i += 4) {
+      *reinterpret_cast<int4*>(g_req + (long)r * kReqInts + i) = int4{v[i], v[i + 1], v[i + 2], v[i + 3]};
+      if (req != g_req) *reinterpret_cast<int4*>(req + r * kReqInts + i) = int4{v[i], v[i + 1], v[i + 2], v[i + 3]};
+    }
+    seq[st.NG + r] = (int)(((long)o.count * st.G + a.cols - 1) / a.cols);
+  }
+  if (tid == 0) lds[kPlanWaves] = 0;                    // rows to join
+  for (long i = tid; i < (long)kPlanWaves * st.NG; i += 1024) count[i] = 0;
+  __syncthreads();
   // rows of each group, and each request's place among them
-  if (a.depth > 0) {
-    for (long i = tid; i < (long)kPlanWaves * a.NG; i += 1024) count[i] = 0;
-    __syncthreads();
-    walk_groups(a, count, false);
+  if (st.depth > 0) {
+    walk_groups(a, req, pos, count, false);
     __syncthreads();
     int before = 0;
-    for (int b = 0; b < a.NG; b += 1024) {
+    for (int b = 0; b < st.NG; b += 1024) {
       const int g = b + tid;
       int n = 0;
-      if (g < a.NG)
+      if (g < st.NG)
         for (int w = 0; w < kPlanWaves; ++w) {          // counts become places
-          const int x = count[(long)w * a.NG + g];
-          count[(long)w * a.NG + g] = n;
+          const int x = count[(long)w * st.NG + g];
+          count[(long)w * st.NG + g] = n;
           n += x;
         }
       int sum;
       const int incl = scan1024(n, lds, &sum);
-      if (g < a.NG) {
+      if (g < st.NG) {
         off[g] = before + incl - n;
         // tiles of the group
-        seq[g] = clampi(a.plen[g], 0, a.max_p) > 0 ? (int)(((long)n * a.G + a.cols - 1) / a.cols) : 0;
+        seq[g] = clampi(st.plen[g], 0, st.max_p) > 0 ? (int)(((long)n * st.G + a.cols - 1) / a.cols) : 0;
       }
       before += sum;
     }
-    if (tid == 0) off[a.NG] = before;
+    if (tid == 0) off[st.NG] = before;
     __syncthreads();
-    walk_groups(a, count, true);
+    walk_groups(a, req, pos, count, true);
+    __syncthreads();
   }
-  for (int r = tid; r < a.R; r += 1024)
-    seq[a.NG + r] = (int)(((long)own_rows(a, r).count * a.G + a.cols - 1) / a.cols);
-  __syncthreads();
   // tiles become first entries
-  const int nseq = a.NG + a.R;
   int entries = 0;
   for (int b = 0; b < nseq; b += 1024) {
     const int i = b + tid;
@@ -149,6 +176,7 @@ __global__ __launch_bounds__(1024) void k_cache8_plan(Plan8Args a) {
     entries += sum;
   }
   entries = min(entries, a.max_entries);
+  int* cost = entries <= kPlanSeqs ? l_cost : a.plan + a.at.cost;
   __syncthreads();
 
   // the entries, and where each starts in the cost
@@ -164,22 +192,29 @@ __global__ __launch_bounds__(1024) void k_cache8_plan(Plan8Args a) {
       }
       const int tile = e - seq[lo];
       v[kEntCol0] = tile * a.cols;
-      if (lo < a.NG) {
+      if (lo < st.NG) {
         const int n = off[lo + 1] - off[lo];
         v[kEntSeq] = ~lo;
-        v[kEntCols] = (int)min((long)a.cols, (long)n * a.G - v[kEntCol0]);
-        v[kEntKeys] = v[kEntBase] = clampi(a.plen[lo], 0, a.max_p);
+        v[kEntCols] = (int)min((long)a.cols, (long)n * st.G - v[kEntCol0]);
+        v[kEntKeys] = v[kEntBase] = clampi(st.plen[lo], 0, st.max_p);
         v[kEntFirst] = off[lo];
+        v[kEntUnits] = (v[kEntKeys] + kUnit - 1) / kUnit;
+        v[kEntFlags] = n * (long)st.G <= a.cols ? kEntOnce : 0;
       } else {
-        const Own8 o = own_rows(a, lo - a.NG);
-        v[kEntSeq] = lo - a.NG;
-        v[kEntCols] = (int)min((long)a.cols, (long)o.count * a.G - v[kEntCol0]);
-        const int from = o.keys - o.count;              // row j sees own tokens 0 .. from + j
-        v[kEntKeys] = from + (v[kEntCol0] + v[kEntCols] - 1) / a.G + 1;
+        const int* o = req + (long)(lo - st.NG) * kReqInts;
+        v[kEntSeq] = lo - st.NG;
+        v[kEntCols] = (int)min((long)a.cols, (long)o[kReqCount] * st.G - v[kEntCol0]);
+        const int from = o[kReqKeys] - o[kReqCount];    // row j sees own tokens 0 .. from + j
+        v[kEntKeys] = from + (v[kEntCol0] + v[kEntCols] - 1) / st.G + 1;
         v[kEntBase] = from;
-        v[kEntFirst] = o.first;
+        v[kEntFirst] = o[kReqFirst];
+        v[kEntUnits] = (v[kEntKeys] + kUnit - 1) / kUnit;
+        v[kEntFlags] = (long)o[kReqCount] * st.G <= a.cols ? kEntOnce : 0;
+        if (o[kReqReads] < 0 && o[kReqChain] >= 0) {
+          v[kEntFlags] |= kEntChained;
+          for (int l = 0; l < kMaxDepth; ++l) v[kEntUnits] += (o[kReqChain + 2 * l + 1] + kUnit - 1) / kUnit;
+        }
       }
-      v[kEntUnits] = (v[kEntKeys] + kUnit - 1) / kUnit;
       c = v[kEntUnits] + kPieceSetup;
     }
     int sum;
@@ -194,7 +229,17 @@ __global__ __launch_bounds__(1024) void k_cache8_plan(Plan8Args a) {
     }
     total += sum;
   }
+  __syncthreads();
   const int q = max(a.min_run, (int)(((long)total + a.runs - 1) / a.runs));
+  // the first entry of each run
+  for (int run = tid; run < a.runs && (long)run * q < total; run += 1024) {
+    int lo = 0, hi = entries;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (cost[mid] <= run * q) lo = mid; else hi = mid;
+    }
+    a.plan[a.at.run + run] = lo;
+  }
   // pieces, and the slots of their partial results
   int slots = 0;
   for (int b = 0; b < entries; b += 1024) {
@@ -204,9 +249,8 @@ __global__ __launch_bounds__(1024) void k_cache8_plan(Plan8Args a) {
     if (e < entries) {                                  // (its own entries)
       const int s0 = v[kEntCost] + kPieceSetup;
       pieces = (s0 + v[kEntUnits] - 1) / q - s0 / q + 1;
-      const int r = v[kEntSeq], grp = r >= 0 ? a.gid[r] : 0;
-      const bool alone = r >= 0 && !(a.depth > 0 && grp >= 0 && grp < a.NG);
-      n = alone && pieces == 1 ? 0 : pieces * v[kEntCols];
+      const int r = v[kEntSeq];
+      n = r >= 0 && pieces == 1 && req[(long)r * kReqInts + kReqReads] < 0 ? 0 : pieces * v[kEntCols];
     }
     int sum;
     const int incl = scan1024(n, lds, &sum);
@@ -216,46 +260,86 @@ __global__ __launch_bounds__(1024) void k_cache8_plan(Plan8Args a) {
     }
     slots += sum;
   }
-  if (tid == 0) {
-    head[0] = entries;
-    head[1] = q;
-    head[2] = total;
-    head[3] = slots;
-  }
-  // the groups' row lists, and what the join needs of each row
-  const int used = clampi(a.qoff[a.R], 0, a.T);
-  for (int t = tid; t < a.T; t += 1024) {
-    if (t >= used) { rows[(long)t * kRowInts + kRowLevels] = -1; continue; }        // padding
-    int lo = 0, hi = a.R;                               // the last request that starts at or before t
+  __syncthreads();
+  // the groups' row lists, what the join needs of each row, and the rows that it takes
+  const int used = clampi(st.qoff[st.R], 0, st.T);
+  for (int t = tid; t < used; t += 1024) {
+    int lo = 0, hi = st.R;                              // the last request that starts at or before t
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (a.qoff[mid] <= t) lo = mid; else hi = mid;
+      if (req[(long)mid * kReqInts + kReqFirst] <= t) lo = mid; else hi = mid;
     }
-    const Own8 o = own_rows(a, lo);
-    const int j = t - o.first;
-    int* d = rows + (long)t * kRowInts;
-    if (j < 0 || j >= o.count) { d[kRowLevels] = -1; continue; }     // no request holds it
-    d[kRowEntry] = seq[a.NG + lo];
-    d[kRowPlace] = j;
-    int levels = 0;
-    int grp = a.gid[lo];
-    for (int l = 0; l < a.depth && grp >= 0 && grp < a.NG; ++l) {
-      const int at = pos[(long)lo * kMaxDepth + l] + j;
-      if (clampi(a.plen[grp], 0, a.max_p) > 0) {
-        d[kRowGroup + 2 * levels] = seq[grp];
-        d[kRowGroup + 2 * levels + 1] = at;
-        ++levels;
+    const int* o = req + (long)lo * kReqInts;
+    const int j = t - o[kReqFirst];
+    if (j < 0 || j >= o[kReqCount]) continue;           // no request holds it
+    int v[kRowInts] = {};
+    const int first = seq[st.NG + lo];
+    v[kRowEntry] = first;
+    v[kRowPlace] = j;
+    if (o[kReqReads] >= 0)
+#pragma unroll
+      for (int l = 0; l < kMaxDepth; ++l) {
+        const int grp = o[kReqChain + 2 * l];
+        if (grp >= 0) {
+          const int at = pos[(long)lo * kMaxDepth + l] + j;
+          if (o[kReqChain + 2 * l + 1] > 0) {
+            v[kRowGroup + 2 * l] = seq[grp];
+            v[kRowGroup + 2 * l + 1] = at;
+            v[kRowLevels] = l + 1;
+          }
+          list[min((long)off[grp] + at, (long)st.T * st.depth - 1)] = t;
+        }
       }
-      list[min((long)off[grp] + at, (long)a.T * a.depth - 1)] = t;
-      grp = a.parents ? a.parents[grp] : -1;
-    }
-    d[kRowLevels] = levels;
+    int4* d = reinterpret_cast<int4*>(rows + (long)t * kRowInts);
+    d[0] = int4{v[0], v[1], v[2], v[3]};
+    d[1] = int4{v[4], v[5], v[6], v[7]};
+    d[2] = int4{v[8], v[9], v[10], v[11]};
+    // (the row's columns are in one or more of its request's tiles)
+    bool parts = false;
+    for (int e = first + (int)((long)j * st.G / a.cols); e <= first + (int)(((long)j * st.G + st.G - 1) / a.cols) && e < entries; ++e)
+      parts = parts || ent[(long)e * kEntryInts + kEntSlot] >= 0;
+    // (their order is of no matter: each row is joined by itself)
+    if (parts) joins[min(atomicAdd(&lds[kPlanWaves], 1), st.T - 1)] = t;
   }
+  __syncthreads();
+  if (tid == 0) *reinterpret_cast<int4*>(a.plan) = int4{entries, q, total, lds[kPlanWaves]};
 }
 
 // ----------------------------------------------------------- partial results
-// An entry as the kernels read it: wave-uniform, every index clamped to what it may address.
-struct Entry { int seq, col0, cols, cost, units, slot, keys, base, first; };
+// Keys of one sequence of a call: a request's own tokens, or a group's prefix.
+PARROT_DEV Range8 range_of(const Attend8Args& a, bool own, int seq, int keys, int u0, int u1) {
+  Range8 rg;
+  rg.pool = own ? a.own : a.pre;
+  rg.tbl = own ? a.stab + (long)seq * a.sstride : a.ptab + (long)seq * a.pstride;
+  rg.npool = own ? a.nsblk : a.npblk;
+  rg.u0 = u0;
+  rg.u1 = u1;
+  rg.end = rg.plain = keys;
+  rg.once = false;
+  return rg;
+}
+
+// Output of a column that saw its whole context.  Every row sees itself: no weights mean that each
+// logit is -inf.
+template <int DT, int D, int NS>
+PARROT_DEV void write_column(const Attend8Args& a, const Tile8<DT, D, NS>& tile, int c, long at, float inv, float lse2) {
+  const int g = tile.lane >> 4;
+  char* dst = (char*)a.out + (at * D + 16 * g) * Elem<DT>::kBytes;
+  const float f = lse2 == -INFINITY ? __builtin_nanf("") : inv;
+#pragma unroll
+  for (int x = 0; x < D / 64; ++x)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f32x4 v = tile.four(c, x, i) * f;
+      char* to = dst + (64 * x + 4 * i) * Elem<DT>::kBytes;
+      if constexpr (DT == kF32) *reinterpret_cast<f32x4*>(to) = v;
+      else *reinterpret_cast<uint2*>(to) = uint2{Wide8<DT>::pack(v[0], v[1]), Wide8<DT>::pack(v[2], v[3])};
+    }
+  if (g == 0) a.lse[at] = lse2 == -INFINITY ? __builtin_nanf("") : lse2 * kLn2;
+}
+
+// An entry as the kernel reads it: wave-uniform, every index clamped to what it may address.
+struct Entry { int seq, col0, cols, cost, units, slot, keys, base, first, flags; };
 PARROT_DEV Entry load_entry(const Attend8Args& a, int e) {
   const int* p = a.plan + a.at.entry + (long)e * kEntryInts;
   Entry v;
@@ -265,10 +349,11 @@ PARROT_DEV Entry load_entry(const Attend8Args& a, int e) {
   v.cols = clampi(ld_uniform(p + kEntCols), 0, 16 * a.sets);
   v.cost = ld_uniform(p + kEntCost);
   v.keys = clampi(ld_uniform(p + kEntKeys), 0, v.seq >= 0 ? a.max_s : a.max_p);
-  v.units = clampi(ld_uniform(p + kEntUnits), 0, (v.keys + kUnit - 1) / kUnit);
+  v.units = max(ld_uniform(p + kEntUnits), 0);
   v.slot = ld_uniform(p + kEntSlot);
   v.base = ld_uniform(p + kEntBase);
   v.first = max(ld_uniform(p + kEntFirst), 0);
+  v.flags = ld_uniform(p + kEntFlags);
   return v;
 }
 
@@ -276,8 +361,9 @@ PARROT_DEV Entry load_entry(const Attend8Args& a, int e) {
 template <int DT, int D, int NS>
 PARROT_DEV void attend_piece(const Attend8Args& a, const Entry& e, int h, int u0, int u1, int piece) {
   const int HQ = a.H * a.G;
+  const bool own = e.seq >= 0;
   Tile8<DT, D, NS> tile(a.H, h);
-  int at[NS];                                           // the columns' places in [T][HQ], or -1
+  int at[NS], sees[NS];                                 // the columns' places in [T][HQ], or -1, and own keys
 #pragma unroll
   for (int c = 0; c < NS; ++c) {
     const int col = tile.column(c);
@@ -285,22 +371,31 @@ PARROT_DEV void attend_piece(const Attend8Args& a, const Entry& e, int h, int u0
     at[c] = -1;
     if (col < e.cols) {
       int row = e.first + j;
-      if (e.seq < 0) row = a.plan[a.at.list + min((long)row, (long)a.T * max(a.depth, 1) - 1)];
+      if (!own) row = a.plan[a.at.list + min((long)row, (long)a.T * max(a.depth, 1) - 1)];
       at[c] = clampi(row, 0, a.T - 1) * HQ + h * a.G + (x - j * a.G);
     }
-    tile.lim[c] = e.seq < 0 ? e.keys : min(e.keys, e.base + j + 1);
+    sees[c] = min(e.keys, e.base + j + 1);
   }
   tile.load_queries(a.q, a.flip != 0, [&](int c) { return (long)at[c]; });
-  Range8 rg;
-  const bool own = e.seq >= 0;
-  rg.pool = own ? a.own : a.pre;
-  rg.tbl = own ? a.stab + (long)e.seq * a.sstride : a.ptab + (long)~e.seq * a.pstride;
-  rg.npool = own ? a.nsblk : a.npblk;
-  rg.u0 = u0;
-  rg.u1 = u1;
-  rg.end = e.keys;
-  rg.plain = own ? min(e.keys, e.base + e.col0 / a.G + 1) : e.keys;
-  tile.run(rg, a.scale_log2);
+  // the chain's prefixes where they come first, then the entry's own keys
+  const int* chain = a.plan + a.at.req + (long)(own ? e.seq : 0) * kReqInts + kReqChain;
+  int from = 0;                                         // units before the range
+#pragma unroll 1
+  for (int l = own && (e.flags & kEntChained) ? 0 : kMaxDepth; l <= kMaxDepth; ++l) {
+    const bool pre = l < kMaxDepth;
+    const int grp = pre ? clampi(ld_uniform(chain + 2 * l), 0, max(a.NG - 1, 0)) : 0;
+    const int keys = pre ? clampi(ld_uniform(chain + 2 * l + 1), 0, a.NG > 0 ? a.max_p : 0) : e.keys;
+    const int units = (keys + kUnit - 1) / kUnit;
+    const int b = max(u0 - from, 0), f = min(u1 - from, units);
+    from += units;
+    if (b >= f) continue;
+    Range8 rg = range_of(a, own && !pre, pre ? grp : own ? e.seq : ~e.seq, keys, b, f);
+    if (own && !pre) rg.plain = min(keys, e.base + e.col0 / a.G + 1);
+    rg.once = !pre && (e.flags & kEntOnce);
+#pragma unroll
+    for (int c = 0; c < NS; ++c) tile.lim[c] = own && !pre ? sees[c] : keys;
+    tile.run(rg, a.scale_log2);
+  }
 
   const int g = tile.lane >> 4;
   const long slot = e.slot + (long)piece * e.cols;
@@ -309,19 +404,7 @@ PARROT_DEV void attend_piece(const Attend8Args& a, const Entry& e, int h, int u0
   tile.finish([&](int c, int col, float inv, float lse2) {
     if (at[c] < 0) return;
     if (direct) {
-      char* dst = (char*)a.out + ((long)at[c] * D + 16 * g) * Elem<DT>::kBytes;
-      // (every row sees itself: no weights mean that each logit is -inf)
-      const float f = lse2 == -INFINITY ? __builtin_nanf("") : inv;
-#pragma unroll
-      for (int x = 0; x < D / 64; ++x)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const f32x4 v = tile.four(c, x, i) * f;
-          char* to = dst + (64 * x + 4 * i) * Elem<DT>::kBytes;
-          if constexpr (DT == kF32) *reinterpret_cast<f32x4*>(to) = v;
-          else *reinterpret_cast<uint2*>(to) = uint2{Wide8<DT>::pack(v[0], v[1]), Wide8<DT>::pack(v[2], v[3])};
-        }
-      if (g == 0) a.lse[at[c]] = lse2 == -INFINITY ? __builtin_nanf("") : lse2 * kLn2;
+      write_column(a, tile, c, at[c], inv, lse2);
     } else {
       const long sl = (long)h * a.slots + slot + col;
       float* dst = a.o_part + sl * D + 16 * g;
@@ -335,9 +418,9 @@ PARROT_DEV void attend_piece(const Attend8Args& a, const Entry& e, int h, int u0
 }
 
 template <int DT, int D, int SETS>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SETS > 2 || (DT == kF32 && SETS > 1) ? 1 : 2)))
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DT == kF32 && SETS > 1 ? 1 : 2)))
 void k_cache8_attend(Attend8Args a) {
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int run, h;
   if (a.wide) {                                         // neighbouring tiles of one head, on one XCD
     h = blockIdx.x % a.H;
@@ -348,121 +431,212 @@ void k_cache8_attend(Attend8Args a) {
     run = w / a.H;
   }
   if (run >= a.runs) return;
-  const int entries = clampi(ld_uniform(a.plan), 0, a.max_entries);
-  const int q = max(ld_uniform(a.plan + 1), 1), total = ld_uniform(a.plan + 2);
+  const int entries = clampi(ld_uniform(a.plan + kHeadEntries), 0, a.max_entries);
+  const int q = max(ld_uniform(a.plan + kHeadRun), 1), total = ld_uniform(a.plan + kHeadCost);
+  const int first = ld_uniform(a.plan + a.at.run + run);
   const long c0 = (long)run * q, c1 = min((long)total, c0 + q);
-  if (c0 >= total || entries == 0) return;
-  // the last entry that starts at or before the run, a factor of 64 a round trip
-  const int* cost = a.plan + a.at.cost;
-  int e = 0;
-  for (int n = entries; n > 1;) {
-    const int step = (n + kWave - 1) / kWave;
-    const int at = lane * step;
-    const int k = __popcll(__ballot(at < n && cost[e + min(at, n - 1)] <= c0));
-    e += max(k - 1, 0) * step;
-    n = min(step, n - max(k - 1, 0) * step);
-    if (step == 1) break;
-  }
-  e = __builtin_amdgcn_readfirstlane(e);
+  if (c0 >= total) return;
 #pragma unroll 1
-  for (; e < entries; ++e) {
+  for (int e = max(first, 0); e < entries; ++e) {
     const Entry v = load_entry(a, e);
     if (v.cost >= c1) break;
     const long s0 = (long)v.cost + kPieceSetup;
     const int u0 = (int)max(c0 - s0, 0L), u1 = (int)min(c1 - s0, (long)v.units);
     if (u0 >= u1 || v.cols == 0) continue;
     const int piece = run - (int)(s0 / q);
-    if (SETS > 2 && v.cols > 32) attend_piece<DT, D, SETS>(a, v, h, u0, u1, piece);
-    else if (SETS > 1 && v.cols > 16) attend_piece<DT, D, SETS < 2 ? SETS : 2>(a, v, h, u0, u1, piece);
+    if (SETS > 1 && v.cols > 16) attend_piece<DT, D, SETS>(a, v, h, u0, u1, piece);
     else attend_piece<DT, D, 1>(a, v, h, u0, u1, piece);
+  }
+}
+
+// ---------------------------------------------------------------- one launch
+// A workgroup per (request, cache head, column tile): its waves share the units of the whole
+// context (the chain's prefixes, then the own tokens) and meet in LDS.  For small calls, which
+// are bound by latency: no plan, no partial results, one launch.
+constexpr int kDirectWaves = 8;
+template <int DT, int D, int NS>
+__global__ __launch_bounds__(kDirectWaves * 64) void k_cache8_direct(Attend8Args a) {
+  constexpr int NW = kDirectWaves, COLS = 16 * NS, STRIDE = D + 4;        // (rows off the same banks)
+  __shared__ __attribute__((aligned(16))) float s_o[NW][COLS][STRIDE];
+  __shared__ float s_m[NW][COLS], s_t[NW][COLS];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int tile_no = blockIdx.x % a.tiles, rest = blockIdx.x / a.tiles;
+  const int h = rest % a.H, r = rest / a.H, HQ = a.H * a.G;
+  const Step8& st = a.st;
+  const int S = clampi(ld_uniform(st.slen + r), 0, a.max_s);
+  int grp = a.NG > 0 ? ld_uniform(st.gid + r) : -1;
+  const RowSpan rw = row_span(st.qoff, r, a.T, min(S, st.max_q));
+  const int col0 = tile_no * COLS, ncols = min(COLS, rw.count * a.G - col0);
+  if (ncols <= 0) return;
+  const int base = S - rw.count;
+  const int keys = base + (col0 + ncols - 1) / a.G + 1;   // own tokens that the tile sees
+  Tile8<DT, D, NS> tile(a.H, h);
+  auto row_of = [&](int col) {
+    const int x = col0 + col, j = x / a.G;
+    return (long)(rw.first + j) * HQ + h * a.G + (x - j * a.G);
+  };
+  tile.load_queries(a.q, a.flip != 0, [&](int c) { return tile.column(c) < ncols ? row_of(tile.column(c)) : -1L; });
+  // lengths of the chain's prefixes, innermost first
+  int id[kMaxDepth], len[kMaxDepth], total = (keys + kUnit - 1) / kUnit;
+#pragma unroll
+  for (int l = 0; l < kMaxDepth; ++l) {
+    const bool on = l < st.depth && grp >= 0 && grp < a.NG;
+    id[l] = on ? grp : 0;
+    len[l] = on ? clampi(ld_uniform(st.plen + id[l]), 0, a.max_p) : 0;
+    grp = on && st.parents ? ld_uniform(st.parents + id[l]) : -1;
+    total += (len[l] + kUnit - 1) / kUnit;
+  }
+  const int u0 = (int)((long)total * wave / NW), u1 = (int)((long)total * (wave + 1) / NW);
+  int from = 0;
+#pragma unroll 1
+  for (int l = 0; l <= kMaxDepth; ++l) {
+    int n = keys, gl = r;
+#pragma unroll
+    for (int x = 0; x < kMaxDepth; ++x)
+      if (x == l) { n = len[x]; gl = id[x]; }
+    const bool own = l == kMaxDepth;
+    const int units = (n + kUnit - 1) / kUnit;
+    const int b = max(u0 - from, 0), f = min(u1 - from, units);
+    from += units;
+    if (b >= f) continue;
+    Range8 rg = range_of(a, own, gl, n, b, f);
+    if (own) rg.plain = min(n, base + col0 / a.G + 1);
+#pragma unroll
+    for (int c = 0; c < NS; ++c) tile.lim[c] = own ? min(keys, base + (col0 + tile.column(c)) / a.G + 1) : n;
+    tile.run(rg, a.scale_log2);
+  }
+  // the waves' results meet in LDS: normalised outputs and log-sum-exps
+  tile.finish([&](int c, int col, float inv, float lse2) {
+    const int g = tile.lane >> 4;
+#pragma unroll
+    for (int x = 0; x < D / 64; ++x)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4*>(&s_o[wave][col][64 * x + 16 * g + 4 * i]) = tile.four(c, x, i) * inv;
+    if (g == 0) s_t[wave][col] = lse2;
+  });
+  __syncthreads();
+  for (int col = threadIdx.x; col < COLS; col += NW * 64) {     // weights of the waves, and the sum
+    float mx = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) mx = fmaxf(mx, s_t[w][col]);
+    float sum = 0.f, wt[NW];
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      wt[w] = s_t[w][col] == -INFINITY ? 0.f : fast_exp2(s_t[w][col] - mx);
+      sum += wt[w];
+    }
+#pragma unroll
+    for (int w = 0; w < NW; ++w) s_m[w][col] = wt[w] / sum;       // (no weights at all: NaN)
+    if (col < ncols) a.lse[row_of(col)] = sum == 0.f ? __builtin_nanf("") : (mx + fast_log2(sum)) * kLn2;
+  }
+  __syncthreads();
+  for (int x = threadIdx.x; x < ncols * (D / 4); x += NW * 64) {
+    const int col = x / (D / 4), d = x % (D / 4) * 4;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) acc += s_m[w][col] * *reinterpret_cast<const f32x4*>(&s_o[w][col][d]);
+    char* dst = (char*)a.out + (row_of(col) * D + d) * Elem<DT>::kBytes;
+    if constexpr (DT == kF32) *reinterpret_cast<f32x4*>(dst) = acc;
+    else *reinterpret_cast<uint2*>(dst) = uint2{Wide8<DT>::pack(acc[0], acc[1]), Wide8<DT>::pack(acc[2], acc[3])};
   }
 }
 
 // ---------------------------------------------------------------------- join
 // With base-2 log-sum-exps l_i and normalised outputs o_i of disjoint keys, l = log2 sum 2^l_i
-// and o = sum 2^(l_i - l) o_i.  A workgroup per row and HPW query heads: D / 4 lanes a head (16
-// bytes a lane), the workgroup's other lane groups take every GROUPS-th partial result.
-template <int DT, int D, int HPW>
+// and o = sum 2^(l_i - l) o_i.  D / 4 lanes hold a query head (16 bytes a lane); GROUPS of them
+// share a head's partial results where few heads have many, and meet in LDS.
+template <int DT, int D, int GROUPS>
 __global__ __launch_bounds__(256) void k_cache8_join(Attend8Args a) {
-  constexpr int GW = D / 4, GROUPS = 256 / (GW * HPW);
-  __shared__ float s_m[GROUPS][HPW], s_l[GROUPS][HPW];
-  __shared__ f32x4 s_o[GROUPS][HPW][GW];
-  const int HQ = a.H * a.G, parts = (HQ + HPW - 1) / HPW;
-  const int t = blockIdx.x / parts, i0 = threadIdx.x % GW, sub = threadIdx.x / GW;
-  const int mine = sub % HPW, grp = sub / HPW;
-  const int hq = (int)(blockIdx.x % parts) * HPW + mine;
-  const int* d = a.plan + a.at.row + (long)t * kRowInts;
-  const int levels = ld_uniform(d + kRowLevels);
-  if (levels < 0) return;
-  const bool live = hq < HQ;
-  const int h = min(hq, HQ - 1) / a.G, gq = min(hq, HQ - 1) % a.G, cols = 16 * a.sets;
-  float m = -INFINITY, l = 0.f;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  bool direct = false;
+  constexpr int GW = D / 4, HEADS = 256 / (GW * GROUPS);    // query heads of a workgroup
+  constexpr bool MEET = GROUPS > 1;
+  __shared__ float s_m[MEET ? GROUPS : 1][HEADS], s_l[MEET ? GROUPS : 1][HEADS];
+  __shared__ f32x4 s_o[MEET ? GROUPS : 1][HEADS][GW];
+  const int HQ = a.H * a.G, parts = (HQ + HEADS - 1) / HEADS, cols = 16 * a.sets;
+  const int i0 = threadIdx.x % GW, sub = threadIdx.x / GW, mine = sub % HEADS, grp = sub / HEADS;
+  const long work = (long)clampi(ld_uniform(a.plan + kHeadJoins), 0, a.T) * parts;
+  for (long w = blockIdx.x; w < work; w += gridDim.x) {
+    const int t = clampi(ld_uniform(a.plan + a.at.join + (int)(w / parts)), 0, a.T - 1);
+    const int hq = (int)(w % parts) * HEADS + mine;
+    const bool live = hq < HQ;
+    const int h = min(hq, HQ - 1) / a.G, gq = min(hq, HQ - 1) % a.G;
+    const int* d = a.plan + a.at.row + (long)t * kRowInts;
+    const int levels = clampi(ld_uniform(d + kRowLevels), 0, kMaxDepth);
+    float m = -INFINITY, l = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    bool direct = false;
 #pragma unroll 1
-  for (int s = -1; s < min(levels, a.depth); ++s) {     // own tokens, then the chain's prefixes
-    const int x = (s < 0 ? ld_uniform(d + kRowPlace) : ld_uniform(d + kRowGroup + 2 * s + 1)) * a.G + gq;
-    const int e = (s < 0 ? ld_uniform(d + kRowEntry) : ld_uniform(d + kRowGroup + 2 * s)) + x / cols;
-    const int* v = a.plan + a.at.entry + (long)clampi(e, 0, a.max_entries - 1) * kEntryInts;
-    const int slot = v[kEntSlot], nc = v[kEntCols], n = min(v[kEntPieces], a.runs);   // (a piece per run at most)
-    if (slot < 0) { direct = true; continue; }          // the piece wrote the output
-    const int col = x % cols;
+    for (int s = -1; s < levels; ++s) {                 // own tokens, then the chain's prefixes
+      const int x = (s < 0 ? ld_uniform(d + kRowPlace) : ld_uniform(d + kRowGroup + 2 * s + 1)) * a.G + gq;
+      const int e = (s < 0 ? ld_uniform(d + kRowEntry) : ld_uniform(d + kRowGroup + 2 * s)) + x / cols;
+      const int* v = a.plan + a.at.entry + (long)clampi(e, 0, a.max_entries - 1) * kEntryInts;
+      const int slot = v[kEntSlot], nc = v[kEntCols], n = min(v[kEntPieces], a.runs);   // (a piece per run at most)
+      if (s < 0 && slot < 0) { direct = true; break; }  // the piece wrote the output
+      const int col = x % cols;
 #pragma unroll 1
-    for (int i = grp; i < n; i += 4 * GROUPS) {
-      float lp[4];
-      f32x4 op[4];
+      for (int i = grp; i < n; i += 4 * GROUPS) {
+        float lp[4];
+        f32x4 op[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int k = i + u * GROUPS;
-        const long at = slot + (long)k * nc + col;
-        const bool on = k < n && at >= 0 && at < a.slots;
-        const long sl = (long)h * a.slots + (on ? at : 0);
-        lp[u] = on ? a.lse_part[sl] : -INFINITY;
-        op[u] = on ? *reinterpret_cast<const f32x4*>(a.o_part + sl * D + 4 * i0) : f32x4{0.f, 0.f, 0.f, 0.f};
-      }
+        for (int u = 0; u < 4; ++u) {
+          const int k = i + u * GROUPS;
+          const long at = slot + (long)k * nc + col;
+          const bool on = k < n && at >= 0 && at < a.slots;
+          const long sl = (long)h * a.slots + (on ? at : 0);
+          lp[u] = -INFINITY;
+          if (on) {
+            lp[u] = a.lse_part[sl];
+            op[u] = *reinterpret_cast<const f32x4*>(a.o_part + sl * D + 4 * i0);
+          }
+        }
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        if (lp[u] == -INFINITY) continue;               // no key the row sees
-        const float mn = fmaxf(m, lp[u]);
-        const float f = fast_exp2(m - mn), w = fast_exp2(lp[u] - mn);
-        // (a logit that is no number, or +inf, makes the sums NaN)
-        m = lp[u] != lp[u] ? lp[u] : mn;
-        l = l * f + w;
-        acc = acc * f + op[u] * w;
+        for (int u = 0; u < 4; ++u) {
+          if (lp[u] == -INFINITY) continue;             // no key the row sees
+          const float mn = fmaxf(m, lp[u]);
+          const float f = fast_exp2(m - mn), wt = fast_exp2(lp[u] - mn);
+          // (a logit that is no number, or +inf, makes the sums NaN)
+          m = lp[u] != lp[u] ? lp[u] : mn;
+          l = l * f + wt;
+          acc = acc * f + op[u] * wt;
+        }
       }
     }
-  }
-  s_m[grp][mine] = m;
-  s_l[grp][mine] = l;
-  s_o[grp][mine][i0] = acc;
-  __syncthreads();
-  if (grp != 0 || !live || direct) return;
-  float mx = s_m[0][mine];
+    if constexpr (MEET) {
+      __syncthreads();                                  // (the last row's results have been read)
+      s_m[grp][mine] = m;
+      s_l[grp][mine] = l;
+      s_o[grp][mine][i0] = acc;
+      __syncthreads();
+      if (grp == 0) {
 #pragma unroll
-  for (int k = 1; k < GROUPS; ++k) mx = fmaxf(mx, s_m[k][mine]);
-  float sum = 0.f;
-  acc = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int k = 0; k < GROUPS; ++k) m = fmaxf(m, s_m[k][mine]);
+        l = 0.f;
+        acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int k = 0; k < GROUPS; ++k) {
-    const float mk = s_m[k][mine];
-    const float w = mk == -INFINITY ? 0.f : fast_exp2(mk - mx);
-    sum += w * s_l[k][mine];
-    acc += w * s_o[k][mine][i0];
+        for (int k = 0; k < GROUPS; ++k) {
+          const float mk = s_m[k][mine];
+          const float wt = mk == -INFINITY ? 0.f : fast_exp2(mk - m);
+          l += wt * s_l[k][mine];
+          acc += wt * s_o[k][mine][i0];
+        }
+      }
+    }
+    if (grp != 0 || !live || direct) continue;
+    // (no weights at all: every logit is -inf, as the one piece gives it)
+    const float inv = l == 0.f ? __builtin_nanf("") : 1.f / l;
+    const f32x4 res = l == 0.f ? f32x4{inv, inv, inv, inv} : acc * inv;
+    const size_t at = (size_t)t * HQ + hq;
+    char* dst = (char*)a.out + (at * D + 4 * i0) * Elem<DT>::kBytes;
+    if constexpr (DT == kF32) *reinterpret_cast<f32x4*>(dst) = res;
+    else *reinterpret_cast<uint2*>(dst) = uint2{Wide8<DT>::pack(res[0], res[1]), Wide8<DT>::pack(res[2], res[3])};
+    if (i0 == 0) a.lse[at] = l == 0.f ? __builtin_nanf("") : (m + fast_log2(l)) * kLn2;
   }
-  // (no weights at all: every logit is -inf, as the one piece gives it)
-  const float inv = 1.f / sum;
-  const f32x4 res = sum == 0.f ? f32x4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")} : acc * inv;
-  const size_t at = (size_t)t * HQ + hq;
-  char* dst = (char*)a.out + (at * D + 4 * i0) * Elem<DT>::kBytes;
-  if constexpr (DT == kF32) *reinterpret_cast<f32x4*>(dst) = res;
-  else *reinterpret_cast<uint2*>(dst) = uint2{Wide8<DT>::pack(res[0], res[1]), Wide8<DT>::pack(res[2], res[3])};
-  if (i0 == 0) a.lse[at] = sum == 0.f ? __builtin_nanf("") : (mx + fast_log2(sum)) * kLn2;
 }
 
 // ------------------------------------------------------------------ launches
 hipError_t launch_plan8(const Plan8Args& a, hipStream_t s) {
-  if (a.T < 1 || a.R < 1 || a.G < 1 || a.cols < 16 || a.runs < 1 || a.min_run < 1 || a.max_entries < 1 ||
-      a.depth < 0 || a.depth > kMaxDepth || (a.NG > 0) != (a.depth > 0))
+  if (a.st.T < 1 || a.st.R < 1 || a.st.G < 1 || a.cols < 16 || a.chain_cols < 1 || a.runs < 1 || a.min_run < 1 ||
+      a.max_entries < 1 || a.st.depth < 0 || a.st.depth > kMaxDepth || (a.st.NG > 0) != (a.st.depth > 0))
     return hipErrorInvalidValue;
   hipLaunchKernelGGL(k_cache8_plan, dim3(1), dim3(1024), 0, s, a);
   return hipGetLastError();
@@ -475,16 +649,28 @@ static hipError_t launch_attend_t(const Attend8Args& a, hipStream_t s, hipEvent_
   if (wgs * 256 > 0xffffffffL) return hipErrorInvalidValue;
   const dim3 grid((unsigned)wgs);
   if (a.sets == 1) hipExtLaunchKernelGGL((k_cache8_attend<DT, D, 1>), grid, dim3(256), 0, s, e0, e1, 0, a);
-  else if (a.sets == 2) hipExtLaunchKernelGGL((k_cache8_attend<DT, D, 2>), grid, dim3(256), 0, s, e0, e1, 0, a);
-  else if constexpr (DT != kF32) hipExtLaunchKernelGGL((k_cache8_attend<DT, D, 4>), grid, dim3(256), 0, s, e0, e1, 0, a);
+  else hipExtLaunchKernelGGL((k_cache8_attend<DT, D, 2>), grid, dim3(256), 0, s, e0, e1, 0, a);
   return hipGetLastError();
 }
-constexpr int kJoinHeads = 2;            // query heads of a join workgroup
+template <int DT, int D>
+static hipError_t launch_direct_t(const Attend8Args& a, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
+  const long wgs = (long)a.R * a.H * a.tiles;
+  if (a.tiles < 1 || wgs * kDirectWaves * 64 > 0xffffffffL) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)wgs), wg(kDirectWaves * 64);
+  hipExtLaunchKernelGGL((k_cache8_direct<DT, D, 1>), grid, wg, 0, s, e0, e1, 0, a);
+  return hipGetLastError();
+}
+constexpr int kJoinWgs = 2048;           // workgroups of a join: eight a CU
 template <int DT, int D>
 static hipError_t launch_join_t(const Attend8Args& a, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
-  const long parts = ((long)a.H * a.G + kJoinHeads - 1) / kJoinHeads;
-  if (parts * a.T * 256 > 0xffffffffL) return hipErrorInvalidValue;
-  hipExtLaunchKernelGGL((k_cache8_join<DT, D, kJoinHeads>), dim3((unsigned)(parts * a.T)), dim3(256), 0, s, e0, e1, 0, a);
+  constexpr int MANY = 256 / (D / 4) / 2;
+  const long heads = (long)a.T * a.H * a.G;
+  if (heads / 2 <= kJoinWgs) {                          // few heads, whose partial results may be many
+    hipExtLaunchKernelGGL((k_cache8_join<DT, D, MANY>), dim3((unsigned)((heads + 1) / 2 + a.T)), dim3(256), 0, s, e0, e1, 0, a);
+  } else {
+    const long wgs = heads / (256 / (D / 4)) + a.T;
+    hipExtLaunchKernelGGL((k_cache8_join<DT, D, 1>), dim3((unsigned)(wgs < kJoinWgs ? wgs : kJoinWgs)), dim3(256), 0, s, e0, e1, 0, a);
+  }
   return hipGetLastError();
 }
 
@@ -499,18 +685,27 @@ static hipError_t launch_join_t(const Attend8Args& a, hipStream_t s, hipEvent_t 
   }                                                                       \
   return hipErrorInvalidValue
 
-static bool attend_ok(const Attend8Args& a, int dtype) {
-  return a.T >= 1 && a.R >= 1 && a.H >= 1 && a.G >= 1 && a.runs >= 1 && a.max_entries >= 1 && a.sstride >= 1 &&
-         a.nsblk >= 1 && (a.NG == 0 || (a.npblk >= 1 && a.pstride >= 1)) && a.o_part && a.lse_part && a.slots >= 1 &&
-         (a.sets == 1 || a.sets == 2 || (a.sets == 4 && dtype != kF32));
+static bool attend_ok(const Attend8Args& a) {
+  return a.T >= 1 && a.R >= 1 && a.H >= 1 && a.G >= 1 && a.sstride >= 1 && a.nsblk >= 1 &&
+         (a.NG == 0 || (a.npblk >= 1 && a.pstride >= 1)) && (a.sets == 1 || a.sets == 2);
+}
+static bool parts_ok(const Attend8Args& a) {
+  return attend_ok(a) && a.runs >= 1 && a.max_entries >= 1 && a.plan && a.o_part && a.lse_part && a.slots >= 1;
 }
 hipError_t launch_attend8(const Attend8Args& a, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
-  if (!attend_ok(a, dtype)) return hipErrorInvalidValue;
+  if (!parts_ok(a)) return hipErrorInvalidValue;
   PARROT_CACHE8_LAUNCH(launch_attend_t);
 }
 hipError_t launch_join8(const Attend8Args& a, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
-  if (!attend_ok(a, dtype)) return hipErrorInvalidValue;
+  if (!parts_ok(a)) return hipErrorInvalidValue;
   PARROT_CACHE8_LAUNCH(launch_join_t);
+}
+hipError_t launch_direct8(const Attend8Args& a, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
+  const Step8& st = a.st;
+  if (!attend_ok(a) || !st.qoff || !st.slen || (a.NG > 0 && (!st.gid || !st.plen)) || st.depth > kMaxDepth ||
+      (long)a.tiles * 16 < (long)st.max_q * a.G)
+    return hipErrorInvalidValue;
+  PARROT_CACHE8_LAUNCH(launch_direct_t);
 }
 
 }  // namespace parrot

@@ -11,7 +11,8 @@
 // No LDS and no lane exchange: a lane's S^T values (tokens 4 g .. 4 g + 3 of a block for
 // g = lane / 16, column lane % 16) are the PV operand's k group g, and the layout of the
 // values holds the same four tokens side by side (cache8_args.h).  So a wave needs nothing but
-// its own loads, 16 bytes a lane, which come into registers 16 KiB ahead.
+// its own loads, 16 bytes a lane: 8 KiB on their way, the next keys as soon as the last ones
+// have been multiplied, the next values behind the last products.
 //
 // Types: bfloat16 and float16 round P once, and the output is divided by the sum of the rounded
 // weights (a dominant weight's rounding cancels).  float32 queries and weights are cut into
@@ -70,13 +71,20 @@ struct Range8 {
   int u0, u1;                            // units
   int end;                               // keys; from here on slots hold anything
   int plain;                             // keys before it are seen by every column
+  bool once;                             // no other tile reads them: streaming loads
 };
+
+PARROT_DEV float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
 
 template <int DT, int D, int NS>
 struct Tile8 {
   using W = Wide8<DT>;
   static constexpr int X = D / 64;                    // 16-byte loads of each tensor, per block and lane
-  static constexpr int NU = 4 / X;                    // units on their way: 16 KiB
+  static constexpr int NU = 2 / X;                    // units on their way: 8 KiB
   static constexpr int PARTS = DT == kF32 ? 3 : 1;
   static constexpr int BLK_B = kBlockTokens * D;
   static constexpr float kNoKey = -3.0e38f;           // a reference that every finite logit moves
@@ -150,40 +158,66 @@ struct Tile8 {
     const unsigned koff = (lane & 15) * D + g * 16, voff = lane * 16;
     u32x4 kr[NU][2][X], vr[NU][2][X];
     unsigned sc[NU][2];                               // a block's scale bytes: keys, values
-    int nid[2];
-    auto ids = [&](int u) {                           // of unit u (past the end: the last block)
-#pragma unroll
-      for (int b = 0; b < 2; ++b) nid[b] = ld_uniform(rg.tbl + min(2 * u + b, last));
-    };
-    auto issue = [&](int n, int u) {
+    size_t bh[2];                                     // block-heads of the next unit to request
+    auto find = [&](int u) {                          // (past the end: the last block)
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        const int id = (int)min((unsigned)nid[b], (unsigned)(rg.npool - 1));
-        const size_t bh = (size_t)id * H + h;
-        const char* kp = (const char*)rg.pool.k + bh * BLK_B;
-        const char* vp = (const char*)rg.pool.v + bh * BLK_B;
-#pragma unroll
-        for (int x = 0; x < X; ++x) kr[n][b][x] = ld16(kp + koff + x * 64);
-#pragma unroll
-        for (int x = 0; x < X; ++x) vr[n][b][x] = ld16(vp + voff + x * 1024);
-        const unsigned word = (unsigned)ld_uniform((const int*)((const char*)rg.pool.scales + ((bh * 2) & ~(size_t)3)));
-        sc[n][b] = (bh & 1 ? word >> 16 : word) & 0xFFFFu;
+        const int id = (int)min((unsigned)ld_uniform(rg.tbl + min(2 * u + b, last)), (unsigned)(rg.npool - 1));
+        bh[b] = (size_t)id * H + h;
       }
-      ids(u + 1);
     };
-    ids(rg.u0);
+    auto request = [&](const void* pool, unsigned off, unsigned step, u32x4 (&to)[2][X]) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const char* p = (const char*)pool + bh[b] * BLK_B + off;
+        if (rg.once) {
+#pragma unroll
+          for (int x = 0; x < X; ++x) to[b][x] = ld16_stream(p + x * step);
+        } else {
+#pragma unroll
+          for (int x = 0; x < X; ++x) to[b][x] = ld16(p + x * step);
+        }
+      }
+    };
+    auto scales = [&](unsigned (&to)[2]) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const unsigned word = (unsigned)ld_uniform((const int*)((const char*)rg.pool.scales + ((bh[b] * 2) & ~(size_t)3)));
+        to[b] = (bh[b] & 1 ? word >> 16 : word) & 0xFFFFu;
+      }
+    };
+    find(rg.u0);
 #pragma unroll
     for (int n = 0; n < NU; ++n)
-      if (rg.u0 + n < rg.u1) issue(n, rg.u0 + n);
+      if (rg.u0 + n < rg.u1) {
+        request(rg.pool.k, koff, 64, kr[n]);
+        request(rg.pool.v, voff, 1024, vr[n]);
+        scales(sc[n]);
+        find(rg.u0 + n + 1);
+      }
 #pragma unroll 1
     for (int ub = rg.u0; ub < rg.u1; ub += NU) {
 #pragma unroll
       for (int n = 0; n < NU; ++n) {
         const int u = ub + n;
         if (u >= rg.u1) break;
-        unit(rg, u * kUnit, kr[n], vr[n], sc[n], scale_log2);
-        __builtin_amdgcn_sched_barrier(0);            // (the next loads take this unit's registers)
-        if (u + NU < rg.u1) issue(n, u + NU);
+        const bool more = u + NU < rg.u1;
+        unsigned next[2] = {0, 0};
+        // (the next loads take this unit's registers: not before they are free)
+        unit(rg, u * kUnit, kr[n], vr[n], sc[n], scale_log2, [&] {
+          __builtin_amdgcn_sched_barrier(0);
+          if (more) {
+            request(rg.pool.k, koff, 64, kr[n]);
+            scales(next);
+          }
+        });
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) {
+          request(rg.pool.v, voff, 1024, vr[n]);
+          sc[n][0] = next[0];
+          sc[n][1] = next[1];
+          find(u + NU + 1);
+        }
       }
     }
   }
@@ -207,7 +241,10 @@ struct Tile8 {
   }
 
  private:
-  PARROT_DEV void unit(const Range8& rg, int tok0, u32x4 (&k)[2][X], u32x4 (&v)[2][X], unsigned (&sc)[2], float scale_log2) {
+  // keys_read(): the unit's keys have been read.
+  template <class F>
+  PARROT_DEV void unit(const Range8& rg, int tok0, u32x4 (&k)[2][X], u32x4 (&v)[2][X], unsigned (&sc)[2], float scale_log2,
+                       F keys_read) {
     const int g = lane >> 4;
     f32x4 s[NS][2];
 #pragma unroll
@@ -223,6 +260,7 @@ struct Tile8 {
 #pragma unroll
           for (int p = PARTS - 1; p >= 0; --p) s[c][b] = W::mma(kf, qf[c][p][st], s[c][b]);
       }
+    keys_read();
     const bool masked = tok0 + kUnit > rg.plain;
     bool bad = false;                                  // a value that some columns see is no number
     if (masked) {
@@ -272,14 +310,17 @@ struct Tile8 {
 #pragma unroll
     for (int c = 0; c < NS; ++c) {
       float x[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = s[c][i >> 2][i & 3] * cb[i >> 2];
+      float mx;
       if (masked) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          if (tok0 + 16 * (i >> 2) + 4 * g + (i & 3) >= lim[c]) x[i] = -INFINITY;
+          x[i] = tok0 + 16 * (i >> 2) + 4 * g + (i & 3) < lim[c] ? s[c][i >> 2][i & 3] * cb[i >> 2] : -INFINITY;
+        mx = max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), fmaxf(x[6], x[7]));
+      } else {                                         // (scales are not negative)
+        const float m0 = max3(max3(s[c][0][0], s[c][0][1], s[c][0][2]), s[c][0][3], s[c][0][3]);
+        const float m1 = max3(max3(s[c][1][0], s[c][1][1], s[c][1][2]), s[c][1][3], s[c][1][3]);
+        mx = fmaxf(m0 * cb[0], m1 * cb[1]);
       }
-      const float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
       if (__ballot(mx > mref[c] + 8.f)) {
         const float m = fmaxf(mref[c], max_xor32(max_xor16(mx)));
         const float f = fast_exp2(mref[c] - m);
@@ -288,11 +329,15 @@ struct Tile8 {
         lw[c] *= f;
         scale_outputs(f, c);
       }
+      if (masked) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        x[i] = fast_exp2(x[i] - mref[c]);
-        lt[c] += x[i];
+        for (int i = 0; i < 8; ++i) x[i] = fast_exp2(x[i] - mref[c]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = fast_exp2(__builtin_fmaf(s[c][i >> 2][i & 3], cb[i >> 2], -mref[c]));
       }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) lt[c] += x[i];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if constexpr (DT == kF32) {

@@ -34,15 +34,19 @@ def plan(lib, prob=None, rows=None, size=1 << 40, **over):
     return lib.parrot_cache8_plan(ctypes.byref(prob), ctypes.byref(rows), *addresses(PLAN, over), size, None)
 
 
+ATTEND = ["q", "query_offsets", "ptab", "plen", "prefix_parents", "stab", "slen", "gid", "plan", "out", "lse", "ws"]
+
+
 def attend(lib, prob=None, rows=None, plan_bytes=1 << 40, room=1 << 45, prefix=None, suffix=None, **over):
     prob, rows = prob or problem(), rows or parrot.make_tree_rows(20, 10, 20, 8)
     prefix = pool(1 << 17) if prefix is None else prefix
     suffix = pool(1 << 18) if suffix is None else suffix
-    v = dict(zip(["q", "ptab", "stab", "plan", "out", "lse", "ws"], addresses(["q", "ptab", "stab", "plan", "out", "lse", "ws"], {})))
+    v = dict(zip(ATTEND, addresses(ATTEND, {})))
     v.update(over)
     ref = lambda x: ctypes.byref(x) if x else None
-    return lib.parrot_cache8_attention(ctypes.byref(prob), ctypes.byref(rows), v["q"], ref(prefix), ref(suffix), v["ptab"],
-                                       v["stab"], v["plan"], plan_bytes, v["out"], v["lse"], v["ws"], room, None, None)
+    return lib.parrot_cache8_attention(ctypes.byref(prob), ctypes.byref(rows), v["q"], v["query_offsets"], ref(prefix),
+                                       ref(suffix), *(v[n] for n in ATTEND[2:9]), plan_bytes, v["out"], v["lse"], v["ws"],
+                                       room, None, None)
 
 
 def refused(status, msg, want=B.PARROT_ERR_INVALID_ARGUMENT):
@@ -92,8 +96,9 @@ def test_attention_pointers(parrot_lib):
         if n != "prefix_parents":
             refused(plan(parrot_lib, **{n: None}), "NULL")
         refused(plan(parrot_lib, **{n: FAKE + 1}), "aligned")
-    for n in ("q", "ptab", "stab", "plan", "out", "lse", "ws"):
-        refused(attend(parrot_lib, **{n: None}), "NULL")
+    for n in ATTEND:
+        if n != "prefix_parents":
+            refused(attend(parrot_lib, **{n: None}), "NULL")
         refused(attend(parrot_lib, **{n: FAKE + 1}), "aligned")
     refused(attend(parrot_lib, plan=FAKE + 128), "plan")
     for which in ("prefix", "suffix"):

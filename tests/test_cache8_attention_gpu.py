@@ -10,6 +10,18 @@ from cache8_util import du
 
 pytestmark = pytest.mark.gpu
 
+PATHS = {"one": 0, "plan": 1}
+
+
+@pytest.fixture(autouse=True, params=["one", "plan"])
+def path(request):
+    """Every test runs on one launch, and on plan, partial results and join."""
+    import paper_2405_19888_amd as parrot
+    force = parrot.load_library().parrot_test_cache8_path
+    force(PATHS[request.param])
+    yield request.param
+    force(-1)
+
 
 def batch_of(case, seed=3, scale=None):
     dtype, heads, ratio, dim, groups, plen, cached, rows, parents = case
