@@ -40,7 +40,7 @@ parrot::Pool8 pool(const parrot_cache8* c) { return {c->k, c->v, c->scales}; }
 struct Plan8 {
   int depth;                       // levels of prefixes that the plan has room for
   bool direct;                     // one launch without a plan
-  int tiles;                       // its column tiles per request
+  int tiles, waves;                // its column tiles per request, waves of a workgroup
   int sets, cols, runs, min_run;
   bool wide;                       // neighbouring waves take runs of one head, else neighbouring heads
   int max_entries;
@@ -50,13 +50,39 @@ struct Plan8 {
 };
 
 // Overrides the rule below for tests and tuning (per thread, set through
-// parrot_test_cache8_path): 0 one launch, 1 plan, partial results and join.
+// parrot_test_cache8_path): 0 one launch of eight waves a workgroup, 2 of four, 1 plan, partial
+// results and join.
 thread_local int g_path = -1;
 
 constexpr int kMinRun = 6;         // cost of a run at least: four units and a tile's setup
 
-bool takes_one_launch(const parrot_problem* p, const parrot_tree_rows* rows, int depth, int tiles, long cus) {
-  return false;
+// One launch or plan, partial results and join, by estimates of both in microseconds a layer (the
+// plan's own 9 us spread over four), lengths taken as 0.7 of their bounds.
+//  * one launch: 7 us, 1.5 more per round of workgroups (three of four waves a CU), and the largest of a
+//    workgroup's latency (1.15 us per unit of 32 keys of a wave, 1.55 in fp32), its bytes (own keys at
+//    5.5 TB/s; what other tiles or requests read again, from the caches, at 12) and its products at
+//    400 TFLOP/s;
+//  * plan: 16 us, its bytes at 6.4 TB/s, its products at 600 TFLOP/s.
+// Four waves a workgroup where there are more of them than CUs, or few keys for eight.
+// Measured, bfloat16, 128-element heads, one launch (eight waves, four) and plan, us a layer of four: one request
+// on 4000 tokens, 8 cache heads of four query heads 24, 31, 20; 8 on 1500 12.7, 14.9, 20; 32 cache heads of
+// one: 8 requests on 1500 19.6, 22.5, 24; 64 on 300 51, 31, 32; 64 on 1500 107, 100, 96; 16 requests of
+// 8 heads on one prefix of 2000 17.4, 20.7, 24.8.
+struct OneLaunch { bool taken; int waves; };
+OneLaunch one_launch(const parrot_problem* p, const parrot_tree_rows* rows, int depth, long tiles, long cus) {
+  const double mean = 0.7, R = p->num_requests, H = p->num_heads, kv = 2.0 * p->head_dim * H;
+  const double pre = p->num_groups > 0 ? (double)depth * p->max_prefix_len : 0, longest = p->max_suffix_len + pre;
+  const bool f32 = p->dtype == PARROT_DTYPE_F32;
+  const double wgs = R * H * tiles;
+  const int waves = wgs > cus || longest <= 16 * parrot::kUnit ? 4 : 8;
+  const double flops = 4.0 * rows->num_query_rows * rows->num_query_heads * p->head_dim * mean * longest;
+  const double own = R * mean * p->max_suffix_len * kv;
+  const double latency = longest / (parrot::kUnit * waves) * (f32 ? 1.55 : 1.15);
+  const double one = 7 + 1.5 * wgs / (3 * cus) +
+                     std::max({latency, own / 5.5e6 + ((tiles - 1) * own + R * tiles * mean * pre * kv) / 12e6, flops / 4e8});
+  const double shared = std::min(R, (double)p->num_groups) * mean * pre * kv;
+  const double plan = 16 + std::max((own + shared) / 6.4e6, flops / 6e8);
+  return {one < plan, waves};
 }
 
 parrot_status check_attend(const parrot_problem* p, const parrot_tree_rows* rows, Plan8* pl) {
@@ -118,7 +144,9 @@ parrot_status check_attend(const parrot_problem* p, const parrot_tree_rows* rows
   pl->lse_bytes = align256((size_t)H * pl->slots * sizeof(float));
   pl->tiles = (int)ceil_div(rows->max_query_rows * G, 16);
   const bool fits = R * H * pl->tiles <= 1L << 22;
-  pl->direct = fits && (g_path >= 0 ? g_path == 0 : takes_one_launch(p, rows, pl->depth, pl->tiles, cus));
+  const OneLaunch one = one_launch(p, rows, pl->depth, pl->tiles, cus);
+  pl->waves = g_path >= 0 ? (g_path == 2 ? 4 : 8) : one.waves;
+  pl->direct = fits && (g_path >= 0 ? g_path != 1 : one.taken);
   return PARROT_OK;
 }
 
@@ -256,7 +284,7 @@ parrot_status parrot_cache8_attention(
   a.pstride = p->prefix_table_stride; a.sstride = p->suffix_table_stride;
   a.max_p = a.st.max_p; a.max_s = p->max_suffix_len;
   a.npblk = p->num_groups > 0 ? p->num_prefix_blocks : 1; a.nsblk = p->num_suffix_blocks;
-  a.runs = pl.runs; a.sets = pl.sets; a.wide = pl.wide; a.max_entries = pl.max_entries; a.tiles = pl.tiles;
+  a.runs = pl.runs; a.sets = pl.sets; a.wide = pl.wide; a.max_entries = pl.max_entries; a.tiles = pl.tiles; a.waves = pl.waves;
   a.flip = p->sm_scale < 0.f;
   a.scale_log2 = std::fabs(p->sm_scale) * parrot::kLog2e;
   const parrot_trace none = {nullptr, nullptr, nullptr, nullptr};
@@ -273,7 +301,7 @@ parrot_status parrot_cache8_attention(
 
 // Test hooks (not in parrot_attn.h): the path of this thread's calls (see g_path; -1 gives the
 // choice back), and the one these arguments take (-1: invalid).
-void parrot_test_cache8_path(int path) { g_path = path == 0 || path == 1 ? path : -1; }
+void parrot_test_cache8_path(int path) { g_path = path >= 0 && path <= 2 ? path : -1; }
 int parrot_test_cache8_planned(const parrot_problem* p, const parrot_tree_rows* rows) {
   Plan8 pl;
   return check_attend(p, rows, &pl) == PARROT_OK ? !pl.direct : -1;

@@ -83,7 +83,7 @@ struct Attend8Args {
   int T, R, H, G, NG, depth;             // depth: levels that the plan has room for
   int pstride, sstride, max_p, max_s, npblk, nsblk;
   int runs, sets, wide, max_entries;     // sets: column sets of a tile; wide: a workgroup's waves take runs of one head
-  int tiles;                             // one launch: column tiles of a request
+  int tiles, waves;                      // one launch: column tiles of a request, waves of a workgroup (4 or 8)
   int flip;                              // sm_scale < 0: queries change sign
   float scale_log2;                      // |sm_scale| log2(e)
 };

@@ -315,7 +315,6 @@ PARROT_DEV Range8 range_of(const Attend8Args& a, bool own, int seq, int keys, in
   rg.u0 = u0;
   rg.u1 = u1;
   rg.end = rg.plain = keys;
-  rg.once = false;
   return rg;
 }
 
@@ -391,10 +390,10 @@ PARROT_DEV void attend_piece(const Attend8Args& a, const Entry& e, int h, int u0
     if (b >= f) continue;
     Range8 rg = range_of(a, own && !pre, pre ? grp : own ? e.seq : ~e.seq, keys, b, f);
     if (own && !pre) rg.plain = min(keys, e.base + e.col0 / a.G + 1);
-    rg.once = !pre && (e.flags & kEntOnce);
 #pragma unroll
     for (int c = 0; c < NS; ++c) tile.lim[c] = own && !pre ? sees[c] : keys;
-    tile.run(rg, a.scale_log2);
+    if (NS == 1 && (e.flags & kEntOnce)) tile.template run<NS == 1>(rg, a.scale_log2);
+    else tile.template run<false>(rg, a.scale_log2);
   }
 
   const int g = tile.lane >> 4;
@@ -453,10 +452,10 @@ void k_cache8_attend(Attend8Args a) {
 // A workgroup per (request, cache head, column tile): its waves share the units of the whole
 // context (the chain's prefixes, then the own tokens) and meet in LDS.  For small calls, which
 // are bound by latency: no plan, no partial results, one launch.
-constexpr int kDirectWaves = 8;
-template <int DT, int D, int NS>
-__global__ __launch_bounds__(kDirectWaves * 64) void k_cache8_direct(Attend8Args a) {
-  constexpr int NW = kDirectWaves, COLS = 16 * NS, STRIDE = D + 4;        // (rows off the same banks)
+template <int DT, int D, int NW>
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(DT == kF32 ? 2 : 3)))
+void k_cache8_direct(Attend8Args a) {
+  constexpr int NS = 1, COLS = 16 * NS, STRIDE = D + 4;                   // (rows off the same banks)
   __shared__ __attribute__((aligned(16))) float s_o[NW][COLS][STRIDE];
   __shared__ float s_m[NW][COLS], s_t[NW][COLS];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -503,7 +502,7 @@ __global__ __launch_bounds__(kDirectWaves * 64) void k_cache8_direct(Attend8Args
     if (own) rg.plain = min(n, base + col0 / a.G + 1);
 #pragma unroll
     for (int c = 0; c < NS; ++c) tile.lim[c] = own ? min(keys, base + (col0 + tile.column(c)) / a.G + 1) : n;
-    tile.run(rg, a.scale_log2);
+    tile.template run<false>(rg, a.scale_log2);
   }
   // the waves' results meet in LDS: normalised outputs and log-sum-exps
   tile.finish([&](int c, int col, float inv, float lse2) {
@@ -655,9 +654,10 @@ static hipError_t launch_attend_t(const Attend8Args& a, hipStream_t s, hipEvent_
 template <int DT, int D>
 static hipError_t launch_direct_t(const Attend8Args& a, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
   const long wgs = (long)a.R * a.H * a.tiles;
-  if (a.tiles < 1 || wgs * kDirectWaves * 64 > 0xffffffffL) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)wgs), wg(kDirectWaves * 64);
-  hipExtLaunchKernelGGL((k_cache8_direct<DT, D, 1>), grid, wg, 0, s, e0, e1, 0, a);
+  if (a.tiles < 1 || wgs * 512 > 0xffffffffL) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)wgs);
+  if (a.waves == 8) hipExtLaunchKernelGGL((k_cache8_direct<DT, D, 8>), grid, dim3(512), 0, s, e0, e1, 0, a);
+  else hipExtLaunchKernelGGL((k_cache8_direct<DT, D, 4>), grid, dim3(256), 0, s, e0, e1, 0, a);
   return hipGetLastError();
 }
 constexpr int kJoinWgs = 2048;           // workgroups of a join: eight a CU

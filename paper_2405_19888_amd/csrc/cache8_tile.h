@@ -71,7 +71,6 @@ struct Range8 {
   int u0, u1;                            // units
   int end;                               // keys; from here on slots hold anything
   int plain;                             // keys before it are seen by every column
-  bool once;                             // no other tile reads them: streaming loads
 };
 
 PARROT_DEV float max3(float a, float b, float c) {
@@ -151,6 +150,10 @@ struct Tile8 {
     for (int t = 0; t < 4 * X; ++t) o[c][t] *= f;
   }
 
+  // ONCE: no other tile reads the keys, and streaming loads take them (438 MB of 64 requests in
+  // bfloat16, four query heads on each of 8: 72 us, 82 with cached loads; as a flag at run time the
+  // compiler makes one load of the two).
+  template <bool ONCE>
   PARROT_DEV void run(const Range8& rg, float scale_log2) {
     const int g = lane >> 4;
     const int last = max((rg.end - 1) / kBlockTokens, 0);
@@ -170,13 +173,8 @@ struct Tile8 {
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         const char* p = (const char*)pool + bh[b] * BLK_B + off;
-        if (rg.once) {
 #pragma unroll
-          for (int x = 0; x < X; ++x) to[b][x] = ld16_stream(p + x * step);
-        } else {
-#pragma unroll
-          for (int x = 0; x < X; ++x) to[b][x] = ld16(p + x * step);
-        }
+        for (int x = 0; x < X; ++x) to[b][x] = ONCE ? ld16_stream(p + x * step) : ld16(p + x * step);
       }
     };
     auto scales = [&](unsigned (&to)[2]) {

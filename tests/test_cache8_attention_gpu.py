@@ -10,12 +10,12 @@ from cache8_util import du
 
 pytestmark = pytest.mark.gpu
 
-PATHS = {"one": 0, "plan": 1}
+PATHS = {"one_of_8": 0, "plan": 1, "one_of_4": 2}
 
 
-@pytest.fixture(autouse=True, params=["one", "plan"])
+@pytest.fixture(autouse=True, params=["one_of_8", "plan", "one_of_4"])
 def path(request):
-    """Every test runs on one launch, and on plan, partial results and join."""
+    """Every test runs on one launch, of eight and four waves a workgroup, and on plan, partial results and join."""
     import paper_2405_19888_amd as parrot
     force = parrot.load_library().parrot_test_cache8_path
     force(PATHS[request.param])
@@ -51,6 +51,8 @@ CASES = {
     "prompts": ("bfloat16", 2, 4, 64, [0, 0, -1], [200], [0, 33, 0], [300, 121, 417], None),
     "prompts_f32": ("float32", 1, 3, 128, [0, -1], [50], [7, 0], [90, 133], None),
     "many_heads": ("float16", 40, 1, 128, [-1, -1, 0], [60], [100, 31, 4], [1, 2, 1], None),
+    # prompts that go through the prefixes by themselves beside single tokens that share them
+    "prompts_and_tokens": ("float16", 2, 4, 64, [0, 1, 0, 1, 1, -1], [70, 150], [10, 0, 40, 33, 7, 64], [1, 100, 2, 1, 60, 90], [-1, 0]),
     "ratio_71": ("bfloat16", 1, 71, 64, [0, -1, 0], [90], [40, 17, 0], [1, 3, 2], None),
     "groups_unread": ("float16", 2, 1, 64, [2, -1], [40, 50, 33], [10, 20], [1, 1], None),
 }
