@@ -199,7 +199,9 @@ parrot_status parrot_cache8_fill(
   a.f.sk = suffix->k; a.f.sv = suffix->v; a.scales = suffix->scales;
   const long elt = p->dtype == PARROT_DTYPE_F32 ? 4 : 2;
   const long units = rows->max_query_rows == 1 ? p->num_requests : rows->num_query_rows / 16 + 2L * p->num_requests;
-  parrot::fill_slabs(&a.f, 4096 / (p->head_dim * elt), std::max(1L, std::min((long)rows->num_query_rows, units)));
+  // heads of a workgroup's step: a lane group each for single rows, a wave or half of one for a block's
+  const long step = rows->max_query_rows == 1 ? 4096 / (p->head_dim * elt) : p->head_dim * elt == 128 ? 8 : 4;
+  parrot::fill_slabs(&a.f, step, std::max(1L, std::min((long)rows->num_query_rows, units)));
   if (units * a.f.slabs * 256 > 0xffffffffL)
     return set_error(PARROT_ERR_UNSUPPORTED, "fill needs %ld workgroups", units * a.f.slabs);
   a.units = (int)units;
