@@ -199,9 +199,23 @@ parrot_status parrot_cache8_fill(
   a.f.sk = suffix->k; a.f.sv = suffix->v; a.scales = suffix->scales;
   const long elt = p->dtype == PARROT_DTYPE_F32 ? 4 : 2;
   const long units = rows->max_query_rows == 1 ? p->num_requests : rows->num_query_rows / 16 + 2L * p->num_requests;
-  // heads of a workgroup's step: a lane group each for single rows, a wave or half of one for a block's
-  const long step = rows->max_query_rows == 1 ? 4096 / (p->head_dim * elt) : p->head_dim * elt == 128 ? 8 : 4;
-  parrot::fill_slabs(&a.f, step, std::max(1L, std::min((long)rows->num_query_rows, units)));
+  if (rows->max_query_rows == 1) {         // a lane group per head
+    parrot::fill_slabs(&a.f, 4096 / (p->head_dim * elt), p->num_requests);
+  } else {
+    // a wave or half of one per head; four workgroups a CU are there at once, and the units' heads
+    // go over as many as leave the last round fullest (470 units of 96 heads in bfloat16: two a unit 89 us,
+    // three 104, one 131, nine 96)
+    const long step = p->head_dim * elt == 128 ? 8 : 4, steps = ceil_div(a.f.HQ + 2L * a.f.H, step);
+    const long busy = ceil_div(rows->num_query_rows, 16) + p->num_requests, room = 4L * parrot::device_cus();
+    long best = 1;
+    double least = 1e30;
+    for (long n = 1; n <= std::min(steps, 24L); ++n) {
+      const double t = (double)ceil_div(busy * n, room) * ceil_div(steps, n) + 0.1 * n;
+      if (t < least) { least = t; best = n; }
+    }
+    a.f.slab_heads = (int)(ceil_div(steps, best) * step);
+    a.f.slabs = (int)ceil_div(a.f.HQ + 2L * a.f.H, a.f.slab_heads);
+  }
   if (units * a.f.slabs * 256 > 0xffffffffL)
     return set_error(PARROT_ERR_UNSUPPORTED, "fill needs %ld workgroups", units * a.f.slabs);
   a.units = (int)units;

@@ -142,7 +142,7 @@ PARROT_DEV void turn_row(const FillArgs& a, const Head8Of& hd, const float* w, c
 #pragma unroll
     for (int e = 0; e < EPL; ++e) ss = __builtin_fmaf(y[e], y[e], ss);
     ss = group_sum<LPH>(ss);
-    rs = 1.f / sqrtf(ss * (1.f / D) + a.eps);
+    rs = __builtin_amdgcn_rsqf(ss * (1.f / D) + a.eps);
 #pragma unroll
     for (int e = 0; e < EPL; ++e) y[e] = y[e] * rs * w[e];
   }
@@ -290,7 +290,8 @@ __global__ __launch_bounds__(256) void k_cache8_fill_tokens(FillArgs a, unsigned
 // block's 16 slots, so that values' four tokens lie in one lane and a block-head's largest element is
 // a wave's maximum.  Bound by memory: see the figures at the launch.
 template <int DT, int D, int PARTNER>
-__global__ __launch_bounds__(256) void k_cache8_fill(FillArgs a, unsigned char* scales) {
+__global__ __launch_bounds__(256)
+void k_cache8_fill(FillArgs a, unsigned char* scales) {
   using E = Elem<DT>;
   constexpr int EB = E::kBytes, EPL = E::kPerLoad, LPH = D / EPL;
   constexpr int GROUPS = LPH == 32 ? 2 : 4, RPG = kBlockTokens / GROUPS;
@@ -312,7 +313,7 @@ __global__ __launch_bounds__(256) void k_cache8_fill(FillArgs a, unsigned char* 
 #pragma unroll
     for (int j = 0; j < RPG; ++j) {
       raw[j] = u32x4{0u, 0u, 0u, 0u};
-      if (slot0 + j >= phi && slot0 + j < end_slot) raw[j] = ld16(hd.src + row_of(slot0 + j) * hd.stride + sub * 16);
+      if (slot0 + j >= phi && slot0 + j < end_slot) raw[j] = ld16_stream(hd.src + row_of(slot0 + j) * hd.stride + sub * 16);
     }
     const size_t bh = (size_t)un.id * a.H + hd.h;
     unsigned char* scale = scales + bh * 2 + (hd.kind == 2);
