@@ -41,8 +41,8 @@ struct Plan8 {
   int depth;                       // levels of prefixes that the plan has room for
   bool direct;                     // one launch without a plan
   int tiles, waves;                // its column tiles per request, waves of a workgroup
-  int sets, cols, runs, min_run;
-  bool wide;                       // neighbouring waves take runs of one head, else neighbouring heads
+  int sets, cols, wgs, min_run;    // column sets and columns of a narrow tile, workgroups of a cache head
+  int wide;                        // columns of a wide tile, 0 where the call has none
   int max_entries;
   long slots;
   parrot::Plan8Layout at;
@@ -105,24 +105,30 @@ parrot_status check_attend(const parrot_problem* p, const parrot_tree_rows* rows
   const bool f32 = p->dtype == PARROT_DTYPE_F32;
   pl->depth = NG > 0 ? std::max(1, (int)p->max_prefix_depth) : 0;
   const long most = G * std::max((long)rows->max_query_rows, NG > 0 ? (long)rows->max_group_rows : 0L);
-  pl->sets = most <= 16 ? 1 : 2;
+  const int dt = (int)p->dtype;
+  pl->sets = most <= 16 || f32 ? 1 : 2;
   pl->cols = 16 * pl->sets;
-  pl->wide = most > pl->cols;
-  const auto waves = [&](int sets) { return cus * (f32 && sets > 1 ? 4 : 8); };
-  pl->runs = (int)std::max(1L, waves(pl->sets) / H);
+  pl->wide = most > parrot::wide_from(dt) ? parrot::wide_cols(dt) : 0;
+  // two workgroups a CU (three of a cache of 64-element heads whose calls have 16 columns at most: 64
+  // requests on 3000 tokens 43 us, 48 with two; 128-element heads 75 and 73)
+  const auto wgs_of = [&](int sets, bool wide) {
+    return std::max(2L, cus * (p->head_dim == 64 && sets == 1 && !wide ? 3 : 2) / H);
+  };
+  pl->wgs = (int)wgs_of(pl->sets, pl->wide != 0);
   pl->min_run = kMinRun;
   // column tiles: those that columns fill, and one more for each sequence (sizes as for the
   // narrowest tiles and the most slots of calls of fewer columns, so that they never decrease)
   const long tiles = (1 + pl->depth) * T * G / 16 + R + NG;
   const long units = ceil_div(p->max_suffix_len, parrot::kUnit) +
                      (NG > 0 ? pl->depth * ceil_div(p->max_prefix_len, parrot::kUnit) : 0);
-  long spread = 16 * std::max(1L, waves(1) / H);
-  if (pl->sets > 1) spread = std::max(spread, 32 * std::max(1L, waves(2) / H));
+  long spread = 4 * wgs_of(1, false) * 16;
+  if (pl->sets > 1) spread = std::max(spread, 4 * wgs_of(2, false) * 32);
+  if (pl->wide) spread = std::max(spread, std::max(4L * pl->wgs * pl->cols, (long)pl->wgs * pl->wide));
   pl->slots = (1 + pl->depth) * T * G + spread;
-  const double ints = (double)tiles * (1 + parrot::kEntryInts) + (double)T * (1 + parrot::kRowInts + pl->depth) + waves(1) +
-                      (NG + R) * (1.0 + parrot::kMaxDepth + parrot::kReqInts) + (parrot::kPlanWaves + 1.0) * NG;
+  const double ints = (double)tiles * (1 + parrot::kEntryInts) + (double)T * (1 + parrot::kRowInts + pl->depth) + 4.0 * wgs_of(1, false) +
+                      (NG + R) * (2.0 + parrot::kMaxDepth + parrot::kReqInts) + (parrot::kPlanWaves + 1.0) * NG;
   if (((1.0 + pl->depth) * T * G / pl->cols + R + NG) * (units + parrot::kPieceSetup) > 1.5e9 || pl->slots > 0x7fffffffL || ints > 1.0e9 ||
-      R + NG > 0x3fffffffL || pl->runs * H * 64 > 0xffffffffL)
+      R + NG > 0x3fffffffL || pl->wgs * H * 256 > 0xffffffffL)
     return set_error(PARROT_ERR_UNSUPPORTED, "attention over 8 bits: %ld rows in %ld column tiles of %ld units", T, tiles, units);
   pl->max_entries = (int)tiles;
   auto& at = pl->at;
@@ -130,11 +136,11 @@ parrot_status check_attend(const parrot_problem* p, const parrot_tree_rows* rows
   auto take = [&n](long ints) { const long first = n; n = (n + ints + 3) & ~3L; return first; };
   at.cost = take(tiles);
   at.entry = take(tiles * parrot::kEntryInts);
-  at.run = take(waves(1));
+  at.run = take(4 * wgs_of(1, false));
   at.row = take(T * parrot::kRowInts);
   at.join = take(T);
   at.list = take(T * std::max(pl->depth, 1));
-  at.seq = take(NG + R + 1);
+  at.seq = take(2 * (NG + R) + 1);
   at.req = take(R * parrot::kReqInts);
   at.pos = take(R * parrot::kMaxDepth);
   at.count = take((parrot::kPlanWaves + 1) * NG + 1);
@@ -255,8 +261,10 @@ parrot_status parrot_cache8_plan(
   if (pl.direct) return set_error(PARROT_OK, "");
   a.plan = reinterpret_cast<int*>(plan);
   a.at = pl.at;
-  a.cols = pl.cols; a.chain_cols = parrot::kChainTiles * pl.cols;
-  a.runs = pl.runs; a.min_run = pl.min_run;
+  a.cols = pl.cols;
+  a.wide_cols = parrot::wide_cols((int)p->dtype);
+  a.wide_from = pl.wide ? parrot::wide_from((int)p->dtype) : 0x7fffffff;
+  a.wgs = pl.wgs; a.min_run = pl.min_run;
   a.max_entries = pl.max_entries; a.max_slots = pl.slots;
   return launched(parrot::launch_plan8(a, reinterpret_cast<hipStream_t>(stream)), "plan kernel");
 }
@@ -300,7 +308,7 @@ parrot_status parrot_cache8_attention(
   a.pstride = p->prefix_table_stride; a.sstride = p->suffix_table_stride;
   a.max_p = a.st.max_p; a.max_s = p->max_suffix_len;
   a.npblk = p->num_groups > 0 ? p->num_prefix_blocks : 1; a.nsblk = p->num_suffix_blocks;
-  a.runs = pl.runs; a.sets = pl.sets; a.wide = pl.wide; a.max_entries = pl.max_entries; a.tiles = pl.tiles; a.waves = pl.waves;
+  a.wgs = pl.wgs; a.sets = pl.sets; a.wide = pl.wide; a.max_entries = pl.max_entries; a.tiles = pl.tiles; a.waves = pl.waves;
   a.flip = p->sm_scale < 0.f;
   a.scale_log2 = std::fabs(p->sm_scale) * parrot::kLog2e;
   const parrot_trace none = {nullptr, nullptr, nullptr, nullptr};

@@ -26,8 +26,10 @@ hipError_t launch_fill8(const Fill8Args& a, int partner, int dtype, int D, hipSt
 // Where a plan holds what, in ints from its start.  Entries are the column tiles of sequences:
 // the groups first (their columns are the rows of all requests that read the group's prefix, times
 // the query heads of a cache head), then the requests (their own rows' columns), in order.
-// A request whose own columns fill kChainTiles tiles goes through its group chain by itself, in
-// one piece with its own tokens, and is no reader of the groups.
+// Sequences of more than wide_from columns have tiles of wide_cols columns, which a workgroup's four
+// waves take together; their entries come before the others', whose tiles a wave takes alone.  A
+// request with a wide tile's columns of its own goes through its group chain by itself, in one
+// piece with its own tokens, and is no reader of the groups.
 struct Plan8Layout {
   long cost, entry, run, row, join, list, seq, req, pos, count, total;
 };
@@ -37,16 +39,19 @@ constexpr int kRowInts = 12;
 constexpr int kReqInts = 12;
 constexpr int kPlanWaves = 16;           // waves of the planning workgroup
 constexpr int kPieceSetup = 2;           // cost of a tile beside its units
-constexpr int kChainTiles = 4;
 
-// The head: entries, run length, total cost, rows to join.
-enum Head8 { kHeadEntries, kHeadRun, kHeadCost, kHeadJoins };
+// Columns of a wide tile, and of a sequence from which on it has them (more than half full).
+constexpr int wide_cols(int dtype) { return dtype == kF32 ? 64 : 128; }
+constexpr int wide_from(int dtype) { return wide_cols(dtype) / 2; }
+
+// The head: entries, wide ones among them, rows to join, cost of the wide entries, cost of all, a
+// cache head's workgroups of the wide role, run lengths of wide and narrow roles.
+enum Head8 { kHeadEntries, kHeadWide, kHeadJoins, kHeadWideCost, kHeadCost, kHeadWideWgs, kHeadWideRun, kHeadRun };
 // An entry: sequence (request r, or ~g for group), its columns [col0, col0 + ncols), cost at which it
 // starts, units, first slot of its partial results (-1: it writes the output), pieces, own keys (of a
 // group: its prefix's), keys that every column sees, first row (group: first place in the row
-// list), flags: the chain's prefixes come first; no other tile reads the keys.
-enum Entry8 { kEntSeq, kEntCol0, kEntCols, kEntCost, kEntUnits, kEntSlot, kEntPieces, kEntKeys, kEntBase, kEntFirst, kEntFlags };
-constexpr int kEntChained = 1, kEntOnce = 2;
+// list), whether the chain's prefixes come first.
+enum Entry8 { kEntSeq, kEntCol0, kEntCols, kEntCost, kEntUnits, kEntSlot, kEntPieces, kEntKeys, kEntBase, kEntFirst, kEntChained };
 // A row: entry of its request's first tile, its place in the request, levels of prefixes, then
 // for each level the entry of the group's first tile and the row's place in the group's list.
 enum Row8 { kRowEntry, kRowPlace, kRowLevels, kRowUnused, kRowGroup };
@@ -63,9 +68,9 @@ struct Plan8Args {
   Step8 st;
   int* plan;
   Plan8Layout at;
-  int cols;                              // columns of a tile
-  int chain_cols;                        // own columns from which a request is no reader of groups
-  int runs, min_run;
+  int cols;                              // columns of a narrow tile
+  int wide_cols, wide_from;              // of a wide tile; columns above which a sequence has wide ones
+  int wgs, min_run;                      // workgroups of a cache head; cost of a run at least
   int max_entries; long max_slots;
 };
 hipError_t launch_plan8(const Plan8Args& a, hipStream_t s);
@@ -82,7 +87,8 @@ struct Attend8Args {
   long slots;
   int T, R, H, G, NG, depth;             // depth: levels that the plan has room for
   int pstride, sstride, max_p, max_s, npblk, nsblk;
-  int runs, sets, wide, max_entries;     // sets: column sets of a tile; wide: a workgroup's waves take runs of one head
+  int wgs, max_entries;                  // workgroups of a cache head
+  int sets, wide;                        // column sets of a narrow tile, columns of a wide one (0: the call has none)
   int tiles, waves;                      // one launch: column tiles of a request, waves of a workgroup (4 or 8)
   int flip;                              // sm_scale < 0: queries change sign
   float scale_log2;                      // |sm_scale| log2(e)

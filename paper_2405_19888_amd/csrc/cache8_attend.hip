@@ -1,12 +1,13 @@
 // Attention over a cache held in 8 bits (cache8_args.h has the format, cache8_tile.h the
 // wave's mathematics): plan, partial results and join, or one launch for small calls.
 //
-// What a step has to read is laid end to end as one list of costs: column tiles of the groups'
+// What a step has to read is laid end to end as a list of costs: column tiles of the groups'
 // prefixes (the rows of all requests below a group, stacked, so that a prefix is read once per tile
-// and not once per request), then column tiles of the requests' own tokens.  A tile costs its units
+// and not once per request), and column tiles of the requests' own tokens.  A tile costs its units
 // of 32 keys and kPieceSetup.  The list is cut into equal runs, a wave of each cache head takes
 // one, and where a run ends inside a tile, the pieces are joined.  Nothing depends on how
-// ragged the contexts are, and no wave waits for another.
+// ragged the contexts are.  Sequences of many columns have a list of their own, of wide tiles, whose
+// runs workgroups take; both lists share the device by their costs.
 //
 // The list depends on lengths and groups alone, so one plan serves every layer of a step.
 #include "cache8_tile.h"
@@ -14,14 +15,20 @@
 namespace parrot {
 
 // ---------------------------------------------------------------------- plan
+// Inclusive sum over the wave: within rows of 16 lanes, then the rows before.
+PARROT_DEV int scan_wave(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // row_shr 1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // row_bcast 15 into rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // row_bcast 31 into rows 2 and 3
+  return x;
+}
 // Inclusive sum over the workgroup's 1024 threads; *total is the whole sum.
 PARROT_DEV int scan1024(int x, int* lds, int* total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) {
-    const int v = __shfl_up(x, d);
-    if (lane >= d) x += v;
-  }
+  x = scan_wave(x);
   __syncthreads();
   if (lane == kWave - 1) lds[wave] = x;
   __syncthreads();
@@ -49,53 +56,54 @@ PARROT_DEV Own8 own_rows(const Step8& a, int r) {
   return o;
 }
 
-// Rows of each of the wave's requests that read groups, by level of the chain: counts of the
-// wave's rows per group (assign false), or each request's place in the group's list.
-PARROT_DEV void walk_groups(const Plan8Args& a, const int* req, int* pos, int* count, bool assign) {
+// Rows of each of the wave's requests that read groups, by level of the chain: the wave's rows of each
+// group, and each request's place among them.
+PARROT_DEV void walk_groups(const Plan8Args& a, const int* req, int* pos, int* count) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, NG = a.st.NG;
   const int r0 = (int)((long)a.st.R * wave / kPlanWaves), r1 = (int)((long)a.st.R * (wave + 1) / kPlanWaves);
   int* mine = count + (long)wave * NG;
   for (int b = r0; b < r1; b += kWave) {
     const int r = b + lane;
-    int n = 0, grp = -1;
+    int n = 0, grp = -1, place[kMaxDepth] = {};
     if (r < r1) {
       n = req[(long)r * kReqInts + kReqCount];
       grp = req[(long)r * kReqInts + kReqReads];
     }
-    for (int l = 0; l < a.st.depth; ++l) {
-      const bool on = n > 0 && grp >= 0;
+#pragma unroll
+    for (int l = 0; l < kMaxDepth; ++l) {
+      const bool on = n > 0 && grp >= 0;                // (no levels below the call's)
       unsigned long long todo = __ballot(on);
-      if (!todo) break;
       while (todo) {
         const int leader = __ffsll(todo) - 1;
-        const int gl = __shfl(grp, leader);
+        const int gl = __builtin_amdgcn_readlane(grp, leader);
         const bool same = on && grp == gl;
-        const unsigned long long all = __ballot(same);
-        int incl = same ? n : 0;
-#pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) {
-          const int x = __shfl_up(incl, d);
-          if (lane >= d) incl += x;
-        }
+        const int incl = scan_wave(same ? n : 0);
         const int base = mine[gl];
-        if (assign && same) pos[(long)r * kMaxDepth + l] = base + incl - n;
-        const int sum = __shfl(incl, kWave - 1);
-        if (lane == leader) mine[gl] = base + sum;
-        todo &= ~all;
+        if (same) place[l] = base + incl - n;
+        if (lane == leader) mine[gl] = base + __builtin_amdgcn_readlane(incl, kWave - 1);
+        todo &= ~__ballot(same);
         __threadfence_block();                          // (a wave's own writes come back in order)
       }
       grp = on && l + 1 < kMaxDepth ? req[(long)r * kReqInts + kReqChain + 2 * (l + 1)] : -1;
     }
+    if (r < r1) *reinterpret_cast<int4*>(pos + (long)r * kMaxDepth) = int4{place[0], place[1], place[2], place[3]};
   }
 }
+static_assert(kMaxDepth == 4, "a request's places are one store");
+// The planning wave that counted request r (plans hold fewer than 2^26 requests).
+PARROT_DEV int wave_of(int r, int R) { return (int)(((unsigned)r * kPlanWaves + kPlanWaves - 1) / (unsigned)R); }
 
 // One workgroup: a few round trips and scans for a usual batch, 1024 requests, groups or entries a
 // round.  What it looks up again and again is in LDS where it fits.
 constexpr int kPlanReqs = 1024, kPlanCounts = 4096, kPlanSeqs = 2048;
+// Tiles of a sequence of n columns: wide or narrow ones.
+PARROT_DEV int2 tiles_of(const Plan8Args& a, long n) {
+  return n > a.wide_from ? int2{(int)((n + a.wide_cols - 1) / a.wide_cols), 0} : int2{0, (int)((n + a.cols - 1) / a.cols)};
+}
 __global__ __launch_bounds__(1024) void k_cache8_plan(Plan8Args a) {
   __shared__ int lds[kPlanWaves + 2];
   __shared__ __attribute__((aligned(16))) int l_req[kPlanReqs * kReqInts];
-  __shared__ int l_count[kPlanCounts], l_seq[kPlanSeqs], l_cost[kPlanSeqs];
+  __shared__ int l_count[kPlanCounts], l_seq[2 * kPlanSeqs], l_cost[kPlanSeqs], l_slot[kPlanSeqs];
   const int tid = threadIdx.x;
   const Step8& st = a.st;
   int* ent = a.plan + a.at.entry;
@@ -107,7 +115,9 @@ __global__ __launch_bounds__(1024) void k_cache8_plan(Plan8Args a) {
   int* const g_req = a.plan + a.at.req;
   int* req = st.R <= kPlanReqs ? l_req : g_req;
   int* count = (long)(kPlanWaves + 1) * st.NG + 1 <= kPlanCounts ? l_count : a.plan + a.at.count;
+  // first entries of each sequence: wide ones, and narrow ones counted from the first of them
   int* seq = nseq < kPlanSeqs ? l_seq : a.plan + a.at.seq;
+  int* seqn = seq + nseq;
   int* off = count + (long)kPlanWaves * st.NG;          // first place of each group's rows
 
   // the requests
@@ -115,7 +125,7 @@ __global__ __launch_bounds__(1024) void k_cache8_plan(Plan8Args a) {
     const Own8 o = own_rows(st, r);
     int v[kReqInts] = {o.first, o.count, o.keys, -1, -1, 0, -1, 0, -1, 0, -1, 0};
     int grp = st.gid[r];
-    const bool chained = (long)o.count * st.G >= a.chain_cols;
+    const bool chained = (long)o.count * st.G >= a.wide_cols;
 #pragma unroll
     for (int l = 0; l < kMaxDepth; ++l)
       if (l < st.depth && grp >= 0 && grp < st.NG) {
@@ -132,14 +142,16 @@ __global__ __launch_bounds__(1024) void k_cache8_plan(Plan8Args a) {
       *reinterpret_cast<int4*>(g_req + (long)r * kReqInts + i) = int4{v[i], v[i + 1], v[i + 2], v[i + 3]};
       if (req != g_req) *reinterpret_cast<int4*>(req + r * kReqInts + i) = int4{v[i], v[i + 1], v[i + 2], v[i + 3]};
     }
-    seq[st.NG + r] = (int)(((long)o.count * st.G + a.cols - 1) / a.cols);
+    const int2 tiles = tiles_of(a, (long)o.count * st.G);
+    seq[st.NG + r] = tiles.x;
+    seqn[st.NG + r] = tiles.y;
   }
   if (tid == 0) lds[kPlanWaves] = 0;                    // rows to join
   for (long i = tid; i < (long)kPlanWaves * st.NG; i += 1024) count[i] = 0;
   __syncthreads();
   // rows of each group, and each request's place among them
   if (st.depth > 0) {
-    walk_groups(a, req, pos, count, false);
+    walk_groups(a, req, pos, count);
     __syncthreads();
     int before = 0;
     for (int b = 0; b < st.NG; b += 1024) {
@@ -155,63 +167,70 @@ __global__ __launch_bounds__(1024) void k_cache8_plan(Plan8Args a) {
       const int incl = scan1024(n, lds, &sum);
       if (g < st.NG) {
         off[g] = before + incl - n;
-        // tiles of the group
-        seq[g] = clampi(st.plen[g], 0, st.max_p) > 0 ? (int)(((long)n * st.G + a.cols - 1) / a.cols) : 0;
+        const int2 tiles = tiles_of(a, clampi(st.plen[g], 0, st.max_p) > 0 ? (long)n * st.G : 0);
+        seq[g] = tiles.x;
+        seqn[g] = tiles.y;
       }
       before += sum;
     }
     if (tid == 0) off[st.NG] = before;
     __syncthreads();
-    walk_groups(a, req, pos, count, true);
-    __syncthreads();
   }
   // tiles become first entries
-  int entries = 0;
+  int wide = 0, narrow = 0;
   for (int b = 0; b < nseq; b += 1024) {
     const int i = b + tid;
-    const int n = i < nseq ? seq[i] : 0;
-    int sum;
-    const int incl = scan1024(n, lds, &sum);
-    if (i < nseq) seq[i] = entries + incl - n;
-    entries += sum;
+    const int n = i < nseq ? seq[i] : 0, m = i < nseq ? seqn[i] : 0;
+    int sum = 0, summ;
+    int incl = 0;
+    if (a.wide_from < 0x7fffffff) incl = scan1024(n, lds, &sum);
+    const int inclm = scan1024(m, lds, &summ);
+    if (i < nseq) {
+      seq[i] = wide + incl - n;
+      seqn[i] = narrow + inclm - m;
+    }
+    wide += sum;
+    narrow += summ;
   }
-  entries = min(entries, a.max_entries);
+  const int entries = min(wide + narrow, a.max_entries);
   int* cost = entries <= kPlanSeqs ? l_cost : a.plan + a.at.cost;
   __syncthreads();
 
   // the entries, and where each starts in the cost
   int total = 0;
+  int e_cost = 0, e_units = 0, e_cols = 0;              // of the thread's entry, if there is one round of them
+  bool e_parts = false;
   for (int b = 0; b < entries; b += 1024) {
     const int e = b + tid;
     int c = 0, v[kEntryInts] = {};
     if (e < entries) {
+      const bool w = e < wide;
+      const int* first = w ? seq : seqn;
+      const int cols = w ? a.wide_cols : a.cols, at = w ? e : e - wide;
       int lo = 0, hi = nseq;                            // the last sequence that starts at or before e
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (seq[mid] <= e) lo = mid; else hi = mid;
+        if (first[mid] <= at) lo = mid; else hi = mid;
       }
-      const int tile = e - seq[lo];
-      v[kEntCol0] = tile * a.cols;
+      v[kEntCol0] = (at - first[lo]) * cols;
       if (lo < st.NG) {
         const int n = off[lo + 1] - off[lo];
         v[kEntSeq] = ~lo;
-        v[kEntCols] = (int)min((long)a.cols, (long)n * st.G - v[kEntCol0]);
+        v[kEntCols] = (int)min((long)cols, (long)n * st.G - v[kEntCol0]);
         v[kEntKeys] = v[kEntBase] = clampi(st.plen[lo], 0, st.max_p);
         v[kEntFirst] = off[lo];
         v[kEntUnits] = (v[kEntKeys] + kUnit - 1) / kUnit;
-        v[kEntFlags] = n * (long)st.G <= a.cols ? kEntOnce : 0;
       } else {
         const int* o = req + (long)(lo - st.NG) * kReqInts;
         v[kEntSeq] = lo - st.NG;
-        v[kEntCols] = (int)min((long)a.cols, (long)o[kReqCount] * st.G - v[kEntCol0]);
+        v[kEntCols] = (int)min((long)cols, (long)o[kReqCount] * st.G - v[kEntCol0]);
         const int from = o[kReqKeys] - o[kReqCount];    // row j sees own tokens 0 .. from + j
         v[kEntKeys] = from + (v[kEntCol0] + v[kEntCols] - 1) / st.G + 1;
         v[kEntBase] = from;
         v[kEntFirst] = o[kReqFirst];
         v[kEntUnits] = (v[kEntKeys] + kUnit - 1) / kUnit;
-        v[kEntFlags] = (long)o[kReqCount] * st.G <= a.cols ? kEntOnce : 0;
         if (o[kReqReads] < 0 && o[kReqChain] >= 0) {
-          v[kEntFlags] |= kEntChained;
+          v[kEntChained] = 1;
           for (int l = 0; l < kMaxDepth; ++l) v[kEntUnits] += (o[kReqChain + 2 * l + 1] + kUnit - 1) / kUnit;
         }
       }
@@ -222,6 +241,10 @@ __global__ __launch_bounds__(1024) void k_cache8_plan(Plan8Args a) {
     if (e < entries) {
       v[kEntCost] = total + incl - c;
       cost[e] = v[kEntCost];
+      e_cost = v[kEntCost];
+      e_units = v[kEntUnits];
+      e_cols = v[kEntCols];
+      e_parts = v[kEntSeq] < 0 || req[(long)v[kEntSeq] * kReqInts + kReqReads] >= 0;
       int4* to = reinterpret_cast<int4*>(ent + (long)e * kEntryInts);
       to[0] = int4{v[0], v[1], v[2], v[3]};
       to[1] = int4{v[4], v[5], v[6], v[7]};
@@ -230,13 +253,24 @@ __global__ __launch_bounds__(1024) void k_cache8_plan(Plan8Args a) {
     total += sum;
   }
   __syncthreads();
-  const int q = max(a.min_run, (int)(((long)total + a.runs - 1) / a.runs));
-  // the first entry of each run
-  for (int run = tid; run < a.runs && (long)run * q < total; run += 1024) {
-    int lo = 0, hi = entries;
+  // a cache head's workgroups are shared by the two costs: a wide unit comes out of LDS and keeps a
+  // workgroup half as long as a narrow one, which streams, keeps a wave (288 requests, 256 of them
+  // below 8 prefixes, us a layer: 123; as 0.3 of it 161, as long 131)
+  const int wcost = wide == 0 ? 0 : wide < entries ? cost[wide] : total;
+  const int wwgs = wide == 0 ? 0 : wide == entries ? a.wgs
+                 : clampi((int)((2L * a.wgs * wcost + ((long)wcost + total) / 2) / ((long)wcost + total)), 1, a.wgs - 1);
+  const int nruns = 4 * (a.wgs - wwgs);
+  const int qw = wwgs == 0 ? 1 : max(a.min_run, (int)(((long)wcost + wwgs - 1) / wwgs));
+  const int q = nruns == 0 ? 1 : max(a.min_run, (int)(((long)total - wcost + nruns - 1) / nruns));
+  // the first entry of each run: the wide role's, then the narrow one's
+  for (int run = tid; run < wwgs + nruns; run += 1024) {
+    const bool w = run < wwgs;
+    const long c0 = w ? (long)run * qw : wcost + (long)(run - wwgs) * q;
+    if (c0 >= (w ? wcost : total)) continue;
+    int lo = w ? 0 : wide, hi = w ? wide : entries;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (cost[mid] <= run * q) lo = mid; else hi = mid;
+      if (cost[mid] <= c0) lo = mid; else hi = mid;
     }
     a.plan[a.at.run + run] = lo;
   }
@@ -247,19 +281,28 @@ __global__ __launch_bounds__(1024) void k_cache8_plan(Plan8Args a) {
     int n = 0, pieces = 0;
     int* v = ent + (long)e * kEntryInts;
     if (e < entries) {                                  // (its own entries)
-      const int s0 = v[kEntCost] + kPieceSetup;
-      pieces = (s0 + v[kEntUnits] - 1) / q - s0 / q + 1;
-      const int r = v[kEntSeq];
-      n = r >= 0 && pieces == 1 && req[(long)r * kReqInts + kReqReads] < 0 ? 0 : pieces * v[kEntCols];
+      if (entries > 1024) {
+        e_cost = v[kEntCost];
+        e_units = v[kEntUnits];
+        e_cols = v[kEntCols];
+        e_parts = v[kEntSeq] < 0 || req[(long)v[kEntSeq] * kReqInts + kReqReads] >= 0;
+      }
+      const int s0 = e_cost + kPieceSetup - (e < wide ? 0 : wcost), len = e < wide ? qw : q;
+      pieces = (s0 + e_units - 1) / len - s0 / len + 1;
+      n = pieces == 1 && !e_parts ? 0 : pieces * e_cols;
     }
     int sum;
     const int incl = scan1024(n, lds, &sum);
     if (e < entries) {
-      v[kEntSlot] = n == 0 ? -1 : slots + incl - n;
+      const int slot = n == 0 ? -1 : slots + incl - n;
+      v[kEntSlot] = slot;
       v[kEntPieces] = pieces;
+      if (e < kPlanSeqs) l_slot[e] = slot;
     }
     slots += sum;
   }
+  const int* const e_slot = entries <= kPlanSeqs ? l_slot : ent + kEntSlot;
+  const int e_step = entries <= kPlanSeqs ? 1 : kEntryInts;
   __syncthreads();
   // the groups' row lists, what the join needs of each row, and the rows that it takes
   const int used = clampi(st.qoff[st.R], 0, st.T);
@@ -273,7 +316,8 @@ __global__ __launch_bounds__(1024) void k_cache8_plan(Plan8Args a) {
     const int j = t - o[kReqFirst];
     if (j < 0 || j >= o[kReqCount]) continue;           // no request holds it
     int v[kRowInts] = {};
-    const int first = seq[st.NG + lo];
+    const bool w = (long)o[kReqCount] * st.G > a.wide_from;
+    const int first = w ? seq[st.NG + lo] : wide + seqn[st.NG + lo], cols = w ? a.wide_cols : a.cols;
     v[kRowEntry] = first;
     v[kRowPlace] = j;
     if (o[kReqReads] >= 0)
@@ -281,9 +325,9 @@ __global__ __launch_bounds__(1024) void k_cache8_plan(Plan8Args a) {
       for (int l = 0; l < kMaxDepth; ++l) {
         const int grp = o[kReqChain + 2 * l];
         if (grp >= 0) {
-          const int at = pos[(long)lo * kMaxDepth + l] + j;
+          const int at = count[(long)wave_of(lo, st.R) * st.NG + grp] + pos[(long)lo * kMaxDepth + l] + j;
           if (o[kReqChain + 2 * l + 1] > 0) {
-            v[kRowGroup + 2 * l] = seq[grp];
+            v[kRowGroup + 2 * l] = (long)(off[grp + 1] - off[grp]) * st.G > a.wide_from ? seq[grp] : wide + seqn[grp];
             v[kRowGroup + 2 * l + 1] = at;
             v[kRowLevels] = l + 1;
           }
@@ -296,22 +340,28 @@ __global__ __launch_bounds__(1024) void k_cache8_plan(Plan8Args a) {
     d[2] = int4{v[8], v[9], v[10], v[11]};
     // (the row's columns are in one or more of its request's tiles)
     bool parts = false;
-    for (int e = first + (int)((long)j * st.G / a.cols); e <= first + (int)(((long)j * st.G + st.G - 1) / a.cols) && e < entries; ++e)
-      parts = parts || ent[(long)e * kEntryInts + kEntSlot] >= 0;
+    for (int e = first + (int)((long)j * st.G / cols); e <= first + (int)(((long)j * st.G + st.G - 1) / cols) && e < entries; ++e)
+      parts = parts || e_slot[(long)e * e_step] >= 0;
     // (their order is of no matter: each row is joined by itself)
     if (parts) joins[min(atomicAdd(&lds[kPlanWaves], 1), st.T - 1)] = t;
   }
   __syncthreads();
-  if (tid == 0) *reinterpret_cast<int4*>(a.plan) = int4{entries, q, total, lds[kPlanWaves]};
+  if (tid == 0) {
+    *reinterpret_cast<int4*>(a.plan) = int4{entries, wide, lds[kPlanWaves], wcost};
+    *reinterpret_cast<int4*>(a.plan + 4) = int4{total, wwgs, qw, q};
+  }
 }
 
 // ----------------------------------------------------------- partial results
 // Keys of one sequence of a call: a request's own tokens, or a group's prefix.
 PARROT_DEV Range8 range_of(const Attend8Args& a, bool own, int seq, int keys, int u0, int u1) {
   Range8 rg;
-  rg.pool = own ? a.own : a.pre;
-  rg.tbl = own ? a.stab + (long)seq * a.sstride : a.ptab + (long)seq * a.pstride;
-  rg.npool = own ? a.nsblk : a.npblk;
+  const Pool8 pool = own ? a.own : a.pre;
+  rg.pool.k = alone(pool.k);
+  rg.pool.v = alone(pool.v);
+  rg.pool.scales = alone(pool.scales);
+  rg.tbl = alone(own ? a.stab + (long)seq * a.sstride : a.ptab + (long)seq * a.pstride);
+  rg.npool = alone(own ? a.nsblk : a.npblk);
   rg.u0 = u0;
   rg.u1 = u1;
   rg.end = rg.plain = keys;
@@ -338,34 +388,36 @@ PARROT_DEV void write_column(const Attend8Args& a, const Tile8<DT, D, NS>& tile,
 }
 
 // An entry as the kernel reads it: wave-uniform, every index clamped to what it may address.
-struct Entry { int seq, col0, cols, cost, units, slot, keys, base, first, flags; };
+struct Entry { int seq, col0, cols, cost, units, slot, keys, base, first, chained; };
 PARROT_DEV Entry load_entry(const Attend8Args& a, int e) {
   const int* p = a.plan + a.at.entry + (long)e * kEntryInts;
   Entry v;
   v.seq = ld_uniform(p + kEntSeq);
   v.seq = v.seq >= 0 ? min(v.seq, a.R - 1) : max(v.seq, -max(a.NG, 1));
   v.col0 = max(ld_uniform(p + kEntCol0), 0);
-  v.cols = clampi(ld_uniform(p + kEntCols), 0, 16 * a.sets);
+  v.cols = clampi(ld_uniform(p + kEntCols), 0, max(16 * a.sets, a.wide));
   v.cost = ld_uniform(p + kEntCost);
   v.keys = clampi(ld_uniform(p + kEntKeys), 0, v.seq >= 0 ? a.max_s : a.max_p);
   v.units = max(ld_uniform(p + kEntUnits), 0);
   v.slot = ld_uniform(p + kEntSlot);
   v.base = ld_uniform(p + kEntBase);
   v.first = max(ld_uniform(p + kEntFirst), 0);
-  v.flags = ld_uniform(p + kEntFlags);
+  v.chained = ld_uniform(p + kEntChained);
   return v;
 }
 
-// Units [u0, u1) of an entry, piece number `piece`.
-template <int DT, int D, int NS>
-PARROT_DEV void attend_piece(const Attend8Args& a, const Entry& e, int h, int u0, int u1, int piece) {
+// Units [u0, u1) of an entry, piece number `piece`.  WIDE: a workgroup's waves take 16 * NS columns
+// of it each.
+template <int DT, int D, int NS, bool WIDE>
+PARROT_DEV void attend_piece(const Attend8Args& a, const Entry& e, int h, int u0, int u1, int piece, char* ring) {
   const int HQ = a.H * a.G;
   const bool own = e.seq >= 0;
+  const int first_col = WIDE ? (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 16 * NS : 0;
   Tile8<DT, D, NS> tile(a.H, h);
   int at[NS], sees[NS];                                 // the columns' places in [T][HQ], or -1, and own keys
 #pragma unroll
   for (int c = 0; c < NS; ++c) {
-    const int col = tile.column(c);
+    const int col = first_col + tile.column(c);
     const int x = e.col0 + col, j = x / a.G;
     at[c] = -1;
     if (col < e.cols) {
@@ -376,11 +428,15 @@ PARROT_DEV void attend_piece(const Attend8Args& a, const Entry& e, int h, int u0
     sees[c] = min(e.keys, e.base + j + 1);
   }
   tile.load_queries(a.q, a.flip != 0, [&](int c) { return (long)at[c]; });
+  const int cols = min(e.cols - first_col, 16 * NS);    // (below 1: a wave that loads for the others)
+  // own keys that every column of the wave sees, and that any does
+  const int plain = min(e.keys, e.base + (e.col0 + first_col) / a.G + 1);
+  const int most = min(e.keys, e.base + (e.col0 + first_col + cols - 1) / a.G + 1);
   // the chain's prefixes where they come first, then the entry's own keys
   const int* chain = a.plan + a.at.req + (long)(own ? e.seq : 0) * kReqInts + kReqChain;
   int from = 0;                                         // units before the range
 #pragma unroll 1
-  for (int l = own && (e.flags & kEntChained) ? 0 : kMaxDepth; l <= kMaxDepth; ++l) {
+  for (int l = own && e.chained ? 0 : kMaxDepth; l <= kMaxDepth; ++l) {
     const bool pre = l < kMaxDepth;
     const int grp = pre ? clampi(ld_uniform(chain + 2 * l), 0, max(a.NG - 1, 0)) : 0;
     const int keys = pre ? clampi(ld_uniform(chain + 2 * l + 1), 0, a.NG > 0 ? a.max_p : 0) : e.keys;
@@ -389,11 +445,12 @@ PARROT_DEV void attend_piece(const Attend8Args& a, const Entry& e, int h, int u0
     from += units;
     if (b >= f) continue;
     Range8 rg = range_of(a, own && !pre, pre ? grp : own ? e.seq : ~e.seq, keys, b, f);
-    if (own && !pre) rg.plain = min(keys, e.base + e.col0 / a.G + 1);
+    if (own && !pre) rg.plain = plain;
 #pragma unroll
     for (int c = 0; c < NS; ++c) tile.lim[c] = own && !pre ? sees[c] : keys;
-    if (NS == 1 && (e.flags & kEntOnce)) tile.template run<NS == 1>(rg, a.scale_log2);
-    else tile.template run<false>(rg, a.scale_log2);
+    if constexpr (WIDE) tile.run_shared(rg, alone(a.scale_log2), ring, cols < 1 ? 0 : own && !pre ? most : keys);
+    // (16 columns are nearly always all that read their keys; wider tiles have neighbours)
+    else tile.template run<NS == 1>(rg, alone(a.scale_log2));
   }
 
   const int g = tile.lane >> 4;
@@ -405,7 +462,7 @@ PARROT_DEV void attend_piece(const Attend8Args& a, const Entry& e, int h, int u0
     if (direct) {
       write_column(a, tile, c, at[c], inv, lse2);
     } else {
-      const long sl = (long)h * a.slots + slot + col;
+      const long sl = (long)h * a.slots + slot + first_col + col;
       float* dst = a.o_part + sl * D + 16 * g;
 #pragma unroll
       for (int x = 0; x < D / 64; ++x)
@@ -416,36 +473,55 @@ PARROT_DEV void attend_piece(const Attend8Args& a, const Entry& e, int h, int u0
   });
 }
 
-template <int DT, int D, int SETS>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DT == kF32 && SETS > 1 ? 1 : 2)))
-void k_cache8_attend(Attend8Args a) {
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int run, h;
-  if (a.wide) {                                         // neighbouring tiles of one head, on one XCD
-    h = blockIdx.x % a.H;
-    run = (int)(blockIdx.x / a.H) * 4 + wave;
-  } else {                                              // neighbouring heads of the same blocks
-    const int w = blockIdx.x * 4 + wave;
-    h = w % a.H;
-    run = w / a.H;
-  }
-  if (run >= a.runs) return;
-  const int entries = clampi(ld_uniform(a.plan + kHeadEntries), 0, a.max_entries);
-  const int q = max(ld_uniform(a.plan + kHeadRun), 1), total = ld_uniform(a.plan + kHeadCost);
-  const int first = ld_uniform(a.plan + a.at.run + run);
-  const long c0 = (long)run * q, c1 = min((long)total, c0 + q);
-  if (c0 >= total) return;
+// A run of a cost list: entries from `first` on, costs [c0, c1) after `base`.
+template <class F>
+PARROT_DEV void walk_run(const Attend8Args& a, int first, int end, long base, long c0, long c1, int q, int run, F piece) {
+  Entry next = load_entry(a, clampi(first, 0, a.max_entries - 1));
 #pragma unroll 1
-  for (int e = max(first, 0); e < entries; ++e) {
-    const Entry v = load_entry(a, e);
-    if (v.cost >= c1) break;
-    const long s0 = (long)v.cost + kPieceSetup;
+  for (int e = max(first, 0); e < end; ++e) {
+    const Entry v = next;
+    const long s0 = v.cost - base + kPieceSetup;
+    if (s0 - kPieceSetup >= c1) break;
+    next = load_entry(a, min(e + 1, a.max_entries - 1));  // (on its way while this one is worked on)
     const int u0 = (int)max(c0 - s0, 0L), u1 = (int)min(c1 - s0, (long)v.units);
     if (u0 >= u1 || v.cols == 0) continue;
-    const int piece = run - (int)(s0 / q);
-    if (SETS > 1 && v.cols > 16) attend_piece<DT, D, SETS>(a, v, h, u0, u1, piece);
-    else attend_piece<DT, D, 1>(a, v, h, u0, u1, piece);
+    piece(v, u0, u1, run - (int)(s0 / q));
   }
+}
+
+// SETS: column sets of narrow tiles, at most.  WIDE: wide tiles too.
+template <int DT, int D, int SETS, bool WIDE>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
+void k_cache8_attend(Attend8Args a) {
+  constexpr int WSETS = DT == kF32 ? 1 : 2;
+  __shared__ __attribute__((aligned(16))) char ring[WIDE ? Tile8<DT, D, WSETS>::RING * Tile8<DT, D, WSETS>::UNIT_B : 16];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int entries = clampi(ld_uniform(a.plan + kHeadEntries), 0, a.max_entries);
+  const int wcost = ld_uniform(a.plan + kHeadWideCost), total = ld_uniform(a.plan + kHeadCost);
+  const int wwgs = WIDE ? clampi(ld_uniform(a.plan + kHeadWideWgs), 0, a.wgs) : 0;
+  if constexpr (WIDE) {
+    if ((int)blockIdx.x < wwgs * a.H) {                 // neighbouring runs of a head on one XCD
+      const int h = blockIdx.x % a.H, run = blockIdx.x / a.H;
+      const int q = max(ld_uniform(a.plan + kHeadWideRun), 1), end = clampi(ld_uniform(a.plan + kHeadWide), 0, entries);
+      const long c0 = (long)run * q, c1 = min((long)wcost, c0 + q);
+      if (c0 >= wcost) return;
+      walk_run(a, ld_uniform(a.plan + a.at.run + run), end, 0, c0, c1, q, run, [&](const Entry& v, int u0, int u1, int piece) {
+        attend_piece<DT, D, WSETS, true>(a, v, h, u0, u1, piece, ring);
+      });
+      return;
+    }
+  }
+  // neighbouring heads of the same blocks
+  const int w = ((int)blockIdx.x - wwgs * a.H) * 4 + wave;
+  const int h = w % a.H, run = w / a.H;
+  const int q = max(ld_uniform(a.plan + kHeadRun), 1);
+  const long c0 = (long)run * q, c1 = min((long)total - wcost, c0 + q);
+  if (c0 >= (long)total - wcost || run >= 4 * (a.wgs - wwgs)) return;
+  walk_run(a, ld_uniform(a.plan + a.at.run + wwgs + run), entries, wcost, c0, c1, q, run,
+           [&](const Entry& v, int u0, int u1, int piece) {
+    if (SETS > 1 && v.cols > 16) attend_piece<DT, D, SETS, false>(a, v, h, u0, u1, piece, ring);
+    else attend_piece<DT, D, 1, false>(a, v, h, u0, u1, piece, ring);
+  });
 }
 
 // ---------------------------------------------------------------- one launch
@@ -502,7 +578,7 @@ void k_cache8_direct(Attend8Args a) {
     if (own) rg.plain = min(n, base + col0 / a.G + 1);
 #pragma unroll
     for (int c = 0; c < NS; ++c) tile.lim[c] = own ? min(keys, base + (col0 + tile.column(c)) / a.G + 1) : n;
-    tile.template run<false>(rg, a.scale_log2);
+    tile.template run<false>(rg, alone(a.scale_log2));
   }
   // the waves' results meet in LDS: normalised outputs and log-sum-exps
   tile.finish([&](int c, int col, float inv, float lse2) {
@@ -551,7 +627,8 @@ __global__ __launch_bounds__(256) void k_cache8_join(Attend8Args a) {
   constexpr bool MEET = GROUPS > 1;
   __shared__ float s_m[MEET ? GROUPS : 1][HEADS], s_l[MEET ? GROUPS : 1][HEADS];
   __shared__ f32x4 s_o[MEET ? GROUPS : 1][HEADS][GW];
-  const int HQ = a.H * a.G, parts = (HQ + HEADS - 1) / HEADS, cols = 16 * a.sets;
+  const int HQ = a.H * a.G, parts = (HQ + HEADS - 1) / HEADS;
+  const int wide = ld_uniform(a.plan + kHeadWide);
   const int i0 = threadIdx.x % GW, sub = threadIdx.x / GW, mine = sub % HEADS, grp = sub / HEADS;
   const long work = (long)clampi(ld_uniform(a.plan + kHeadJoins), 0, a.T) * parts;
   for (long w = blockIdx.x; w < work; w += gridDim.x) {
@@ -567,9 +644,10 @@ __global__ __launch_bounds__(256) void k_cache8_join(Attend8Args a) {
 #pragma unroll 1
     for (int s = -1; s < levels; ++s) {                 // own tokens, then the chain's prefixes
       const int x = (s < 0 ? ld_uniform(d + kRowPlace) : ld_uniform(d + kRowGroup + 2 * s + 1)) * a.G + gq;
-      const int e = (s < 0 ? ld_uniform(d + kRowEntry) : ld_uniform(d + kRowGroup + 2 * s)) + x / cols;
+      const int e0 = s < 0 ? ld_uniform(d + kRowEntry) : ld_uniform(d + kRowGroup + 2 * s);
+      const int cols = e0 < wide ? max(a.wide, 1) : 16 * a.sets, e = e0 + x / cols;
       const int* v = a.plan + a.at.entry + (long)clampi(e, 0, a.max_entries - 1) * kEntryInts;
-      const int slot = v[kEntSlot], nc = v[kEntCols], n = min(v[kEntPieces], a.runs);   // (a piece per run at most)
+      const int slot = v[kEntSlot], nc = v[kEntCols], n = min(v[kEntPieces], 4 * a.wgs);   // (a piece per run at most)
       if (s < 0 && slot < 0) { direct = true; break; }  // the piece wrote the output
       const int col = x % cols;
 #pragma unroll 1
@@ -634,7 +712,7 @@ __global__ __launch_bounds__(256) void k_cache8_join(Attend8Args a) {
 
 // ------------------------------------------------------------------ launches
 hipError_t launch_plan8(const Plan8Args& a, hipStream_t s) {
-  if (a.st.T < 1 || a.st.R < 1 || a.st.G < 1 || a.cols < 16 || a.chain_cols < 1 || a.runs < 1 || a.min_run < 1 ||
+  if (a.st.T < 1 || a.st.R < 1 || a.st.G < 1 || a.cols < 16 || a.wide_cols < 1 || a.wide_from < 1 || a.wgs < 2 || a.min_run < 1 ||
       a.max_entries < 1 || a.st.depth < 0 || a.st.depth > kMaxDepth || (a.st.NG > 0) != (a.st.depth > 0))
     return hipErrorInvalidValue;
   hipLaunchKernelGGL(k_cache8_plan, dim3(1), dim3(1024), 0, s, a);
@@ -643,12 +721,13 @@ hipError_t launch_plan8(const Plan8Args& a, hipStream_t s) {
 
 template <int DT, int D>
 static hipError_t launch_attend_t(const Attend8Args& a, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
-  const long waves = (long)a.runs * a.H;
-  const long wgs = a.wide ? (a.runs + 3L) / 4 * a.H : (waves + 3) / 4;
-  if (wgs * 256 > 0xffffffffL) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)wgs);
-  if (a.sets == 1) hipExtLaunchKernelGGL((k_cache8_attend<DT, D, 1>), grid, dim3(256), 0, s, e0, e1, 0, a);
-  else hipExtLaunchKernelGGL((k_cache8_attend<DT, D, 2>), grid, dim3(256), 0, s, e0, e1, 0, a);
+  constexpr int MOST = DT == kF32 ? 1 : 2;
+  const long wgs = (long)a.wgs * a.H;
+  if (wgs * 256 > 0xffffffffL || a.sets > MOST || (a.wide != 0 && a.wide != wide_cols(DT))) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)wgs), wg(256);
+  if (a.wide) hipExtLaunchKernelGGL((k_cache8_attend<DT, D, MOST, true>), grid, wg, 0, s, e0, e1, 0, a);
+  else if (a.sets == 1) hipExtLaunchKernelGGL((k_cache8_attend<DT, D, 1, false>), grid, wg, 0, s, e0, e1, 0, a);
+  else if constexpr (MOST > 1) hipExtLaunchKernelGGL((k_cache8_attend<DT, D, 2, false>), grid, wg, 0, s, e0, e1, 0, a);
   return hipGetLastError();
 }
 template <int DT, int D>
@@ -690,7 +769,7 @@ static bool attend_ok(const Attend8Args& a) {
          (a.NG == 0 || (a.npblk >= 1 && a.pstride >= 1)) && (a.sets == 1 || a.sets == 2);
 }
 static bool parts_ok(const Attend8Args& a) {
-  return attend_ok(a) && a.runs >= 1 && a.max_entries >= 1 && a.plan && a.o_part && a.lse_part && a.slots >= 1;
+  return attend_ok(a) && a.wgs >= 2 && a.max_entries >= 1 && a.plan && a.o_part && a.lse_part && a.slots >= 1;
 }
 hipError_t launch_attend8(const Attend8Args& a, int dtype, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
   if (!parts_ok(a)) return hipErrorInvalidValue;

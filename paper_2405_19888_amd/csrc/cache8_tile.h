@@ -73,6 +73,14 @@ struct Range8 {
   int plain;                             // keys before it are seen by every column
 };
 
+// A wave-uniform value in scalar registers of its own.  Kernel arguments come sixteen registers a
+// load, and a loop that uses one of them keeps (or spills, lane by lane) all sixteen.
+template <class V>
+PARROT_DEV V alone(V v) {
+  asm("" : "+s"(v));
+  return v;
+}
+
 PARROT_DEV float max3(float a, float b, float c) {
   float r;
   asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
@@ -95,7 +103,7 @@ struct Tile8 {
   int lim[NS];                                        // keys the lane's column sees
   int vexp;                                           // float16: o is in units of 2^(vexp - 127)
 
-  PARROT_DEV Tile8(int heads, int head) : lane(threadIdx.x & 63), h(head), H(heads) {
+  PARROT_DEV Tile8(int heads, int head) : lane(threadIdx.x & 63), h(head), H(alone(heads)) {
 #pragma unroll
     for (int c = 0; c < NS; ++c) {
       mref[c] = kNoKey; lt[c] = 0.f; lw[c] = 0.f; lim[c] = 0;
@@ -220,6 +228,89 @@ struct Tile8 {
     }
   }
 
+  // The same range for four waves of a workgroup, each with columns of its own: the keys' and
+  // values' bytes come into a ring in LDS, three units ahead, once for all of them (a wave alone reads
+  // them again from the L2, one unit ahead, for its columns).  `keys`: the wave's columns see no further; below 1:
+  // it has no columns and loads for the others.  Rows of keys are swizzled, granule j of 16 bytes
+  // of row r at j ^ f(r), on the global side of the loads, so that the 16 rows of a read lie in
+  // different banks.
+  static constexpr int RING = 4;                      // units
+  static constexpr int UNIT_B = 4 * BLK_B;
+  PARROT_DEV void run_shared(const Range8& rg, float scale_log2, char* ring, int keys) {
+    constexpr int PER_WAVE = X;                       // loads of a wave and unit
+    const int g = lane >> 4, r = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int last = max((rg.end - 1) / kBlockTokens, 0);
+    const int blk = X == 2 ? wave >> 1 : wave & 1;    // the block of a unit that the wave loads from
+    const unsigned ksrc = X == 2 ? (lane >> 3) * 128 + (((lane & 7) ^ (lane >> 3)) << 4)
+                                 : (lane >> 2) * 64 + (((lane & 3) ^ (lane >> 4 & 3)) << 4);
+    const unsigned vsrc = lane * 16;
+    const unsigned f = X == 2 ? r & 7 : r >> 2 & 3;
+    const unsigned to = lds_addr(ring) + wave * 1024;
+    auto id_of = [&](int u, int b) {                  // (past the end: the last block)
+      return (int)min((unsigned)ld_uniform(rg.tbl + min(2 * u + b, last)), (unsigned)(rg.npool - 1));
+    };
+    auto issue = [&](int id, unsigned buf) {
+      const size_t off = ((size_t)id * H + h) * BLK_B;
+      if constexpr (X == 2) {
+        const size_t half = off + (wave & 1) * 1024;
+        lds_dma16_sbase((const char*)rg.pool.k + half, ksrc, to + buf);
+        lds_dma16_sbase((const char*)rg.pool.v + half, vsrc, to + buf + 2 * BLK_B);
+      } else {
+        lds_dma16_sbase((const char*)(wave < 2 ? rg.pool.k : rg.pool.v) + off, wave < 2 ? ksrc : vsrc, to + buf);
+      }
+    };
+    auto scale_of = [&](int id) {
+      const size_t bh = (size_t)id * H + h;
+      const unsigned word = (unsigned)ld_uniform((const int*)((const char*)rg.pool.scales + ((bh * 2) & ~(size_t)3)));
+      return (bh & 1 ? word >> 16 : word) & 0xFFFFu;
+    };
+    wait_vmcnt<0>();                                  // (queries)
+    lds_sync();                                       // the ring of the range before has been read
+#pragma unroll
+    for (int i = 0; i < RING - 1; ++i) issue(id_of(min(rg.u0 + i, rg.u1 - 1), blk), i * UNIT_B);
+    int next_id = id_of(min(rg.u0 + RING - 1, rg.u1 - 1), blk);
+    unsigned sc[2] = {scale_of(id_of(rg.u0, 0)), scale_of(id_of(rg.u0, 1))};
+    int id1[2] = {id_of(rg.u0 + 1, 0), id_of(rg.u0 + 1, 1)};
+    unsigned buf = 0;
+    u32x4 kr[2][X], vr[2][X];
+    auto keys_at = [&](unsigned at) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int x = 0; x < X; ++x)
+          kr[b][x] = *reinterpret_cast<const u32x4*>(ring + at + b * BLK_B + r * D + (((x * 4 + g) ^ f) << 4));
+    };
+    wait_vmcnt<(RING - 2) * PER_WAVE>();
+    lds_sync();
+    keys_at(0);
+#pragma unroll 1
+    for (int u = rg.u0; u < rg.u1; ++u) {
+      wait_vmcnt<(RING - 3) * PER_WAVE>();            // the next unit's loads are the oldest
+      lds_sync();                                     // ... of every wave, and the last unit has been read
+      issue(next_id, (buf + (RING - 1) * UNIT_B) % (RING * UNIT_B));
+      next_id = id_of(min(u + RING, rg.u1 - 1), blk);
+      const unsigned ahead[2] = {scale_of(id1[0]), scale_of(id1[1])};
+      id1[0] = id_of(u + 2, 0);
+      id1[1] = id_of(u + 2, 1);
+      const unsigned after = (buf + UNIT_B) % (RING * UNIT_B);
+      if (u * kUnit < keys) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int x = 0; x < X; ++x) vr[b][x] = *reinterpret_cast<const u32x4*>(ring + buf + (2 + b) * BLK_B + x * 1024 + lane * 16);
+        unit(rg, u * kUnit, kr, vr, sc, scale_log2, [&] {
+          __builtin_amdgcn_sched_barrier(0);
+          keys_at(after);
+        });
+      }
+      sc[0] = ahead[0];
+      sc[1] = ahead[1];
+      buf = after;
+    }
+    wait_vmcnt<0>();                                  // the last unit's loads, repeated by the last rounds
+  }
+
   // Output of column c and its log-sum-exp: f(c, column, factor of o, log2 of the sum, rounded sum).
   template <class F>
   PARROT_DEV void finish(F f) {
@@ -247,6 +338,7 @@ struct Tile8 {
     f32x4 s[NS][2];
 #pragma unroll
     for (int c = 0; c < NS; ++c) s[c][0] = s[c][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int st = 0; st < 2 * X; ++st)
 #pragma unroll
@@ -258,6 +350,7 @@ struct Tile8 {
 #pragma unroll
           for (int p = PARTS - 1; p >= 0; --p) s[c][b] = W::mma(kf, qf[c][p][st], s[c][b]);
       }
+    __builtin_amdgcn_s_setprio(0);
     keys_read();
     const bool masked = tok0 + kUnit > rg.plain;
     bool bad = false;                                  // a value that some columns see is no number
@@ -365,6 +458,7 @@ struct Tile8 {
       }
     }
     if (bad) mark_bad(v, x_seen(tok0));
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int x = 0; x < X; ++x)
 #pragma unroll
@@ -377,6 +471,7 @@ struct Tile8 {
           for (int p = PARTS - 1; p >= 0; --p)
             o[c][4 * x + dd] = W::mma(vf, u32x4{pw[c][p][0], pw[c][p][1], pw[c][p][2], pw[c][p][3]}, o[c][4 * x + dd]);
       }
+    __builtin_amdgcn_s_setprio(0);
   }
 
   // 1 where the lane's column sees the token of its P operand, as that operand.
@@ -414,8 +509,8 @@ struct Tile8 {
         for (int c = 0; c < NS; ++c) {
           const f32x4 n = W::mma(one, seen.w[c], f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (n[i] > 0.f) o[c][4 * x + dd][i] = __builtin_nanf("");
+          for (int i = 0; i < 4; ++i)                  // (n counts: all bits set where it is not 0)
+            o[c][4 * x + dd][i] = __int_as_float(__float_as_int(o[c][4 * x + dd][i]) | ((0 - __float_as_int(n[i])) >> 31));
         }
       }
   }
