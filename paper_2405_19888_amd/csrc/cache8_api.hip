@@ -125,7 +125,7 @@ parrot_status check_attend(const parrot_problem* p, const parrot_tree_rows* rows
   if (pl->sets > 1) spread = std::max(spread, 4 * wgs_of(2, false) * 32);
   if (pl->wide) spread = std::max(spread, std::max(4L * pl->wgs * pl->cols, (long)pl->wgs * pl->wide));
   pl->slots = (1 + pl->depth) * T * G + spread;
-  const double ints = (double)tiles * (1 + parrot::kEntryInts) + (double)T * (1 + parrot::kRowInts + pl->depth) + 4.0 * wgs_of(1, false) +
+  const double ints = (double)tiles * (1 + parrot::kEntryInts) + (double)T * (parrot::kRowInts + pl->depth) + 4.0 * wgs_of(1, false) +
                       (NG + R) * (2.0 + parrot::kMaxDepth + parrot::kReqInts) + (parrot::kPlanWaves + 1.0) * NG;
   if (((1.0 + pl->depth) * T * G / pl->cols + R + NG) * (units + parrot::kPieceSetup) > 1.5e9 || pl->slots > 0x7fffffffL || ints > 1.0e9 ||
       R + NG > 0x3fffffffL || pl->wgs * H * 256 > 0xffffffffL)
@@ -138,7 +138,6 @@ parrot_status check_attend(const parrot_problem* p, const parrot_tree_rows* rows
   at.entry = take(tiles * parrot::kEntryInts);
   at.run = take(4 * wgs_of(1, false));
   at.row = take(T * parrot::kRowInts);
-  at.join = take(T);
   at.list = take(T * std::max(pl->depth, 1));
   at.seq = take(2 * (NG + R) + 1);
   at.req = take(R * parrot::kReqInts);
@@ -265,7 +264,7 @@ parrot_status parrot_cache8_plan(
   a.wide_cols = parrot::wide_cols((int)p->dtype);
   a.wide_from = pl.wide ? parrot::wide_from((int)p->dtype) : 0x7fffffff;
   a.wgs = pl.wgs; a.min_run = pl.min_run;
-  a.max_entries = pl.max_entries; a.max_slots = pl.slots;
+  a.max_entries = pl.max_entries;
   return launched(parrot::launch_plan8(a, reinterpret_cast<hipStream_t>(stream)), "plan kernel");
 }
 

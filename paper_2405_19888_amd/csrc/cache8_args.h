@@ -31,7 +31,7 @@ hipError_t launch_fill8(const Fill8Args& a, int partner, int dtype, int D, hipSt
 // request with a wide tile's columns of its own goes through its group chain by itself, in one
 // piece with its own tokens, and is no reader of the groups.
 struct Plan8Layout {
-  long cost, entry, run, row, join, list, seq, req, pos, count, total;
+  long cost, entry, run, row, list, seq, req, pos, count, total;
 };
 constexpr int kPlanHead = 16;            // ints of the head, see Head8
 constexpr int kEntryInts = 12;
@@ -40,9 +40,12 @@ constexpr int kReqInts = 12;
 constexpr int kPlanWaves = 16;           // waves of the planning workgroup
 constexpr int kPieceSetup = 2;           // cost of a tile beside its units
 
-// Columns of a wide tile, and of a sequence from which on it has them (more than half full).
+// Columns of a wide tile, and columns above which a sequence has wide tiles: what one narrow tile
+// holds.  bfloat16, 8 cache heads of 128 elements, four query heads on each, us a layer with wide tiles and
+// with several narrow ones: four prompts of 400 rows on 8000 tokens 314 and 448, 64 requests of ten rows on
+// 3000 137 and 173, ten rows on one prefix of 16000 34 and 38; 400 rows on 1000 in float32 109 and 197.
 constexpr int wide_cols(int dtype) { return dtype == kF32 ? 64 : 128; }
-constexpr int wide_from(int dtype) { return wide_cols(dtype) / 2; }
+constexpr int wide_from(int dtype) { return wide_cols(dtype) / 4; }
 
 // The head: entries, wide ones among them, rows to join, cost of the wide entries, cost of all, a
 // cache head's workgroups of the wide role, run lengths of wide and narrow roles.
@@ -52,9 +55,10 @@ enum Head8 { kHeadEntries, kHeadWide, kHeadJoins, kHeadWideCost, kHeadCost, kHea
 // group: its prefix's), keys that every column sees, first row (group: first place in the row
 // list), whether the chain's prefixes come first.
 enum Entry8 { kEntSeq, kEntCol0, kEntCols, kEntCost, kEntUnits, kEntSlot, kEntPieces, kEntKeys, kEntBase, kEntFirst, kEntChained };
-// A row: entry of its request's first tile, its place in the request, levels of prefixes, then
-// for each level the entry of the group's first tile and the row's place in the group's list.
-enum Row8 { kRowEntry, kRowPlace, kRowLevels, kRowUnused, kRowGroup };
+// A row that is joined, in no order: its token, entry of its request's first tile, its place in the
+// request, levels of prefixes, then for each level the entry of the group's first tile and the row's
+// place in the group's list.
+enum Row8 { kRowToken, kRowEntry, kRowPlace, kRowLevels, kRowGroup };
 // A request: first row, rows, own tokens, its group where it reads groups' results (-1), then
 // its chain's groups and their tokens, innermost first.
 enum Req8 { kReqFirst, kReqCount, kReqKeys, kReqReads, kReqChain };
@@ -71,7 +75,7 @@ struct Plan8Args {
   int cols;                              // columns of a narrow tile
   int wide_cols, wide_from;              // of a wide tile; columns above which a sequence has wide ones
   int wgs, min_run;                      // workgroups of a cache head; cost of a run at least
-  int max_entries; long max_slots;
+  int max_entries;
 };
 hipError_t launch_plan8(const Plan8Args& a, hipStream_t s);
 

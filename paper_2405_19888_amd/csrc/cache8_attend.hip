@@ -109,7 +109,6 @@ __global__ __launch_bounds__(1024) void k_cache8_plan(Plan8Args a) {
   int* ent = a.plan + a.at.entry;
   int* rows = a.plan + a.at.row;
   int* list = a.plan + a.at.list;
-  int* joins = a.plan + a.at.join;
   int* pos = a.plan + a.at.pos;
   const int nseq = st.NG + st.R;
   int* const g_req = a.plan + a.at.req;
@@ -318,6 +317,7 @@ __global__ __launch_bounds__(1024) void k_cache8_plan(Plan8Args a) {
     int v[kRowInts] = {};
     const bool w = (long)o[kReqCount] * st.G > a.wide_from;
     const int first = w ? seq[st.NG + lo] : wide + seqn[st.NG + lo], cols = w ? a.wide_cols : a.cols;
+    v[kRowToken] = t;
     v[kRowEntry] = first;
     v[kRowPlace] = j;
     if (o[kReqReads] >= 0)
@@ -334,16 +334,16 @@ __global__ __launch_bounds__(1024) void k_cache8_plan(Plan8Args a) {
           list[min((long)off[grp] + at, (long)st.T * st.depth - 1)] = t;
         }
       }
-    int4* d = reinterpret_cast<int4*>(rows + (long)t * kRowInts);
-    d[0] = int4{v[0], v[1], v[2], v[3]};
-    d[1] = int4{v[4], v[5], v[6], v[7]};
-    d[2] = int4{v[8], v[9], v[10], v[11]};
     // (the row's columns are in one or more of its request's tiles)
     bool parts = false;
     for (int e = first + (int)((long)j * st.G / cols); e <= first + (int)(((long)j * st.G + st.G - 1) / cols) && e < entries; ++e)
       parts = parts || e_slot[(long)e * e_step] >= 0;
-    // (their order is of no matter: each row is joined by itself)
-    if (parts) joins[min(atomicAdd(&lds[kPlanWaves], 1), st.T - 1)] = t;
+    if (parts) {                                        // (their order is of no matter: each is joined by itself)
+      int4* d = reinterpret_cast<int4*>(rows + (long)min(atomicAdd(&lds[kPlanWaves], 1), st.T - 1) * kRowInts);
+      d[0] = int4{v[0], v[1], v[2], v[3]};
+      d[1] = int4{v[4], v[5], v[6], v[7]};
+      d[2] = int4{v[8], v[9], v[10], v[11]};
+    }
   }
   __syncthreads();
   if (tid == 0) {
@@ -632,33 +632,44 @@ __global__ __launch_bounds__(256) void k_cache8_join(Attend8Args a) {
   const int i0 = threadIdx.x % GW, sub = threadIdx.x / GW, mine = sub % HEADS, grp = sub / HEADS;
   const long work = (long)clampi(ld_uniform(a.plan + kHeadJoins), 0, a.T) * parts;
   for (long w = blockIdx.x; w < work; w += gridDim.x) {
-    const int t = clampi(ld_uniform(a.plan + a.at.join + (int)(w / parts)), 0, a.T - 1);
+    const int* d = a.plan + a.at.row + (w / parts) * kRowInts;
+    const int t = clampi(ld_uniform(d + kRowToken), 0, a.T - 1);
     const int hq = (int)(w % parts) * HEADS + mine;
     const bool live = hq < HQ;
     const int h = min(hq, HQ - 1) / a.G, gq = min(hq, HQ - 1) % a.G;
-    const int* d = a.plan + a.at.row + (long)t * kRowInts;
     const int levels = clampi(ld_uniform(d + kRowLevels), 0, kMaxDepth);
+    // own tokens, then the chain's prefixes: slots, columns, pieces and the row's column of each
+    int slot[1 + kMaxDepth], nc[1 + kMaxDepth], n[1 + kMaxDepth], col[1 + kMaxDepth];
+#pragma unroll
+    for (int s = 0; s <= kMaxDepth; ++s) {
+      n[s] = 0;
+      if (s <= levels) {
+        const int x = ld_uniform(d + (s ? kRowGroup + 2 * s - 1 : (int)kRowPlace)) * a.G + gq;
+        const int e0 = ld_uniform(d + (s ? kRowGroup + 2 * s - 2 : (int)kRowEntry));
+        const int cols = e0 < wide ? max(a.wide, 1) : 16 * a.sets;
+        const int* v = a.plan + a.at.entry + (long)clampi(e0 + x / cols, 0, a.max_entries - 1) * kEntryInts;
+        slot[s] = v[kEntSlot];
+        nc[s] = v[kEntCols];
+        n[s] = min(v[kEntPieces], 4 * a.wgs);           // (a piece per run at most)
+        col[s] = x % cols;
+      }
+    }
+    const bool direct = slot[0] < 0;                    // the piece wrote the output
     float m = -INFINITY, l = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    bool direct = false;
+#pragma unroll
+    for (int s = 0; s <= kMaxDepth; ++s) {
+      if (s > levels) break;
+      const int pieces = direct ? 0 : n[s];
 #pragma unroll 1
-    for (int s = -1; s < levels; ++s) {                 // own tokens, then the chain's prefixes
-      const int x = (s < 0 ? ld_uniform(d + kRowPlace) : ld_uniform(d + kRowGroup + 2 * s + 1)) * a.G + gq;
-      const int e0 = s < 0 ? ld_uniform(d + kRowEntry) : ld_uniform(d + kRowGroup + 2 * s);
-      const int cols = e0 < wide ? max(a.wide, 1) : 16 * a.sets, e = e0 + x / cols;
-      const int* v = a.plan + a.at.entry + (long)clampi(e, 0, a.max_entries - 1) * kEntryInts;
-      const int slot = v[kEntSlot], nc = v[kEntCols], n = min(v[kEntPieces], 4 * a.wgs);   // (a piece per run at most)
-      if (s < 0 && slot < 0) { direct = true; break; }  // the piece wrote the output
-      const int col = x % cols;
-#pragma unroll 1
-      for (int i = grp; i < n; i += 4 * GROUPS) {
+      for (int i = grp; i < pieces; i += 4 * GROUPS) {
         float lp[4];
         f32x4 op[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           const int k = i + u * GROUPS;
-          const long at = slot + (long)k * nc + col;
-          const bool on = k < n && at >= 0 && at < a.slots;
+          const long at = slot[s] + (long)k * nc[s] + col[s];
+          const bool on = k < pieces && at >= 0 && at < a.slots;
           const long sl = (long)h * a.slots + (on ? at : 0);
           lp[u] = -INFINITY;
           if (on) {

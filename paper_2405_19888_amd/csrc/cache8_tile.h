@@ -91,7 +91,8 @@ template <int DT, int D, int NS>
 struct Tile8 {
   using W = Wide8<DT>;
   static constexpr int X = D / 64;                    // 16-byte loads of each tensor, per block and lane
-  static constexpr int NU = 2 / X;                    // units on their way: 8 KiB
+  // (units on their way: 8 KiB; 16 KiB changes nothing, 64 requests on 3000 tokens 72 us both ways)
+  static constexpr int NU = 2 / X;
   static constexpr int PARTS = DT == kF32 ? 3 : 1;
   static constexpr int BLK_B = kBlockTokens * D;
   static constexpr float kNoKey = -3.0e38f;           // a reference that every finite logit moves
