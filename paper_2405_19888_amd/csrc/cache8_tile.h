@@ -8,11 +8,17 @@
 // Widening is exact (a code has four significant bits), so the operands are the values the
 // cache stands for; the only roundings are those of P and of the fp32 sums.
 //
-// No LDS and no lane exchange: a lane's S^T values (tokens 4 g .. 4 g + 3 of a block for
+// No lane exchange: a lane's S^T values (tokens 4 g .. 4 g + 3 of a block for
 // g = lane / 16, column lane % 16) are the PV operand's k group g, and the layout of the
-// values holds the same four tokens side by side (cache8_args.h).  So a wave needs nothing but
-// its own loads, 16 bytes a lane: 8 KiB on their way, the next keys as soon as the last ones
-// have been multiplied, the next values behind the last products.
+// values holds the same four tokens side by side (cache8_args.h).  A wave whose columns are all
+// that read its keys (run) needs nothing but its own loads, 16 bytes a lane: 8 KiB on their way, the
+// next keys as soon as the last ones have been multiplied, the next values behind the last
+// products.  Waves that share keys (run_shared) take them from a ring in LDS.
+//
+// Bounds: 16 columns read memory (64 requests on 3000 tokens, 393 MB in 64 us: 6.1 TB/s of the 7.1 that
+// plain reads reach).  More columns are bound by issue: of a unit's 1700 cycles for 32 columns of 128
+// elements, the matrix products are 670, widening 370, the exponentials and sums of 1024 weights 600
+// (measured by instruction; products and the rest overlap between two waves of a SIMD).
 //
 // Types: bfloat16 and float16 round P once, and the output is divided by the sum of the rounded
 // weights (a dominant weight's rounding cancels).  float32 queries and weights are cut into
@@ -331,7 +337,8 @@ struct Tile8 {
   }
 
  private:
-  // keys_read(): the unit's keys have been read.
+  // keys_read(): the unit's keys have been read.  The products go ahead of the other wave's softmax
+  // (four prompts of 400 rows on 8000 tokens 314 us a layer, 341 without).
   template <class F>
   PARROT_DEV void unit(const Range8& rg, int tok0, u32x4 (&k)[2][X], u32x4 (&v)[2][X], unsigned (&sc)[2], float scale_log2,
                        F keys_read) {
@@ -398,36 +405,41 @@ struct Tile8 {
         rest[b] = rel < -15 ? ldexpf(1.f, max(rel + 15, -30)) : 1.f;
       }
     }
-    unsigned pw[NS][PARTS][4];
+    float w[NS][8], mx[NS];
+    bool raise = false;
 #pragma unroll
     for (int c = 0; c < NS; ++c) {
-      float x[8];
-      float mx;
       if (masked) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          x[i] = tok0 + 16 * (i >> 2) + 4 * g + (i & 3) < lim[c] ? s[c][i >> 2][i & 3] * cb[i >> 2] : -INFINITY;
-        mx = max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), fmaxf(x[6], x[7]));
+          w[c][i] = tok0 + 16 * (i >> 2) + 4 * g + (i & 3) < lim[c] ? s[c][i >> 2][i & 3] * cb[i >> 2] : -INFINITY;
+        mx[c] = max3(max3(w[c][0], w[c][1], w[c][2]), max3(w[c][3], w[c][4], w[c][5]), fmaxf(w[c][6], w[c][7]));
       } else {                                         // (scales are not negative)
         const float m0 = max3(max3(s[c][0][0], s[c][0][1], s[c][0][2]), s[c][0][3], s[c][0][3]);
         const float m1 = max3(max3(s[c][1][0], s[c][1][1], s[c][1][2]), s[c][1][3], s[c][1][3]);
-        mx = fmaxf(m0 * cb[0], m1 * cb[1]);
+        mx[c] = fmaxf(m0 * cb[0], m1 * cb[1]);
       }
-      if (__ballot(mx > mref[c] + 8.f)) {
-        const float m = fmaxf(mref[c], max_xor32(max_xor16(mx)));
+      raise = raise || mx[c] > mref[c] + 8.f;
+    }
+    // (one branch for all sets: 64 requests of 16 rows on 3000 tokens 130 us, 137 with one for each)
+    if (__ballot(raise)) {
+#pragma unroll
+      for (int c = 0; c < NS; ++c) {
+        const float m = fmaxf(mref[c], max_xor32(max_xor16(mx[c])));
         const float f = fast_exp2(mref[c] - m);
         mref[c] = m;
         lt[c] *= f;
         lw[c] *= f;
         scale_outputs(f, c);
       }
-      if (masked) {
+    }
+    unsigned pw[NS][PARTS][4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = fast_exp2(x[i] - mref[c]);
-      } else {
+    for (int c = 0; c < NS; ++c) {
+      float (&x)[8] = w[c];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = fast_exp2(__builtin_fmaf(s[c][i >> 2][i & 3], cb[i >> 2], -mref[c]));
-      }
+      for (int i = 0; i < 8; ++i)
+        x[i] = fast_exp2(masked ? x[i] - mref[c] : __builtin_fmaf(s[c][i >> 2][i & 3], cb[i >> 2], -mref[c]));
 #pragma unroll
       for (int i = 0; i < 8; ++i) lt[c] += x[i];
 #pragma unroll
