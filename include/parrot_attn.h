@@ -714,8 +714,8 @@ parrot_status parrot_validate_cache8_inputs(
 
 /*
  * Copies cache blocks: block dst[i] of every pool becomes block src[i] of it, for
- * i < num_copies, in one launch (a fork's last block, blocks moved together; the lists come from
- * parrot_store_take_copies).  Any cache: a pool is an array of blocks of block_bytes bytes each.
+ * i < num_copies, in a launch for every 128 pools (a fork's last block, blocks moved together; the lists
+ * come from parrot_store_take_copies).  Any cache: a pool is an array of blocks of block_bytes bytes each.
  *   pools                (host) [num_pools]; base 16-byte aligned where block_bytes is a
  *                        multiple of 16, else 2-byte; block_bytes even
  *   num_blocks           blocks of every pool (of the smallest)

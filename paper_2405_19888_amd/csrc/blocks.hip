@@ -1,5 +1,5 @@
 // Copy of cache blocks: pool[dst[i]] = pool[src[i]] for every pool of a call (keys, values and
-// scales of all layers), in one launch.
+// scales of all layers), in a launch for every kCopyPools of them.
 //
 // Bound by memory: each byte is read and written once.  A workgroup copies 16 KiB of one block of
 // one pool, 16 bytes a lane and four loads in flight; a block smaller than that (scales) takes one

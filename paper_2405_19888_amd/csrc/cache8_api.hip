@@ -362,7 +362,7 @@ parrot_status parrot_copy_blocks(const parrot_block_pool* pools, int32_t num_poo
       return bad("block_bytes of pool %ld is not even and in [2, 2^31]", i);
     if (reinterpret_cast<uintptr_t>(x.base) % (x.block_bytes % 16 ? 2 : 16)) return bad("pool %ld is not aligned", i);
   }
-  // pools whose blocks have one size go together
+  // (a launch's arguments hold kCopyPools pools)
   int32_t done = 0;
   while (done < num_pools) {
     parrot::CopyArgs a{};
