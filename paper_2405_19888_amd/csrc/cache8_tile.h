@@ -3,7 +3,7 @@
 // A column is a (row, query head) pair that reads the wave's cache head.  Per unit of 32
 // tokens (two blocks), with c_b the block's key scale times sm_scale log2(e):
 //   S^T = K Q^T        (tokens x columns) on the matrix cores, codes widened to the queries' type
-//   p   = 2^(c_b s - m), m a reference no more than 8 below the column's largest logit
+//   p   = 2^(c_b s - m), m a reference no more than 11 below the column's largest logit
 //   O^T += V^T P       (elements x columns), values widened and scaled by their block's 2^e
 // Widening is exact (a code has four significant bits), so the operands are the values the
 // cache stands for; the only roundings are those of P and of the fp32 sums.
@@ -87,12 +87,6 @@ PARROT_DEV V alone(V v) {
   return v;
 }
 
-PARROT_DEV float max3(float a, float b, float c) {
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
-}
-
 template <int DT, int D, int NS>
 struct Tile8 {
   using W = Wide8<DT>;
@@ -101,6 +95,7 @@ struct Tile8 {
   static constexpr int NU = 2 / X;
   static constexpr int PARTS = DT == kF32 ? 3 : 1;
   static constexpr int BLK_B = kBlockTokens * D;
+  static constexpr float kMostSum = 2048.f;           // of a lane's eight weights
   static constexpr float kNoKey = -3.0e38f;           // a reference that every finite logit moves
 
   int lane, h, H;
@@ -405,43 +400,54 @@ struct Tile8 {
         rest[b] = rel < -15 ? ldexpf(1.f, max(rel + 15, -30)) : 1.f;
       }
     }
-    float w[NS][8], mx[NS];
+    // weights against the references at hand; their sums tell where one is more than 2^8 (a first
+    // key's is infinite), and no maximum is taken until then.  A column's reference is raised by its own
+    // sums alone, so that no row's bits depend on another row.
+    float w[NS][8], sum[NS];
     bool raise = false;
 #pragma unroll
     for (int c = 0; c < NS; ++c) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[c][i] = __builtin_fmaf(s[c][i >> 2][i & 3], cb[i >> 2], -mref[c]);
       if (masked) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          w[c][i] = tok0 + 16 * (i >> 2) + 4 * g + (i & 3) < lim[c] ? s[c][i >> 2][i & 3] * cb[i >> 2] : -INFINITY;
-        mx[c] = max3(max3(w[c][0], w[c][1], w[c][2]), max3(w[c][3], w[c][4], w[c][5]), fmaxf(w[c][6], w[c][7]));
-      } else {                                         // (scales are not negative)
-        const float m0 = max3(max3(s[c][0][0], s[c][0][1], s[c][0][2]), s[c][0][3], s[c][0][3]);
-        const float m1 = max3(max3(s[c][1][0], s[c][1][1], s[c][1][2]), s[c][1][3], s[c][1][3]);
-        mx[c] = fmaxf(m0 * cb[0], m1 * cb[1]);
+          w[c][i] = tok0 + 16 * (i >> 2) + 4 * g + (i & 3) < lim[c] ? w[c][i] : -INFINITY;
       }
-      raise = raise || mx[c] > mref[c] + 8.f;
+      sum[c] = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum[c] += w[c][i] = fast_exp2(w[c][i]);
+      raise = raise || sum[c] > kMostSum;
     }
     // (one branch for all sets: 64 requests of 16 rows on 3000 tokens 130 us, 137 with one for each)
     if (__ballot(raise)) {
+      const int tok1 = alone(tok0);                    // (or the masks above are kept in scalar registers)
 #pragma unroll
       for (int c = 0; c < NS; ++c) {
-        const float m = fmaxf(mref[c], max_xor32(max_xor16(mx[c])));
+        float mx = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          mx = fmaxf(mx, !masked || tok1 + 16 * (i >> 2) + 4 * g + (i & 3) < lim[c] ? s[c][i >> 2][i & 3] * cb[i >> 2] : -INFINITY);
+        const float m = max_xor32(max_xor16(sum[c])) > kMostSum ? fmaxf(mref[c], max_xor32(max_xor16(mx))) : mref[c];
         const float f = fast_exp2(mref[c] - m);
         mref[c] = m;
         lt[c] *= f;
         lw[c] *= f;
         scale_outputs(f, c);
+        sum[c] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float y = __builtin_fmaf(s[c][i >> 2][i & 3], cb[i >> 2], -m);
+          w[c][i] = fast_exp2(!masked || tok1 + 16 * (i >> 2) + 4 * g + (i & 3) < lim[c] ? y : -INFINITY);
+          sum[c] += w[c][i];
+        }
       }
     }
     unsigned pw[NS][PARTS][4];
 #pragma unroll
     for (int c = 0; c < NS; ++c) {
-      float (&x)[8] = w[c];
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        x[i] = fast_exp2(masked ? x[i] - mref[c] : __builtin_fmaf(s[c][i >> 2][i & 3], cb[i >> 2], -mref[c]));
-#pragma unroll
-      for (int i = 0; i < 8; ++i) lt[c] += x[i];
+      const float (&x)[8] = w[c];
+      lt[c] += sum[c];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if constexpr (DT == kF32) {

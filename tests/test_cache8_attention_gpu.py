@@ -191,6 +191,25 @@ def test_queries_that_are_no_numbers():
     assert torch.isnan(out[hit]).all() and torch.equal(out[~hit], clean[~hit])
 
 
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16", "float32"])
+@pytest.mark.parametrize("rows", [2, 9])
+def test_rows_depend_on_themselves_alone(dtype, rows):
+    """A row whose logits are many times larger moves no bit of the rows beside it."""
+    plan, batch, off = batch_of((dtype, 2, 4, 128, [0, -1, 0], [200], [300, 90, 17], [rows, rows, 1], None))
+    pools, dense = cu.pools_of(batch)
+    q = du.queries(2 * rows + 1, 8, 128, dtype)
+    clean, clean_lse, *_ = cu.run(plan, batch, pools, q, off)
+    clean, clean_lse = clean.clone(), clean_lse.clone()
+    for row, head in ((0, 1), (rows, 6), (2 * rows, 3)):
+        other = q.clone()
+        other[row, head] *= 40
+        out, lse, *_ = cu.run(plan, batch, pools, other, off)
+        rest = torch.ones(2 * rows + 1, 8, dtype=torch.bool, device="cuda")
+        rest[row, head] = False
+        assert torch.equal(out[rest], clean[rest]) and torch.equal(lse[rest], clean_lse[rest])
+        cu.check(plan, dense, other, off, out, lse, what=f"{dtype} {rows} rows, one large")
+
+
 def test_nothing_else_is_written():
     plan, batch, off = batch_of(("float16", 2, 2, 64, [0, -1], [70], [40, 9], [3, 2], None))
     pools, dense = cu.pools_of(batch)
