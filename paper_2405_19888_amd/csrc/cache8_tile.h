@@ -42,9 +42,6 @@ template <> struct Wide8<kF16> {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
   }
   PARROT_DEV static unsigned pack(float x, float y) { return __builtin_bit_cast(unsigned, f16x2{(_Float16)x, (_Float16)y}); }
-  PARROT_DEV static float add(unsigned p, float acc) {
-    return __builtin_amdgcn_fdot2(as_f16x2(p), f16x2{(_Float16)1.f, (_Float16)1.f}, acc, false);
-  }
 };
 struct WideBf16 {
   typedef bf16x8 v8;
@@ -56,9 +53,6 @@ struct WideBf16 {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
   }
   PARROT_DEV static unsigned pack(float x, float y) { return __builtin_bit_cast(unsigned, bf16x2{(__bf16)x, (__bf16)y}); }
-  PARROT_DEV static float add(unsigned p, float acc) {
-    return __builtin_amdgcn_fdot2_f32_bf16(as_bf16x2(p), bf16x2{(__bf16)1.f, (__bf16)1.f}, acc, false);
-  }
 };
 template <> struct Wide8<kBF16> : WideBf16 {};
 template <> struct Wide8<kF32> : WideBf16 {};
@@ -101,14 +95,15 @@ struct Tile8 {
   int lane, h, H;
   u32x4 qf[NS][PARTS][2 * X];
   f32x4 o[NS][4 * X];
-  float mref[NS], lt[NS], lw[NS];
+  float mref[NS], lt[NS];
+  f32x4 lw[NS];                                       // the rounded weights' sum, four times
   int lim[NS];                                        // keys the lane's column sees
   int vexp;                                           // float16: o is in units of 2^(vexp - 127)
 
   PARROT_DEV Tile8(int heads, int head) : lane(threadIdx.x & 63), h(head), H(alone(heads)) {
 #pragma unroll
     for (int c = 0; c < NS; ++c) {
-      mref[c] = kNoKey; lt[c] = 0.f; lw[c] = 0.f; lim[c] = 0;
+      mref[c] = kNoKey; lt[c] = 0.f; lw[c] = f32x4{0.f, 0.f, 0.f, 0.f}; lim[c] = 0;
 #pragma unroll
       for (int t = 0; t < 4 * X; ++t) o[c][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -320,7 +315,7 @@ struct Tile8 {
     for (int c = 0; c < NS; ++c) {
       const float t = sum_xor32(sum_xor16(lt[c]));
       float w = t;
-      if constexpr (DT != kF32) w = sum_xor32(sum_xor16(lw[c]));
+      if constexpr (DT != kF32) w = lw[c][0];
       float inv = w == 0.f ? 0.f : 1.f / w;
       if constexpr (DT == kF16) inv *= vexp > 0 ? __uint_as_float((unsigned)vexp << 23) : 1.f;
       f(c, column(c), inv, t == 0.f ? -INFINITY : mref[c] + fast_log2(t));
@@ -419,7 +414,7 @@ struct Tile8 {
       for (int i = 0; i < 8; ++i) sum[c] += w[c][i] = fast_exp2(w[c][i]);
       raise = raise || sum[c] > kMostSum;
     }
-    // (one branch for all sets: 64 requests of 16 rows on 3000 tokens 130 us, 137 with one for each)
+    // (one branch for all sets: 64 requests of 16 rows on 3000 tokens 130 us a layer, 137 with one for each)
     if (__ballot(raise)) {
       const int tok1 = alone(tok0);                    // (or the masks above are kept in scalar registers)
 #pragma unroll
@@ -443,6 +438,8 @@ struct Tile8 {
         }
       }
     }
+    const unsigned two = W::pack(1.f, 1.f);
+    const u32x4 ones = {two, two, two, two};
     unsigned pw[NS][PARTS][4];
 #pragma unroll
     for (int c = 0; c < NS; ++c) {
@@ -460,9 +457,10 @@ struct Tile8 {
           }
         } else {
           pw[c][0][i] = W::pack(x[2 * i], x[2 * i + 1]);
-          lw[c] = W::add(pw[c][0][i], lw[c]);
         }
       }
+      // (the matrix cores have time for the sum: as dot products 64 requests of 16 rows take 129 us a layer, 113 so)
+      if constexpr (DT != kF32) lw[c] = W::mma(ones, u32x4{pw[c][0][0], pw[c][0][1], pw[c][0][2], pw[c][0][3]}, lw[c]);
       if constexpr (DT == kF16) {
 #pragma unroll
         for (int b = 0; b < 2; ++b)
