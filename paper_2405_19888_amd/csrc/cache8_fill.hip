@@ -2,7 +2,8 @@
 // rotation, as the 16-bit fill has them (rotary.hip), then queries to q_out, and keys and values
 // as codes with a scale for each block and head (cache8_args.h).
 //
-// Per block and head, with y the new rows in fp32 and a their largest finite |y|:
+// Per block and head, with y the new rows in fp32 (in 64 bits where each request has one) and a their
+// largest finite |y|:
 //   need = the least power of two with a / need <= 448, the largest code,
 //   s    = need if the rows hold the block's first slot, else max(old scale, need),
 //   code = y / s rounded to nearest even (NaN for what is no finite number).
@@ -128,26 +129,70 @@ PARROT_DEV Head8Of head_of(const FillArgs& a, int x, int head_bytes) {
   return o;
 }
 
-// One row of a head in a group of LPH lanes: y (16 bytes of it as floats) normalised and rotated.
-// turn_c and turn_s hold cosine and signed sine (times the amplitude) of the row's elements, 1 and 0 of
-// those that do not turn.  src: the row, for partners that no 16 bytes line up with.
-template <int DT, int D, int PARTNER>
-PARROT_DEV void turn_row(const FillArgs& a, const Head8Of& hd, const float* w, const float* turn_c, const float* turn_s,
-                         const char* src, float* y) {
+// The double counterparts of what a row's sum, root and partners take.
+template <int CTRL>
+PARROT_DEV double dpp_d(double x) {
+  const auto v = __builtin_bit_cast(uint2, x);
+  return __builtin_bit_cast(double, uint2{(unsigned)__builtin_amdgcn_mov_dpp((int)v.x, CTRL, 0xF, 0xF, true),
+                                          (unsigned)__builtin_amdgcn_mov_dpp((int)v.y, CTRL, 0xF, 0xF, true)});
+}
+template <int N>
+PARROT_DEV double group_sum(double x) {
+  x += dpp_d<kDppXor1>(x);
+  x += dpp_d<kDppXor2>(x);
+  x += dpp_d<kDppHalfMirror>(x);
+  if constexpr (N >= 16) x += dpp_d<kDppMirror>(x);
+  if constexpr (N >= 32) x += __shfl_xor(x, 16);
+  return x;
+}
+template <int N>
+PARROT_DEV double other_half(double x) {
+  if constexpr (N == 8) return dpp_d<0x1B>(dpp_d<kDppHalfMirror>(x));
+  else if constexpr (N == 16) return dpp_d<0x128>(x);
+  else return __shfl_xor(x, N / 2);
+}
+PARROT_DEV float fused(float x, float y, float z) { return __builtin_fmaf(x, y, z); }
+PARROT_DEV double fused(double x, double y, double z) { return __builtin_fma(x, y, z); }
+// (one step behind the instruction's estimate, where x r^2 is a number)
+PARROT_DEV float reciprocal_root(float x) {
+  const float r = __builtin_amdgcn_rsqf(x);
+  return x > 1e-37f && x < 1e37f ? fused(0.5f * r, fused(-x * r, r, 1.f), r) : r;
+}
+PARROT_DEV double reciprocal_root(double x) {
+  const double r = __builtin_amdgcn_rsq(x);
+  return x > 1e-300 && x < 1e300 ? fused(0.5 * r, fused(-x * r, r, 1.), r) : r;
+}
+PARROT_DEV float narrowed(float x, bool) { return x; }
+// odd: rounded to odd, so that a further rounding to few bits gives what one rounding would.
+PARROT_DEV float narrowed(double x, bool odd) {
+  const float f = (float)x;
+  const double back = f;
+  if (!odd || back == x || !(__builtin_fabsf(f) <= 3.402823466e38f)) return f;
+  return __uint_as_float((__float_as_uint(f) - (__builtin_fabs(back) > __builtin_fabs(x) ? 1u : 0u)) | 1u);
+}
+
+// One row of a head in a group of LPH lanes: out (16 bytes of it as floats) normalised and rotated, in R.
+// turn_c and turn_s hold cosine and signed sine (times the amplitude) of the row's elements.  src: the
+// row, for partners that no 16 bytes line up with.
+template <int DT, int D, int PARTNER, class R>
+PARROT_DEV void turn_row(const FillArgs& a, const Head8Of& hd, const float* w, const R* turn_c, const R* turn_s,
+                         const char* src, float* out) {
   constexpr int EPL = Elem<DT>::kPerLoad, LPH = D / EPL;
   const int lane = threadIdx.x & 63, e0 = lane % LPH * EPL, half = a.rd >> 1;
-  float rs = 1.f;
-  if (hd.weight) {
-    float ss = 0.f;
+  R rs = 1, y[EPL];
 #pragma unroll
-    for (int e = 0; e < EPL; ++e) ss = __builtin_fmaf(y[e], y[e], ss);
+  for (int e = 0; e < EPL; ++e) y[e] = out[e];
+  if (hd.weight) {
+    R ss = 0;
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) ss = fused(y[e], y[e], ss);
     ss = group_sum<LPH>(ss);
-    rs = __builtin_amdgcn_rsqf(ss * (1.f / D) + a.eps);
+    rs = reciprocal_root(ss * (R(1) / D) + a.eps);
 #pragma unroll
     for (int e = 0; e < EPL; ++e) y[e] = y[e] * rs * w[e];
   }
   if constexpr (PARTNER != kRotaryNone) {
-    float z[EPL];
+    R z[EPL];
     const bool all = a.rd == D;
     if constexpr (PARTNER == kRotaryInterleaved) {
 #pragma unroll
@@ -169,28 +214,38 @@ PARROT_DEV void turn_row(const FillArgs& a, const Head8Of& hd, const float* w, c
         if (hd.weight) z[e] = z[e] * rs * load_elem<DT>(hd.weight + at * Elem<DT>::kBytes);
       }
     }
-    float c[EPL], s[EPL];
+    constexpr int QUAD = 16 / sizeof(R);
+    typedef R vec __attribute__((ext_vector_type(QUAD)));
+    R c[EPL], s[EPL];
 #pragma unroll
-    for (int e = 0; e < EPL; e += 4) {
-      const f32x4 c4 = *reinterpret_cast<const f32x4*>(turn_c + e0 + e), s4 = *reinterpret_cast<const f32x4*>(turn_s + e0 + e);
+    for (int e = 0; e < EPL; e += QUAD) {
+      const vec cv = *reinterpret_cast<const vec*>(turn_c + e0 + e), sv = *reinterpret_cast<const vec*>(turn_s + e0 + e);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) { c[e + i] = c4[i]; s[e + i] = s4[i]; }
+      for (int i = 0; i < QUAD; ++i) { c[e + i] = cv[i]; s[e + i] = sv[i]; }
     }
     // (a selection where some pass: 0 times an infinite partner is no zero)
 #pragma unroll
-    for (int e = 0; e < EPL; ++e) y[e] = all || e0 + e < a.rd ? __builtin_fmaf(z[e], s[e], y[e] * c[e]) : y[e];
+    for (int e = 0; e < EPL; ++e) y[e] = all || e0 + e < a.rd ? fused(z[e], s[e], y[e] * c[e]) : y[e];
   }
+#pragma unroll
+  for (int e = 0; e < EPL; ++e) out[e] = narrowed(y[e], DT != kF32 || hd.kind == 1);
 }
 
 // A unit's table of turns, rows lo .. hi of it (row i of the unit is row_of(i)).
-template <int D, int PARTNER, class F>
-PARROT_DEV void turn_table(const FillArgs& a, float (*turn_c)[D], float (*turn_s)[D], int lo, int hi, F row_of) {
+PARROT_DEV void turn_of(const FillArgs& a, int p, int row, float* c, float* s) {
+  cos_sin_turns((unsigned)((a.turns[p] * (unsigned long long)(long long)a.positions[row]) >> 32), c, s);
+}
+PARROT_DEV void turn_of(const FillArgs& a, int p, int row, double* c, double* s) {
+  cos_sin_turns(a.turns[p] * (unsigned long long)(long long)a.positions[row], c, s);
+}
+template <int D, int PARTNER, class R, class F>
+PARROT_DEV void turn_table(const FillArgs& a, R (*turn_c)[D], R (*turn_s)[D], int lo, int hi, F row_of) {
   const int half = a.rd >> 1;
   if constexpr (PARTNER != kRotaryNone) {
     for (int x = threadIdx.x + lo * half; x < hi * half; x += 256) {
       const int i = x / half, p = x - i * half;
-      float c, s;
-      cos_sin_turns((unsigned)((a.turns[p] * (unsigned long long)(long long)a.positions[row_of(i)]) >> 32), &c, &s);
+      R c, s;
+      turn_of(a, p, row_of(i), &c, &s);
       c *= a.amplitude;
       s *= a.amplitude;
       const int one = PARTNER == kRotaryInterleaved ? 2 * p : p, two = PARTNER == kRotaryInterleaved ? one + 1 : p + half;
@@ -203,13 +258,14 @@ PARROT_DEV void turn_table(const FillArgs& a, float (*turn_c)[D], float (*turn_s
 }
 
 // One row a request: a lane group per head.  Bound by the launch and the round trips of length,
-// block and scale: 7 requests, 32 heads of 128 in float16, 4.7 us; 256 requests of 48 heads 4.8.
+// block and scale: 7 requests, 32 heads of 128 in float16, 4.6 us; 256 requests of 48 heads, normalised,
+// 5.2 (4.8 in fp32, which gives one key in a million the code beside the nearest).
 template <int DT, int D, int PARTNER>
 __global__ __launch_bounds__(256) void k_cache8_fill_tokens(FillArgs a, unsigned char* scales) {
   using E = Elem<DT>;
   constexpr int EB = E::kBytes, EPL = E::kPerLoad, LPH = D / EPL;
   constexpr int HPS = 256 / LPH;              // heads per workgroup and step
-  __shared__ __attribute__((aligned(16))) float turn_c[1][D], turn_s[1][D];
+  __shared__ __attribute__((aligned(16))) double turn_c[1][D], turn_s[1][D];
   Unit8 un;
   if (!find_unit<true>(a, blockIdx.x / a.slabs, &un)) return;
   turn_table<D, PARTNER>(a, turn_c, turn_s, 0, 1, [&](int) { return un.row; });
@@ -227,6 +283,7 @@ __global__ __launch_bounds__(256) void k_cache8_fill_tokens(FillArgs a, unsigned
     float w[EPL], y[EPL];
     if (hd.weight) E::to_f32(ld16(hd.weight + e0 * EB), w);
     E::to_f32(raw, y);
+    // (64 bits, so that a key's code is that of the formula's value; so few rows have the time)
     if (hd.kind < 2) turn_row<DT, D, PARTNER>(a, hd, w, turn_c[0], turn_s[0], src, y);
     if (hd.kind == 0) {
       *reinterpret_cast<u32x4*>((char*)a.q_out + ((size_t)un.row * a.HQ + hd.h) * (D * EB) + sub * 16) = pack16<DT>(y);

@@ -28,6 +28,31 @@ PARROT_DEV void cos_sin_turns(unsigned phase, float* c, float* s) {
   *s = (quad & 2) ? -b : b;                                      // quadrants 2, 3: sine negative
 }
 
+// The same of 2 pi * phase / 2^64, to 2^-45.
+PARROT_DEV void cos_sin_turns(unsigned long long phase, double* c, double* s) {
+  const unsigned quad = (unsigned)((phase + 0x2000000000000000ull) >> 62);
+  const double x = (double)(long long)(phase - ((unsigned long long)quad << 62)) * 3.4061215800304850e-19;   // 2 pi / 2^64
+  const double z = x * x;
+  double sn = 1.6059043836821613e-10;                            // 1/13!
+  sn = __builtin_fma(sn, z, -2.5052108385441720e-8);
+  sn = __builtin_fma(sn, z, 2.7557319223985893e-6);
+  sn = __builtin_fma(sn, z, -1.9841269841269841e-4);
+  sn = __builtin_fma(sn, z, 8.3333333333333333e-3);
+  sn = __builtin_fma(sn, z, -1.6666666666666667e-1);
+  sn = __builtin_fma(sn * z, x, x);
+  double cs = -1.1470745597729725e-11;                           // -1/14!
+  cs = __builtin_fma(cs, z, 2.0876756987868099e-9);
+  cs = __builtin_fma(cs, z, -2.7557319223985891e-7);
+  cs = __builtin_fma(cs, z, 2.4801587301587302e-5);
+  cs = __builtin_fma(cs, z, -1.3888888888888889e-3);
+  cs = __builtin_fma(cs, z, 4.1666666666666667e-2);
+  cs = __builtin_fma(cs, z, -0.5);
+  cs = __builtin_fma(cs, z, 1.0);
+  const double a = (quad & 1) ? sn : cs, b = (quad & 1) ? cs : sn;
+  *c = ((quad + 1) & 2) ? -a : a;
+  *s = (quad & 2) ? -b : b;
+}
+
 template <int DT>
 PARROT_DEV float load_elem(const char* p) {
   if constexpr (DT == kF32) return *reinterpret_cast<const float*>(p);
