@@ -137,6 +137,25 @@ def test_norm_and_rotation(rotary_dim, interleaved, dtype, single):
     assert (np.abs(f.q_out.double().cpu().numpy() - yq) <= tol).all()
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16", "float32"])
+def test_single_rows_have_the_formulas_codes(dtype, interleaved):
+    """Of 200000 keys, normalised and rotated, each has the code nearest to its value in 64 bits (in
+    fp32 about one in a million has the one beside it)."""
+    import paper_2405_19888_amd as parrot
+    cached = np.random.default_rng(7).integers(0, 40, 200).tolist()
+    plan, batch, off = setup(dtype, 8, 128, cached, [1] * 200)
+    k, v = du.queries(200, 8, 128, dtype, seed=1), du.queries(200, 8, 128, dtype, seed=2)
+    wk = 1 + 0.1 * du.queries(1, 1, 128, dtype, seed=9)[0, 0]
+    positions = np.array(cached) * 311
+    rotary = parrot.make_rotary(128, interleaved=interleaved)
+    pool = random_pool(plan, 5)
+    f, got, _ = fill(plan, off, pool, None, k, v, positions, rotary, k_norm=wk)
+    radians, amplitude = drafts_oracle.rotary_frequencies(128)
+    y, _ = drafts_oracle.rotate(k, positions, radians, interleaved, amplitude, wk, EPS)
+    same(got[0], oracle.fill(y, *pool[0], off, plan.suffix_tables, plan.suffix_lens), "keys")
+
+
 @pytest.mark.parametrize("dtype", ["float16", "bfloat16", "float32"])
 @pytest.mark.parametrize("rows", [1, 7])
 def test_values_at_the_borders(dtype, rows):
