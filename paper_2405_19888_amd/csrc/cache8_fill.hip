@@ -232,26 +232,20 @@ PARROT_DEV void turn_row(const FillArgs& a, const Head8Of& hd, const float* w, c
 }
 
 // A unit's table of turns, rows lo .. hi of it (row i of the unit is row_of(i)).
-PARROT_DEV void turn_of(const FillArgs& a, int p, int row, float* c, float* s) {
-  cos_sin_turns((unsigned)((a.turns[p] * (unsigned long long)(long long)a.positions[row]) >> 32), c, s);
-}
-PARROT_DEV void turn_of(const FillArgs& a, int p, int row, double* c, double* s) {
-  cos_sin_turns(a.turns[p] * (unsigned long long)(long long)a.positions[row], c, s);
-}
 template <int D, int PARTNER, class R, class F>
 PARROT_DEV void turn_table(const FillArgs& a, R (*turn_c)[D], R (*turn_s)[D], int lo, int hi, F row_of) {
   const int half = a.rd >> 1;
   if constexpr (PARTNER != kRotaryNone) {
     for (int x = threadIdx.x + lo * half; x < hi * half; x += 256) {
       const int i = x / half, p = x - i * half;
-      R c, s;
-      turn_of(a, p, row_of(i), &c, &s);
+      double c, s;                                         // (rounded once, to R)
+      cos_sin_turns(a.turns[p] * (unsigned long long)(long long)a.positions[row_of(i)], &c, &s);
       c *= a.amplitude;
       s *= a.amplitude;
       const int one = PARTNER == kRotaryInterleaved ? 2 * p : p, two = PARTNER == kRotaryInterleaved ? one + 1 : p + half;
-      turn_c[i][one] = turn_c[i][two] = c;
-      turn_s[i][one] = -s;
-      turn_s[i][two] = s;
+      turn_c[i][one] = turn_c[i][two] = (R)c;
+      turn_s[i][one] = (R)-s;
+      turn_s[i][two] = (R)s;
     }
     __syncthreads();
   }
