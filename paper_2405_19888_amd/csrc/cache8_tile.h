@@ -16,9 +16,10 @@
 // products.  Waves that share keys (run_shared) take them from a ring in LDS.
 //
 // Bounds: 16 columns read memory (64 requests on 3000 tokens, 393 MB in 64 us: 6.1 TB/s of the 7.1 that
-// plain reads reach).  More columns are bound by issue: of a unit's 1700 cycles for 32 columns of 128
-// elements, the matrix products are 670, widening 370, the exponentials and sums of 1024 weights 600
-// (measured by instruction; products and the rest overlap between two waves of a SIMD).
+// plain reads reach).  More columns are bound by issue: of a unit's 1450 cycles for 32 columns of 128
+// elements (four prompts of 400 rows on 8000 tokens, 749 TFLOP/s), the matrix products are 710, widening 370,
+// the exponentials and sums of 1024 weights 400 (by each instruction's own rate; products and the rest
+// overlap in part, between two waves of a SIMD).
 //
 // Types: bfloat16 and float16 round P once, and the output is divided by the sum of the rounded
 // weights (a dominant weight's rounding cancels).  float32 queries and weights are cut into
@@ -328,7 +329,7 @@ struct Tile8 {
 
  private:
   // keys_read(): the unit's keys have been read.  The products go ahead of the other wave's softmax
-  // (four prompts of 400 rows on 8000 tokens 314 us a layer, 341 without).
+  // (four prompts of 400 rows on 8000 tokens 314 us a layer, 341 without, before the steps below).
   template <class F>
   PARROT_DEV void unit(const Range8& rg, int tok0, u32x4 (&k)[2][X], u32x4 (&v)[2][X], unsigned (&sc)[2], float scale_log2,
                        F keys_read) {
