@@ -296,6 +296,36 @@ def test_graphs_replay_over_changing_lengths():
             assert torch.equal(torch.nan_to_num(x.float(), nan=9e9), torch.nan_to_num(y.float(), nan=9e9))
 
 
+def test_two_streams_at_once():
+    """Two layers that share a plan and have workspaces of their own run on two streams at once, again
+    and again, and give each what it gives alone."""
+    import paper_2405_19888_amd as parrot
+    plan, batch, off = batch_of(("bfloat16", 4, 4, 128, [0, 1, 0, -1, 1, 0], [900, 77], [40, 9, 2000, 800, 31, 5],
+                                 [4, 40, 2, 1, 9, 1], None))
+    pools, dense = cu.pools_of(batch)
+    q = [du.queries(int(off[-1]), 16, 128, "bfloat16", seed=s).cuda() for s in (1, 2)]
+    planner, one = cu.handles(plan, off, 4)
+    layers = [one, parrot.Cache8Decoder(planner)]
+    t = cu.ints_of(batch, off)
+    t["prefix"] = t["suffix"] = pools
+    planner(t)
+    want = []
+    for d, x in zip(layers, q):
+        d({**t, "q_rows": x})
+        torch.cuda.synchronize()
+        want.append((d.out.clone(), d.lse.clone()))
+        d.out.fill_(float("nan"))
+    streams = [torch.cuda.Stream() for _ in layers]
+    torch.cuda.synchronize()
+    calls = [d.bind({**t, "q_rows": x}, stream=s) for d, x, s in zip(layers, q, streams)]
+    for _ in range(20):
+        for call in calls:
+            call()
+    torch.cuda.synchronize()
+    for d, (out, lse) in zip(layers, want):
+        assert torch.equal(d.out, out) and torch.equal(d.lse, lse)
+
+
 def test_plan_of_another_step():
     """A call with the plan of a longer step gives unspecified values; the cache, the queries and the
     next planned call are untouched by it."""
