@@ -657,7 +657,10 @@ parrot_status parrot_cache8_fill(
  *                        or +inf, or whose logits are all -inf.  16-bit types: the weights
  *                        are rounded to dtype for their product with V and divided by the
  *                        rounded ones' sum.  float32: weights and logits in fp32
- * Keys and values of tokens a row does not see never reach its result, whatever they hold.
+ * Keys and values of tokens a row does not see never reach its result, whatever they hold.  A code
+ * whose value is 2^128 or more (256 under byte 247, which the fill writes for the largest fp32
+ * numbers) counts as no finite number: its element is none in the rows that see it.  Sums are in
+ * fp32, with weights of up to 2^11 before the division: values from 2^100 on may exceed it.
  *
  * What a step reads is laid out by parrot_cache8_plan, once for all layers of the step: it depends on
  * the row offsets, lengths and groups alone, and on the problem's and rows' fields but for

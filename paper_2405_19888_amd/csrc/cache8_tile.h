@@ -352,7 +352,7 @@ struct Tile8 {
     __builtin_amdgcn_s_setprio(0);
     keys_read();
     const bool masked = tok0 + kUnit > rg.plain;
-    bool bad = false;                                  // a value that some columns see is no number
+    bool bad = false;                                  // a value that some columns see may be no finite number
     if (masked) {
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
@@ -367,7 +367,7 @@ struct Tile8 {
             v[b][x][i] = w;
             any |= (w & 0x7F7F7F7Fu) + 0x01010101u;
           }
-        bad = bad || (any & 0x80808080u) != 0;
+        bad = bad || (any & 0x80808080u) != 0 || (DT != kF16 && alone(sc[b]) >= kLeastOver << 8);
       }
       bad = __ballot(bad) != 0;
     }
@@ -475,7 +475,7 @@ struct Tile8 {
           }
       }
     }
-    if (bad) mark_bad(v, x_seen(tok0));
+    if (bad) mark_bad(v, sc, x_seen(tok0));
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int x = 0; x < X; ++x)
@@ -506,9 +506,16 @@ struct Tile8 {
       }
     return r;
   }
-  // Values that are no numbers, in a unit that not all columns see whole: they make NaN of the
+  // What carries into the high bit of the bytes of codes that are no finite numbers: NaN (127) and, where
+  // values keep a block's scale of byte kLeastOver or more, the codes from (262 - byte) 8 on: 2^128 and more.
+  static constexpr unsigned kLeastOver = 247;
+  PARROT_DEV static unsigned over(unsigned byte) {
+    return (DT == kF16 || byte < kLeastOver ? 1u : 8u * byte - 1968u) * 0x01010101u;
+  }
+  // Values that are no finite numbers, in a unit that not all columns see whole: they make NaN of the
   // element in the columns that see their token, and are cleared for the others.
-  PARROT_DEV void mark_bad(u32x4 (&v)[2][X], const Seen& seen) {
+  PARROT_DEV void mark_bad(u32x4 (&v)[2][X], const unsigned (&sc)[2], const Seen& seen) {
+    const unsigned up[2] = {over(sc[0] >> 8), over(sc[1] >> 8)};
 #pragma unroll
     for (int x = 0; x < X; ++x)
 #pragma unroll
@@ -517,7 +524,7 @@ struct Tile8 {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
           const unsigned w = v[b][x][dd];
-          const unsigned nan = (((w & 0x7F7F7F7Fu) + 0x01010101u) >> 7) & 0x01010101u;     // 1 in such bytes
+          const unsigned nan = (((w & 0x7F7F7F7Fu) + up[b]) >> 7) & 0x01010101u;             // 1 in such bytes
           v[b][x][dd] = w & ~(nan * 255u);
           const unsigned code = nan * 0x38u;                                               // 1.0 in e4m3
           one[2 * b] = W::two(code, 1.f, false);

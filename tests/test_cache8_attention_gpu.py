@@ -378,3 +378,33 @@ def test_large_block_ids():
     out, lse = parrot.cache8_attention(*args(pools, ids))
     near, near_lse = parrot.cache8_attention(*args(small, [0, 1, 2, 3]))
     assert torch.equal(out, near) and torch.equal(lse, near_lse)
+
+
+def value_at(blk, head, tok, e):
+    return blk, head, e // 64, tok // 4, e % 64 // 4, e % 4, tok % 4
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32", "float16"])
+@pytest.mark.parametrize("rows", [3, 40])
+def test_unseen_codes_of_no_finite_value_stay_out(dtype, rows):
+    """A finite code times a large scale may be 2^128 or more (3.39e38 is cached as 256 * 2^120): rows that
+    do not see it keep their bits, in those that do its element is no finite number."""
+    e = 21
+    for where, byte, code in ((1, 247, 0x78), (2, 247, 0xFE), (1, 254, 0x40), (rows - 1, 250, 0x68)):
+        # the block holds zeros but for that code, which rows from `where` on see
+        plan, batch, off = batch_of((dtype, 2, 3, 64, [-1, 0], [20], [37, 5], [rows, 2], None))
+        pools, dense = cu.pools_of(batch)
+        q = du.queries(rows + 2, 6, 64, dtype)
+        p = 37 + where
+        blk, tok = int(plan.suffix_tables[0][p // 16]), p % 16
+        v = pools["v"].view(torch.uint8)
+        v[blk, 1] = 0
+        pools["scales"].view(torch.uint8)[blk, 1, 1] = byte
+        clean, clean_lse, *_ = cu.run(plan, batch, pools, q, off)
+        clean, clean_lse = clean.clone(), clean_lse.clone()
+        v[value_at(blk, 1, tok, e)] = code
+        out, lse, *_ = cu.run(plan, batch, pools, q, off)
+        hit = torch.zeros_like(out, dtype=torch.bool)
+        hit[where:rows, 3:6, e] = True               # rows that see it, heads that read cache head 1
+        assert torch.equal(out[~hit], clean[~hit]) and torch.equal(lse, clean_lse), (where, byte)
+        assert not torch.isfinite(out[hit]).any(), (where, byte)
