@@ -24,8 +24,9 @@
 // Types: bfloat16 and float16 round P once, and the output is divided by the sum of the rounded
 // weights (a dominant weight's rounding cancels).  float32 queries and weights are cut into
 // three bfloat16 parts, which hold all 24 bits: three products for one, at 16 times the rate of
-// the fp32 ones.  float16 does not hold every scale: values are taken relative to 2^vexp, raised as
-// blocks need it, exact down to 2^-15 of it, and smaller blocks pass the rest to their weights.
+// the fp32 ones.  float16 does not hold every scale: values are taken relative to a power of two that
+// is raised as blocks need it, in the columns that see them alone; they are exact down to 2^-15 of
+// it, and smaller blocks are multiplied by themselves, while the sums are scaled up.
 #pragma once
 
 #include "cache8_args.h"
@@ -99,12 +100,13 @@ struct Tile8 {
   float mref[NS], lt[NS];
   f32x4 lw[NS];                                       // the rounded weights' sum, four times
   int lim[NS];                                        // keys the lane's column sees
-  int vexp;                                           // float16: o is in units of 2^(vexp - 127)
+  // float16: o is in units of 2^(cexp - 127); columns that see the unit at hand have vexp
+  int vexp, cexp[NS];
 
   PARROT_DEV Tile8(int heads, int head) : lane(threadIdx.x & 63), h(head), H(alone(heads)) {
 #pragma unroll
     for (int c = 0; c < NS; ++c) {
-      mref[c] = kNoKey; lt[c] = 0.f; lw[c] = f32x4{0.f, 0.f, 0.f, 0.f}; lim[c] = 0;
+      mref[c] = kNoKey; lt[c] = 0.f; lw[c] = f32x4{0.f, 0.f, 0.f, 0.f}; lim[c] = cexp[c] = 0;
 #pragma unroll
       for (int t = 0; t < 4 * X; ++t) o[c][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -154,6 +156,16 @@ struct Tile8 {
   PARROT_DEV void scale_outputs(float f, int c) {
 #pragma unroll
     for (int t = 0; t < 4 * X; ++t) o[c][t] *= f;
+  }
+  // float16: the columns that see token tok (or all) change their unit to 2^(to - 127).
+  PARROT_DEV void raise_unit(int to, bool all, int tok) {
+#pragma unroll
+    for (int c = 0; c < NS; ++c) {
+      const bool sees = all || tok < lim[c];
+      if (__builtin_expect(vexp > 0 && to != vexp, false)) scale_outputs(sees ? ldexpf(1.f, cexp[c] - to) : 1.f, c);
+      cexp[c] = sees ? to : cexp[c];
+    }
+    vexp = to;
   }
 
   // ONCE: no other tile reads the keys, and streaming loads take them (438 MB of 64 requests in
@@ -318,7 +330,7 @@ struct Tile8 {
       float w = t;
       if constexpr (DT != kF32) w = lw[c][0];
       float inv = w == 0.f ? 0.f : 1.f / w;
-      if constexpr (DT == kF16) inv *= vexp > 0 ? __uint_as_float((unsigned)vexp << 23) : 1.f;
+      if constexpr (DT == kF16) inv *= cexp[c] > 0 ? __uint_as_float((unsigned)cexp[c] << 23) : 1.f;
       f(c, column(c), inv, t == 0.f ? -INFINITY : mref[c] + fast_log2(t));
     }
   }
@@ -371,30 +383,27 @@ struct Tile8 {
       }
       bad = __ballot(bad) != 0;
     }
-    float cb[2], vs[2], rest[2];
+    float cb[2], vs[2];
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       cb[b] = __uint_as_float((sc[b] & 0xFFu) << 23) * scale_log2;
       vs[b] = __uint_as_float((sc[b] >> 8) << 23);
-      rest[b] = 1.f;
     }
+    // float16: the blocks go one after the other where one lies more than 2^15 below the unit (448 * 2^7 is a
+    // float16: so far above it a block may lie), or where some columns see the first alone and the second
+    // needs another unit; a column's bits depend on the blocks that it sees
+    bool apart = false;
+    int last = 0;                                      // the unit behind the second block
     if constexpr (DT == kF16) {
-      // (up to 2^7 above vexp: 448 * 2^7 is a float16)
-      const int e0 = sc[0] >> 8, e1 = sc[1] >> 8, top = max(e0, e1);
-      if (top > vexp + 7 || vexp == 0) {
-        if (vexp > 0) {
-          const float f = ldexpf(1.f, vexp - top);
-#pragma unroll
-          for (int c = 0; c < NS; ++c) scale_outputs(f, c);
-        }
-        vexp = top;
+      const int e0 = sc[0] >> 8, e1 = sc[1] >> 8;
+      if (__builtin_expect(vexp == 0 || (unsigned)(e0 - vexp + 15) > 22u || (unsigned)(e1 - vexp + 15) > 22u, false)) {
+        const int first = e0 > vexp + 7 || vexp == 0 ? e0 : vexp;
+        last = e1 > first + 7 || first == 0 ? e1 : first;
+        apart = (masked && last != first && first > 0) || (e0 > 0 && e0 < last - 15) || (e1 > 0 && e1 < last - 15);
+        raise_unit(apart ? first : last, !masked, tok0);
       }
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const int rel = (b ? e1 : e0) - vexp;
-        vs[b] = __uint_as_float((unsigned)(127 + max(rel, -15)) << 23);
-        rest[b] = rel < -15 ? ldexpf(1.f, max(rel + 15, -30)) : 1.f;
-      }
+      for (int b = 0; b < 2; ++b) vs[b] = __uint_as_float((unsigned)(127 + max((b ? e1 : e0) - vexp, -15)) << 23);
     }
     // weights against the references at hand; their sums tell where one is more than 2^8 (a first
     // key's is infinite), and no maximum is taken until then.  A column's reference is raised by its own
@@ -462,34 +471,43 @@ struct Tile8 {
       }
       // (the matrix cores have time for the sum: as dot products 64 requests of 16 rows take 129 us a layer, 113 so)
       if constexpr (DT != kF32) lw[c] = W::mma(ones, u32x4{pw[c][0][0], pw[c][0][1], pw[c][0][2], pw[c][0][3]}, lw[c]);
-      if constexpr (DT == kF16) {
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-          if (rest[b] != 1.f) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              f16x2 y = as_f16x2(pw[c][0][2 * b + i]);
-              y *= f16x2{(_Float16)rest[b], (_Float16)rest[b]};
-              pw[c][0][2 * b + i] = __builtin_bit_cast(unsigned, y);
-            }
-          }
-      }
     }
     if (bad) mark_bad(v, sc, x_seen(tok0));
-    __builtin_amdgcn_s_setprio(1);
+    // (twice where the float16 blocks go one after the other: 2^-126 makes zeros of the other block's codes)
+#pragma unroll 1
+    for (int part = apart ? 0 : 1;; ++part) {
+      int up = 0;
+      if constexpr (DT == kF16)
+        if (__builtin_expect(apart, false)) {
+          if (part) raise_unit(last, !masked, tok0 + kBlockTokens);
+          const int e = (part ? sc[1] : sc[0]) >> 8, rel = e - vexp;
+          up = e > 0 ? clampi(-15 - rel, 0, 60) : 0;     // (sums are below 2^58: scaled by as much they are floats)
+          const float in = __uint_as_float((unsigned)(127 + max(rel + up, -126)) << 23), zero = __uint_as_float(1u << 23);
+          vs[0] = part ? zero : in;
+          vs[1] = part ? in : zero;
+          if (__builtin_expect(up > 0, false))
 #pragma unroll
-    for (int x = 0; x < X; ++x)
+            for (int c = 0; c < NS; ++c) scale_outputs(__uint_as_float((unsigned)(127 + up) << 23), c);
+        }
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-      for (int dd = 0; dd < 4; ++dd) {
-        const unsigned w0 = v[0][x][dd], w1 = v[1][x][dd];
-        const u32x4 vf = {W::two(w0, vs[0], false), W::two(w0, vs[0], true), W::two(w1, vs[1], false), W::two(w1, vs[1], true)};
+      for (int x = 0; x < X; ++x)
 #pragma unroll
-        for (int c = 0; c < NS; ++c)
+        for (int dd = 0; dd < 4; ++dd) {
+          const unsigned w0 = v[0][x][dd], w1 = v[1][x][dd];
+          const u32x4 vf = {W::two(w0, vs[0], false), W::two(w0, vs[0], true), W::two(w1, vs[1], false), W::two(w1, vs[1], true)};
 #pragma unroll
-          for (int p = PARTS - 1; p >= 0; --p)
-            o[c][4 * x + dd] = W::mma(vf, u32x4{pw[c][p][0], pw[c][p][1], pw[c][p][2], pw[c][p][3]}, o[c][4 * x + dd]);
-      }
-    __builtin_amdgcn_s_setprio(0);
+          for (int c = 0; c < NS; ++c)
+#pragma unroll
+            for (int p = PARTS - 1; p >= 0; --p)
+              o[c][4 * x + dd] = W::mma(vf, u32x4{pw[c][p][0], pw[c][p][1], pw[c][p][2], pw[c][p][3]}, o[c][4 * x + dd]);
+        }
+      __builtin_amdgcn_s_setprio(0);
+      if (__builtin_expect(up > 0, false))
+#pragma unroll
+        for (int c = 0; c < NS; ++c) scale_outputs(__uint_as_float((unsigned)(127 - up) << 23), c);
+      if (__builtin_expect(part, 1)) break;
+    }
   }
 
   // 1 where the lane's column sees the token of its P operand, as that operand.

@@ -408,3 +408,63 @@ def test_unseen_codes_of_no_finite_value_stay_out(dtype, rows):
         hit[where:rows, 3:6, e] = True               # rows that see it, heads that read cache head 1
         assert torch.equal(out[~hit], clean[~hit]) and torch.equal(lse, clean_lse), (where, byte)
         assert not torch.isfinite(out[hit]).any(), (where, byte)
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16", "float32"])
+@pytest.mark.parametrize("up", [9, 20, 45, 100])
+@pytest.mark.parametrize("rows", [2, 40])
+def test_unseen_scales_stay_out(dtype, up, rows):
+    """Values of later rows, 2^up times the others', in the other block of a unit and in units behind it: no bit
+    of the rows before them changes."""
+    cached = 48 - rows // 2                      # row rows / 2 is the first that sees block 3, the other one of its unit
+    plan, batch, off = batch_of((dtype, 2, 3, 128, [-1, 0], [70], [cached, 9], [rows, 1], None))
+    pools, dense = cu.pools_of(batch)
+    q = du.queries(rows + 1, 6, 128, dtype)
+    clean, clean_lse, *_ = cu.run(plan, batch, pools, q, off)
+    clean, clean_lse = clean.clone(), clean_lse.clone()
+    late = plan.suffix_tables[0][3: (cached + rows + 15) // 16]
+    pools["scales"].view(torch.uint8)[torch.tensor(late, device="cuda").long(), :, 1] += up
+    out, lse, *_ = cu.run(plan, batch, pools, q, off)
+    before = rows // 2
+    assert torch.equal(out[:before], clean[:before]) and torch.equal(lse, clean_lse)
+    assert torch.equal(out[rows:], clean[rows:])
+    assert not torch.equal(out[before:rows], clean[before:rows])
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16", "float32"])
+@pytest.mark.parametrize("span", [14, 22, 40])
+def test_blocks_of_many_sizes_within_range(dtype, span):
+    """As test_blocks_of_many_sizes, with values whose blocks reach 2^(2 span) below the largest
+    and outputs that every type holds."""
+    plan, batch, off = batch_of((dtype, 2, 2, 128, [0, -1, 0], [300], [400, 250, 3], [2, 5, 1], None))
+    rng = np.random.default_rng(span)
+    v = batch.v_pool.double().numpy() * 2.0 ** rng.integers(8 - 2 * span, 9, batch.v_pool.shape[0])[:, None, None, None]
+    k = batch.k_pool.double().numpy() * 2.0 ** rng.integers(-2, 2, batch.v_pool.shape[0])[:, None, None, None]
+    (ck, bk), (cv, bv) = cu.oracle.pack(k), cu.oracle.pack(v)
+    pools = cu.device_pools(ck, cu.oracle.value_order(cv), np.stack([bk, bv], -1))
+    dense = [cu.oracle.values(ck, bk), cu.oracle.values(cv, bv)]
+    q = du.queries(8, 4, 128, dtype)
+    out, lse, *_ = cu.run(plan, batch, pools, q, off)
+    assert np.abs(cu.reference(plan, dense, q, off)[0]).max() < 60000
+    cu.check(plan, dense, q, off, out, lse, what=f"{dtype} span {span} in range")
+
+
+def test_small_blocks_beside_a_large_one_of_no_weight():
+    """float16: a block of values 2^30 to 2^60 above the others, whose logits lie so far below that its tokens
+    add nothing: the result is the other blocks', whichever half of a unit they are."""
+    for up in (20, 30, 60):
+        for large in range(4):
+            plan, batch, off = batch_of(("float16", 1, 1, 64, [-1], [], [63], [1], None))
+            k, v = 0.01 * batch.k_pool.double().numpy(), batch.v_pool.double().numpy()
+            ids = plan.suffix_tables[0][:4]
+            q = torch.ones(1, 1, 64, dtype=torch.float16)
+            k[ids[large]] -= 12.0                # logits 96 below the others': weights of about 2^-138
+            (ck, bk), (cv, bv) = cu.oracle.pack(k), cu.oracle.pack(v)
+            bv[ids[large]] += up
+            pools = cu.device_pools(ck, cu.oracle.value_order(cv), np.stack([bk, bv], -1))
+            dense = [cu.oracle.values(ck, bk), cu.oracle.values(cv, bv)]
+            out, lse, *_ = cu.run(plan, batch, pools, q, off)
+            ref = cu.reference(plan, dense, q, off)[0]
+            # the weights' rounding (of at most 1, on values below 4) and the output's
+            tol = 2.0 ** -11 * 4 + 2.0 ** -11 * np.abs(ref) + 2.0 ** -24
+            assert (np.abs(out.double().cpu().numpy() - ref) <= tol).all(), (up, large)
