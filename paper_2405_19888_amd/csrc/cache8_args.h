@@ -57,7 +57,7 @@ enum Head8 { kHeadEntries, kHeadWide, kHeadJoins, kHeadWideCost, kHeadCost, kHea
 enum Entry8 { kEntSeq, kEntCol0, kEntCols, kEntCost, kEntUnits, kEntSlot, kEntPieces, kEntKeys, kEntBase, kEntFirst, kEntChained };
 // A row that is joined, in no order: its token, entry of its request's first tile, its place in the
 // request, levels of prefixes, then for each level the entry of the group's first tile and the row's
-// place in the group's list.
+// place in the group's list (-1: a prefix without tokens).
 enum Row8 { kRowToken, kRowEntry, kRowPlace, kRowLevels, kRowGroup };
 // A request: first row, rows, own tokens, its group where it reads groups' results (-1), then
 // its chain's groups and their tokens, innermost first.

@@ -326,7 +326,8 @@ __global__ __launch_bounds__(1024) void k_cache8_plan(Plan8Args a) {
         const int grp = o[kReqChain + 2 * l];
         if (grp >= 0) {
           const int at = count[(long)wave_of(lo, st.R) * st.NG + grp] + pos[(long)lo * kMaxDepth + l] + j;
-          if (o[kReqChain + 2 * l + 1] > 0) {
+          v[kRowGroup + 2 * l + 1] = -1;
+          if (o[kReqChain + 2 * l + 1] > 0) {           // (a prefix without tokens has no entries)
             v[kRowGroup + 2 * l] = (long)(off[grp + 1] - off[grp]) * st.G > a.wide_from ? seq[grp] : wide + seqn[grp];
             v[kRowGroup + 2 * l + 1] = at;
             v[kRowLevels] = l + 1;
@@ -644,13 +645,13 @@ __global__ __launch_bounds__(256) void k_cache8_join(Attend8Args a) {
     for (int s = 0; s <= kMaxDepth; ++s) {
       n[s] = 0;
       if (s <= levels) {
-        const int x = ld_uniform(d + (s ? kRowGroup + 2 * s - 1 : (int)kRowPlace)) * a.G + gq;
+        const int place = ld_uniform(d + (s ? kRowGroup + 2 * s - 1 : (int)kRowPlace)), x = place * a.G + gq;
         const int e0 = ld_uniform(d + (s ? kRowGroup + 2 * s - 2 : (int)kRowEntry));
         const int cols = e0 < wide ? max(a.wide, 1) : 16 * a.sets;
         const int* v = a.plan + a.at.entry + (long)clampi(e0 + x / cols, 0, a.max_entries - 1) * kEntryInts;
         slot[s] = v[kEntSlot];
         nc[s] = v[kEntCols];
-        n[s] = min(v[kEntPieces], 4 * a.wgs);           // (a piece per run at most)
+        n[s] = place < 0 ? 0 : min(v[kEntPieces], 4 * a.wgs);   // (a piece per run at most)
         col[s] = x % cols;
       }
     }

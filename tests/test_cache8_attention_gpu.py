@@ -468,3 +468,20 @@ def test_small_blocks_beside_a_large_one_of_no_weight():
             # the weights' rounding (of at most 1, on values below 4) and the output's
             tol = 2.0 ** -11 * 4 + 2.0 ** -11 * np.abs(ref) + 2.0 ** -24
             assert (np.abs(out.double().cpu().numpy() - ref) <= tol).all(), (up, large)
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+def test_empty_prefixes_in_a_chain(rows):
+    """A prefix without tokens, which calls do not ask for, adds nothing, wherever it is in a chain."""
+    from dataclasses import replace
+    for empty in ((1,), (0,), (3,), (1, 2), (0, 1, 3)):
+        plan, batch, off = batch_of(("float16", 2, 2, 64, [3, 0, 2, 1, -1], [70, 16, 33, 50], [40, 64, 5, 12, 30],
+                                     [rows, 1, 2, 1, 1], [-1, 0, 1, 2]))
+        lens = plan.prefix_lens.copy()
+        lens[list(empty)] = 0
+        plan = replace(plan, prefix_lens=lens)
+        batch = replace(batch, plan=plan)
+        pools, dense = cu.pools_of(batch)
+        q = du.queries(int(off[-1]), 4, 64, "float16")
+        out, lse, *_ = cu.run(plan, batch, pools, q, off, check_inputs=False)
+        cu.check(plan, dense, q, off, out, lse, what=f"empty {empty}")
