@@ -58,7 +58,10 @@ struct parrot_context_store {
   int32_t live_nodes = 0;
   std::vector<int32_t> users;                     // per block: nodes and contexts that hold it
   std::vector<int32_t> holds;                     // per block: copies not taken yet that read it
-  std::vector<std::pair<int32_t, int32_t>> copies;   // (source, destination), not taken yet
+  // (source, destination), not taken yet, in no order: no destination is another's source or destination, and
+  // there is room for one into every block
+  std::vector<std::pair<int32_t, int32_t>> copies;
+  std::vector<int32_t> copy_at;                   // per block: place of the copy into it, -1 for none
 
   static uint64_t key(int32_t parent, uint64_t h) {
     return h ^ (0x9e3779b97f4a7c15ull * static_cast<uint64_t>(parent + 1));
@@ -89,25 +92,21 @@ struct parrot_context_store {
   void drop_block(int32_t b) {
     if (--users[b] > 0) return;
     // a copy into a block that nobody holds any more is not owed; nothing reads such a block
-    for (size_t i = 0; i < copies.size(); ++i)
-      if (copies[i].second == b) {
-        const int32_t from = copies[i].first;
-        copies.erase(copies.begin() + i);
-        --holds[from];
-        free_if_unused(from);
-        break;
-      }
+    if (const int32_t i = copy_at[b]; i >= 0) {
+      const int32_t from = copies[i].first;
+      copies[i] = copies.back();
+      copy_at[copies[i].second] = i;
+      copies.pop_back();
+      copy_at[b] = -1;
+      --holds[from];
+      free_if_unused(from);
+    }
     free_if_unused(b);
   }
-  // What block b will hold is in this one: where b itself is still to be copied to, its source.
-  size_t copy_into(int32_t b) const {
-    size_t i = 0;
-    while (i < copies.size() && copies[i].second != b) ++i;
-    return i;
-  }
+  // `to` is to hold what block `from` will hold: where that is still to be copied to, its source.
   void owe_copy(int32_t from, int32_t to) {
-    const size_t i = copy_into(from);
-    if (i < copies.size()) from = copies[i].first;
+    if (copy_at[from] >= 0) from = copies[copy_at[from]].first;
+    copy_at[to] = static_cast<int32_t>(copies.size());
     copies.emplace_back(from, to);
     ++holds[from];
   }
@@ -141,6 +140,8 @@ parrot_context_store* parrot_store_create(int32_t block_size, int32_t num_blocks
   for (int32_t i = 0; i < num_blocks; ++i) st->free_list[i] = num_blocks - 1 - i;
   st->users.resize(num_blocks);
   st->holds.resize(num_blocks);
+  st->copies.reserve(num_blocks);
+  st->copy_at.assign(num_blocks, -1);
   return st;
 }
 
@@ -225,11 +226,6 @@ parrot_status parrot_store_append(parrot_context_store* st, int32_t ctx, int32_t
     // the new token goes into a block that other contexts read: this one gets its own
     if (st->free_list.empty())
       return parrot::set_error(PARROT_ERR_WORKSPACE_TOO_SMALL, "no free KV block for context %d", ctx);
-    try {
-      st->copies.reserve(st->copies.size() + 1);
-    } catch (const std::bad_alloc&) {
-      return parrot::set_error(PARROT_ERR_WORKSPACE_TOO_SMALL, "no host memory for a copy");
-    }
     const int32_t mine = st->take_block();
     st->owe_copy(last, mine);
     --st->users[last];
@@ -297,7 +293,6 @@ int32_t parrot_store_compact(parrot_context_store* st, int32_t most) {
   std::vector<int32_t> now;
   try {
     now.resize(n);
-    st->copies.reserve(st->copies.size() + n);
   } catch (const std::bad_alloc&) {
     parrot::set_error(PARROT_ERR_WORKSPACE_TOO_SMALL, "no host memory to compact");
     return -1;
@@ -309,12 +304,12 @@ int32_t parrot_store_compact(parrot_context_store* st, int32_t most) {
     while (to < from && (st->users[to] > 0 || st->holds[to] > 0)) ++to;
     if (to >= from) break;
     // a block that is still to be copied to is copied to its new place instead
-    const size_t i = st->copy_into(from);
-    if (i < st->copies.size()) {
+    if (const int32_t i = st->copy_at[from]; i >= 0) {
       st->copies[i].second = to;
+      st->copy_at[to] = i;
+      st->copy_at[from] = -1;
     } else {
-      st->copies.emplace_back(from, to);
-      ++st->holds[from];
+      st->owe_copy(from, to);
     }
     st->users[to] = st->users[from];
     st->users[from] = 0;
@@ -343,6 +338,7 @@ parrot_status parrot_store_take_copies(parrot_context_store* st, int32_t* src, i
   for (int32_t i = 0; i < n; ++i) {
     src[i] = st->copies[i].first;
     dst[i] = st->copies[i].second;
+    st->copy_at[dst[i]] = -1;
     --st->holds[src[i]];
     st->free_if_unused(src[i]);
   }

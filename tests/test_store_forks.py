@@ -267,3 +267,80 @@ def test_under_sanitizers(tmp_path):
     p = subprocess.run([sys.executable, "-c", code], env=env, capture_output=True, text=True, timeout=600)
     assert p.returncode == 0, p.stdout[-3000:] + p.stderr[-3000:]
     assert "passed" in p.stdout
+
+
+def test_owed_copies_cost_what_they_copy():
+    """Moving 120000 blocks, and freeing them while the copies are owed, take the time of a list that long, not of
+    its square (about 0.01 s; with a search of all copies for each block 2.5 s and more)."""
+    import time
+    n = 120000
+    st = ContextStore(1, 2 * n)
+    a = st.fill(np.zeros(n, dtype=np.int32))
+    b = st.fill(np.zeros(n, dtype=np.int32))
+    st.free(a)
+    start = time.perf_counter()
+    assert st.compact() == n and st.num_copies == n and st.block_end == 2 * n
+    st.free(b)
+    assert time.perf_counter() - start < 1.0
+    assert st.num_copies == 0 and st.block_end == 0 and st.free_blocks == 2 * n
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_random_operations_while_copies_are_owed(seed):
+    """Forks, compactions, truncations, frees and appends with copies not yet taken: a copy owed to a block that
+    moves goes to its new place, a dropped one is not owed.  The cache is written only after the copies."""
+    rng = np.random.default_rng(100 + seed)
+    B = [4, 16][seed % 2]
+    st = ContextStore(B, 70)
+    m = Cache(st)
+    token, redirected = 1000, 0
+    for step in range(250):
+        for _ in range(int(rng.integers(0, 7))):         # copies of these stay owed
+            live = list(m.want)
+            if not live:
+                break
+            pick, op = live[int(rng.integers(0, len(live)))], rng.random()
+            if op < 0.35 and len(live) < 30:
+                m.fork(pick)
+            elif op < 0.6:
+                owed = st.num_copies
+                moved = st.compact(int(rng.integers(1, 30)))
+                redirected += moved - (st.num_copies - owed)
+            elif op < 0.8:
+                m.truncate(pick, int(rng.integers(0, len(m.want[pick]) + 1)))
+            elif len(live) > 4:
+                m.free(pick)
+        # a step of an engine: several contexts append, the copies are taken, the rows are written
+        live = list(m.want)
+        token += 100
+        if not live or rng.random() < 0.3:
+            try:
+                m.fill([token * 100 + i for i in range(int(rng.integers(1, 40)))])
+            except (MemoryError, ParrotError):
+                pass
+        else:
+            new = []
+            for c in rng.permutation(live)[:int(rng.integers(1, 6))]:
+                try:
+                    st.append(int(c))
+                    new.append(int(c))
+                except ParrotError:
+                    pass
+            if rng.random() < 0.3:                       # (owed copies whose destination moves)
+                owed = st.num_copies
+                moved = st.compact(20)
+                redirected += moved - (st.num_copies - owed)
+            m.settle()
+            for c in new:
+                token += 1
+                i = len(m.want[c])
+                m.blocks[m.own_row(c)[i // B]][i % B] = token
+                m.want[c].append(token)
+        m.settle()
+        used = m.check()
+        assert st.free_blocks == 70 - len(used), step
+        assert st.block_end == (max(used) + 1 if used else 0), step
+    assert redirected > 0                                # some owed copies went to another place
+    for c in list(m.want):
+        m.free(c)
+    assert st.free_blocks == 70 and st.block_end == 0
