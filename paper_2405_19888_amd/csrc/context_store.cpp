@@ -62,6 +62,7 @@ struct parrot_context_store {
   // there is room for one into every block
   std::vector<std::pair<int32_t, int32_t>> copies;
   std::vector<int32_t> copy_at;                   // per block: place of the copy into it, -1 for none
+  bool compacted = false;                         // moves are among the copies
 
   static uint64_t key(int32_t parent, uint64_t h) {
     return h ^ (0x9e3779b97f4a7c15ull * static_cast<uint64_t>(parent + 1));
@@ -315,6 +316,7 @@ int32_t parrot_store_compact(parrot_context_store* st, int32_t most) {
     st->users[from] = 0;
     now[from] = to;
     ++moved;
+    st->compacted = true;
   }
   for (Node& nd : st->nodes)
     for (int32_t& b : nd.blocks) b = now[b];
@@ -334,7 +336,6 @@ parrot_status parrot_store_take_copies(parrot_context_store* st, int32_t* src, i
   const int32_t n = static_cast<int32_t>(st->copies.size());
   if (most < n) return parrot::set_error(PARROT_ERR_WORKSPACE_TOO_SMALL, "%d copies, room for %d", n, most);
   if (n > 0 && (!src || !dst)) return parrot::set_error(PARROT_ERR_INVALID_ARGUMENT, "src or dst is NULL");
-  const size_t freed = st->free_list.size();
   for (int32_t i = 0; i < n; ++i) {
     src[i] = st->copies[i].first;
     dst[i] = st->copies[i].second;
@@ -343,8 +344,9 @@ parrot_status parrot_store_take_copies(parrot_context_store* st, int32_t* src, i
     st->free_if_unused(src[i]);
   }
   st->copies.clear();
-  // (lowest ids first, so that a compacted pool stays so; in place)
-  if (st->free_list.size() > freed) std::sort(st->free_list.begin(), st->free_list.end(), std::greater<int32_t>());
+  // (after moves lowest ids first, so that a compacted pool stays so; in place)
+  if (st->compacted) std::sort(st->free_list.begin(), st->free_list.end(), std::greater<int32_t>());
+  st->compacted = false;
   return parrot::set_error(PARROT_OK, "");
 }
 
