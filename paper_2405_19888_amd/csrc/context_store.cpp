@@ -135,15 +135,20 @@ parrot_context_store* parrot_store_create(int32_t block_size, int32_t num_blocks
   if (block_size < 1 || num_blocks < 0) return nullptr;
   auto* st = new (std::nothrow) parrot_context_store();
   if (!st) return nullptr;
-  st->B = block_size;
-  st->free_list.resize(num_blocks);
-  // hand out low block ids first
-  for (int32_t i = 0; i < num_blocks; ++i) st->free_list[i] = num_blocks - 1 - i;
-  st->users.resize(num_blocks);
-  st->holds.resize(num_blocks);
-  st->copies.reserve(num_blocks);
-  st->copy_at.assign(num_blocks, -1);
-  return st;
+  try {
+    st->B = block_size;
+    st->free_list.resize(num_blocks);
+    // hand out low block ids first
+    for (int32_t i = 0; i < num_blocks; ++i) st->free_list[i] = num_blocks - 1 - i;
+    st->users.resize(num_blocks);
+    st->holds.resize(num_blocks);
+    st->copies.reserve(num_blocks);
+    st->copy_at.assign(num_blocks, -1);
+    return st;
+  } catch (const std::bad_alloc&) {
+    delete st;
+    return nullptr;
+  }
 }
 
 void parrot_store_destroy(parrot_context_store* st) { delete st; }

@@ -366,3 +366,26 @@ def test_taking_a_forks_copies_leaves_the_free_list():
         c = one
     assert sorted(times)[6] < 0.002
     assert st.free_blocks == 1000000 - 2
+
+
+def test_a_store_that_memory_does_not_hold(tmp_path):
+    """No memory for a pool's lists gives NULL, as the header says, and ends nothing."""
+    import os
+    import shutil
+    import subprocess
+    import sys
+    from test_store_sanitized import ROOT
+    if shutil.which("g++") is None or os.environ.get("PARROT_STORE_SANITIZED"):
+        pytest.skip("no g++, or running under sanitizers")
+    lib = str(tmp_path / "libstore.so")
+    csrc = os.path.join(ROOT, "paper_2405_19888_amd", "csrc")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", csrc,
+                    os.path.join(csrc, "context_store.cpp"), os.path.join(ROOT, "tests", "sanitizer_stub.cpp"), "-o", lib],
+                   check=True)
+    # each list of 2^28 blocks is 1 GiB or more: one to four of them fit the limits
+    code = ("import ctypes, resource, sys; lib = ctypes.CDLL(sys.argv[1]); lib.parrot_store_create.restype = ctypes.c_void_p\n"
+            "gib = int(sys.argv[2]); resource.setrlimit(resource.RLIMIT_AS, (gib << 30, gib << 30))\n"
+            "assert lib.parrot_store_create(16, 1 << 28) is None and lib.parrot_store_create(16, 100) is not None; print('fine')")
+    for gib in (1, 2, 3):
+        p = subprocess.run([sys.executable, "-c", code, lib, str(gib)], capture_output=True, text=True, timeout=120)
+        assert p.returncode == 0 and "fine" in p.stdout, (gib, p.stdout, p.stderr)
