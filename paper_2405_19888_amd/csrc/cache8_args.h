@@ -41,9 +41,10 @@ constexpr int kPlanWaves = 16;           // waves of the planning workgroup
 constexpr int kPieceSetup = 2;           // cost of a tile beside its units
 
 // Columns of a wide tile, and columns above which a sequence has wide tiles: what one narrow tile
-// holds.  bfloat16, 8 cache heads of 128 elements, four query heads on each, us a layer with wide tiles and
-// with several narrow ones: four prompts of 400 rows on 8000 tokens 314 and 448, 64 requests of ten rows on
-// 3000 137 and 173, ten rows on one prefix of 16000 34 and 38; 400 rows on 1000 in float32 109 and 197.
+// holds.  bfloat16, 8 cache heads of 128 elements, four query heads on each, us for the plan and a layer with
+// wide tiles and with several narrow ones: four prompts of 400 rows on 8000 tokens 282 and 445, 64 requests of ten
+// rows on 3000 118 and 178, ten rows on one prefix of 16000 39 and 44; four of 400 rows on 1000 in
+// float32 109 and 196.
 constexpr int wide_cols(int dtype) { return dtype == kF32 ? 64 : 128; }
 constexpr int wide_from(int dtype) { return wide_cols(dtype) / 4; }
 

@@ -254,7 +254,7 @@ __global__ __launch_bounds__(1024) void k_cache8_plan(Plan8Args a) {
   __syncthreads();
   // a cache head's workgroups are shared by the two costs: a wide unit comes out of LDS and keeps a
   // workgroup half as long as a narrow one, which streams, keeps a wave (288 requests, 256 of them
-  // below 8 prefixes, us a layer: 123; as 0.3 of it 161, as long 131)
+  // below 8 prefixes, us for the plan and two layers: 237; as 0.3 of it 294, as long 253)
   const int wcost = wide == 0 ? 0 : wide < entries ? cost[wide] : total;
   const int wwgs = wide == 0 ? 0 : wide == entries ? a.wgs
                  : clampi((int)((2L * a.wgs * wcost + ((long)wcost + total) / 2) / ((long)wcost + total)), 1, a.wgs - 1);
@@ -450,7 +450,8 @@ PARROT_DEV void attend_piece(const Attend8Args& a, const Entry& e, int h, int u0
 #pragma unroll
     for (int c = 0; c < NS; ++c) tile.lim[c] = own && !pre ? sees[c] : keys;
     if constexpr (WIDE) tile.run_shared(rg, alone(a.scale_log2), ring, cols < 1 ? 0 : own && !pre ? most : keys);
-    // (16 columns are nearly always all that read their keys; wider tiles have neighbours)
+    // (one set alone takes streaming loads; a narrow tile of two sets is its keys' only reader too: 64 requests of
+    // eight rows of four query heads on 3000 tokens 108 us with cached loads, 94 with streaming ones)
     else tile.template run<NS == 1>(rg, alone(a.scale_log2));
   }
 

@@ -252,8 +252,10 @@ PARROT_DEV void turn_table(const FillArgs& a, R (*turn_c)[D], R (*turn_s)[D], in
 }
 
 // One row a request: a lane group per head.  Bound by the launch and the round trips of length,
-// block and scale: 7 requests, 32 heads of 128 in float16, 4.6 us; 256 requests of 48 heads, normalised,
-// 5.2 (4.8 in fp32, which gives one key in a million the code beside the nearest).
+// block and scale: 7 requests, 32 heads of 128 in float16, 4.7 us; 256 requests of 48 heads, normalised,
+// 5.1 (in fp32 0.4 less, and one key in a million gets the code beside the nearest).  So where no scale grows; where
+// some do, as in most steps, tokens that a raised block held are brought to the new scale one after the
+// other, up to 15 round trips more: 10.7 and 15.0 us.
 template <int DT, int D, int PARTNER>
 __global__ __launch_bounds__(256) void k_cache8_fill_tokens(FillArgs a, unsigned char* scales) {
   using E = Elem<DT>;

@@ -16,10 +16,11 @@
 // products.  Waves that share keys (run_shared) take them from a ring in LDS.
 //
 // Bounds: 16 columns read memory (64 requests on 3000 tokens, 393 MB in 64 us: 6.1 TB/s of the 7.1 that
-// plain reads reach).  More columns are bound by issue: of a unit's 1450 cycles for 32 columns of 128
-// elements (four prompts of 400 rows on 8000 tokens, 749 TFLOP/s), the matrix products are 710, widening 370,
+// plain reads reach).  Wide tiles are bound by issue: of a unit's 1430 cycles for 32 columns of 128
+// elements (four prompts of 400 rows on 8000 tokens, 760 TFLOP/s), the matrix products are 710, widening 370,
 // the exponentials and sums of 1024 weights 400 (by each instruction's own rate; products and the rest
-// overlap in part, between two waves of a SIMD).
+// overlap in part, between two waves of a SIMD).  Narrow tiles of 17 to 32 columns wait for memory (3.9 TB/s):
+// their registers leave two waves a SIMD and one unit ahead.
 //
 // Types: bfloat16 and float16 round P once, and the output is divided by the sum of the rounded
 // weights (a dominant weight's rounding cancels).  float32 queries and weights are cut into
