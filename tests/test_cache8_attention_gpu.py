@@ -385,7 +385,7 @@ def value_at(blk, head, tok, e):
 
 
 @pytest.mark.parametrize("dtype", ["bfloat16", "float32", "float16"])
-@pytest.mark.parametrize("rows", [3, 40])
+@pytest.mark.parametrize("rows", [3, 8, 40])
 def test_unseen_codes_of_no_finite_value_stay_out(dtype, rows):
     """A finite code times a large scale may be 2^128 or more (3.39e38 is cached as 256 * 2^120): rows that
     do not see it keep their bits, in those that do its element is no finite number."""
@@ -412,14 +412,14 @@ def test_unseen_codes_of_no_finite_value_stay_out(dtype, rows):
 
 @pytest.mark.parametrize("dtype", ["float16", "bfloat16", "float32"])
 @pytest.mark.parametrize("up", [9, 20, 45, 100])
-@pytest.mark.parametrize("rows", [2, 40])
-def test_unseen_scales_stay_out(dtype, up, rows):
+@pytest.mark.parametrize("rows,dim", [(2, 128), (8, 128), (40, 128), (2, 64), (8, 64), (40, 64)])
+def test_unseen_scales_stay_out(dtype, up, rows, dim):
     """Values of later rows, 2^up times the others', in the other block of a unit and in units behind it: no bit
     of the rows before them changes."""
     cached = 48 - rows // 2                      # row rows / 2 is the first that sees block 3, the other one of its unit
-    plan, batch, off = batch_of((dtype, 2, 3, 128, [-1, 0], [70], [cached, 9], [rows, 1], None))
+    plan, batch, off = batch_of((dtype, 2, 3, dim, [-1, 0], [70], [cached, 9], [rows, 1], None))
     pools, dense = cu.pools_of(batch)
-    q = du.queries(rows + 1, 6, 128, dtype)
+    q = du.queries(rows + 1, 6, dim, dtype)
     clean, clean_lse, *_ = cu.run(plan, batch, pools, q, off)
     clean, clean_lse = clean.clone(), clean_lse.clone()
     late = plan.suffix_tables[0][3: (cached + rows + 15) // 16]
